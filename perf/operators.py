@@ -231,14 +231,16 @@ def prepare(case, seed):
                  out_mass=torch.zeros_like(m), out_row_pos=torch.zeros_like(row_pos),
                  out_kv_len=torch.zeros_like(s["kv_len"]), out_n_evicted=torch.zeros_like(s["kv_len"]))
     if own:
-        s["h"], s["plan"] = _handle(c)
+        s["h"], s["plan"] = _handle(c, Lcap)
     return s
 
 
-def _handle(c):
+def _handle(c, Lcap):
     from paper_2412_00061_b200 import binding
     h = binding.Handle(c["B"], 256, 1000, c.get("T", 5), 3, 16, 8, c.get("nodes", 2), c.get("Hq", c["Hkv"]), c["Hkv"], c["D"],
                        binding.DTYPE_BF16 if c["dtype"] == "bf16" else binding.DTYPE_F32, device=DEVICE)
+    if c["op"] == "evict":
+        return h, h.make_eviction(Lcap)
     return h, (h.make_shared_attention() if c["op"] == "attention" else None)
 
 
@@ -343,8 +345,8 @@ def _evict(s):
     out = {"K": s["K"][:, :, :budget], "V": s["V"][:, :, :budget], "mass": s["out_mass"][:, :, :budget],
            "row_pos": s["out_row_pos"][:, :, :budget], "kv_len": s["out_kv_len"], "n_evicted": s["out_n_evicted"]}
     if own:
-        s["h"].evict_rows(s["K"], s["V"], s["mass"], s["row_pos"], s["kv_len"], s["n_evicted"], budget, c["sinks"],
-                          c["recent"], s["out_mass"], s["out_row_pos"], s["out_kv_len"], s["out_n_evicted"])
+        s["h"].evict_rows(s["plan"], s["K"], s["V"], s["mass"], s["row_pos"], s["kv_len"], s["n_evicted"], budget,
+                          c["sinks"], c["recent"], s["out_mass"], s["out_row_pos"], s["out_kv_len"], s["out_n_evicted"])
         return out
     Lcap = s["mass"].shape[2]
     j = torch.arange(Lcap, device=DEVICE)
