@@ -283,6 +283,58 @@ int ctcsd_commit_accepted(ctcsd_handle* h, void* stream, void* K, void* V, int L
                           int* out_kv_len, int* out_sel_row);
 
 /*
+ * Cache eviction (the paper has no counterpart; it is what keeps a long-running batch inside a fixed cache).
+ * Two calls after ctcsd_commit_accepted: the first adds up how much attention every cached row draws,
+ * the second cuts every sequence's cache to a budget of rows and drops those that drew least.
+ * Per cached row they keep, both [B,Hkv,Lcap] and owned by the caller:
+ *   mass     float32, the attention weight the row has gathered (start: 0, or weights from the prompt);
+ *   row_pos  int32, the position of the row's token among the sequence's own tokens (start: 0,1,2,...).
+ * n_evicted [B] int32 counts the rows a sequence has lost so far (start: 0); kv_len + n_evicted is the
+ * number of its tokens.  Once rows have been dropped, a tree node's position is no longer kv_len + depth:
+ * pass kv_len + n_evicted (+ the shared prefix's length) as ctcsd_build_tree's kv_len, which serves
+ * out_pos alone there.
+ *
+ * ctcsd_attention_mass: query l = 0..acc_len[b] of the accepted path (l = 0 the root, then acc_nodes) sits at
+ * cache row base + l, base = kv_len[b] - 1 - acc_len[b], and sees rows 0..base+l of its sequence:
+ *   w[b,g,j] = sum_l sum_h exp( scale * q[b,node_l,h].k[b,g,j] - lse[b,node_l,h] ),  h over the heads of group g;
+ *   mass[b,g,j] = decay * mass[b,g,j] + w[b,g,j]  for j < base;
+ *   mass[b,g,j] = w[b,g,j], row_pos[b,g,j] = n_evicted[b] + j  for the step's new rows base <= j < kv_len[b].
+ * Q [B,max_nodes,Hq,D] dtype, the tree's queries;  K [B,Hkv,Lcap,D] dtype, kv_len [B]: as AFTER
+ * ctcsd_commit_accepted;  acc_len [B], acc_nodes [B,T] of that step;  lse [B,max_nodes,Hq] float32: the log-sum-exp
+ * ctcsd_tree_attention_shared returned (entries of nodes off the path are not read; -inf: the query
+ * adds nothing);  scale > 0;  0 <= decay <= 1;  n_evicted [B] int32 or NULL (zeros);  mass, row_pos updated IN PLACE.
+ * Sums are formed in float32 in a fixed order.  A sequence whose acc_len, acc_nodes or kv_len lie outside their
+ * arrays is left unchanged and CTCSD_ERR_INVALID_ARG is recorded in the device status word.
+ * Needs B <= 1024 (else CTCSD_ERR_UNSUPPORTED); Q and K 16-byte aligned.
+ */
+int ctcsd_attention_mass(ctcsd_handle* h, void* stream, const void* Q, const void* K, int Lcap,
+                         const int* kv_len, const int* acc_len, const int* acc_nodes, const float* lse,
+                         float scale, float decay, const int* n_evicted, float* mass, int* row_pos);
+
+/*
+ * ctcsd_evict_rows: a sequence with more than `budget` cached rows keeps `budget` of them, chosen per kv head:
+ * rows with row_pos < sinks and rows with row_pos >= n_evicted + kv_len - recent first, then by mass
+ * descending (NaN last), equal ranks by lower row index.  Row order means nothing to attention, so rows are
+ * not shifted: the k-th kept row at or behind `budget` moves into the k-th dropped row before it, in K, V, mass
+ * and row_pos; all other kept rows stay where they are.  Rows from the new length on are not meaningful.
+ * A sequence with kv_len <= budget keeps everything.
+ *   K, V [B,Hkv,Lcap,D] dtype, updated IN PLACE;  mass, row_pos [B,Hkv,Lcap];  kv_len, n_evicted [B];
+ *   budget >= 1, sinks, recent >= 0, sinks + recent <= budget;
+ *   out_mass, out_row_pos [B,Hkv,Lcap]: rows 0..new length-1 are written; either both are the arrays mass and
+ *   row_pos (in place: only what moves is written) or neither;
+ *   out_kv_len [B] = min(kv_len, budget), out_n_evicted [B] = n_evicted + kv_len - out_kv_len; they may be the
+ *   arrays kv_len and n_evicted.
+ * workspace: device memory of ctcsd_evict_rows_workspace_bytes(cfg, Lcap) bytes, 256-byte aligned, owned by the
+ * caller, used only during the call.  K and V 16-byte aligned.  A sequence with kv_len outside 0..Lcap is left
+ * unchanged and CTCSD_ERR_INVALID_ARG is recorded in the device status word.
+ */
+int ctcsd_evict_rows_workspace_bytes(const ctcsd_config* cfg, int Lcap, size_t* out_bytes);
+int ctcsd_evict_rows(ctcsd_handle* h, void* stream, void* workspace, size_t workspace_bytes,
+                     void* K, void* V, int Lcap, const float* mass, const int* row_pos,
+                     const int* kv_len, const int* n_evicted, int budget, int sinks, int recent,
+                     float* out_mass, int* out_row_pos, int* out_kv_len, int* out_n_evicted);
+
+/*
  * The paper's own verification layout (Sec. 3.3): instead of collapsing the slot paths before
  * the tree is built, the most probable RAW paths - blanks and repeats still in place - form the
  * token tree, and the CTC transform acts through the attention map: a position whose symbol the

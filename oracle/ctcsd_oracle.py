@@ -677,3 +677,91 @@ def draft_module(F_new: np.ndarray, n_new: np.ndarray, kv_len: np.ndarray, Kd: n
         F_hat[b] = h1 + Wdn @ act
         new_len[b] = n_keys
     return F_hat, Kd, Vd, new_len
+
+
+# --------------------------------------------------------------------------------------
+# Cache operators of a long-running batch (no counterpart in the paper): attention over a
+# prefix that the sequences share, the attention weight a cached row has gathered, and the
+# eviction of the rows that gathered least.
+# --------------------------------------------------------------------------------------
+def tree_attention_shared(Q: np.ndarray, Kp: np.ndarray, Vp: np.ndarray, prefix_len: np.ndarray,
+                          K: np.ndarray, Vc: np.ndarray, kv_len: np.ndarray, n_nodes: np.ndarray,
+                          mask: np.ndarray, scale: float) -> Tuple[np.ndarray, np.ndarray]:
+    """Sequence b's keys are the first prefix_len[b] rows of Kp [Hkv,Pcap,D], then its own as in
+    tree_attention.  Returns O [B,n_max,Hq,D] and the log-sum-exp [B,n_max,Hq] (dead rows 0 and -inf;
+    so is a live row that sees nothing)."""
+    B, n_max, Hq, D = Q.shape
+    grp = Hq // K.shape[1]
+    O = np.zeros((B, n_max, Hq, D), dtype=np.float64)
+    lse = np.full((B, n_max, Hq), NEG_INF, dtype=np.float64)
+    for b in range(B):
+        P, L, n = int(prefix_len[b]), int(kv_len[b]), int(n_nodes[b])
+        for h in range(Hq):
+            g = h // grp
+            keys = np.concatenate([np.asarray(Kp[g, :P], dtype=np.float64), np.asarray(K[b, g, :L + n], dtype=np.float64)])
+            vals = np.concatenate([np.asarray(Vp[g, :P], dtype=np.float64), np.asarray(Vc[b, g, :L + n], dtype=np.float64)])
+            for i in range(n):
+                seen = [j for j in range(P + L)] + [P + L + t for t in range(n) if (int(mask[b, i, t // 64]) >> (t % 64)) & 1]
+                if not seen:
+                    continue
+                s = (keys[seen] @ np.asarray(Q[b, i, h], dtype=np.float64)) * scale
+                top = s.max()
+                p = np.exp(s - top)
+                O[b, i, h] = (p / p.sum()) @ vals[seen]
+                lse[b, i, h] = top + np.log(p.sum())
+    return O, lse
+
+
+def attention_mass(Q: np.ndarray, K: np.ndarray, kv_len: np.ndarray, acc_len: np.ndarray, acc_nodes: np.ndarray,
+                   lse: np.ndarray, scale: float, decay: float, mass: np.ndarray, row_pos: np.ndarray,
+                   n_evicted: Optional[np.ndarray] = None) -> Tuple[np.ndarray, np.ndarray]:
+    """After the history update (kv_len counts the accepted rows): the accepted path's softmax weights on every
+    cached row, summed over its queries and the query heads of a kv head.  Returns new (mass, row_pos)."""
+    B, n_max, Hq, D = Q.shape
+    Hkv = K.shape[1]
+    grp = Hq // Hkv
+    mass, row_pos = np.array(mass, dtype=np.float64), np.array(row_pos)
+    for b in range(B):
+        acc, kv = int(acc_len[b]), int(kv_len[b])
+        base = kv - 1 - acc
+        mass[b, :, :base] *= decay
+        mass[b, :, base:kv] = 0.0
+        for j in range(base, kv):
+            row_pos[b, :, j] = (0 if n_evicted is None else int(n_evicted[b])) + j
+        path = [0] + [int(a) for a in acc_nodes[b, :acc]]
+        for l, node in enumerate(path):
+            for h in range(Hq):
+                if lse[b, node, h] == NEG_INF:
+                    continue
+                keys = np.asarray(K[b, h // grp, :base + l + 1], dtype=np.float64)
+                s = (keys @ np.asarray(Q[b, node, h], dtype=np.float64)) * scale
+                mass[b, h // grp, :base + l + 1] += np.exp(s - float(lse[b, node, h]))
+    return mass, row_pos
+
+
+def evict_rows(K: np.ndarray, Vc: np.ndarray, mass: np.ndarray, row_pos: np.ndarray, kv_len: np.ndarray,
+               n_evicted: np.ndarray, budget: int, sinks: int, recent: int):
+    """Keeps at most `budget` rows per (sequence, kv head): protected rows (the first `sinks` positions, the newest
+    `recent` ones), then the largest mass (NaN last), equal ranks by lower row; the k-th kept row at or behind
+    the budget moves into the k-th dropped row before it.  Returns new (K, Vc, mass, row_pos, kv_len, n_evicted)."""
+    K, Vc, mass, row_pos = (np.array(a, copy=True) for a in (K, Vc, mass, row_pos))
+    kv_len, n_evicted = np.array(kv_len, copy=True), np.array(n_evicted, copy=True)
+    for b in range(K.shape[0]):
+        L = int(kv_len[b])
+        if L <= budget:
+            continue
+        newest = int(n_evicted[b]) + L - recent
+        for g in range(K.shape[1]):
+            def rank(j):
+                safe = row_pos[b, g, j] < sinks or row_pos[b, g, j] >= newest
+                m = float(mass[b, g, j])
+                return (0 if safe else 1, 0 if safe else (1 if math.isnan(m) else 0), 0.0 if safe or math.isnan(m) else -m, j)
+            kept = set(sorted(range(L), key=rank)[:budget])
+            holes = [j for j in range(budget) if j not in kept]
+            movers = [j for j in range(budget, L) if j in kept]
+            for dst, src in zip(holes, movers):
+                K[b, g, dst], Vc[b, g, dst] = K[b, g, src], Vc[b, g, src]
+                mass[b, g, dst], row_pos[b, g, dst] = mass[b, g, src], row_pos[b, g, src]
+        n_evicted[b] += L - budget
+        kv_len[b] = budget
+    return K, Vc, mass, row_pos, kv_len, n_evicted

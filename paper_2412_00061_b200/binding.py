@@ -26,6 +26,7 @@ EXPORTS = [
     "ctcsd_verify_accept", "ctcsd_commit_accepted", "ctcsd_tree_attention_static", "ctcsd_draft_logits_rows",
     "ctcsd_verify_accept_sampled", "ctcsd_draft_module_workspace_bytes", "ctcsd_draft_module",
     "ctcsd_select_raw_paths", "ctcsd_build_raw_tree", "ctcsd_verify_accept_raw",
+    "ctcsd_attention_mass", "ctcsd_evict_rows_workspace_bytes", "ctcsd_evict_rows",
 ]
 
 
@@ -83,6 +84,9 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.ctcsd_select_raw_paths.argtypes = [vp, vp, ci] + [vp] * 6
     lib.ctcsd_build_raw_tree.argtypes = [vp, vp] + [vp] * 13
     lib.ctcsd_verify_accept_raw.argtypes = [vp, vp] + [vp] * 12
+    lib.ctcsd_attention_mass.argtypes = [vp, vp, vp, vp, ci, vp, vp, vp, vp, ctypes.c_float, ctypes.c_float, vp, vp, vp]
+    lib.ctcsd_evict_rows_workspace_bytes.argtypes = [ctypes.POINTER(CConfig), ci, ctypes.POINTER(cs)]
+    lib.ctcsd_evict_rows.argtypes = [vp, vp, vp, cs, vp, vp, ci, vp, vp, vp, vp, ci, ci, ci, vp, vp, vp, vp]
     lib.ctcsd_tree_attention_static.argtypes = [vp, ci, ci, ci, ci, ci, vp, vp, vp, ci, vp, vp, vp,
                                                 ctypes.c_float, vp, vp]
     for name in EXPORTS:
@@ -381,6 +385,49 @@ class Handle:
             _ptr(acc_nodes, i32, c.B * c.T, "acc_nodes"), _ptr(out_kv_len, i32, c.B, "out_kv_len"),
             _ptr(out_sel_row, i32, c.B, "out_sel_row"))
         self._check(rc, "commit_accepted")
+
+    # ---- cache eviction by gathered attention weight ----
+    def attention_mass(self, Q, K, kv_len, acc_len, acc_nodes, lse, scale, mass, row_pos, n_evicted=None, decay=1.0,
+                       stream=None):
+        """After commit_accepted: adds the accepted path's attention weights to `mass` (in place) and writes the
+        new rows' positions to `row_pos`.  kv_len is the length after the commit."""
+        c = self.cfg
+        i32, f32 = torch.int32, torch.float32
+        Lcap = K.shape[2]
+        rc = self.lib.ctcsd_attention_mass(
+            self._h, _stream_ptr(stream),
+            _ptr(Q, self.act_dtype, c.B * c.max_nodes * c.Hq * c.D, "Q"),
+            _ptr(K, self.act_dtype, c.B * c.Hkv * Lcap * c.D, "K"), Lcap,
+            _ptr(kv_len, i32, c.B, "kv_len"), _ptr(acc_len, i32, c.B, "acc_len"), _ptr(acc_nodes, i32, c.B * c.T, "acc_nodes"),
+            _ptr(lse, f32, c.B * c.max_nodes * c.Hq, "lse"), float(scale), float(decay),
+            _ptr(n_evicted, i32, c.B, "n_evicted"),
+            _ptr(mass, f32, c.B * c.Hkv * Lcap, "mass"), _ptr(row_pos, i32, c.B * c.Hkv * Lcap, "row_pos"))
+        self._check(rc, "attention_mass")
+
+    def make_eviction(self, Lcap):
+        """Allocates the workspace evict_rows needs for caches of Lcap rows."""
+        n = ctypes.c_size_t(0)
+        self._check(self.lib.ctcsd_evict_rows_workspace_bytes(ctypes.byref(self.cfg), Lcap, ctypes.byref(n)),
+                    "evict_rows_workspace_bytes")
+        ws = torch.empty(n.value + 256, dtype=torch.uint8, device=self.device)
+        return dict(ws=ws, ws_ptr=(ws.data_ptr() + 255) // 256 * 256, ws_bytes=n.value)
+
+    def evict_rows(self, ev, K, V, mass, row_pos, kv_len, n_evicted, budget, sinks, recent,
+                   out_mass, out_row_pos, out_kv_len, out_n_evicted, stream=None):
+        """Cuts every sequence's cache to `budget` rows (K, V in place).  out_mass / out_row_pos may be
+        mass / row_pos themselves, out_kv_len / out_n_evicted may be kv_len / n_evicted."""
+        c = self.cfg
+        i32, f32 = torch.int32, torch.float32
+        Lcap = K.shape[2]
+        rows = c.B * c.Hkv * Lcap
+        rc = self.lib.ctcsd_evict_rows(
+            self._h, _stream_ptr(stream), ev["ws_ptr"], ev["ws_bytes"],
+            _ptr(K, self.act_dtype, rows * c.D, "K"), _ptr(V, self.act_dtype, rows * c.D, "V"), Lcap,
+            _ptr(mass, f32, rows, "mass"), _ptr(row_pos, i32, rows, "row_pos"), _ptr(kv_len, i32, c.B, "kv_len"),
+            _ptr(n_evicted, i32, c.B, "n_evicted"), int(budget), int(sinks), int(recent),
+            _ptr(out_mass, f32, rows, "out_mass"), _ptr(out_row_pos, i32, rows, "out_row_pos"),
+            _ptr(out_kv_len, i32, c.B, "out_kv_len"), _ptr(out_n_evicted, i32, c.B, "out_n_evicted"))
+        self._check(rc, "evict_rows")
 
 
 def tree_attention_static(Q, K, V, kv_len, n_nodes, mask, scale, out_O, out_status=None, stream=None):

@@ -1,0 +1,308 @@
+// ctcsd_evict_rows: cuts every sequence's cache to a budget of rows, per kv head the ones with the most
+// gathered attention weight (ctcsd_attention_mass), the first `sinks` and the newest `recent` positions.
+//
+// Attention does not care about the order of cache rows, so nothing is shifted: the k-th kept row behind
+// the new length moves into the k-th dropped row before it.  Sources and destinations are then
+// disjoint ranges - no ordering between the copies - and a step that drops three rows moves three.  row_pos
+// holds every row's position, which is what "newest" is decided on.
+//
+// One thread-block cluster per (kv head, sequence): radix selection of the threshold (11 + 11 + 10 bits, the
+// histograms added up through distributed shared memory), ranks by ballots, then the copies.
+#include "common.cuh"
+#include "tc_primitives.cuh"
+
+#include <math.h>
+
+namespace ctcsd {
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+constexpr int kBins = 2048;
+constexpr int kCacheKeys = 8192;       // keys a CTA keeps in shared memory; a longer share is read again from L2
+constexpr int kMaxCluster = 8;
+
+struct EvictParams {
+    void* K; void* V;                  // [B,Hkv,Lcap,D]
+    const float* mass; const int* row_pos;         // [B,Hkv,Lcap]
+    const int* kv_len; const int* n_evicted;       // [B]
+    float* out_mass; int* out_row_pos; int* out_kv_len; int* out_n_evicted;
+    int* lists;                        // workspace [B,Hkv,Lcap]: dropped rows from the front, moving rows from the back
+    int B, Hkv, Lcap, row_bytes, budget, sinks, recent;
+    unsigned* seq_ticket;              // [B], zero between calls
+    int* status;
+};
+
+__device__ __forceinline__ void cluster_sync(int cs) {
+    if (cs == 1) __syncthreads();
+    else asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ int ld_peer(const int* local, int rank) {
+    uint32_t a;
+    int v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tc::smem_u32(local)), "r"(rank));
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+
+// Ranking key: larger is kept first.  Protected rows lead; then the weight, +0 and -0 alike, NaN last.
+__device__ __forceinline__ unsigned rank_key(float m, int pos, int sinks, int newest_from) {
+    if (pos < sinks || pos >= newest_from) return 0xffffffffu;
+    if (m != m) return 0u;
+    const unsigned u = __float_as_uint(m + 0.f);
+    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+struct EvictShared {
+    int hist[3][kBins];
+    int tot[kWarps];
+    int warp_cnt[3][kWarps];           // ties, dropped rows, moving rows per warp
+    int cta_cnt[3];
+    int pick[3];                       // digit, rows above it, rows in it
+};
+
+__global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, int cs) {
+    extern __shared__ __align__(16) unsigned char dyn[];
+    EvictShared* sh = reinterpret_cast<EvictShared*>(dyn);
+    unsigned* cache = reinterpret_cast<unsigned*>(sh + 1);                 // [kCacheKeys]
+    const int g = blockIdx.y, b = blockIdx.z, rank = blockIdx.x;           // a cluster is one row of the grid
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    pdl_wait();
+    pdl_trigger();
+    const int L = p.kv_len[b], ev = p.n_evicted[b];
+    const bool bad = L < 0 || L > p.Lcap;
+    if (bad && tid == 0 && rank == 0 && g == 0) report_error(p.status, CTCSD_ERR_INVALID_ARG, b);
+    const size_t row0 = ((size_t)b * p.Hkv + g) * (size_t)p.Lcap;
+    const float* mass = p.mass + row0;
+    const int* row_pos = p.row_pos + row0;
+    float* out_mass = p.out_mass + row0;
+    int* out_pos = p.out_row_pos + row0;
+    const bool in_place = p.mass == p.out_mass && p.row_pos == p.out_row_pos;
+    const int keep = L < p.budget ? L : p.budget;
+    const int share = ((L + cs - 1) / cs + 31) / 32 * 32;                  // rows of this CTA: [lo, hi)
+    const int lo = min(rank * share, L), hi = min(lo + share, L);
+
+    if (!bad && L <= p.budget) {
+        if (!in_place)
+            for (int j = lo + tid; j < hi; j += kThreads) { out_mass[j] = mass[j]; out_pos[j] = row_pos[j]; }
+    } else if (!bad) {
+        const int newest_from = ev + L - p.recent;
+        const bool cached = hi - lo <= kCacheKeys;
+        for (int i = tid; i < 3 * kBins; i += kThreads) sh->hist[i / kBins][i % kBins] = 0;
+        auto key_of = [&](int j) -> unsigned { return rank_key(mass[j], row_pos[j], p.sinks, newest_from); };
+        auto key_at = [&](int j) -> unsigned { return cached ? cache[j - lo] : key_of(j); };
+        __syncthreads();
+        // ---- threshold: the keep-th largest key, 11 + 11 + 10 bits from the top ----
+        unsigned prefix = 0u;
+        int shift = 32, left = keep;                                       // rows still to be found among the keys with this prefix
+        for (int rd = 0; rd < 3; ++rd) {
+            const int bits = rd == 2 ? 10 : 11, up = shift;
+            shift -= bits;
+            for (int j = lo + tid; j < hi; j += kThreads) {
+                unsigned key;
+                if (rd == 0) {
+                    key = key_of(j);
+                    if (cached) cache[j - lo] = key;
+                } else {
+                    key = key_at(j);
+                    if ((key >> up) != prefix) continue;
+                }
+                atomicAdd(&sh->hist[rd][(key >> shift) & ((1u << bits) - 1u)], 1);
+            }
+            cluster_sync(cs);
+            const int nb = 1 << bits;
+            // descending order of bins: thread t looks after bins nb-1-4t .. nb-4-4t
+            int v[kBins / kThreads], sum = 0;
+#pragma unroll
+            for (int i = 0; i < kBins / kThreads; ++i) {
+                const int bin = nb - 1 - (tid * (kBins / kThreads) + i);
+                v[i] = 0;
+                if (bin >= 0) {
+                    if (cs == 1) v[i] = sh->hist[rd][bin];
+                    else for (int c = 0; c < cs; ++c) v[i] += ld_peer(&sh->hist[rd][bin], c);
+                }
+                sum += v[i];
+            }
+            int incl = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += u;
+            }
+            if (lane == 31) sh->tot[warp] = incl;
+            __syncthreads();
+            int before = incl - sum;
+            for (int w = 0; w < warp; ++w) before += sh->tot[w];
+#pragma unroll
+            for (int i = 0; i < kBins / kThreads; ++i) {
+                if (before < left && before + v[i] >= left) {              // exactly one bin of one thread
+                    sh->pick[0] = nb - 1 - (tid * (kBins / kThreads) + i);
+                    sh->pick[1] = before;
+                    sh->pick[2] = v[i];
+                }
+                before += v[i];
+            }
+            __syncthreads();
+            prefix = (prefix << bits) | (unsigned)sh->pick[0];
+            left -= sh->pick[1];
+            const bool all = sh->pick[2] == left;                          // the whole bin stays: no need to look closer
+            __syncthreads();
+            if (all) break;
+        }
+        // rows whose key's top bits are above the threshold stay; of those equal to it the first `left`
+        const bool ties_split = shift == 0;
+        // every warp owns a contiguous run of rows, so that ranks follow row order
+        const int run = ((hi - lo + kWarps - 1) / kWarps + 31) / 32 * 32;
+        const int w0 = min(lo + warp * run, hi), w1 = min(w0 + run, hi);
+        int tie_base = 0;
+        if (ties_split) {
+            int cnt = 0;
+            for (int j = w0; j < w1; j += 32) {
+                const bool tie = j + lane < w1 && key_at(j + lane) == prefix;
+                cnt += __popc(__ballot_sync(0xffffffffu, tie));
+            }
+            if (lane == 0) sh->warp_cnt[0][warp] = cnt;
+            __syncthreads();
+            if (tid == 0) {
+                int s = 0;
+                for (int w = 0; w < kWarps; ++w) s += sh->warp_cnt[0][w];
+                sh->cta_cnt[0] = s;
+            }
+            cluster_sync(cs);
+            for (int c = 0; c < rank; ++c) tie_base += ld_peer(&sh->cta_cnt[0], c);
+            for (int w = 0; w < warp; ++w) tie_base += sh->warp_cnt[0][w];
+        }
+        // visits this warp's rows in order with (row, dropped before the new length, kept behind it)
+        auto visit = [&](auto&& f) {
+            int tie_rank = tie_base;
+            for (int j = w0; j < w1; j += 32) {
+                const int r = j + lane;
+                const bool in = r < w1;
+                const unsigned top = in ? key_at(r) >> shift : 0u;
+                bool kept = in && top > prefix;
+                const bool tie = in && top == prefix;
+                if (ties_split) {
+                    const unsigned m = __ballot_sync(0xffffffffu, tie);
+                    kept = kept || (tie && tie_rank + __popc(m & ((1u << lane) - 1u)) < left);
+                    tie_rank += __popc(m);
+                } else {
+                    kept = kept || tie;
+                }
+                f(r, in && !kept && r < keep, kept && r >= keep, kept && r < keep);
+            }
+        };
+        int holes = 0, movers = 0;
+        visit([&](int, bool hole, bool mover, bool) {
+            holes += __popc(__ballot_sync(0xffffffffu, hole));
+            movers += __popc(__ballot_sync(0xffffffffu, mover));
+        });
+        if (lane == 0) { sh->warp_cnt[1][warp] = holes; sh->warp_cnt[2][warp] = movers; }
+        __syncthreads();
+        if (tid < 2) {
+            int s = 0;
+            for (int w = 0; w < kWarps; ++w) s += sh->warp_cnt[1 + tid][w];
+            sh->cta_cnt[1 + tid] = s;
+        }
+        cluster_sync(cs);
+        int hole_at = 0, mover_at = 0, n_move = 0;
+        for (int c = 0; c < cs; ++c) {
+            const int x = ld_peer(&sh->cta_cnt[1], c), y = ld_peer(&sh->cta_cnt[2], c);
+            if (c < rank) { hole_at += x; mover_at += y; }
+            n_move += x;
+        }
+        for (int w = 0; w < warp; ++w) { hole_at += sh->warp_cnt[1][w]; mover_at += sh->warp_cnt[2][w]; }
+        // as many rows move as there are holes, at most half of L: the lists share one array of L entries
+        int* hole_list = p.lists + row0;
+        int* mover_list = p.lists + row0 + p.Lcap / 2;
+        visit([&](int r, bool hole, bool mover, bool stays) {
+            const unsigned mh = __ballot_sync(0xffffffffu, hole), mm = __ballot_sync(0xffffffffu, mover);
+            const unsigned below = (1u << lane) - 1u;
+            if (hole && CTCSD_IN_BOUNDS(p.status, 61, hole_at + __popc(mh & below), p.Lcap / 2)) hole_list[hole_at + __popc(mh & below)] = r;
+            if (mover && CTCSD_IN_BOUNDS(p.status, 62, mover_at + __popc(mm & below), p.Lcap - p.Lcap / 2))
+                mover_list[mover_at + __popc(mm & below)] = r;
+            hole_at += __popc(mh);
+            mover_at += __popc(mm);
+            if (stays && !in_place) { out_mass[r] = mass[r]; out_pos[r] = row_pos[r]; }
+        });
+        cluster_sync(cs);                                                  // the lists are complete; every weight has been read
+        // ---- the moves: 16 bytes per thread and tensor, neighbours on one row ----
+        const int chunks = p.row_bytes / 16;
+        unsigned char* Kb = static_cast<unsigned char*>(p.K) + row0 * p.row_bytes;
+        unsigned char* Vb = static_cast<unsigned char*>(p.V) + row0 * p.row_bytes;
+        const long long pieces = (long long)n_move * chunks;
+        for (long long i = (long long)rank * kThreads + tid; i < pieces; i += (long long)cs * kThreads) {
+            const int k = (int)(i / chunks), c = (int)(i - (long long)k * chunks);
+            const size_t src = (size_t)__ldcg(mover_list + k) * p.row_bytes + c * 16;
+            const size_t dst = (size_t)__ldcg(hole_list + k) * p.row_bytes + c * 16;
+            const uint4 kk = *reinterpret_cast<const uint4*>(Kb + src);
+            const uint4 vv = *reinterpret_cast<const uint4*>(Vb + src);
+            *reinterpret_cast<uint4*>(Kb + dst) = kk;
+            *reinterpret_cast<uint4*>(Vb + dst) = vv;
+        }
+        for (int k = rank * kThreads + tid; k < n_move; k += cs * kThreads) {
+            const int src = __ldcg(mover_list + k), dst = __ldcg(hole_list + k);
+            out_mass[dst] = mass[src];
+            out_pos[dst] = row_pos[src];
+        }
+    }
+    // out_kv_len / out_n_evicted may be the very input arrays: the last kv head's cluster writes them, when
+    // every head has read the old values (all CTAs of this cluster have: barrier)
+    cluster_sync(cs);
+    if (rank == 0 && tid == 0) {
+        __threadfence();
+        if (atomicAdd(&p.seq_ticket[b], 1u) == (unsigned)p.Hkv - 1u) {
+            p.seq_ticket[b] = 0u;
+            p.out_kv_len[b] = bad ? L : keep;
+            p.out_n_evicted[b] = bad ? ev : ev + (L - keep);
+        }
+    }
+}
+
+}  // namespace
+}  // namespace ctcsd
+
+using namespace ctcsd;
+
+extern "C" int ctcsd_evict_rows_workspace_bytes(const ctcsd_config* cfg, int Lcap, size_t* out_bytes) {
+    if (!cfg || !out_bytes || Lcap < 1) return CTCSD_ERR_INVALID_ARG;
+    const int rc = validate_config(*cfg);
+    if (rc != CTCSD_OK) return rc;
+    *out_bytes = align_up(sizeof(int) * (size_t)cfg->B * cfg->Hkv * Lcap, 256);
+    return CTCSD_OK;
+}
+
+extern "C" int ctcsd_evict_rows(ctcsd_handle* hh, void* stream, void* workspace, size_t workspace_bytes,
+                                void* K, void* V, int Lcap, const float* mass, const int* row_pos,
+                                const int* kv_len, const int* n_evicted, int budget, int sinks, int recent,
+                                float* out_mass, int* out_row_pos, int* out_kv_len, int* out_n_evicted) {
+    if (!hh || !K || !V || !mass || !row_pos || !kv_len || !n_evicted || !out_mass || !out_row_pos || !out_kv_len || !out_n_evicted)
+        return CTCSD_ERR_INVALID_ARG;
+    Handle* h = &hh->h;
+    const ctcsd_config& c = h->cfg;
+    if (Lcap < 1 || budget < 1 || sinks < 0 || recent < 0 || sinks > budget || recent > budget - sinks) return CTCSD_ERR_INVALID_ARG;
+    if ((out_mass == mass) != (out_row_pos == row_pos)) return CTCSD_ERR_INVALID_ARG;      // both in place or neither
+    if ((reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) & 15) return CTCSD_ERR_INVALID_ARG;
+    if (c.B > 65535 || c.Hkv > 65535) return CTCSD_ERR_UNSUPPORTED;
+    size_t need = 0;
+    const int rc = ctcsd_evict_rows_workspace_bytes(&c, Lcap, &need);
+    if (rc != CTCSD_OK) return rc;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < need) return CTCSD_ERR_WORKSPACE;
+    EvictParams p;
+    p.K = K; p.V = V; p.mass = mass; p.row_pos = row_pos; p.kv_len = kv_len; p.n_evicted = n_evicted;
+    p.out_mass = out_mass; p.out_row_pos = out_row_pos; p.out_kv_len = out_kv_len; p.out_n_evicted = out_n_evicted;
+    p.lists = static_cast<int*>(workspace);
+    p.B = c.B; p.Hkv = c.Hkv; p.Lcap = Lcap; p.budget = budget; p.sinks = sinks; p.recent = recent;
+    p.row_bytes = c.D * (c.dtype == CTCSD_DTYPE_BF16 ? 2 : 4);
+    p.seq_ticket = reinterpret_cast<unsigned*>(h->ws + h->lay.seq_ticket_off);
+    p.status = status_ptr(h);
+    // a cluster per (kv head, sequence): more CTAs while they all run at once (two fit on an SM) and each
+    // still has rows to look at
+    int cs = 1;
+    while (cs < kMaxCluster && (long long)c.B * c.Hkv * cs * 2 <= 2ll * h->num_sms && Lcap / (cs * 2) >= 1024) cs *= 2;
+    const size_t smem = sizeof(EvictShared) + sizeof(unsigned) * kCacheKeys;
+    CTCSD_CUDA_CHECK(h, cudaFuncSetAttribute(evict_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    CTCSD_CUDA_CHECK(h, launch_pdl(evict_rows_kernel, dim3(cs, c.Hkv, c.B), dim3(kThreads), smem,
+                                   static_cast<cudaStream_t>(stream), cs, p, cs));
+    h->launches++;
+    return CTCSD_OK;
+}
