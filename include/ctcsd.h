@@ -283,6 +283,36 @@ int ctcsd_commit_accepted(ctcsd_handle* h, void* stream, void* K, void* V, int L
                           int* out_kv_len, int* out_sel_row);
 
 /*
+ * Tree attention for a batch whose sequences share a prefix (a system prompt, few-shot examples, a document):
+ * the shared rows are kept once and read once for all sequences (the paper has no counterpart).
+ *   keys of sequence b = rows 0..prefix_len[b]-1 of the shared cache, rows 0..kv_len[b]-1 of its own cache,
+ *   and the tree rows of node i's mask, stored and masked as for ctcsd_tree_attention;
+ *   O[b,i,h,:] = softmax_j( scale * q[b,i,h,:].k_j ) v_j;   lse[b,i,h] = log sum_j exp( scale * q.k_j ).
+ * Without a prefix (Pcap = 0) it is ctcsd_tree_attention with the log-sum-exp as a second output, for any batch
+ * from single tokens (n_nodes = 1) to full trees: query rows of different sequences share a tile.
+ * Q [B,max_nodes,Hq,D] dtype;  Kp, Vp [Hkv,Pcap,D] dtype (NULL when Pcap is 0);  prefix_len [B] int32 in 0..Pcap
+ *   (NULL when Pcap is 0): sequences may share different lengths of the prefix, or none of it;
+ * K, V [B,Hkv,Lcap,D] dtype, node j's key/value at row kv_len[b]+j;  kv_len, n_nodes [B] int32, kv_len + n_nodes <= Lcap;
+ * mask as produced by ctcsd_build_tree;  scale > 0;
+ * out_O [B,max_nodes,Hq,D] dtype;  out_lse [B,max_nodes,Hq] float32 or NULL.  Rows of unused nodes, and of nodes
+ *   that see no key at all, are written as 0 and -inf.
+ * Positions: the tree nodes of sequence b sit at prefix_len + kv_len + depth (see ctcsd_evict_rows).
+ * What a row's mask hides does not reach it: keys or values there may be anything, NaN and infinities
+ * included (rows behind the lengths, other branches of the tree, other sequences).  A row that does see
+ * a NaN or infinite value is not meaningful.
+ * workspace: device memory of ctcsd_tree_attention_shared_workspace_bytes(cfg) bytes, 256-byte aligned, owned by the
+ *   caller, used only during the call (calls that overlap on the device need one each).
+ * Q, Kp, Vp, K, V, out_O 16-byte aligned.  A sequence whose lengths lie outside its arrays is treated as having no nodes and
+ * CTCSD_ERR_INVALID_ARG is recorded in the device status word.  Needs B <= 1024 and B*max_nodes*Hq/Hkv <= 524288
+ * (else CTCSD_ERR_UNSUPPORTED).
+ */
+int ctcsd_tree_attention_shared_workspace_bytes(const ctcsd_config* cfg, size_t* out_bytes);
+int ctcsd_tree_attention_shared(ctcsd_handle* h, void* stream, void* workspace, size_t workspace_bytes,
+                                const void* Q, const void* Kp, const void* Vp, int Pcap, const int* prefix_len,
+                                const void* K, const void* V, int Lcap, const int* kv_len, const int* n_nodes,
+                                const unsigned long long* mask, float scale, void* out_O, float* out_lse);
+
+/*
  * Cache eviction (the paper has no counterpart; it is what keeps a long-running batch inside a fixed cache).
  * Two calls after ctcsd_commit_accepted: the first adds up how much attention every cached row draws,
  * the second cuts every sequence's cache to a budget of rows and drops those that drew least.

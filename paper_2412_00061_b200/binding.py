@@ -26,7 +26,7 @@ EXPORTS = [
     "ctcsd_verify_accept", "ctcsd_commit_accepted", "ctcsd_tree_attention_static", "ctcsd_draft_logits_rows",
     "ctcsd_verify_accept_sampled", "ctcsd_draft_module_workspace_bytes", "ctcsd_draft_module",
     "ctcsd_select_raw_paths", "ctcsd_build_raw_tree", "ctcsd_verify_accept_raw",
-    "ctcsd_attention_mass", "ctcsd_evict_rows_workspace_bytes", "ctcsd_evict_rows",
+    "ctcsd_tree_attention_shared_workspace_bytes", "ctcsd_tree_attention_shared", "ctcsd_attention_mass", "ctcsd_evict_rows_workspace_bytes", "ctcsd_evict_rows",
 ]
 
 
@@ -84,6 +84,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.ctcsd_select_raw_paths.argtypes = [vp, vp, ci] + [vp] * 6
     lib.ctcsd_build_raw_tree.argtypes = [vp, vp] + [vp] * 13
     lib.ctcsd_verify_accept_raw.argtypes = [vp, vp] + [vp] * 12
+    lib.ctcsd_tree_attention_shared_workspace_bytes.argtypes = [ctypes.POINTER(CConfig), ctypes.POINTER(cs)]
+    lib.ctcsd_tree_attention_shared.argtypes = [vp, vp, vp, cs, vp, vp, vp, ci, vp, vp, vp, ci, vp, vp, vp, ctypes.c_float, vp, vp]
     lib.ctcsd_attention_mass.argtypes = [vp, vp, vp, vp, ci, vp, vp, vp, vp, ctypes.c_float, ctypes.c_float, vp, vp, vp]
     lib.ctcsd_evict_rows_workspace_bytes.argtypes = [ctypes.POINTER(CConfig), ci, ctypes.POINTER(cs)]
     lib.ctcsd_evict_rows.argtypes = [vp, vp, vp, cs, vp, vp, ci, vp, vp, vp, vp, ci, ci, ci, vp, vp, vp, vp]
@@ -385,6 +387,35 @@ class Handle:
             _ptr(acc_nodes, i32, c.B * c.T, "acc_nodes"), _ptr(out_kv_len, i32, c.B, "out_kv_len"),
             _ptr(out_sel_row, i32, c.B, "out_sel_row"))
         self._check(rc, "commit_accepted")
+
+    # ---- tree attention over a shared prefix ----
+    def make_shared_attention(self):
+        """Allocates the workspace tree_attention_shared needs."""
+        n = ctypes.c_size_t(0)
+        self._check(self.lib.ctcsd_tree_attention_shared_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(n)),
+                    "tree_attention_shared_workspace_bytes")
+        ws = torch.empty(n.value + 256, dtype=torch.uint8, device=self.device)
+        return dict(ws=ws, ws_ptr=(ws.data_ptr() + 255) // 256 * 256, ws_bytes=n.value)
+
+    def tree_attention_shared(self, sa, Q, Kp, Vp, prefix_len, K, V, kv_len, n_nodes, mask, scale, out_O, out_lse=None,
+                              stream=None):
+        """Tree attention whose sequences share the first prefix_len[b] rows of Kp, Vp [Hkv,Pcap,D] (all three None:
+        no prefix); out_lse receives the log-sum-exp."""
+        c = self.cfg
+        i32, act = torch.int32, self.act_dtype
+        Lcap = K.shape[2]
+        Pcap = 0 if Kp is None else Kp.shape[1]
+        W = (c.max_nodes + 63) // 64
+        rows = c.B * c.max_nodes * c.Hq
+        rc = self.lib.ctcsd_tree_attention_shared(
+            self._h, _stream_ptr(stream), sa["ws_ptr"], sa["ws_bytes"],
+            _ptr(Q, act, rows * c.D, "Q"), _ptr(Kp, act, c.Hkv * Pcap * c.D, "Kp"), _ptr(Vp, act, c.Hkv * Pcap * c.D, "Vp"),
+            Pcap, _ptr(prefix_len, i32, c.B, "prefix_len"),
+            _ptr(K, act, c.B * c.Hkv * Lcap * c.D, "K"), _ptr(V, act, c.B * c.Hkv * Lcap * c.D, "V"), Lcap,
+            _ptr(kv_len, i32, c.B, "kv_len"), _ptr(n_nodes, i32, c.B, "n_nodes"),
+            _ptr(mask, torch.int64, c.B * c.max_nodes * W, "mask"), float(scale),
+            _ptr(out_O, act, rows * c.D, "out_O"), _ptr(out_lse, torch.float32, rows, "out_lse"))
+        self._check(rc, "tree_attention_shared")
 
     # ---- cache eviction by gathered attention weight ----
     def attention_mass(self, Q, K, kv_len, acc_len, acc_nodes, lse, scale, mass, row_pos, n_evicted=None, decay=1.0,

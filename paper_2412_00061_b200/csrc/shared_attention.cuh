@@ -1,0 +1,262 @@
+// Shared-prefix tree attention: parameters, and the division of its work that the kernels share.
+//
+// Query rows.  All live rows of a kv head g - every live tree node of every sequence times the query
+// heads of the group - are numbered densely ("packed rows"): sequence b owns rows
+// row_off[b] .. row_off[b+1]-1, node by node, head by head.  A tile is TR consecutive packed rows and
+// may hold rows of several sequences, so that a batch of single tokens fills a tile as well as trees do.
+// Keys.  A tile's keys come in blocks of KB: first the shared prefix (as far as the longest share
+// among the tile's sequences), then each of its sequences' own rows (cache, then tree).  A row takes no
+// weight from keys that are not its own.
+// Balance.  The blocks of all (kv head, tile) pairs form one line, which is cut into equal spans, one
+// per CTA.  A tile inside one span is finished there; a tile that crosses a cut leaves (O, reference,
+// sum) of each part in the workspace and the merge kernel joins the parts.  A span has at most two such
+// parts: slot 0 continues a tile of the previous span, slot 1 begins a tile that the next one continues.
+#pragma once
+
+#include "common.cuh"
+
+namespace ctcsd {
+
+struct SharedAttnParams {
+    const void* Q;          // [B,max_nodes,Hq,D]
+    const void* Kp;         // [Hkv,Pcap,D], null without a prefix
+    const void* Vp;
+    const void* K;          // [B,Hkv,Lcap,D]
+    const void* V;
+    void* O;                // [B,max_nodes,Hq,D]
+    float* lse;             // [B,max_nodes,Hq] or null
+    const int* prefix_len;  // [B] or null
+    const int* kv_len;      // [B]
+    const int* n_nodes;     // [B]
+    const unsigned long long* mask;   // [B,max_nodes,ceil(max_nodes/64)]
+    int B, Hq, Hkv, D, max_nodes, Lcap, Pcap;
+    float scale;
+    int* status;
+    int* plan;              // workspace: header, row_off, tile_cum (written by CTA 0, read by the merge)
+    float4* part_o;         // workspace: [span][2][D/4][TR]
+    float2* part_ml;        // workspace: [span][2][TR] (reference in log2 units, sum)
+    int min_blocks;         // spans are not cut finer than this
+};
+
+constexpr int kSharedMaxB = 1024;              // sequences
+constexpr int kSharedMaxRows = 1 << 19;        // packed rows per kv head
+constexpr int kSharedSpansPerSm = 2;           // upper bound over the kernels
+constexpr int kPlanHeader = 8;                 // ints: rows, tiles, blocks per kv head, spans
+
+constexpr int kSimpleRows = 64;                // tile and block of the kernel without tensor cores
+constexpr int kSimpleKeys = 64;
+constexpr int kTcRows = 256;                   // of the tensor-core kernel (two 128-row halves)
+constexpr int kTcKeys = 128;
+
+// The plan's arrays in shared memory (kernels) or in host memory (tests).
+struct SharedPlan {
+    int* row_off;    // [B+1]
+    int* own_len;    // [B] own keys: cached + tree rows (0: the sequence takes no part)
+    int* kv;         // [B] cached rows
+    int* pre;        // [B] share of the prefix
+    int* tile_cum;   // [tiles+1] key blocks before each tile
+    int rows, tiles;
+};
+
+__host__ __device__ inline int plan_ints(int B, int max_tiles) { return 4 * (B + 1) + max_tiles + 1; }
+
+// Sequence that owns packed row r (0 <= r < rows).
+__host__ __device__ inline int plan_seq_of_row(const SharedPlan& p, int B, int r) {
+    int lo = 0, hi = B - 1;                    // smallest b with row_off[b+1] > r
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (p.row_off[mid + 1] > r) hi = mid; else lo = mid + 1;
+    }
+    return lo;
+}
+
+// What a tile looks at.
+struct TileInfo {
+    int row0, nrows;     // packed rows
+    int b0, b1;          // its first and last sequence
+    int pmax, pmin;      // longest and shortest share of the prefix among its sequences
+};
+
+__host__ __device__ inline TileInfo plan_tile(const SharedPlan& p, int B, int TR, int t) {
+    TileInfo ti;
+    ti.row0 = t * TR;
+    ti.nrows = p.rows - ti.row0 < TR ? p.rows - ti.row0 : TR;
+    ti.b0 = plan_seq_of_row(p, B, ti.row0);
+    ti.b1 = plan_seq_of_row(p, B, ti.row0 + ti.nrows - 1);
+    ti.pmax = 0;
+    ti.pmin = 0x7fffffff;
+    for (int b = ti.b0; b <= ti.b1; ++b) {
+        if (p.own_len[b] == 0) continue;
+        ti.pmax = p.pre[b] > ti.pmax ? p.pre[b] : ti.pmax;
+        ti.pmin = p.pre[b] < ti.pmin ? p.pre[b] : ti.pmin;
+    }
+    return ti;
+}
+
+__host__ __device__ inline int plan_tile_blocks(const SharedPlan& p, const TileInfo& ti, int KB) {
+    int n = (ti.pmax + KB - 1) / KB;
+    for (int b = ti.b0; b <= ti.b1; ++b) n += (p.own_len[b] + KB - 1) / KB;
+    return n;
+}
+
+// The line of blocks and its spans.
+struct SpanMap {
+    long long total;     // blocks of all kv heads
+    int per_head, spans;
+    __host__ __device__ long long start(int c) const { return total * c / spans; }
+    __host__ __device__ int span_of(long long x) const { return (int)(((x + 1) * spans - 1) / total); }
+};
+
+__host__ __device__ inline SpanMap span_map(int per_head, int Hkv, int max_spans, int min_blocks) {
+    SpanMap m;
+    m.per_head = per_head;
+    m.total = (long long)per_head * Hkv;
+    long long want = (m.total + min_blocks - 1) / min_blocks;
+    m.spans = (int)(want < 1 ? 1 : (want < max_spans ? want : max_spans));
+    return m;
+}
+
+// Tile that holds block x (0 <= x < tile_cum[tiles]) of a kv head.
+__host__ __device__ inline int plan_tile_of_block(const int* tile_cum, int tiles, int x) {
+    int lo = 0, hi = tiles - 1;                // smallest t with tile_cum[t+1] > x
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (tile_cum[mid + 1] > x) hi = mid; else lo = mid + 1;
+    }
+    return lo;
+}
+
+// Walks the key blocks of a tile.
+struct BlockIter {
+    int seq;             // -1: the shared prefix, else the sequence whose own rows these are
+    int key0;            // first key of the block within that source
+    int len;             // keys of that source
+    __host__ __device__ void init(const SharedPlan& p, const TileInfo& ti, int KB, int blk) {
+        const int pb = (ti.pmax + KB - 1) / KB;
+        if (blk < pb) { seq = -1; key0 = blk * KB; len = ti.pmax; return; }
+        blk -= pb;
+        int b = ti.b0;
+        for (; b < ti.b1; ++b) {
+            const int nb = (p.own_len[b] + KB - 1) / KB;
+            if (blk < nb) break;
+            blk -= nb;
+        }
+        seq = b; key0 = blk * KB; len = p.own_len[b];
+    }
+    // (only called while another block of the tile follows)
+    __host__ __device__ void next(const SharedPlan& p, const TileInfo& ti, int KB) {
+        key0 += KB;
+        if (key0 < len) return;
+        int b = seq < 0 ? ti.b0 : seq + 1;
+        while (b < ti.b1 && p.own_len[b] == 0) ++b;
+        seq = b; key0 = 0; len = p.own_len[b];
+    }
+};
+
+#ifdef __CUDACC__
+
+// Fills the plan's arrays; executed by the whole block, ends with a barrier.  A sequence whose lengths
+// would read outside its cache is reported (by the block that publishes) and takes no part.
+__device__ inline void plan_build(SharedPlan& p, const SharedAttnParams& a, int TR, int KB, bool publish) {
+    const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31;
+    const int grp = a.Hq / a.Hkv;
+    for (int b = tid; b < a.B; b += nt) {
+        int n = a.n_nodes[b], L = a.kv_len[b];
+        int P = a.prefix_len ? a.prefix_len[b] : 0;
+        if (n < 0 || n > a.max_nodes || L < 0 || L > a.Lcap - n || P < 0 || P > a.Pcap) {
+            if (publish) report_error(a.status, CTCSD_ERR_INVALID_ARG, b);
+            n = 0;
+        }
+        p.row_off[b + 1] = n * grp;
+        p.own_len[b] = n > 0 ? L + n : 0;
+        p.kv[b] = n > 0 ? L : 0;
+        p.pre[b] = n > 0 ? P : 0;
+    }
+    if (tid == 0) p.row_off[0] = 0;
+    __syncthreads();
+    if (tid < 32) {
+        int run = 0;
+        for (int b0 = 0; b0 < a.B; b0 += 32) {
+            int v = b0 + lane < a.B ? p.row_off[b0 + lane + 1] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, v, o);
+                if (lane >= o) v += u;
+            }
+            if (b0 + lane < a.B) p.row_off[b0 + lane + 1] = run + v;
+            run += __shfl_sync(0xffffffffu, v, 31);
+        }
+    }
+    __syncthreads();
+    p.rows = p.row_off[a.B];
+    p.tiles = (p.rows + TR - 1) / TR;
+    for (int t = tid; t < p.tiles; t += nt) p.tile_cum[t + 1] = plan_tile_blocks(p, plan_tile(p, a.B, TR, t), KB);
+    if (tid == 0) p.tile_cum[0] = 0;
+    __syncthreads();
+    if (tid < 32) {
+        int run = 0;
+        for (int t0 = 0; t0 < p.tiles; t0 += 32) {
+            int v = t0 + lane < p.tiles ? p.tile_cum[t0 + lane + 1] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, v, o);
+                if (lane >= o) v += u;
+            }
+            if (t0 + lane < p.tiles) p.tile_cum[t0 + lane + 1] = run + v;
+            run += __shfl_sync(0xffffffffu, v, 31);
+        }
+    }
+    __syncthreads();
+}
+
+// CTA 0 leaves what the merge kernel needs.
+__device__ inline void plan_publish(const SharedPlan& p, const SharedAttnParams& a, int spans) {
+    for (int b = threadIdx.x; b <= a.B; b += blockDim.x) a.plan[kPlanHeader + b] = p.row_off[b];
+    for (int t = threadIdx.x; t <= p.tiles; t += blockDim.x) a.plan[kPlanHeader + a.B + 1 + t] = p.tile_cum[t];
+    if (threadIdx.x == 0) {
+        a.plan[0] = p.rows;
+        a.plan[1] = p.tiles;
+        a.plan[2] = p.tile_cum[p.tiles];
+        a.plan[3] = spans;
+    }
+}
+
+// Visibility of the 32 keys key0 + c0 .. + 31 of a block for one row, as a bit mask.  `m0`, `m1`: the
+// row's first two ancestor words, `mrow` the whole mask row (W words).
+__device__ __forceinline__ uint32_t visible32_of(int seq, int first_key, int row_seq, int row_pre, int row_kv, int row_n,
+                                                 unsigned long long m0, unsigned long long m1,
+                                                 const unsigned long long* mrow, int W) {
+    if (seq < 0 || seq == row_seq) {
+        const int full = (seq < 0 ? row_pre : row_kv) - first_key;     // keys from here on that any row of the sequence sees
+        if (full >= 32) return 0xffffffffu;
+        uint32_t bits = full > 0 ? (1u << full) - 1u : 0u;
+        if (seq >= 0) {
+            const int t0 = first_key - row_kv;                         // tree index of the first key (may be negative)
+            if (t0 >= row_n) return bits;
+            unsigned long long w;
+            if (t0 < 0) {
+                w = t0 > -32 ? m0 << (-t0) : 0ull;
+            } else {
+                const int k = t0 >> 6, s = t0 & 63;
+                auto word = [&](int i) -> unsigned long long { return i == 0 ? m0 : (i == 1 ? m1 : (i < W ? mrow[i] : 0ull)); };
+                w = word(k) >> s;
+                if (s > 32) w |= word(k + 1) << (64 - s);
+            }
+            uint32_t tree = (uint32_t)w;
+            const int left = row_n - t0;                               // bits of nodes past the tree do not count
+            if (left < 32) tree &= (1u << left) - 1u;
+            bits |= tree;
+        }
+        return bits;
+    }
+    return 0u;
+}
+
+#endif  // __CUDACC__
+
+// bf16 on tcgen05 / tensor memory.
+int launch_shared_attention_tc(Handle* h, cudaStream_t s, const SharedAttnParams& p);
+// Joins the parts of tiles that cross a cut, zeroes the rows of unused nodes.
+int launch_shared_attention_merge(Handle* h, cudaStream_t s, const SharedAttnParams& p, int TR);
+
+}  // namespace ctcsd

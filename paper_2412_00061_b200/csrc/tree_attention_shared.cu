@@ -1,0 +1,452 @@
+// ctcsd_tree_attention_shared: tree attention for a batch whose sequences share a prefix, which is
+// read once for all of them.
+//   O[b,i,h] = sum_j p_j v_j,  p = softmax_j(scale q.k_j),  j over the first prefix_len[b] rows of the
+//   shared cache, the kv_len[b] rows of the sequence's own cache and the tree rows of node i's mask;
+//   lse[b,i,h] = log sum_j exp(scale q.k_j).
+// The work is divided as shared_attention.cuh describes.  This file holds the entry points, the kernel
+// without tensor cores (float32) and the merge of tiles that were cut.
+#include "shared_attention.cuh"
+
+#include <math.h>
+
+namespace ctcsd {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// ---------------------------------------------------------------------------------------
+// float32: 64 packed rows x 64 keys per step, 256 threads.  The FP32 pipe bounds it (4 D flops per row
+// and key), so a thread computes 4 x 4 scores and 4 x D/16 outputs from 128-bit shared loads; rows and
+// keys are dealt 16 apart, which keeps the loads free of bank conflicts (row stride D + 4).
+// K and V take turns in one buffer so that two CTAs fit on an SM and hide each other's loads.
+// ---------------------------------------------------------------------------------------
+constexpr int kSimpleThreads = 256;
+
+template <bool B> struct Flag { static constexpr bool value = B; };
+
+template <int D>
+__global__ void __launch_bounds__(kSimpleThreads, 2) shared_attention_simple_kernel(SharedAttnParams p) {
+    constexpr int TR = kSimpleRows, KB = kSimpleKeys, ST = D + 4, PS = KB + 4, DC = D / 64;
+    extern __shared__ __align__(16) float sm[];
+    float* Qs = sm;                      // [TR][ST]
+    float* Ts = Qs + TR * ST;            // [KB][ST]: a K block, then its V block
+    float* Ps = Ts + KB * ST;            // [TR][PS]
+    SharedPlan pl;
+    pl.row_off = reinterpret_cast<int*>(Ps + TR * PS);
+    pl.own_len = pl.row_off + p.B + 1;
+    pl.kv = pl.own_len + p.B;
+    pl.pre = pl.kv + p.B;
+    pl.tile_cum = pl.pre + p.B;
+
+    pdl_wait();
+    pdl_trigger();
+    plan_build(pl, p, TR, KB, blockIdx.x == 0);
+    const SpanMap sp = span_map(pl.tile_cum[pl.tiles], p.Hkv, (int)gridDim.x, p.min_blocks);
+    if (blockIdx.x == 0) plan_publish(pl, p, sp.spans);
+    if ((int)blockIdx.x >= sp.spans || sp.total == 0) return;
+
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    const int grp = p.Hq / p.Hkv;
+    const int W = (p.max_nodes + 63) / 64;
+    const float sl2 = p.scale * kLog2e;
+    const float* Q = static_cast<const float*>(p.Q);
+    const long long x1 = sp.start(blockIdx.x + 1);
+    const long long x0 = sp.start(blockIdx.x);
+    for (long long x = x0; x < x1;) {
+        const int g = (int)(x / sp.per_head);
+        const int xh = (int)(x - (long long)g * sp.per_head);
+        const int t = plan_tile_of_block(pl.tile_cum, pl.tiles, xh);
+        const TileInfo ti = plan_tile(pl, p.B, TR, t);
+        const int blk0 = xh - pl.tile_cum[t], nblk = pl.tile_cum[t + 1] - pl.tile_cum[t];
+        const int blk1 = (int)(x1 - x < nblk - blk0 ? blk0 + (x1 - x) : nblk);
+        x += blk1 - blk0;
+        const bool whole = blk0 == 0 && blk1 == nblk;
+        const int slot = blk0 > 0 ? 0 : 1;
+
+        __syncthreads();                 // the previous tile's shared memory is free
+        for (int i = tid; i < TR * (D / 4); i += kSimpleThreads) {
+            const int r = i / (D / 4), c = i - r * (D / 4);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (r < ti.nrows) {
+                const int pr = ti.row0 + r, b = plan_seq_of_row(pl, p.B, pr), o = pr - pl.row_off[b];
+                const int node = o / grp, hh = o - node * grp;
+                v = reinterpret_cast<const float4*>(Q + (((size_t)b * p.max_nodes + node) * p.Hq + g * grp + hh) * D)[c];
+            }
+            *reinterpret_cast<float4*>(Qs + r * ST + 4 * c) = v;
+        }
+        // what this thread's four rows are
+        int rseq[4], rnode[4];
+        size_t orow[4];                  // output row: ((b * max_nodes + node) * Hq + head)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = ty + 16 * i;
+            rseq[i] = -2; rnode[i] = 0; orow[i] = 0;
+            if (r < ti.nrows) {
+                const int pr = ti.row0 + r, b = plan_seq_of_row(pl, p.B, pr), o = pr - pl.row_off[b];
+                rseq[i] = b;
+                rnode[i] = o / grp;
+                orow[i] = ((size_t)b * p.max_nodes + rnode[i]) * p.Hq + g * grp + (o - rnode[i] * grp);
+            }
+        }
+        float acc[4][4 * DC], ref[4], sum[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            ref[i] = -INFINITY; sum[i] = 0.f;
+#pragma unroll
+            for (int d = 0; d < 4 * DC; ++d) acc[i][d] = 0.f;
+        }
+        BlockIter it;
+        it.init(pl, ti, KB, blk0);
+        for (int blk = blk0; blk < blk1; ++blk) {
+            const float *Kb, *Vb;
+            if (it.seq < 0) {
+                Kb = static_cast<const float*>(p.Kp) + (size_t)g * p.Pcap * D;
+                Vb = static_cast<const float*>(p.Vp) + (size_t)g * p.Pcap * D;
+            } else {
+                const size_t off = ((size_t)it.seq * p.Hkv + g) * (size_t)p.Lcap * D;
+                Kb = static_cast<const float*>(p.K) + off;
+                Vb = static_cast<const float*>(p.V) + off;
+            }
+            const int nkey = it.len - it.key0 < KB ? it.len - it.key0 : KB;
+            __syncthreads();             // V of the previous block has been read
+            for (int i = tid; i < KB * (D / 4); i += kSimpleThreads) {
+                const int k = i / (D / 4), c = i - k * (D / 4);
+                *reinterpret_cast<float4*>(Ts + k * ST + 4 * c) =
+                    k < nkey ? reinterpret_cast<const float4*>(Kb + (size_t)(it.key0 + k) * D)[c] : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            __syncthreads();
+            float s[4][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+            for (int d = 0; d < D; d += 4) {
+                float4 q4[4], k4[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q4[i] = *reinterpret_cast<const float4*>(Qs + (ty + 16 * i) * ST + d);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) k4[j] = *reinterpret_cast<const float4*>(Ts + (tx + 16 * j) * ST + d);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s[i][j] = fmaf(q4[i].x, k4[j].x, s[i][j]);
+                        s[i][j] = fmaf(q4[i].y, k4[j].y, s[i][j]);
+                        s[i][j] = fmaf(q4[i].z, k4[j].z, s[i][j]);
+                        s[i][j] = fmaf(q4[i].w, k4[j].w, s[i][j]);
+                    }
+            }
+            // masked scores become -inf by selection, so a NaN there does not count
+            bool mine = true;            // every key of the block is visible to all of this thread's rows
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t lo = 0u, hi = 0u;
+                if (rseq[i] >= 0) {
+                    const unsigned long long* mrow = p.mask + ((size_t)rseq[i] * p.max_nodes + rnode[i]) * W;
+                    const bool tail = it.seq == rseq[i] && it.key0 + KB > pl.kv[rseq[i]];
+                    const unsigned long long m0 = tail ? mrow[0] : 0ull, m1 = tail && W > 1 ? mrow[1] : 0ull;
+                    const int n = pl.own_len[rseq[i]] - pl.kv[rseq[i]];
+                    lo = visible32_of(it.seq, it.key0, rseq[i], pl.pre[rseq[i]], pl.kv[rseq[i]], n, m0, m1, mrow, W);
+                    hi = visible32_of(it.seq, it.key0 + 32, rseq[i], pl.pre[rseq[i]], pl.kv[rseq[i]], n, m0, m1, mrow, W);
+                }
+                mine = mine && (rseq[i] < 0 || (lo & hi) == 0xffffffffu);
+                float bm = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int k = tx + 16 * j;
+                    const bool vis = ((k < 32 ? lo >> k : hi >> (k - 32)) & 1u) != 0u;
+                    s[i][j] = vis ? s[i][j] * sl2 : -INFINITY;
+                    bm = fmaxf(bm, s[i][j]);
+                }
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, o));
+                const float nref = fmaxf(ref[i], bm);
+                const float base = nref == -INFINITY ? 0.f : nref;
+                const float corr = exp2_fast(ref[i] - base);             // 2^(-inf) = 0 before the first key
+                ref[i] = nref;
+                float ps = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float e = exp2_fast(s[i][j] - base);
+                    ps += e;
+                    Ps[(ty + 16 * i) * PS + tx + 16 * j] = e;
+                }
+                sum[i] = sum[i] * corr + ps;
+#pragma unroll
+                for (int d = 0; d < 4 * DC; ++d) acc[i][d] *= corr;
+            }
+            const bool open = __syncthreads_and(mine ? 1 : 0) != 0;      // K has been read, P is complete
+            for (int i = tid; i < KB * (D / 4); i += kSimpleThreads) {
+                const int k = i / (D / 4), c = i - k * (D / 4);
+                *reinterpret_cast<float4*>(Ts + k * ST + 4 * c) =
+                    k < nkey ? reinterpret_cast<const float4*>(Vb + (size_t)(it.key0 + k) * D)[c] : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            __syncthreads();
+            // In a block that some row sees only in part, a weight of zero must not meet a NaN or an infinity
+            // of a value that is not the row's: such products are left out.
+            auto pv = [&](auto guarded) {
+#pragma unroll 2
+                for (int k = 0; k < KB; k += 4) {
+                    float4 p4[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p4[i] = *reinterpret_cast<const float4*>(Ps + (ty + 16 * i) * PS + k);
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+                        for (int c = 0; c < DC; ++c) {
+                            const float4 v = *reinterpret_cast<const float4*>(Ts + (k + kk) * ST + 64 * c + 4 * tx);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float w = kk == 0 ? p4[i].x : (kk == 1 ? p4[i].y : (kk == 2 ? p4[i].z : p4[i].w));
+                                if (!decltype(guarded)::value || w != 0.f) {
+                                    acc[i][4 * c + 0] = fmaf(w, v.x, acc[i][4 * c + 0]);
+                                    acc[i][4 * c + 1] = fmaf(w, v.y, acc[i][4 * c + 1]);
+                                    acc[i][4 * c + 2] = fmaf(w, v.z, acc[i][4 * c + 2]);
+                                    acc[i][4 * c + 3] = fmaf(w, v.w, acc[i][4 * c + 3]);
+                                }
+                            }
+                        }
+                }
+            };
+            if (open) pv(Flag<false>()); else pv(Flag<true>());
+            if (blk + 1 < blk1) it.next(pl, ti, KB);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float s = sum[i];
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            const int r = ty + 16 * i;
+            if (rseq[i] < 0) continue;
+            if (whole) {
+                const float inv = s > 0.f ? 1.f / s : (s == 0.f ? 0.f : s);      // a NaN sum stays a NaN
+                float* out = static_cast<float*>(p.O) + orow[i] * D;
+#pragma unroll
+                for (int c = 0; c < DC; ++c)
+                    *reinterpret_cast<float4*>(out + 64 * c + 4 * tx) =
+                        make_float4(acc[i][4 * c] * inv, acc[i][4 * c + 1] * inv, acc[i][4 * c + 2] * inv, acc[i][4 * c + 3] * inv);
+                if (tx == 0 && p.lse) p.lse[orow[i]] = s == 0.f ? -INFINITY : (ref[i] + log2f(s)) * kLn2;
+            } else {
+                const size_t part = (size_t)blockIdx.x * 2 + slot;
+#pragma unroll
+                for (int c = 0; c < DC; ++c)
+                    p.part_o[(part * (D / 4) + 16 * c + tx) * TR + r] =
+                        make_float4(acc[i][4 * c], acc[i][4 * c + 1], acc[i][4 * c + 2], acc[i][4 * c + 3]);
+                if (tx == 0) p.part_ml[part * TR + r] = make_float2(ref[i], s);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Merge.  A block looks after 32 packed rows of one kv head (lane = row, so that the transposed parts are
+// read in whole lines; warps share the head dimension), and after as many output rows for the zero
+// rows of unused nodes.  Parts are joined in span order: the result does not depend on timing.
+// ---------------------------------------------------------------------------------------
+template <typename T> __device__ __forceinline__ void store8(T* out, const float (&v)[8]);
+template <> __device__ __forceinline__ void store8<float>(float* out, const float (&v)[8]) {
+    reinterpret_cast<float4*>(out)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+template <> __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16* out, const float (&v)[8]) {
+    __nv_bfloat162 w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<uint4*>(out) = *reinterpret_cast<uint4*>(w);
+}
+
+constexpr int kMergeThreads = 256;
+
+template <typename T, int D, int TR>
+__global__ void __launch_bounds__(kMergeThreads) shared_attention_merge_kernel(SharedAttnParams p, long long units) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int grp = p.Hq / p.Hkv;
+    pdl_wait();
+    pdl_trigger();
+    const int rows = p.plan[0], tiles = p.plan[1];
+    const SpanMap sp = {(long long)p.plan[2] * p.Hkv, p.plan[2], p.plan[3]};
+    const int* row_off = p.plan + kPlanHeader;
+    const int* tile_cum = row_off + p.B + 1;
+    const int max_rows = p.B * p.max_nodes * grp;            // packed rows if every node were live
+    const int chunks = (max_rows + 31) / 32;
+    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+        const int g = (int)(u / chunks), ch = (int)(u - (long long)g * chunks);
+        {   // zero rows: output row (b, node, head of group g) for the nodes that are not used
+            const int m = ch * 32 + lane;
+            if (m < max_rows) {
+                const int b = m / (p.max_nodes * grp), o = m - b * p.max_nodes * grp;
+                if (o >= row_off[b + 1] - row_off[b]) {
+                    const int node = o / grp;
+                    const size_t orow = ((size_t)b * p.max_nodes + node) * p.Hq + g * grp + (o - node * grp);
+                    const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    for (int c = warp; c < D / 8; c += kMergeThreads / 32) store8<T>(static_cast<T*>(p.O) + orow * D + 8 * c, z);
+                    if (warp == 0 && p.lse) p.lse[orow] = -INFINITY;
+                }
+            }
+        }
+        const int pr0 = ch * 32;
+        if (pr0 >= rows) continue;
+        const int t = pr0 / TR;                              // 32 divides TR: one tile for all lanes
+        const long long xs = (long long)g * sp.per_head + tile_cum[t], xe = (long long)g * sp.per_head + tile_cum[t + 1];
+        const int c0 = sp.span_of(xs), c1 = sp.span_of(xe - 1);
+        if (c0 == c1) continue;                              // finished by its span
+        const int pr = pr0 + lane;
+        if (pr >= rows) continue;
+        const int r = pr - t * TR;
+        float ref = -INFINITY, sum = 0.f;
+        for (int c = c0; c <= c1; ++c) {
+            const size_t part = (size_t)c * 2 + (sp.start(c) > xs ? 0 : 1);
+            ref = fmaxf(ref, p.part_ml[part * TR + r].x);
+        }
+        const float base = ref == -INFINITY ? 0.f : ref;
+        int lo = 0, hi = p.B - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (row_off[mid + 1] > pr) hi = mid; else lo = mid + 1;
+        }
+        const int o = pr - row_off[lo], node = o / grp;
+        const size_t orow = ((size_t)lo * p.max_nodes + node) * p.Hq + g * grp + (o - node * grp);
+        float a[(D / 8 + kMergeThreads / 32 - 1) / (kMergeThreads / 32)][8];
+        constexpr int NC = D / 8 / (kMergeThreads / 32);     // chunks of 8 columns per warp
+#pragma unroll
+        for (int k = 0; k < NC; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[k][e] = 0.f;
+        for (int c = c0; c <= c1; ++c) {
+            const size_t part = (size_t)c * 2 + (sp.start(c) > xs ? 0 : 1);
+            const float2 ml = p.part_ml[part * TR + r];
+            const float w = exp2_fast(ml.x - base);
+            sum = fmaf(w, ml.y, sum);
+            if (!(ml.y != 0.f)) continue;                    // this part saw nothing: its output is not meaningful
+#pragma unroll
+            for (int k = 0; k < NC; ++k) {
+                const int col = warp + k * (kMergeThreads / 32);
+                const float4 u0 = p.part_o[(part * (D / 4) + 2 * col) * TR + r];
+                const float4 u1 = p.part_o[(part * (D / 4) + 2 * col + 1) * TR + r];
+                a[k][0] = fmaf(w, u0.x, a[k][0]); a[k][1] = fmaf(w, u0.y, a[k][1]);
+                a[k][2] = fmaf(w, u0.z, a[k][2]); a[k][3] = fmaf(w, u0.w, a[k][3]);
+                a[k][4] = fmaf(w, u1.x, a[k][4]); a[k][5] = fmaf(w, u1.y, a[k][5]);
+                a[k][6] = fmaf(w, u1.z, a[k][6]); a[k][7] = fmaf(w, u1.w, a[k][7]);
+            }
+        }
+        const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[k][e] *= inv;
+            store8<T>(static_cast<T*>(p.O) + orow * D + 8 * (warp + k * (kMergeThreads / 32)), a[k]);
+        }
+        if (warp == 0 && p.lse) p.lse[orow] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+    }
+}
+
+template <typename T, int D, int TR>
+int launch_merge(Handle* h, cudaStream_t s, const SharedAttnParams& p) {
+    const long long max_rows = (long long)p.B * p.max_nodes * (p.Hq / p.Hkv);
+    const long long units = (max_rows + 31) / 32 * p.Hkv;
+    const long long cap = (long long)h->num_sms * 64;
+    CTCSD_CUDA_CHECK(h, launch_pdl(shared_attention_merge_kernel<T, D, TR>, dim3((unsigned)(units < cap ? units : cap)),
+                                   dim3(kMergeThreads), 0, s, 1, p, units));
+    h->launches++;
+    return CTCSD_OK;
+}
+
+template <int D>
+int launch_simple(Handle* h, cudaStream_t s, const SharedAttnParams& p) {
+    constexpr int TR = kSimpleRows, KB = kSimpleKeys;
+    const int max_tiles = (int)(((long long)p.B * p.max_nodes * (p.Hq / p.Hkv) + TR - 1) / TR);
+    const size_t smem = sizeof(float) * (TR * (D + 4) + KB * (D + 4) + TR * (KB + 4)) + sizeof(int) * plan_ints(p.B, max_tiles);
+    auto kern = shared_attention_simple_kernel<D>;
+    CTCSD_CUDA_CHECK(h, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(h->num_sms * kSharedSpansPerSm), dim3(kSimpleThreads), smem, s, 1, p));
+    h->launches++;
+    return CTCSD_OK;
+}
+
+// Workspace: plan, part sums, part outputs; sized for the larger of the two kernels' needs.
+struct SharedLayout { size_t plan, ml, o, total; };
+
+SharedLayout shared_layout(const ctcsd_config& c) {
+    const int sms = 160;
+    const bool tc = c.dtype == CTCSD_DTYPE_BF16;
+    const int TR = tc ? kTcRows : kSimpleRows;
+    const size_t spans = (size_t)sms * (tc ? 1 : kSharedSpansPerSm);
+    const long long rows = (long long)c.B * c.max_nodes * (c.Hq / c.Hkv);
+    SharedLayout l;
+    l.plan = 0;
+    l.ml = align_up(sizeof(int) * (size_t)(kPlanHeader + c.B + 1 + (rows + TR - 1) / TR + 1), 256);
+    l.o = align_up(l.ml + sizeof(float2) * spans * 2 * TR, 256);
+    l.total = align_up(l.o + sizeof(float) * spans * 2 * TR * (size_t)c.D, 256);
+    return l;
+}
+
+bool shared_supported(const ctcsd_config& c) {
+    return c.B <= kSharedMaxB && (long long)c.B * c.max_nodes * (c.Hq / c.Hkv) <= kSharedMaxRows;
+}
+
+}  // namespace
+
+int launch_shared_attention_merge(Handle* h, cudaStream_t s, const SharedAttnParams& p, int TR) {
+    if (TR == kTcRows) {
+        if (p.D == 64) return launch_merge<__nv_bfloat16, 64, kTcRows>(h, s, p);
+        return launch_merge<__nv_bfloat16, 128, kTcRows>(h, s, p);
+    }
+    if (p.D == 64) return launch_merge<float, 64, kSimpleRows>(h, s, p);
+    return launch_merge<float, 128, kSimpleRows>(h, s, p);
+}
+
+}  // namespace ctcsd
+
+using namespace ctcsd;
+
+extern "C" int ctcsd_tree_attention_shared_workspace_bytes(const ctcsd_config* cfg, size_t* out_bytes) {
+    if (!cfg || !out_bytes) return CTCSD_ERR_INVALID_ARG;
+    const int rc = validate_config(*cfg);
+    if (rc != CTCSD_OK) return rc;
+    if (!shared_supported(*cfg)) return CTCSD_ERR_UNSUPPORTED;
+    *out_bytes = shared_layout(*cfg).total;
+    return CTCSD_OK;
+}
+
+extern "C" int ctcsd_tree_attention_shared(ctcsd_handle* hh, void* stream, void* workspace, size_t workspace_bytes,
+                                           const void* Q, const void* Kp, const void* Vp, int Pcap, const int* prefix_len,
+                                           const void* K, const void* V, int Lcap, const int* kv_len, const int* n_nodes,
+                                           const unsigned long long* mask, float scale, void* out_O, float* out_lse) {
+    if (!hh || !Q || !K || !V || !kv_len || !n_nodes || !mask || !out_O) return CTCSD_ERR_INVALID_ARG;
+    Handle* h = &hh->h;
+    const ctcsd_config& c = h->cfg;
+    if (!shared_supported(c)) return CTCSD_ERR_UNSUPPORTED;
+    if (Lcap < 1 || Pcap < 0) return CTCSD_ERR_INVALID_ARG;
+    if (Pcap > 0 && (!Kp || !Vp || !prefix_len)) return CTCSD_ERR_INVALID_ARG;
+    if (!(scale > 0.f) || isinf(scale)) return CTCSD_ERR_INVALID_ARG;      // the row maximum is taken before scaling
+    const uintptr_t all = reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(Kp) | reinterpret_cast<uintptr_t>(Vp) |
+                          reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V) | reinterpret_cast<uintptr_t>(out_O);
+    if (all & 15) return CTCSD_ERR_INVALID_ARG;
+    const SharedLayout l = shared_layout(c);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < l.total) return CTCSD_ERR_WORKSPACE;
+    SharedAttnParams p;
+    p.Q = Q; p.Kp = Pcap > 0 ? Kp : nullptr; p.Vp = Pcap > 0 ? Vp : nullptr; p.K = K; p.V = V; p.O = out_O; p.lse = out_lse;
+    p.prefix_len = Pcap > 0 ? prefix_len : nullptr; p.kv_len = kv_len; p.n_nodes = n_nodes; p.mask = mask;
+    p.B = c.B; p.Hq = c.Hq; p.Hkv = c.Hkv; p.D = c.D; p.max_nodes = c.max_nodes; p.Lcap = Lcap; p.Pcap = Pcap;
+    p.scale = scale;
+    p.status = status_ptr(h);
+    char* ws = static_cast<char*>(workspace);
+    p.plan = reinterpret_cast<int*>(ws + l.plan);
+    p.part_ml = reinterpret_cast<float2*>(ws + l.ml);
+    p.part_o = reinterpret_cast<float4*>(ws + l.o);
+    p.min_blocks = 4;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int rc;
+    if (c.dtype == CTCSD_DTYPE_BF16) rc = launch_shared_attention_tc(h, s, p);
+    else rc = c.D == 64 ? launch_simple<64>(h, s, p) : launch_simple<128>(h, s, p);
+    if (rc != CTCSD_OK) return rc;
+    return launch_shared_attention_merge(h, s, p, c.dtype == CTCSD_DTYPE_BF16 ? kTcRows : kSimpleRows);
+}
