@@ -50,15 +50,27 @@ constexpr int kTcKeys = 128;
 
 // The plan's arrays in shared memory (kernels) or in host memory (tests).
 struct SharedPlan {
-    int* row_off;    // [B+1]
+    int* row_off;    // [B+1] packed rows before each sequence
+    int* own_cum;    // [B+1] blocks of own keys before each sequence
     int* own_len;    // [B] own keys: cached + tree rows (0: the sequence takes no part)
     int* kv;         // [B] cached rows
     int* pre;        // [B] share of the prefix
+    int* edge;       // [2] shortest and longest share among the sequences that take part
     int* tile_cum;   // [tiles+1] key blocks before each tile
     int rows, tiles;
 };
 
-__host__ __device__ inline int plan_ints(int B, int max_tiles) { return 4 * (B + 1) + max_tiles + 1; }
+__host__ __device__ inline int plan_ints(int B, int max_tiles) { return 2 * (B + 1) + 3 * B + 2 + max_tiles + 1; }
+
+__host__ __device__ inline void plan_carve(SharedPlan& p, int* at, int B) {
+    p.row_off = at;
+    p.own_cum = p.row_off + B + 1;
+    p.own_len = p.own_cum + B + 1;
+    p.kv = p.own_len + B;
+    p.pre = p.kv + B;
+    p.edge = p.pre + B;
+    p.tile_cum = p.edge + 2;
+}
 
 // Sequence that owns packed row r (0 <= r < rows).
 __host__ __device__ inline int plan_seq_of_row(const SharedPlan& p, int B, int r) {
@@ -68,6 +80,14 @@ __host__ __device__ inline int plan_seq_of_row(const SharedPlan& p, int B, int r
         if (p.row_off[mid + 1] > r) hi = mid; else lo = mid + 1;
     }
     return lo;
+}
+
+// Longest share of the prefix among sequences b0..b1.
+__host__ __device__ inline int plan_pre_max(const SharedPlan& p, int b0, int b1) {
+    if (p.edge[0] == p.edge[1]) return p.edge[1];          // all alike
+    int m = 0;
+    for (int b = b0; b <= b1; ++b) m = p.pre[b] > m ? p.pre[b] : m;
+    return m;
 }
 
 // What a tile looks at.
@@ -83,37 +103,53 @@ __host__ __device__ inline TileInfo plan_tile(const SharedPlan& p, int B, int TR
     ti.nrows = p.rows - ti.row0 < TR ? p.rows - ti.row0 : TR;
     ti.b0 = plan_seq_of_row(p, B, ti.row0);
     ti.b1 = plan_seq_of_row(p, B, ti.row0 + ti.nrows - 1);
-    ti.pmax = 0;
-    ti.pmin = 0x7fffffff;
-    for (int b = ti.b0; b <= ti.b1; ++b) {
-        if (p.own_len[b] == 0) continue;
-        ti.pmax = p.pre[b] > ti.pmax ? p.pre[b] : ti.pmax;
-        ti.pmin = p.pre[b] < ti.pmin ? p.pre[b] : ti.pmin;
+    ti.pmax = ti.pmin = p.edge[1];
+    if (p.edge[0] != p.edge[1]) {
+        ti.pmax = 0;
+        for (int b = ti.b0; b <= ti.b1; ++b) {
+            if (p.own_len[b] == 0) continue;
+            ti.pmax = p.pre[b] > ti.pmax ? p.pre[b] : ti.pmax;
+            ti.pmin = p.pre[b] < ti.pmin ? p.pre[b] : ti.pmin;
+        }
     }
     return ti;
 }
 
 __host__ __device__ inline int plan_tile_blocks(const SharedPlan& p, const TileInfo& ti, int KB) {
-    int n = (ti.pmax + KB - 1) / KB;
-    for (int b = ti.b0; b <= ti.b1; ++b) n += (p.own_len[b] + KB - 1) / KB;
-    return n;
+    return (ti.pmax + KB - 1) / KB + p.own_cum[ti.b1 + 1] - p.own_cum[ti.b0];
 }
 
-// The line of blocks and its spans.
+// The line of blocks and its spans (their lengths differ by one at most).
 struct SpanMap {
-    long long total;     // blocks of all kv heads
-    int per_head, spans;
-    __host__ __device__ long long start(int c) const { return total * c / spans; }
-    __host__ __device__ int span_of(long long x) const { return (int)(((x + 1) * spans - 1) / total); }
+    long long total, each;   // blocks of all kv heads; blocks of a span
+    int extra, spans;        // the first `extra` spans hold one more
+    int per_head;
+    __host__ __device__ long long start(int c) const { return each * c + (c < extra ? c : extra); }
+    __host__ __device__ int span_of(long long x) const {
+        const long long big = (each + 1) * extra;
+        return x < big ? (int)(x / (each + 1)) : extra + (int)((x - big) / each);
+    }
 };
 
-__host__ __device__ inline SpanMap span_map(int per_head, int Hkv, int max_spans, int min_blocks) {
+__host__ __device__ inline SpanMap span_map_n(int per_head, int Hkv, int spans) {
     SpanMap m;
     m.per_head = per_head;
     m.total = (long long)per_head * Hkv;
-    long long want = (m.total + min_blocks - 1) / min_blocks;
-    m.spans = (int)(want < 1 ? 1 : (want < max_spans ? want : max_spans));
+    m.spans = spans;
+    if (m.total < (1ll << 31)) {                           // (the short division)
+        m.each = (unsigned)m.total / (unsigned)spans;
+        m.extra = (int)((unsigned)m.total - (unsigned)m.each * (unsigned)spans);
+    } else {
+        m.each = m.total / spans;
+        m.extra = (int)(m.total - m.each * spans);
+    }
     return m;
+}
+
+// As many spans as `max_spans` allows, none shorter than min_blocks unless it is the only one.
+__host__ __device__ inline SpanMap span_map(int per_head, int Hkv, int max_spans, int min_blocks) {
+    const long long want = (long long)per_head * Hkv / min_blocks;
+    return span_map_n(per_head, Hkv, want < 1 ? 1 : (want < max_spans ? (int)want : max_spans));
 }
 
 // Tile that holds block x (0 <= x < tile_cum[tiles]) of a kv head.
@@ -126,6 +162,37 @@ __host__ __device__ inline int plan_tile_of_block(const int* tile_cum, int tiles
     return lo;
 }
 
+// Walks a span's parts: a (kv head, tile, range of blocks) at a time.
+struct SpanWalk {
+    int g, t, blk0, blk1, nblk;
+    long long rest;      // blocks of the span from this part on
+    __host__ __device__ bool init(const SharedPlan& p, const SpanMap& m, int span) {
+        const long long x = m.start(span);
+        rest = span < m.spans ? m.start(span + 1) - x : 0;
+        if (rest <= 0) { rest = 0; return false; }
+        g = x < (1ll << 31) ? (int)((unsigned)x / (unsigned)m.per_head) : (int)(x / m.per_head);
+        const int xh = (int)(x - (long long)g * m.per_head);
+        t = plan_tile_of_block(p.tile_cum, p.tiles, xh);
+        blk0 = xh - p.tile_cum[t];
+        clip(p);
+        return true;
+    }
+    __host__ __device__ bool next(const SharedPlan& p) {
+        rest -= blk1 - blk0;
+        if (rest <= 0) return false;
+        blk0 = 0;
+        if (++t == p.tiles) { t = 0; ++g; }
+        clip(p);
+        return true;
+    }
+    __host__ __device__ void clip(const SharedPlan& p) {
+        nblk = p.tile_cum[t + 1] - p.tile_cum[t];
+        blk1 = rest < nblk - blk0 ? blk0 + (int)rest : nblk;
+    }
+    __host__ __device__ bool whole() const { return blk0 == 0 && blk1 == nblk; }
+    __host__ __device__ int slot() const { return blk0 > 0 ? 0 : 1; }
+};
+
 // Walks the key blocks of a tile.
 struct BlockIter {
     int seq;             // -1: the shared prefix, else the sequence whose own rows these are
@@ -134,14 +201,13 @@ struct BlockIter {
     __host__ __device__ void init(const SharedPlan& p, const TileInfo& ti, int KB, int blk) {
         const int pb = (ti.pmax + KB - 1) / KB;
         if (blk < pb) { seq = -1; key0 = blk * KB; len = ti.pmax; return; }
-        blk -= pb;
-        int b = ti.b0;
-        for (; b < ti.b1; ++b) {
-            const int nb = (p.own_len[b] + KB - 1) / KB;
-            if (blk < nb) break;
-            blk -= nb;
+        blk += p.own_cum[ti.b0] - pb;
+        int lo = ti.b0, hi = ti.b1;            // smallest b with own_cum[b+1] > blk
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (p.own_cum[mid + 1] > blk) hi = mid; else lo = mid + 1;
         }
-        seq = b; key0 = blk * KB; len = p.own_len[b];
+        seq = lo; key0 = (blk - p.own_cum[lo]) * KB; len = p.own_len[lo];
     }
     // (only called while another block of the tile follows)
     __host__ __device__ void next(const SharedPlan& p, const TileInfo& ti, int KB) {
@@ -160,36 +226,56 @@ struct BlockIter {
 __device__ inline void plan_build(SharedPlan& p, const SharedAttnParams& a, int TR, int KB, bool publish) {
     const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31;
     const int grp = a.Hq / a.Hkv;
-    for (int b = tid; b < a.B; b += nt) {
-        int n = a.n_nodes[b], L = a.kv_len[b];
-        int P = a.prefix_len ? a.prefix_len[b] : 0;
-        if (n < 0 || n > a.max_nodes || L < 0 || L > a.Lcap - n || P < 0 || P > a.Pcap) {
-            if (publish) report_error(a.status, CTCSD_ERR_INVALID_ARG, b);
-            n = 0;
-        }
-        p.row_off[b + 1] = n * grp;
-        p.own_len[b] = n > 0 ? L + n : 0;
-        p.kv[b] = n > 0 ? L : 0;
-        p.pre[b] = n > 0 ? P : 0;
-    }
-    if (tid == 0) p.row_off[0] = 0;
-    __syncthreads();
     if (tid < 32) {
-        int run = 0;
+        int rows = 0, blocks = 0, pmin = 0x7fffffff, pmax = 0;
         for (int b0 = 0; b0 < a.B; b0 += 32) {
-            int v = b0 + lane < a.B ? p.row_off[b0 + lane + 1] : 0;
+            const int b = b0 + lane;
+            int n = 0, L = 0, P = 0;
+            if (b < a.B) {
+                n = a.n_nodes[b];
+                L = a.kv_len[b];
+                P = a.prefix_len ? a.prefix_len[b] : 0;
+                if (n < 0 || n > a.max_nodes || L < 0 || L > a.Lcap - n || P < 0 || P > a.Pcap) {
+                    if (publish) report_error(a.status, CTCSD_ERR_INVALID_ARG, b);
+                    n = 0;
+                }
+                if (n == 0) { L = 0; P = 0; }
+                p.own_len[b] = L + n;
+                p.kv[b] = L;
+                p.pre[b] = P;
+            }
+            if (n > 0) { pmin = min(pmin, P); pmax = max(pmax, P); }
+            int v = n * grp, w = (L + n + KB - 1) / KB;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v1 = __shfl_up_sync(0xffffffffu, v, o), w1 = __shfl_up_sync(0xffffffffu, w, o);
+                if (lane >= o) { v += v1; w += w1; }
+            }
+            if (b < a.B) { p.row_off[b + 1] = rows + v; p.own_cum[b + 1] = blocks + w; }
+            rows += __shfl_sync(0xffffffffu, v, 31);
+            blocks += __shfl_sync(0xffffffffu, w, 31);
+        }
+        pmin = __reduce_min_sync(0xffffffffu, pmin);
+        pmax = __reduce_max_sync(0xffffffffu, pmax);
+        if (lane == 0) { p.row_off[0] = 0; p.own_cum[0] = 0; p.edge[0] = min(pmin, pmax); p.edge[1] = pmax; }
+    }
+    __syncthreads();
+    p.rows = p.row_off[a.B];
+    p.tiles = (p.rows + TR - 1) / TR;
+    if (p.tiles <= 32) {                       // (one warp does it all)
+        if (tid < 32) {
+            int v = lane < p.tiles ? plan_tile_blocks(p, plan_tile(p, a.B, TR, lane), KB) : 0;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int u = __shfl_up_sync(0xffffffffu, v, o);
                 if (lane >= o) v += u;
             }
-            if (b0 + lane < a.B) p.row_off[b0 + lane + 1] = run + v;
-            run += __shfl_sync(0xffffffffu, v, 31);
+            if (lane < p.tiles) p.tile_cum[lane + 1] = v;
+            if (lane == 0) p.tile_cum[0] = 0;
         }
+        __syncthreads();
+        return;
     }
-    __syncthreads();
-    p.rows = p.row_off[a.B];
-    p.tiles = (p.rows + TR - 1) / TR;
     for (int t = tid; t < p.tiles; t += nt) p.tile_cum[t + 1] = plan_tile_blocks(p, plan_tile(p, a.B, TR, t), KB);
     if (tid == 0) p.tile_cum[0] = 0;
     __syncthreads();
@@ -221,35 +307,31 @@ __device__ inline void plan_publish(const SharedPlan& p, const SharedAttnParams&
     }
 }
 
-// Visibility of the 32 keys key0 + c0 .. + 31 of a block for one row, as a bit mask.  `m0`, `m1`: the
-// row's first two ancestor words, `mrow` the whole mask row (W words).
+// Visibility of the 32 keys from `first_key` on (of the shared prefix if seq < 0, else of that sequence's own
+// keys) for a row of sequence `row_seq`, as a bit mask.  mrow: the row's ancestor mask (W words).
 __device__ __forceinline__ uint32_t visible32_of(int seq, int first_key, int row_seq, int row_pre, int row_kv, int row_n,
-                                                 unsigned long long m0, unsigned long long m1,
                                                  const unsigned long long* mrow, int W) {
-    if (seq < 0 || seq == row_seq) {
-        const int full = (seq < 0 ? row_pre : row_kv) - first_key;     // keys from here on that any row of the sequence sees
-        if (full >= 32) return 0xffffffffu;
-        uint32_t bits = full > 0 ? (1u << full) - 1u : 0u;
-        if (seq >= 0) {
-            const int t0 = first_key - row_kv;                         // tree index of the first key (may be negative)
-            if (t0 >= row_n) return bits;
-            unsigned long long w;
-            if (t0 < 0) {
-                w = t0 > -32 ? m0 << (-t0) : 0ull;
-            } else {
-                const int k = t0 >> 6, s = t0 & 63;
-                auto word = [&](int i) -> unsigned long long { return i == 0 ? m0 : (i == 1 ? m1 : (i < W ? mrow[i] : 0ull)); };
-                w = word(k) >> s;
-                if (s > 32) w |= word(k + 1) << (64 - s);
-            }
-            uint32_t tree = (uint32_t)w;
-            const int left = row_n - t0;                               // bits of nodes past the tree do not count
-            if (left < 32) tree &= (1u << left) - 1u;
-            bits |= tree;
+    if (seq >= 0 && seq != row_seq) return 0u;
+    const int full = (seq < 0 ? row_pre : row_kv) - first_key;     // keys from here on that every row of the sequence sees
+    if (full >= 32) return 0xffffffffu;
+    uint32_t bits = full > 0 ? (1u << full) - 1u : 0u;
+    if (seq >= 0) {
+        const int t0 = first_key - row_kv;                         // tree index of the first key (may be negative)
+        if (t0 >= row_n || t0 <= -32) return bits;
+        unsigned long long w;
+        if (t0 < 0) {
+            w = mrow[0] << (-t0);
+        } else {
+            const int k = t0 >> 6, s = t0 & 63;
+            w = mrow[k] >> s;                                      // (t0 < row_n <= 64 W)
+            if (s > 32 && k + 1 < W) w |= mrow[k + 1] << (64 - s);
         }
-        return bits;
+        uint32_t tree = (uint32_t)w;
+        const int left = row_n - t0;                               // bits of nodes past the tree do not count
+        if (left < 32) tree &= (1u << left) - 1u;
+        bits |= tree;
     }
-    return 0u;
+    return bits;
 }
 
 #endif  // __CUDACC__

@@ -39,36 +39,24 @@ __global__ void __launch_bounds__(kSimpleThreads, 2) shared_attention_simple_ker
     float* Ts = Qs + TR * ST;            // [KB][ST]: a K block, then its V block
     float* Ps = Ts + KB * ST;            // [TR][PS]
     SharedPlan pl;
-    pl.row_off = reinterpret_cast<int*>(Ps + TR * PS);
-    pl.own_len = pl.row_off + p.B + 1;
-    pl.kv = pl.own_len + p.B;
-    pl.pre = pl.kv + p.B;
-    pl.tile_cum = pl.pre + p.B;
+    plan_carve(pl, reinterpret_cast<int*>(Ps + TR * PS), p.B);
 
     pdl_wait();
     pdl_trigger();
     plan_build(pl, p, TR, KB, blockIdx.x == 0);
     const SpanMap sp = span_map(pl.tile_cum[pl.tiles], p.Hkv, (int)gridDim.x, p.min_blocks);
     if (blockIdx.x == 0) plan_publish(pl, p, sp.spans);
-    if ((int)blockIdx.x >= sp.spans || sp.total == 0) return;
+    SpanWalk at;
 
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     const int grp = p.Hq / p.Hkv;
     const int W = (p.max_nodes + 63) / 64;
     const float sl2 = p.scale * kLog2e;
     const float* Q = static_cast<const float*>(p.Q);
-    const long long x1 = sp.start(blockIdx.x + 1);
-    const long long x0 = sp.start(blockIdx.x);
-    for (long long x = x0; x < x1;) {
-        const int g = (int)(x / sp.per_head);
-        const int xh = (int)(x - (long long)g * sp.per_head);
-        const int t = plan_tile_of_block(pl.tile_cum, pl.tiles, xh);
-        const TileInfo ti = plan_tile(pl, p.B, TR, t);
-        const int blk0 = xh - pl.tile_cum[t], nblk = pl.tile_cum[t + 1] - pl.tile_cum[t];
-        const int blk1 = (int)(x1 - x < nblk - blk0 ? blk0 + (x1 - x) : nblk);
-        x += blk1 - blk0;
-        const bool whole = blk0 == 0 && blk1 == nblk;
-        const int slot = blk0 > 0 ? 0 : 1;
+    for (bool more = at.init(pl, sp, blockIdx.x); more; more = at.next(pl)) {
+        const int g = at.g, blk0 = at.blk0, blk1 = at.blk1, slot = at.slot();
+        const bool whole = at.whole();
+        const TileInfo ti = plan_tile(pl, p.B, TR, at.t);
 
         __syncthreads();                 // the previous tile's shared memory is free
         for (int i = tid; i < TR * (D / 4); i += kSimpleThreads) {
@@ -151,11 +139,9 @@ __global__ void __launch_bounds__(kSimpleThreads, 2) shared_attention_simple_ker
                 uint32_t lo = 0u, hi = 0u;
                 if (rseq[i] >= 0) {
                     const unsigned long long* mrow = p.mask + ((size_t)rseq[i] * p.max_nodes + rnode[i]) * W;
-                    const bool tail = it.seq == rseq[i] && it.key0 + KB > pl.kv[rseq[i]];
-                    const unsigned long long m0 = tail ? mrow[0] : 0ull, m1 = tail && W > 1 ? mrow[1] : 0ull;
                     const int n = pl.own_len[rseq[i]] - pl.kv[rseq[i]];
-                    lo = visible32_of(it.seq, it.key0, rseq[i], pl.pre[rseq[i]], pl.kv[rseq[i]], n, m0, m1, mrow, W);
-                    hi = visible32_of(it.seq, it.key0 + 32, rseq[i], pl.pre[rseq[i]], pl.kv[rseq[i]], n, m0, m1, mrow, W);
+                    lo = visible32_of(it.seq, it.key0, rseq[i], pl.pre[rseq[i]], pl.kv[rseq[i]], n, mrow, W);
+                    hi = visible32_of(it.seq, it.key0 + 32, rseq[i], pl.pre[rseq[i]], pl.kv[rseq[i]], n, mrow, W);
                 }
                 mine = mine && (rseq[i] < 0 || (lo & hi) == 0xffffffffu);
                 float bm = -INFINITY;
@@ -272,7 +258,7 @@ __global__ void __launch_bounds__(kMergeThreads) shared_attention_merge_kernel(S
     pdl_wait();
     pdl_trigger();
     const int rows = p.plan[0], tiles = p.plan[1];
-    const SpanMap sp = {(long long)p.plan[2] * p.Hkv, p.plan[2], p.plan[3]};
+    const SpanMap sp = span_map_n(p.plan[2], p.Hkv, p.plan[3]);
     const int* row_off = p.plan + kPlanHeader;
     const int* tile_cum = row_off + p.B + 1;
     const int max_rows = p.B * p.max_nodes * grp;            // packed rows if every node were live

@@ -2,23 +2,26 @@
 //
 // Persistent CTAs, one per SM, each with a span of the line of key blocks (shared_attention.cuh).  A tile
 // is 256 packed query rows in two halves of 128; every 128-key block of K and V is loaded once and serves
-// both halves.  Per half and block:
-//   S[128 x 128] = Q K^T     tcgen05.mma, operands in shared memory (128-byte swizzle), S in tensor memory;
-//   softmax                  one thread per query row reads its 128 scores at once, P = 2^(S - ref) goes back
+// both halves, in two steps of 64 keys.  Per half and step:
+//   S[128 x 64] = Q K^T      tcgen05.mma, operands in shared memory (128-byte swizzle), S in tensor memory;
+//   softmax                  one thread per query row reads its 64 scores at once, P = 2^(S - ref) goes back
 //                            to tensor memory as bf16, over the scores it came from;
 //   O[128 x D] += P V        tcgen05.mma with P from tensor memory and V as an MN-major operand.
-// The halves take turns: while one half's softmax runs, the tensor core works on the other's products.
+// A half's two steps have a place of their own in tensor memory, so the scores of the next step are made while the
+// current one is weighed, and the two halves fill each other's gaps besides.  (Measured: steps of 128 keys, one
+// place per half, ran 1.6 times longer: scores, maximum, exponentials, P V and the next scores then
+// form one chain of about 4600 cycles, against 2700 of tensor-core work for both halves.)
 // With at most 128 rows in a tile both halves work on the same rows, one on the even and one on the odd
 // blocks, and their outputs are joined at the end: short batches keep both pipes busy too.
 // ref, the exponent's reference, follows the row maximum lazily (only when it falls kSlack behind), so that O
 // is hardly ever rescaled; sums and outputs are float32 throughout, P alone is rounded to bf16.
 //
-// Warp 0 loads K/V (TMA), warp 1 issues the MMAs, warps 2-3 look after V rows that hold NaN or infinities, warps
-// 4-7 and 8-11 are the softmax warps of the two halves.
+// Warp 0 loads K/V (TMA), warps 1 and 2 issue the MMAs of one half each, warp 3 looks after V rows that hold NaN
+// or infinities, warps 4-7 and 8-11 are the softmax warps of the two halves.
 //
 // A weight of zero does not cancel a NaN.  In a block that some row of the tile sees only in part (ends of
-// caches, trees, several sequences in one tile), warps 2-3 clear V rows that hold a NaN or an infinity
-// before P V reads them, and leave a note; a row that does see such a key becomes NaN at the end.
+// caches, trees, several sequences in one tile), warp 3 clears V rows that hold a NaN or an infinity
+// before P V reads them, and leaves a note; a row that does see such a key becomes NaN at the end.
 // One sequence's bad cache, or stale rows behind its end, cannot reach another sequence.
 #include "shared_attention.cuh"
 #include "tc_primitives.cuh"
@@ -31,10 +34,14 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kHalf = 128;             // rows per half
 constexpr int kKeys = kTcKeys;
+constexpr int kStep = 64;              // keys weighed at a time
 constexpr float kSlack = 8.f;          // log2 units: P stays below 2^8
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kNoteBits = 2048;
+constexpr int kPolyOf8 = 3;            // of 8 pairs of exponentials, how many the FMA pipe computes
+
+template <bool B> struct Flag { static constexpr bool value = B; };
 
 template <int D> struct Shape;
 template <> struct Shape<128> { static constexpr int kStages = 2; };
@@ -44,7 +51,8 @@ struct __align__(8) SharedState {
     uint64_t q_full;
     uint64_t k_full[4], k_empty[4];
     uint64_t v_full[4], v_empty[4], v_ok[4];     // v_ok: the V block has been looked over
-    uint64_t s_full[2], p_full[2], o_full[2];
+    uint64_t s_full[2][2], p_full[2][2];         // per half and step
+    uint64_t pv_done[2], o_full[2];              // P V of a step; of the piece
     uint32_t tmem_base;
     int abort_flag, never_set;
     int any_note;
@@ -56,6 +64,50 @@ __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// Two float32 in one 64-bit register pair: the packed instructions halve the issue slots.
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void pair_split(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// Maximum of three; a NaN among them comes out.
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// 2^x of a pair on the FMA pipe.  x = i + f with i the nearest integer (taken from the low bits of x + 1.5 * 2^23)
+// and |f| <= 1/2; 2^f is the degree-4 polynomial of least relative error there (computed with the Remez
+// exchange; 2.7e-6 in float32, far below the rounding of P to bf16, and 1e-6 of a log-sum-exp at most);
+// i is added to the exponent field.  x is held at -126: what lies below is zero to any sum.
+__device__ __forceinline__ uint64_t exp2_poly2(uint64_t x) {
+    float a, b;
+    pair_split(x, a, b);
+    x = pair_of(fmaxf(a, -126.f), fmaxf(b, -126.f));
+    const float magic = 12582912.f;
+    const uint64_t t = add2(x, pair_of(magic, magic));
+    const uint64_t r = add2(t, pair_of(-magic, -magic));
+    const uint64_t f = fma2(r, pair_of(-1.f, -1.f), x);
+    uint64_t y = fma2(pair_of(0x1.3997d6p-7f, 0x1.3997d6p-7f), f, pair_of(0x1.ca1440p-5f, 0x1.ca1440p-5f));
+    y = fma2(y, f, pair_of(0x1.ec06dap-3f, 0x1.ec06dap-3f));
+    y = fma2(y, f, pair_of(0x1.62e0dcp-1f, 0x1.62e0dcp-1f));
+    y = fma2(y, f, pair_of(0x1.ffffe8p-1f, 0x1.ffffe8p-1f));
+    float ta, tb, ya, yb;
+    pair_split(t, ta, tb);
+    pair_split(y, ya, yb);
+    return pair_of(__int_as_float(__float_as_int(ya) + (__float_as_int(ta) << 23)), __int_as_float(__float_as_int(yb) + (__float_as_int(tb) << 23)));
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -70,35 +122,32 @@ __device__ __forceinline__ void give_up(SharedState* sh, int* status, int site) 
 // All softmax threads (both halves) meet here.
 __device__ __forceinline__ void halves_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
-// One part of the span: blocks [blk0, blk1) of a tile of a kv head, and what every role has to know of it.
+// What every role has to know of a part of the span.
 struct Piece {
     TileInfo ti;
     int g, blk0, blk1;
-    bool whole, split_keys;            // split_keys: both halves serve the same rows
-    int slot;
-    int sb0[2], sb1[2];                // sequences of each half
-    int spre[2];                       // longest prefix share of each half
+    bool split_keys;                   // both halves serve the same rows
+    int seq_a, seq_b;                  // last sequence of the first half, first sequence of the second
+    int pre_a, pre_b;                  // longest prefix share of each half
 };
 
-__device__ __forceinline__ Piece make_piece(const SharedPlan& pl, const SharedAttnParams& p, const SpanMap& sp, long long x, long long x1) {
+__device__ __forceinline__ Piece make_piece(const SharedPlan& pl, int B, const SpanWalk& at) {
     Piece c;
-    c.g = (int)(x / sp.per_head);
-    const int xh = (int)(x - (long long)c.g * sp.per_head);
-    const int t = plan_tile_of_block(pl.tile_cum, pl.tiles, xh);
-    c.ti = plan_tile(pl, p.B, kTcRows, t);
-    const int nblk = pl.tile_cum[t + 1] - pl.tile_cum[t];
-    c.blk0 = xh - pl.tile_cum[t];
-    c.blk1 = (int)(x1 - x < nblk - c.blk0 ? c.blk0 + (x1 - x) : nblk);
-    c.whole = c.blk0 == 0 && c.blk1 == nblk;
-    c.slot = c.blk0 > 0 ? 0 : 1;
+    c.g = at.g;
+    c.blk0 = at.blk0;
+    c.blk1 = at.blk1;
+    c.ti = plan_tile(pl, B, kTcRows, at.t);
     c.split_keys = c.ti.nrows <= kHalf;
-    c.sb0[0] = c.ti.b0;
-    c.sb1[1] = c.ti.b1;
-    c.sb1[0] = c.split_keys ? c.ti.b1 : plan_seq_of_row(pl, p.B, c.ti.row0 + kHalf - 1);
-    c.sb0[1] = c.split_keys ? c.ti.b0 : plan_seq_of_row(pl, p.B, c.ti.row0 + kHalf);
-    for (int s = 0; s < 2; ++s) {
-        c.spre[s] = 0;
-        for (int b = c.sb0[s]; b <= c.sb1[s]; ++b) c.spre[s] = max(c.spre[s], pl.pre[b]);
+    c.seq_a = c.ti.b1;
+    c.seq_b = c.ti.b0;
+    c.pre_a = c.pre_b = c.ti.pmax;
+    if (!c.split_keys && c.ti.b0 != c.ti.b1) {
+        c.seq_a = plan_seq_of_row(pl, B, c.ti.row0 + kHalf - 1);
+        c.seq_b = plan_seq_of_row(pl, B, c.ti.row0 + kHalf);
+        if (c.ti.pmin != c.ti.pmax) {
+            c.pre_a = plan_pre_max(pl, c.ti.b0, c.seq_a);
+            c.pre_b = plan_pre_max(pl, c.seq_b, c.ti.b1);
+        }
     }
     return c;
 }
@@ -106,13 +155,9 @@ __device__ __forceinline__ Piece make_piece(const SharedPlan& pl, const SharedAt
 // Which halves work on a block, as a bit mask.
 __device__ __forceinline__ unsigned takers(const Piece& c, const BlockIter& it, int blk) {
     if (c.split_keys) return 1u << ((blk - c.blk0) & 1);
-    unsigned m = 0u;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        const bool in = it.seq < 0 ? it.key0 < c.spre[s] : (it.seq >= c.sb0[s] && it.seq <= c.sb1[s]);
-        m |= in ? 1u << s : 0u;
-    }
-    return m;
+    const bool a = it.seq < 0 ? it.key0 < c.pre_a : it.seq <= c.seq_a;
+    const bool b = it.seq < 0 ? it.key0 < c.pre_b : it.seq >= c.seq_b;
+    return (a ? 1u : 0u) | (b ? 2u : 0u);
 }
 
 // Whether some row of the tile sees the block only in part.
@@ -135,11 +180,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
     unsigned char* Vs = Ks + NS * kTile;
     SharedState* sh = reinterpret_cast<SharedState*>(Vs + NS * kTile);
     SharedPlan pl;
-    pl.row_off = reinterpret_cast<int*>(sh + 1);
-    pl.own_len = pl.row_off + p.B + 1;
-    pl.kv = pl.own_len + p.B;
-    pl.pre = pl.kv + p.B;
-    pl.tile_cum = pl.pre + p.B;
+    plan_carve(pl, reinterpret_cast<int*>(sh + 1), p.B);
     if ((tc::smem_u32(dyn) & 1023u) != 0u) {                   // uniform over the CTA
         if (threadIdx.x == 0) report_error(p.status, CTCSD_ERR_INTERNAL, 34);
         return;
@@ -149,13 +190,16 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
     if (tid == 0) {
         tc::mbar_init(&sh->q_full, 8);
         for (int s = 0; s < NS; ++s) {
-            tc::mbar_init(&sh->k_full[s], 1); tc::mbar_init(&sh->k_empty[s], 1);
-            tc::mbar_init(&sh->v_full[s], 1); tc::mbar_init(&sh->v_empty[s], 1);
-            tc::mbar_init(&sh->v_ok[s], 2);
+            tc::mbar_init(&sh->k_full[s], 1); tc::mbar_init(&sh->k_empty[s], 2);
+            tc::mbar_init(&sh->v_full[s], 1); tc::mbar_init(&sh->v_empty[s], 2);
+            tc::mbar_init(&sh->v_ok[s], 1);
         }
         for (int s = 0; s < 2; ++s) {
-            tc::mbar_init(&sh->s_full[s], 1);
-            tc::mbar_init(&sh->p_full[s], 4);
+            for (int e = 0; e < 2; ++e) {
+                tc::mbar_init(&sh->s_full[s][e], 1);
+                tc::mbar_init(&sh->p_full[s][e], 4);
+            }
+            tc::mbar_init(&sh->pv_done[s], 1);
             tc::mbar_init(&sh->o_full[s], 1);
         }
         sh->abort_flag = 0;
@@ -178,18 +222,17 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
     plan_build(pl, p, kTcRows, kKeys, blockIdx.x == 0);
     const SpanMap sp = span_map(pl.tile_cum[pl.tiles], p.Hkv, (int)gridDim.x, p.min_blocks);
     if (blockIdx.x == 0) plan_publish(pl, p, sp.spans);
-    const bool idle = (int)blockIdx.x >= sp.spans || sp.total == 0;
-    const long long xbeg = idle ? 0 : sp.start(blockIdx.x), xend = idle ? 0 : sp.start(blockIdx.x + 1);
     bool failed = false;
+    SpanWalk at;
+    bool more = at.init(pl, sp, blockIdx.x);
 
     if (warp == 0) {
         // ---------------- TMA producer ----------------
         if (lane == 0) {
             const uint64_t pol = tc::policy_evict_last();
             int fill = 0;
-            for (long long x = xbeg; x < xend && !failed;) {
-                const Piece c = make_piece(pl, p, sp, x, xend);
-                x += c.blk1 - c.blk0;
+            for (; more && !failed; more = at.next(pl)) {
+                const Piece c = make_piece(pl, p.B, at);
                 BlockIter it;
                 it.init(pl, c.ti, kKeys, c.blk0);
                 for (int blk = c.blk0; blk < c.blk1; ++blk, ++fill) {
@@ -218,94 +261,100 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                 }
             }
         }
-    } else if (warp == 1) {
-        // ---------------- MMA issuer ----------------
+    } else if (warp < 3) {
+        // ---------------- MMA issuer of one half ----------------
+        // Both issuers visit every fill of the rings in order; for a block that is not its half's, an
+        // issuer only hands the buffers back.
         if (lane == 0) {
-            const uint32_t idesc_s = tc::idesc_bf16_f32(kHalf, kKeys);
+            const int half = warp - 1;
+            const uint32_t idesc_s = tc::idesc_bf16_f32(kHalf, kStep);
             const uint32_t idesc_o = tc::idesc_bf16_f32_b_mn(kHalf, D);
+            const uint32_t tmem_s = tmem + (uint32_t)(half * 128), tmem_o = tmem + 256u + (uint32_t)(half * D);
+            const uint64_t kdesc0 = tc::smem_desc_k_sw128(tc::smem_u32(Ks));
+            const uint64_t vdesc0 = tc::smem_desc_mn_sw128(tc::smem_u32(Vs), kKeys * 128);
             int fill = 0, piece = 0;
-            uint32_t p_count[2] = {0u, 0u};
-            // 4 bits per fill: halves that still have to read its V (twice the stages: S of a fill may be issued
-            // while the stage's previous V is still waiting for a half)
-            unsigned left = 0u;
+            uint32_t count = 0u;                               // blocks whose P this issuer has waited for
             bool ok = true;
-            for (long long x = xbeg; x < xend && ok; ++piece) {
-                const Piece c = make_piece(pl, p, sp, x, xend);
-                x += c.blk1 - c.blk0;
+            for (; more && ok; more = at.next(pl), ++piece) {
+                const Piece c = make_piece(pl, p.B, at);
+                const uint64_t qdesc0 = tc::smem_desc_k_sw128(tc::smem_u32(Qs + (c.split_keys ? 0 : half * kQHalf)));
                 BlockIter it;
                 it.init(pl, c.ti, kKeys, c.blk0);
-                int pend[2] = {-1, -1};                        // block (fill number) whose P V is still to be issued
-                bool first[2] = {true, true};
-                // O (+)= P V of half s for its pending block
-                auto issue_pv = [&](int s) -> bool {
-                    const int f = pend[s], st = f % NS;
-                    const uint32_t ph = (uint32_t)(f / NS) & 1u;
-                    pend[s] = -1;
-                    if (!tc::mbar_wait(&sh->v_full[st], ph, abort_flag)) return false;
-                    if (!tc::mbar_wait(&sh->v_ok[st], ph, abort_flag)) return false;
-                    if (!tc::mbar_wait(&sh->p_full[s], p_count[s] & 1u, abort_flag)) return false;
-                    ++p_count[s];
-                    tc::tc_fence_after_sync();
-                    const uint32_t v_addr = tc::smem_u32(Vs + (size_t)st * kTile);
-#pragma unroll
-                    for (int kk = 0; kk < kKeys / 16; ++kk) {
-                        const uint64_t bdesc = tc::smem_desc_mn_sw128(v_addr + kk * (16 * 128), kKeys * 128);
-                        tc::mma_bf16_ts(tmem + 256u + (uint32_t)(s * D), tmem + (uint32_t)(s * 128 + kk * 8), bdesc, idesc_o,
-                                        !first[s] || kk != 0 ? 1u : 0u);
+                int pend = -1;                                 // block (fill number) whose P V is still to be issued
+                bool first = true;
+                // O (+)= P V of one step of the pending block
+                auto issue_pv = [&](int e) -> bool {
+                    const int st = pend % NS;
+                    const uint32_t ph = (uint32_t)(pend / NS) & 1u;
+                    if (e == 0) {
+                        if (!tc::mbar_wait(&sh->v_full[st], ph, abort_flag)) return false;
+                        if (!tc::mbar_wait(&sh->v_ok[st], ph, abort_flag)) return false;
                     }
-                    first[s] = false;
-                    const int lb = 4 * (f % (2 * NS));
-                    left -= 1u << lb;
-                    if (((left >> lb) & 15u) == 0u) tc::mma_commit(&sh->v_empty[st]);
+                    if (!tc::mbar_wait(&sh->p_full[half][e], count & 1u, abort_flag)) return false;
+                    tc::tc_fence_after_sync();
+                    const uint64_t vdesc = vdesc0 + (uint64_t)((st * kTile + e * kStep * 128) >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < kStep / 16; ++kk)               // 16 keys: 8 columns of P, 16 rows of V
+                        tc::mma_bf16_ts(tmem_o, tmem_s + (uint32_t)(e * kStep + kk * 8), vdesc + (uint64_t)((kk * 16 * 128) >> 4), idesc_o,
+                                        !first || kk != 0 ? 1u : 0u);
+                    tc::mma_commit(&sh->pv_done[half]);
+                    first = false;
+                    if (e == 1) {
+                        tc::mma_commit(&sh->v_empty[st]);
+                        ++count;
+                        pend = -1;
+                    }
+                    return true;
+                };
+                auto issue_s = [&](int e, int st) {
+                    const uint64_t kdesc = kdesc0 + (uint64_t)((st * kTile + e * kStep * 128) >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint64_t along = (uint64_t)((kk / 4) * ((kHalf * 128) >> 4) + 2 * (kk % 4));
+                        tc::mma_bf16_ss(tmem_s + (uint32_t)(e * kStep), qdesc0 + along, kdesc + along, idesc_s, kk != 0 ? 1u : 0u);
+                    }
+                    tc::mma_commit(&sh->s_full[half][e]);
+                };
+                // hands a V buffer of the other half's back
+                auto pass_v = [&](int f) -> bool {
+                    if (!tc::mbar_wait(&sh->v_full[f % NS], (uint32_t)(f / NS) & 1u, abort_flag)) return false;
+                    tc::mbar_arrive(&sh->v_empty[f % NS]);
+                    return true;
+                };
+                auto pass_k = [&](int f) -> bool {
+                    if (!tc::mbar_wait(&sh->k_full[f % NS], (uint32_t)(f / NS) & 1u, abort_flag)) return false;
+                    tc::mbar_arrive(&sh->k_empty[f % NS]);
                     return true;
                 };
                 ok = tc::mbar_wait(&sh->q_full, (uint32_t)piece & 1u, abort_flag);
                 for (int blk = c.blk0; blk < c.blk1 && ok; ++blk, ++fill) {
                     const int st = fill % NS;
-                    const unsigned who = takers(c, it, blk);
-                    left += (unsigned)__popc(who) << (4 * (fill % (2 * NS)));
-                    bool here = false;
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        if (!((who >> s) & 1u) || !ok) continue;
-                        // the half's P is read by P V before S overwrites it: the tensor core works in issue order
-                        if (pend[s] >= 0 && !issue_pv(s)) { ok = false; continue; }
-                        if (!here) {
-                            if (!tc::mbar_wait(&sh->k_full[st], (uint32_t)(fill / NS) & 1u, abort_flag)) { ok = false; continue; }
-                            here = true;
-                        }
+                    if ((takers(c, it, blk) >> half) & 1u) {
+                        // a step's P is read by P V before the next S overwrites it: the tensor core works in issue order
+                        if (pend >= 0 && !issue_pv(0)) { ok = false; break; }
+                        if (!tc::mbar_wait(&sh->k_full[st], (uint32_t)(fill / NS) & 1u, abort_flag)) { ok = false; break; }
                         tc::tc_fence_after_sync();
-                        const uint32_t k_addr = tc::smem_u32(Ks + (size_t)st * kTile);
-                        const uint32_t q_addr = tc::smem_u32(Qs + (c.split_keys ? 0 : s * kQHalf));
-#pragma unroll
-                        for (int kk = 0; kk < D / 16; ++kk) {
-                            const uint64_t adesc = tc::smem_desc_k_sw128(q_addr + (kk / 4) * (kHalf * 128)) + 2 * (kk % 4);
-                            const uint64_t bdesc = tc::smem_desc_k_sw128(k_addr + (kk / 4) * (kKeys * 128)) + 2 * (kk % 4);
-                            tc::mma_bf16_ss(tmem + (uint32_t)(s * 128), adesc, bdesc, idesc_s, kk != 0 ? 1u : 0u);
-                        }
-                        tc::mma_commit(&sh->s_full[s]);
-                        pend[s] = fill;
+                        issue_s(0, st);
+                        if (pend >= 0 && !issue_pv(1)) { ok = false; break; }
+                        issue_s(1, st);
+                        tc::mma_commit(&sh->k_empty[st]);
+                        pend = fill;
+                    } else {
+                        if (pend >= 0 && !(issue_pv(0) && issue_pv(1))) { ok = false; break; }
+                        ok = pass_k(fill) && pass_v(fill);
                     }
-                    if (ok) tc::mma_commit(&sh->k_empty[st]);
-                    // a half that sits out the next blocks must not keep this V block from being refilled
-#pragma unroll
-                    for (int s = 0; s < 2; ++s)
-                        if (ok && pend[s] >= 0 && pend[s] <= fill - NS && !issue_pv(s)) ok = false;
                     if (blk + 1 < c.blk1) it.next(pl, c.ti, kKeys);
                 }
-                const int early = pend[1] >= 0 && (pend[0] < 0 || pend[1] < pend[0]) ? 1 : 0;
-                if (ok && pend[early] >= 0 && !issue_pv(early)) ok = false;
-                if (ok && pend[early ^ 1] >= 0 && !issue_pv(early ^ 1)) ok = false;
-                if (ok) { tc::mma_commit(&sh->o_full[0]); tc::mma_commit(&sh->o_full[1]); }
+                if (ok && pend >= 0) ok = issue_pv(0) && issue_pv(1);
+                if (ok) tc::mma_commit(&sh->o_full[half]);
             }
             if (!ok) give_up(sh, p.status, 32);
         }
-    } else if (warp < 4) {
+    } else if (warp == 3) {
         // ---------------- V rows that hold NaN or infinities ----------------
         int fill = 0;
-        for (long long x = xbeg; x < xend && !failed;) {
-            const Piece c = make_piece(pl, p, sp, x, xend);
-            x += c.blk1 - c.blk0;
+        for (; more && !failed; more = at.next(pl)) {
+            const Piece c = make_piece(pl, p.B, at);
             BlockIter it;
             it.init(pl, c.ti, kKeys, c.blk0);
             for (int blk = c.blk0; blk < c.blk1; ++blk, ++fill) {
@@ -315,8 +364,8 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                 if (failed) break;
                 if (mixed(pl, c, it)) {
 #pragma unroll 1
-                    for (int rr = 0; rr < 2; ++rr) {
-                        unsigned char* row = Vs + (size_t)st * kTile + ((warp - 2) * 64 + rr * 32 + lane) * 128;
+                    for (int rr = 0; rr < kKeys / 32; ++rr) {
+                        unsigned char* row = Vs + (size_t)st * kTile + (rr * 32 + lane) * 128;
                         uint32_t bad = 0u;
 #pragma unroll
                         for (int i = 0; i < DH * 8; ++i) {
@@ -354,40 +403,44 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
         const int grp = p.Hq / p.Hkv;
         const int W = (p.max_nodes + 63) / 64;
         const float sl2 = p.scale * kLog2e;                    // scores are kept in log2 units
-        uint32_t s_count = 0u;
+        const uint64_t sl22 = pair_of(sl2, sl2);
+        uint32_t s_count = 0u, steps = 0u;                     // blocks and steps of this half so far
         int fill0 = 0, piece = 0;
-        for (long long x = xbeg; x < xend; ++piece) {
-            const Piece c = make_piece(pl, p, sp, x, xend);
-            x += c.blk1 - c.blk0;
+        for (; more; more = at.next(pl), ++piece) {
+            const Piece c = make_piece(pl, p.B, at);
             // ---- this thread's row ----
             const int rt = (c.split_keys ? 0 : half * kHalf) + rl;      // row of the tile
             const bool live = rt < c.ti.nrows;
-            int seq = -2, node = 0, row_pre = 0, row_kv = 0, row_n = 0;
-            size_t orow = 0;
-            unsigned long long m0 = 0ull, m1 = 0ull;
-            const unsigned long long* mrow = p.mask;
+            int seq = -2, node = 0, head = 0, row_pre = 0, row_kv = 0, row_n = 0;
             if (live) {
                 const int pr = c.ti.row0 + rt;
-                seq = plan_seq_of_row(pl, p.B, pr);
+                seq = c.ti.b0 == c.ti.b1 ? c.ti.b0 : plan_seq_of_row(pl, p.B, pr);
                 const int o = pr - pl.row_off[seq];
                 node = o / grp;
-                orow = ((size_t)seq * p.max_nodes + node) * p.Hq + c.g * grp + (o - node * grp);
+                head = c.g * grp + (o - node * grp);
                 row_pre = pl.pre[seq];
                 row_kv = pl.kv[seq];
                 row_n = pl.own_len[seq] - row_kv;
-                mrow = p.mask + ((size_t)seq * p.max_nodes + node) * W;
-                m0 = mrow[0];
-                if (W > 1) m1 = mrow[1];
             }
+            auto out_row = [&]() -> size_t { return live ? ((size_t)seq * p.max_nodes + node) * p.Hq + head : 0; };
+            auto visible32 = [&](int src, int key) -> uint32_t {
+                return live ? visible32_of(src, key, seq, row_pre, row_kv, row_n, p.mask + ((size_t)seq * p.max_nodes + node) * W, W) : 0u;
+            };
             const bool warp_live = __any_sync(0xffffffffu, live);
             halves_barrier();                                   // the previous piece is done with Q's memory
             if (!c.split_keys || half == 0) {
-                const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.Q) + orow * D);
-                unsigned char* dst = Qs + half * kQHalf + rl * 128;
+                // neighbouring lanes take neighbouring 16 bytes of a row
+                constexpr int LR = D / 8, RI = 32 / LR;         // lanes per row, rows per instruction
+                unsigned char* dst = Qs + half * kQHalf + (q * 32) * 128;
+                const int cc = lane % LR;
+                const unsigned long long orow = out_row();
 #pragma unroll
-                for (int cc = 0; cc < D / 8; ++cc) {
-                    const uint4 w = live ? __ldg(src + cc) : make_uint4(0u, 0u, 0u, 0u);
-                    *reinterpret_cast<uint4*>(dst + (cc / 8) * (kHalf * 128) + (((cc % 8) ^ (rl & 7)) << 4)) = w;
+                for (int i = 0; i < LR; ++i) {
+                    const int rr = i * RI + lane / LR;
+                    const unsigned long long src = __shfl_sync(0xffffffffu, orow, rr);
+                    const bool on = __shfl_sync(0xffffffffu, live ? 1 : 0, rr) != 0;
+                    const uint4 w = on ? __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.Q) + src * D) + cc) : make_uint4(0u, 0u, 0u, 0u);
+                    *reinterpret_cast<uint4*>(dst + rr * 128 + (cc / 8) * (kHalf * 128) + (((cc % 8) ^ (rr & 7)) << 4)) = w;
                 }
                 tc::fence_proxy_async();
             }
@@ -395,54 +448,60 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
             if (lane == 0) tc::mbar_arrive(&sh->q_full);
 
             float ref = -INFINITY, sum = 0.f;
-            bool first = true;
+            bool first = true, poisoned = false;
             BlockIter it;
             it.init(pl, c.ti, kKeys, c.blk0);
             for (int blk = c.blk0; blk < c.blk1; ++blk) {
                 if ((takers(c, it, blk) >> half) & 1u) {
-                    if (!failed && !tc::mbar_wait(&sh->s_full[half], s_count & 1u, abort_flag)) failed = true;
-                    ++s_count;
-                    failed = __any_sync(0xffffffffu, failed);
-                    if (failed) {
-                        if (lane == 0) give_up(sh, p.status, 35);
-                        break;
-                    }
-                    tc::tc_fence_after_sync();
-                    if (warp_live) {
-                        const bool all = !live || (it.seq < 0 ? it.key0 + kKeys <= row_pre : (it.seq == seq && it.key0 + kKeys <= row_kv));
-                        const bool open = __all_sync(0xffffffffu, all);        // no row of the warp has anything masked
-                        const bool none = !live || (it.seq < 0 ? it.key0 >= row_pre : it.seq != seq);
+#pragma unroll 1
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t tmem_se = tmem_s + (uint32_t)(e * kStep);
+                        if (!failed && !tc::mbar_wait(&sh->s_full[half][e], s_count & 1u, abort_flag)) failed = true;
+                        failed = __any_sync(0xffffffffu, failed);
+                        if (failed) break;
+                        tc::tc_fence_after_sync();
+                        const int key = it.key0 + e * kStep;
+                        // keys from here on that this row sees without a look at its mask, and whether there are others
+                        const int sees = !live ? 0 : (it.seq < 0 ? row_pre - key : (it.seq == seq ? row_kv - key : 0));
+                        const bool none = sees <= 0 && !(live && it.seq == seq && row_kv + row_n > key);
                         if (__all_sync(0xffffffffu, none)) {
-                            // nothing to see for this warp: P is zero
-                            uint32_t z[32];
+                            // nothing to see for this warp: P is zero (rows that are not there take no part at all)
+                            if (warp_live) {
+                                uint32_t z[32];
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) z[j] = 0u;
-                            tc::tmem_st32(tmem_s, z);
-                            tc::tmem_st32(tmem_s + 32u, z);
+                                for (int j = 0; j < 32; ++j) z[j] = 0u;
+                                tc::tmem_st32(tmem_se, z);
+                            }
                         } else {
-                            uint32_t v[4][32];
-#pragma unroll
-                            for (int cc = 0; cc < 4; ++cc) tc::tmem_ld32(tmem_s + (uint32_t)(cc * 32), v[cc]);
+                            uint32_t v[2][32];
+                            tc::tmem_ld32(tmem_se, v[0]);
+                            tc::tmem_ld32(tmem_se + 32u, v[1]);
+                            const bool open = __all_sync(0xffffffffu, !live || sees >= kStep);    // no row of the warp has anything masked
                             tc::tmem_ld_wait();
                             if (!open) {
 #pragma unroll
-                                for (int cc = 0; cc < 4; ++cc) {
-                                    const uint32_t vis = live ? visible32_of(it.seq, it.key0 + cc * 32, seq, row_pre, row_kv, row_n, m0, m1, mrow, W) : 0u;
+                                for (int cc = 0; cc < 2; ++cc) {
+                                    const uint32_t vis = visible32(it.seq, key + cc * 32);
 #pragma unroll
                                     for (int j = 0; j < 32; ++j) v[cc][j] = ((vis >> j) & 1u) ? v[cc][j] : 0xff800000u;
                                 }
                             }
                             float b4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                            for (int cc = 0; cc < 4; ++cc)
+                            for (int cc = 0; cc < 2; ++cc)
 #pragma unroll
-                                for (int j = 0; j < 32; ++j) b4[j & 3] = fmaxf(b4[j & 3], __uint_as_float(v[cc][j]));
-                            const float bm = fmaxf(fmaxf(b4[0], b4[1]), fmaxf(b4[2], b4[3])) * sl2;
-                            const bool move = bm > ref + kSlack;               // also the first visible key (ref = -inf)
+                                for (int j = 0; j < 32; j += 2)
+                                    b4[(j >> 1) & 3] = max3_nan(b4[(j >> 1) & 3], __uint_as_float(v[cc][j]), __uint_as_float(v[cc][j + 1]));
+                            float bm = max3_nan(max3_nan(b4[0], b4[1], b4[2]), b4[3], -INFINITY);
+                            poisoned = poisoned || !(bm < INFINITY);       // a NaN or +inf score: the row is not meaningful
+                            bm *= sl2;
+                            const bool move = bm > ref + kSlack;           // also the first visible key (ref = -inf)
                             if (__any_sync(0xffffffffu, move)) {
                                 const float corr = move ? exp2_fast(ref - bm) : 1.f;
-                                // S of this block was issued after P V of the half's last one: O is at rest
                                 if (!first) {
+                                    // O must be at rest: P V of the step before (older ones precede this step's scores)
+                                    if (!tc::mbar_wait(&sh->pv_done[half], (steps - 1u) & 1u, abort_flag)) failed = true;
+                                    tc::tc_fence_after_sync();
 #pragma unroll 1
                                     for (int c0 = 0; c0 < D; c0 += 32) {
                                         uint32_t o[32];
@@ -457,32 +516,51 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                                 ref = move ? bm : ref;
                             }
                             const float off = ref == -INFINITY ? 0.f : -ref;
-                            float s4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                            for (int hh = 0; hh < 2; ++hh) {
-                                uint32_t w[32];
+                            const uint64_t off2 = pair_of(off, off);
+                            uint64_t s2[2] = {0ull, 0ull};
+                            uint32_t w[32];
+                            // the exponential unit does 16 results a clock: a share of them goes to the FMA pipe, which balances
+                            // the two (whole steps only: it does not make a masked score exactly zero)
+                            auto weigh = [&](auto mix) {
 #pragma unroll
                                 for (int j = 0; j < 32; ++j) {
-                                    const int e = 2 * j;
-                                    const float a = exp2_fast(fmaf(__uint_as_float(v[2 * hh + e / 32][e % 32]), sl2, off));
-                                    const float b = exp2_fast(fmaf(__uint_as_float(v[2 * hh + e / 32][e % 32 + 1]), sl2, off));
-                                    s4[(2 * j) & 3] += a;
-                                    s4[(2 * j + 1) & 3] += b;
+                                    uint64_t x = fma2(pair_of(__uint_as_float(v[j / 16][(2 * j) % 32]), __uint_as_float(v[j / 16][(2 * j) % 32 + 1])), sl22, off2);
+                                    float a, b;
+                                    if (decltype(mix)::value && (j % 8) >= 8 - kPolyOf8) {
+                                        x = exp2_poly2(x);
+                                        pair_split(x, a, b);
+                                    } else {
+                                        pair_split(x, a, b);
+                                        a = exp2_fast(a);
+                                        b = exp2_fast(b);
+                                        x = pair_of(a, b);
+                                    }
+                                    s2[j & 1] = add2(s2[j & 1], x);
                                     w[j] = pack_bf16(a, b);
                                 }
-                                tc::tmem_st32(tmem_s + (uint32_t)(hh * 32), w);
-                            }
-                            sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                            };
+                            if (open) weigh(Flag<true>()); else weigh(Flag<false>());
+                            tc::tmem_st32(tmem_se, w);                     // over scores that have been read
+                            float sa, sb;
+                            pair_split(add2(s2[0], s2[1]), sa, sb);
+                            sum += sa + sb;
                         }
+                        first = false;
+                        ++steps;
                         tc::tmem_st_wait();
+                        tc::tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) tc::mbar_arrive(&sh->p_full[half][e]);
                     }
-                    first = false;
-                    tc::tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) tc::mbar_arrive(&sh->p_full[half]);
+                    if (failed) {
+                        if (lane == 0) give_up(sh, p.status, 35);
+                        break;
+                    }
+                    ++s_count;
                 }
                 if (blk + 1 < c.blk1) it.next(pl, c.ti, kKeys);
             }
+            if (poisoned) sum = __uint_as_float(0x7fc00000u);
             // ---- the half's output is complete ----
             if (!failed && !tc::mbar_wait(&sh->o_full[half], (uint32_t)piece & 1u, abort_flag)) failed = true;
             failed = __any_sync(0xffffffffu, failed);
@@ -499,7 +577,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                         const __nv_bfloat16* vb = jt.seq < 0 ? static_cast<const __nv_bfloat16*>(p.Vp) + (size_t)c.g * p.Pcap * D
                                                              : static_cast<const __nv_bfloat16*>(p.V) + ((size_t)jt.seq * p.Hkv + c.g) * (size_t)p.Lcap * D;
                         for (int k = 0; k < kKeys; ++k) {
-                            if (!((visible32_of(jt.seq, jt.key0 + (k & ~31), seq, row_pre, row_kv, row_n, m0, m1, mrow, W) >> (k & 31)) & 1u)) continue;
+                            if (!((visible32(jt.seq, jt.key0 + (k & ~31)) >> (k & 31)) & 1u)) continue;
                             const uint32_t* vr = reinterpret_cast<const uint32_t*>(vb + (size_t)(jt.key0 + k) * D);
                             uint32_t bad = 0u;
                             for (int d = 0; d < D / 2; ++d) bad |= (vr[d] & 0x7f807f80u) + 0x00800080u;
@@ -542,9 +620,12 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
             }
             // ---- output: this thread's row ----
             if (!failed && warp_live && (!c.split_keys || half == 0)) {
-                const float inv = c.whole ? (sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum)) : 1.f;
-                const size_t part = (size_t)blockIdx.x * 2 + c.slot;
-                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.O) + orow * D;
+                const bool whole = at.whole();
+                const float inv = whole ? (sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum)) : 1.f;
+                const size_t part = (size_t)blockIdx.x * 2 + at.slot();
+                // a finished row goes through shared memory (Q's place, or over its own part of the joined
+                // rows, behind what has been read), so that it leaves in whole lines
+                unsigned char* stage = c.split_keys ? Qs + rl * (D * 4) : Qs + half * kQHalf + rl * (D * 2);
 #pragma unroll 1
                 for (int c0 = 0; c0 < D; c0 += 32) {
                     float o[32];
@@ -566,8 +647,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                             o[4 * j + 2] = fmaf(w.z, other, o[4 * j + 2]); o[4 * j + 3] = fmaf(w.w, other, o[4 * j + 3]);
                         }
                     }
-                    if (!live) continue;
-                    if (c.whole) {
+                    if (whole) {
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             uint4 w;
@@ -575,17 +655,33 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                             w.y = pack_bf16(o[8 * j + 2] * inv, o[8 * j + 3] * inv);
                             w.z = pack_bf16(o[8 * j + 4] * inv, o[8 * j + 5] * inv);
                             w.w = pack_bf16(o[8 * j + 6] * inv, o[8 * j + 7] * inv);
-                            *reinterpret_cast<uint4*>(out + c0 + 8 * j) = w;
+                            *reinterpret_cast<uint4*>(stage + (((c0 / 8 + j) ^ (rl & 7)) << 4)) = w;
                         }
-                    } else {
+                    } else if (live) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
                             p.part_o[(part * (D / 4) + c0 / 4 + j) * kTcRows + rt] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
                     }
                 }
+                if (whole) {
+                    __syncwarp();
+                    constexpr int LR = D / 8, RI = 32 / LR;
+                    const int cc = lane % LR;
+                    const unsigned char* from = c.split_keys ? Qs + q * 32 * (D * 4) : Qs + half * kQHalf + q * 32 * (D * 2);
+                    const int stride = c.split_keys ? D * 4 : D * 2;
+                    const unsigned long long orow = out_row();
+#pragma unroll 4
+                    for (int i = 0; i < LR; ++i) {
+                        const int rr = i * RI + lane / LR;
+                        const unsigned long long dst = __shfl_sync(0xffffffffu, orow, rr);
+                        const bool on = __shfl_sync(0xffffffffu, live ? 1 : 0, rr) != 0;
+                        const uint4 w = *reinterpret_cast<const uint4*>(from + rr * stride + ((cc ^ (rr & 7)) << 4));
+                        if (on) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.O) + dst * D + 8 * cc) = w;
+                    }
+                }
                 if (live) {
-                    if (!c.whole) p.part_ml[part * kTcRows + rt] = make_float2(ref, sum);
-                    else if (p.lse) p.lse[orow] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+                    if (!whole) p.part_ml[part * kTcRows + rt] = make_float2(ref, sum);
+                    else if (p.lse) p.lse[out_row()] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
                 }
             }
             tc::tc_fence_before_sync();
