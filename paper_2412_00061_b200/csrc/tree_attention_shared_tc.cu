@@ -39,7 +39,7 @@ constexpr float kSlack = 8.f;          // log2 units: P stays below 2^8
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kNoteBits = 2048;
-constexpr int kPolyOf8 = 3;            // of 8 pairs of exponentials, how many the FMA pipe computes
+constexpr int kPolyOf8 = 2;            // of 8 pairs of exponentials, how many the FMA pipe computes
 
 template <bool B> struct Flag { static constexpr bool value = B; };
 
@@ -239,12 +239,12 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                     const int s = fill % NS;
                     const uint32_t ph = (uint32_t)(fill / NS) & 1u;
                     const bool pre = it.seq < 0;
-                    if (!tc::mbar_wait(&sh->k_empty[s], ph ^ 1u, abort_flag)) { failed = true; break; }
+                    if (!tc::mbar_wait_suspended(&sh->k_empty[s], ph ^ 1u, abort_flag)) { failed = true; break; }
                     tc::mbar_arrive_expect_tx(&sh->k_full[s], (uint32_t)kTile);
                     tc::tma_load_5d(Ks + (size_t)s * kTile, pre ? &tmKp : &tmK, &sh->k_full[s], 0, it.key0, 0, c.g, pre ? 0 : it.seq, pol);
-                    if (!tc::mbar_wait(&sh->v_empty[s], ph ^ 1u, abort_flag)) {
+                    if (!tc::mbar_wait_suspended(&sh->v_empty[s], ph ^ 1u, abort_flag)) {
                         failed = true;
-                        tc::mbar_wait(&sh->k_full[s], ph, &sh->never_set, 1ll << 24);      // the K copy lands first
+                        tc::mbar_wait_suspended(&sh->k_full[s], ph, &sh->never_set, 1ll << 24);      // the K copy lands first
                         break;
                     }
                     tc::mbar_arrive_expect_tx(&sh->v_full[s], (uint32_t)kTile);
@@ -256,8 +256,8 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                 give_up(sh, p.status, 31);
                 for (int back = 1; back <= NS && back <= fill; ++back) {                    // copies in flight land before the exit
                     const int j = fill - back;
-                    tc::mbar_wait(&sh->k_full[j % NS], (uint32_t)(j / NS) & 1u, &sh->never_set, 1ll << 24);
-                    tc::mbar_wait(&sh->v_full[j % NS], (uint32_t)(j / NS) & 1u, &sh->never_set, 1ll << 24);
+                    tc::mbar_wait_suspended(&sh->k_full[j % NS], (uint32_t)(j / NS) & 1u, &sh->never_set, 1ll << 24);
+                    tc::mbar_wait_suspended(&sh->v_full[j % NS], (uint32_t)(j / NS) & 1u, &sh->never_set, 1ll << 24);
                 }
             }
         }
@@ -287,10 +287,10 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                     const int st = pend % NS;
                     const uint32_t ph = (uint32_t)(pend / NS) & 1u;
                     if (e == 0) {
-                        if (!tc::mbar_wait(&sh->v_full[st], ph, abort_flag)) return false;
-                        if (!tc::mbar_wait(&sh->v_ok[st], ph, abort_flag)) return false;
+                        if (!tc::mbar_wait_suspended(&sh->v_full[st], ph, abort_flag)) return false;
+                        if (!tc::mbar_wait_suspended(&sh->v_ok[st], ph, abort_flag)) return false;
                     }
-                    if (!tc::mbar_wait(&sh->p_full[half][e], count & 1u, abort_flag)) return false;
+                    if (!tc::mbar_wait_suspended(&sh->p_full[half][e], count & 1u, abort_flag)) return false;
                     tc::tc_fence_after_sync();
                     const uint64_t vdesc = vdesc0 + (uint64_t)((st * kTile + e * kStep * 128) >> 4);
 #pragma unroll
@@ -317,22 +317,22 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                 };
                 // hands a V buffer of the other half's back
                 auto pass_v = [&](int f) -> bool {
-                    if (!tc::mbar_wait(&sh->v_full[f % NS], (uint32_t)(f / NS) & 1u, abort_flag)) return false;
+                    if (!tc::mbar_wait_suspended(&sh->v_full[f % NS], (uint32_t)(f / NS) & 1u, abort_flag)) return false;
                     tc::mbar_arrive(&sh->v_empty[f % NS]);
                     return true;
                 };
                 auto pass_k = [&](int f) -> bool {
-                    if (!tc::mbar_wait(&sh->k_full[f % NS], (uint32_t)(f / NS) & 1u, abort_flag)) return false;
+                    if (!tc::mbar_wait_suspended(&sh->k_full[f % NS], (uint32_t)(f / NS) & 1u, abort_flag)) return false;
                     tc::mbar_arrive(&sh->k_empty[f % NS]);
                     return true;
                 };
-                ok = tc::mbar_wait(&sh->q_full, (uint32_t)piece & 1u, abort_flag);
+                ok = tc::mbar_wait_suspended(&sh->q_full, (uint32_t)piece & 1u, abort_flag);
                 for (int blk = c.blk0; blk < c.blk1 && ok; ++blk, ++fill) {
                     const int st = fill % NS;
                     if ((takers(c, it, blk) >> half) & 1u) {
                         // a step's P is read by P V before the next S overwrites it: the tensor core works in issue order
                         if (pend >= 0 && !issue_pv(0)) { ok = false; break; }
-                        if (!tc::mbar_wait(&sh->k_full[st], (uint32_t)(fill / NS) & 1u, abort_flag)) { ok = false; break; }
+                        if (!tc::mbar_wait_suspended(&sh->k_full[st], (uint32_t)(fill / NS) & 1u, abort_flag)) { ok = false; break; }
                         tc::tc_fence_after_sync();
                         issue_s(0, st);
                         if (pend >= 0 && !issue_pv(1)) { ok = false; break; }
@@ -359,7 +359,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
             it.init(pl, c.ti, kKeys, c.blk0);
             for (int blk = c.blk0; blk < c.blk1; ++blk, ++fill) {
                 const int st = fill % NS;
-                if (!tc::mbar_wait(&sh->v_full[st], (uint32_t)(fill / NS) & 1u, abort_flag)) failed = true;
+                if (!tc::mbar_wait_suspended(&sh->v_full[st], (uint32_t)(fill / NS) & 1u, abort_flag)) failed = true;
                 failed = __any_sync(0xffffffffu, failed);
                 if (failed) break;
                 if (mixed(pl, c, it)) {
@@ -434,13 +434,18 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                 unsigned char* dst = Qs + half * kQHalf + (q * 32) * 128;
                 const int cc = lane % LR;
                 const unsigned long long orow = out_row();
+                const unsigned there = __ballot_sync(0xffffffffu, live);
+                uint4 w[LR];
+#pragma unroll
+                for (int i = 0; i < LR; ++i) {                  // (a row that is not there reads row 0)
+                    const unsigned long long src = __shfl_sync(0xffffffffu, orow, i * RI + lane / LR);
+                    w[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.Q) + src * D) + cc);
+                }
 #pragma unroll
                 for (int i = 0; i < LR; ++i) {
                     const int rr = i * RI + lane / LR;
-                    const unsigned long long src = __shfl_sync(0xffffffffu, orow, rr);
-                    const bool on = __shfl_sync(0xffffffffu, live ? 1 : 0, rr) != 0;
-                    const uint4 w = on ? __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.Q) + src * D) + cc) : make_uint4(0u, 0u, 0u, 0u);
-                    *reinterpret_cast<uint4*>(dst + rr * 128 + (cc / 8) * (kHalf * 128) + (((cc % 8) ^ (rr & 7)) << 4)) = w;
+                    if (!((there >> rr) & 1u)) w[i] = make_uint4(0u, 0u, 0u, 0u);
+                    *reinterpret_cast<uint4*>(dst + rr * 128 + (cc / 8) * (kHalf * 128) + (((cc % 8) ^ (rr & 7)) << 4)) = w[i];
                 }
                 tc::fence_proxy_async();
             }
@@ -456,7 +461,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
 #pragma unroll 1
                     for (int e = 0; e < 2; ++e) {
                         const uint32_t tmem_se = tmem_s + (uint32_t)(e * kStep);
-                        if (!failed && !tc::mbar_wait(&sh->s_full[half][e], s_count & 1u, abort_flag)) failed = true;
+                        if (!failed && !tc::mbar_wait_suspended(&sh->s_full[half][e], s_count & 1u, abort_flag)) failed = true;
                         failed = __any_sync(0xffffffffu, failed);
                         if (failed) break;
                         tc::tc_fence_after_sync();
@@ -474,10 +479,11 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                             }
                         } else {
                             uint32_t v[2][32];
+                            const bool open = __all_sync(0xffffffffu, !live || sees >= kStep);    // no row of the warp has anything masked
                             tc::tmem_ld32(tmem_se, v[0]);
                             tc::tmem_ld32(tmem_se + 32u, v[1]);
-                            const bool open = __all_sync(0xffffffffu, !live || sees >= kStep);    // no row of the warp has anything masked
-                            tc::tmem_ld_wait();
+                            tc::tmem_ld_wait(v[0]);            // (at once: a register with a load in flight must not be moved)
+                            tc::tmem_ld_wait(v[1]);
                             if (!open) {
 #pragma unroll
                                 for (int cc = 0; cc < 2; ++cc) {
@@ -500,13 +506,13 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                                 const float corr = move ? exp2_fast(ref - bm) : 1.f;
                                 if (!first) {
                                     // O must be at rest: P V of the step before (older ones precede this step's scores)
-                                    if (!tc::mbar_wait(&sh->pv_done[half], (steps - 1u) & 1u, abort_flag)) failed = true;
+                                    if (!tc::mbar_wait_suspended(&sh->pv_done[half], (steps - 1u) & 1u, abort_flag)) failed = true;
                                     tc::tc_fence_after_sync();
 #pragma unroll 1
                                     for (int c0 = 0; c0 < D; c0 += 32) {
                                         uint32_t o[32];
                                         tc::tmem_ld32(tmem_o + (uint32_t)c0, o);
-                                        tc::tmem_ld_wait();
+                                        tc::tmem_ld_wait(o);
 #pragma unroll
                                         for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * corr);
                                         tc::tmem_st32(tmem_o + (uint32_t)c0, o);
@@ -562,7 +568,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
             }
             if (poisoned) sum = __uint_as_float(0x7fc00000u);
             // ---- the half's output is complete ----
-            if (!failed && !tc::mbar_wait(&sh->o_full[half], (uint32_t)piece & 1u, abort_flag)) failed = true;
+            if (!failed && !tc::mbar_wait_suspended(&sh->o_full[half], (uint32_t)piece & 1u, abort_flag)) failed = true;
             failed = __any_sync(0xffffffffu, failed);
             if (failed && lane == 0) give_up(sh, p.status, 36);
             tc::tc_fence_after_sync();
@@ -600,7 +606,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                         for (int c0 = 0; c0 < D; c0 += 32) {
                             uint32_t o[32];
                             tc::tmem_ld32(tmem_o + (uint32_t)c0, o);
-                            tc::tmem_ld_wait();
+                            tc::tmem_ld_wait(o);
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
                                 *reinterpret_cast<uint4*>(join + rl * D + ((((c0 / 4) + j) ^ (rl & 7)) << 2)) =
@@ -632,7 +638,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                     if (!first) {
                         uint32_t u[32];
                         tc::tmem_ld32(tmem_o + (uint32_t)c0, u);
-                        tc::tmem_ld_wait();
+                        tc::tmem_ld_wait(u);
 #pragma unroll
                         for (int j = 0; j < 32; ++j) o[j] = __uint_as_float(u[j]) * mine;
                     } else {
@@ -670,13 +676,13 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                     const unsigned char* from = c.split_keys ? Qs + q * 32 * (D * 4) : Qs + half * kQHalf + q * 32 * (D * 2);
                     const int stride = c.split_keys ? D * 4 : D * 2;
                     const unsigned long long orow = out_row();
+                    const unsigned there = __ballot_sync(0xffffffffu, live);
 #pragma unroll 4
                     for (int i = 0; i < LR; ++i) {
                         const int rr = i * RI + lane / LR;
                         const unsigned long long dst = __shfl_sync(0xffffffffu, orow, rr);
-                        const bool on = __shfl_sync(0xffffffffu, live ? 1 : 0, rr) != 0;
                         const uint4 w = *reinterpret_cast<const uint4*>(from + rr * stride + ((cc ^ (rr & 7)) << 4));
-                        if (on) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.O) + dst * D + 8 * cc) = w;
+                        if ((there >> rr) & 1u) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.O) + dst * D + 8 * cc) = w;
                     }
                 }
                 if (live) {
