@@ -7,7 +7,8 @@
 // holds every row's position, which is what "newest" is decided on.
 //
 // One thread-block cluster per (kv head, sequence): radix selection of the threshold (11 + 11 + 10 bits, the
-// histograms added up through distributed shared memory), ranks by ballots, then the copies.
+// histograms added up through distributed shared memory), ranks by ballots, then the copies.  With few (kv head,
+// sequence) pairs their clusters leave most SMs idle, so the copies then are a second kernel's, spread evenly over all.
 #include "common.cuh"
 #include "tc_primitives.cuh"
 
@@ -28,6 +29,7 @@ struct EvictParams {
     const int* kv_len; const int* n_evicted;       // [B]
     float* out_mass; int* out_row_pos; int* out_kv_len; int* out_n_evicted;
     int* lists;                        // workspace [B,Hkv,Lcap]: dropped rows from the front, moving rows from the back
+    int* n_move;                       // workspace [B,Hkv]: rows that move, where another kernel copies them, else null
     int B, Hkv, Lcap, row_bytes, budget, sinks, recent;
     unsigned* seq_ticket;              // [B], zero between calls
     int* status;
@@ -45,6 +47,49 @@ __device__ __forceinline__ int ld_peer(const int* local, int rank) {
     return v;
 }
 
+__device__ __forceinline__ int4 ld_peer4(const int* local, int rank) {
+    uint32_t a;
+    int4 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tc::smem_u32(local)), "r"(rank));
+    asm volatile("ld.shared::cluster.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+
+// Copies pieces [i, n) in steps of `step`: piece k * chunks + c is 16 bytes (column c) of the k-th moving row, of K and
+// of V.  Four at a time, so that a thread has eight loads on their way.
+__device__ __forceinline__ void move_pieces(unsigned char* Kb, unsigned char* Vb, const int* hole_list, const int* mover_list,
+                                            int row_bytes, long long i, long long n, long long step) {
+    const int chunks = row_bytes / 16;                                     // a power of two: 8, 16 or 32
+    const int sh = 31 - __clz(chunks);
+    constexpr int U = 4;
+    for (; i < n; i += U * step) {
+        size_t src[U], dst[U];
+        uint4 kk[U], vv[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long x = i + u * step;
+            src[u] = dst[u] = 0;
+            if (x < n) {
+                const int k = (int)(x >> sh), c = (int)(x & (chunks - 1));
+                src[u] = (size_t)__ldcg(mover_list + k) * row_bytes + c * 16;
+                dst[u] = (size_t)__ldcg(hole_list + k) * row_bytes + c * 16;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + u * step < n) {
+                kk[u] = *reinterpret_cast<const uint4*>(Kb + src[u]);
+                vv[u] = *reinterpret_cast<const uint4*>(Vb + src[u]);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + u * step < n) {
+                *reinterpret_cast<uint4*>(Kb + dst[u]) = kk[u];
+                *reinterpret_cast<uint4*>(Vb + dst[u]) = vv[u];
+            }
+    }
+}
+
 // Ranking key: larger is kept first.  Protected rows lead; then the weight, +0 and -0 alike, NaN last.
 __device__ __forceinline__ unsigned rank_key(float m, int pos, int sinks, int newest_from) {
     if (pos < sinks || pos >= newest_from) return 0xffffffffu;
@@ -53,7 +98,7 @@ __device__ __forceinline__ unsigned rank_key(float m, int pos, int sinks, int ne
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-struct EvictShared {
+struct __align__(16) EvictShared {
     int hist[3][kBins];
     int tot[kWarps];
     int warp_cnt[3][kWarps];           // ties, dropped rows, moving rows per warp
@@ -98,31 +143,51 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
         for (int rd = 0; rd < 3; ++rd) {
             const int bits = rd == 2 ? 10 : 11, up = shift;
             shift -= bits;
-            for (int j = lo + tid; j < hi; j += kThreads) {
-                unsigned key;
-                if (rd == 0) {
-                    key = key_of(j);
-                    if (cached) cache[j - lo] = key;
-                } else {
-                    key = key_at(j);
-                    if ((key >> up) != prefix) continue;
+            if (rd == 0) {
+                constexpr int U = 8;                                       // loads on their way per thread and array
+                for (int j0 = lo + tid; j0 < hi; j0 += U * kThreads) {
+                    float m[U];
+                    int q[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int j = j0 + u * kThreads;
+                        m[u] = j < hi ? mass[j] : 0.f;
+                        q[u] = j < hi ? row_pos[j] : 0;
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int j = j0 + u * kThreads;
+                        if (j >= hi) break;
+                        const unsigned key = rank_key(m[u], q[u], p.sinks, newest_from);
+                        if (cached) cache[j - lo] = key;
+                        atomicAdd(&sh->hist[0][key >> shift], 1);
+                    }
                 }
-                atomicAdd(&sh->hist[rd][(key >> shift) & ((1u << bits) - 1u)], 1);
+            } else {
+                for (int j = lo + tid; j < hi; j += kThreads) {
+                    const unsigned key = key_at(j);
+                    if ((key >> up) == prefix) atomicAdd(&sh->hist[rd][(key >> shift) & ((1u << bits) - 1u)], 1);
+                }
             }
             cluster_sync(cs);
             const int nb = 1 << bits;
             // descending order of bins: thread t looks after bins nb-1-4t .. nb-4-4t
-            int v[kBins / kThreads], sum = 0;
+            static_assert(kBins / kThreads == 4, "a thread reads its bins as one vector");
+            int v[4] = {0, 0, 0, 0};
+            const int bin0 = nb - 4 - 4 * tid;                             // lowest of this thread's four
+            if (bin0 >= 0) {
+                if (cs == 1) {
+                    const int4 h = *reinterpret_cast<const int4*>(&sh->hist[rd][bin0]);
+                    v[0] = h.w; v[1] = h.z; v[2] = h.y; v[3] = h.x;
+                } else {
+                    int4 h[kMaxCluster];                                   // all requested, then added
 #pragma unroll
-            for (int i = 0; i < kBins / kThreads; ++i) {
-                const int bin = nb - 1 - (tid * (kBins / kThreads) + i);
-                v[i] = 0;
-                if (bin >= 0) {
-                    if (cs == 1) v[i] = sh->hist[rd][bin];
-                    else for (int c = 0; c < cs; ++c) v[i] += ld_peer(&sh->hist[rd][bin], c);
+                    for (int c = 0; c < kMaxCluster; ++c) h[c] = c < cs ? ld_peer4(&sh->hist[rd][bin0], c) : make_int4(0, 0, 0, 0);
+#pragma unroll
+                    for (int c = 0; c < kMaxCluster; ++c) { v[0] += h[c].w; v[1] += h[c].z; v[2] += h[c].y; v[3] += h[c].x; }
                 }
-                sum += v[i];
             }
+            const int sum = v[0] + v[1] + v[2] + v[3];
             int incl = sum;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -226,18 +291,11 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
         });
         cluster_sync(cs);                                                  // the lists are complete; every weight has been read
         // ---- the moves: 16 bytes per thread and tensor, neighbours on one row ----
-        const int chunks = p.row_bytes / 16;
-        unsigned char* Kb = static_cast<unsigned char*>(p.K) + row0 * p.row_bytes;
-        unsigned char* Vb = static_cast<unsigned char*>(p.V) + row0 * p.row_bytes;
-        const long long pieces = (long long)n_move * chunks;
-        for (long long i = (long long)rank * kThreads + tid; i < pieces; i += (long long)cs * kThreads) {
-            const int k = (int)(i / chunks), c = (int)(i - (long long)k * chunks);
-            const size_t src = (size_t)__ldcg(mover_list + k) * p.row_bytes + c * 16;
-            const size_t dst = (size_t)__ldcg(hole_list + k) * p.row_bytes + c * 16;
-            const uint4 kk = *reinterpret_cast<const uint4*>(Kb + src);
-            const uint4 vv = *reinterpret_cast<const uint4*>(Vb + src);
-            *reinterpret_cast<uint4*>(Kb + dst) = kk;
-            *reinterpret_cast<uint4*>(Vb + dst) = vv;
+        if (p.n_move) {
+            if (rank == 0 && tid == 0) p.n_move[b * p.Hkv + g] = n_move;
+        } else {
+            move_pieces(static_cast<unsigned char*>(p.K) + row0 * p.row_bytes, static_cast<unsigned char*>(p.V) + row0 * p.row_bytes, hole_list,
+                        mover_list, p.row_bytes, (long long)rank * kThreads + tid, (long long)n_move * (p.row_bytes / 16), (long long)cs * kThreads);
         }
         for (int k = rank * kThreads + tid; k < n_move; k += cs * kThreads) {
             const int src = __ldcg(mover_list + k), dst = __ldcg(hole_list + k);
@@ -245,6 +303,7 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
             out_pos[dst] = row_pos[src];
         }
     }
+    if (p.n_move && rank == 0 && tid == 0 && (bad || L <= p.budget)) p.n_move[b * p.Hkv + g] = 0;
     // out_kv_len / out_n_evicted may be the very input arrays: the last kv head's cluster writes them, when
     // every head has read the old values (all CTAs of this cluster have: barrier)
     cluster_sync(cs);
@@ -258,6 +317,38 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
     }
 }
 
+// The copies of all pairs, dealt evenly: the pairs' pieces form one line, a CTA takes an equal span of it.
+__global__ void __launch_bounds__(kThreads) evict_move_kernel(EvictParams p) {
+    extern __shared__ long long cum[];                                     // [B*Hkv+1] pieces before each pair
+    pdl_wait();
+    pdl_trigger();
+    const int units = p.B * p.Hkv, chunks = p.row_bytes / 16, lane = threadIdx.x & 31;
+    if (threadIdx.x < 32) {
+        long long run = 0;
+        for (int u0 = 0; u0 < units; u0 += 32) {
+            long long v = u0 + lane < units ? (long long)p.n_move[u0 + lane] * chunks : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long w = __shfl_up_sync(0xffffffffu, v, o);
+                if (lane >= o) v += w;
+            }
+            if (u0 + lane < units) cum[u0 + lane + 1] = run + v;
+            run += __shfl_sync(0xffffffffu, v, 31);
+        }
+        if (lane == 0) cum[0] = 0;
+    }
+    __syncthreads();
+    const long long total = cum[units], x0 = total * blockIdx.x / gridDim.x, x1 = total * (blockIdx.x + 1) / gridDim.x;
+    for (int u = 0; u < units; ++u) {
+        const long long from = x0 > cum[u] ? x0 : cum[u], to = x1 < cum[u + 1] ? x1 : cum[u + 1];
+        if (from >= to) continue;
+        const size_t row0 = (size_t)u * p.Lcap;
+        const int* hole_list = p.lists + row0;
+        move_pieces(static_cast<unsigned char*>(p.K) + row0 * p.row_bytes, static_cast<unsigned char*>(p.V) + row0 * p.row_bytes, hole_list,
+                    hole_list + p.Lcap / 2, p.row_bytes, from - cum[u] + threadIdx.x, to - cum[u], kThreads);
+    }
+}
+
 }  // namespace
 }  // namespace ctcsd
 
@@ -267,7 +358,7 @@ extern "C" int ctcsd_evict_rows_workspace_bytes(const ctcsd_config* cfg, int Lca
     if (!cfg || !out_bytes || Lcap < 1) return CTCSD_ERR_INVALID_ARG;
     const int rc = validate_config(*cfg);
     if (rc != CTCSD_OK) return rc;
-    *out_bytes = align_up(sizeof(int) * (size_t)cfg->B * cfg->Hkv * Lcap, 256);
+    *out_bytes = align_up(sizeof(int) * (size_t)cfg->B * cfg->Hkv * ((size_t)Lcap + 1), 256);
     return CTCSD_OK;
 }
 
@@ -297,12 +388,21 @@ extern "C" int ctcsd_evict_rows(ctcsd_handle* hh, void* stream, void* workspace,
     p.status = status_ptr(h);
     // a cluster per (kv head, sequence): more CTAs while they all run at once (two fit on an SM) and each
     // still has rows to look at
+    const long long pairs = (long long)c.B * c.Hkv;
     int cs = 1;
-    while (cs < kMaxCluster && (long long)c.B * c.Hkv * cs * 2 <= 2ll * h->num_sms && Lcap / (cs * 2) >= 1024) cs *= 2;
+    while (cs < kMaxCluster && pairs * cs * 2 <= 2ll * h->num_sms && Lcap / (cs * 2) >= 1024) cs *= 2;
+    // the clusters cover less than half of the SMs, and there may be enough to copy: a kernel of its own for that
+    const long long movable = budget < Lcap - budget ? budget : Lcap - budget;
+    const bool apart = pairs * cs * 2 <= h->num_sms && movable > 0 && pairs * movable * p.row_bytes >= (4ll << 20);
+    p.n_move = apart ? p.lists + (size_t)pairs * Lcap : nullptr;
     const size_t smem = sizeof(EvictShared) + sizeof(unsigned) * kCacheKeys;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
     CTCSD_CUDA_CHECK(h, cudaFuncSetAttribute(evict_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    CTCSD_CUDA_CHECK(h, launch_pdl(evict_rows_kernel, dim3(cs, c.Hkv, c.B), dim3(kThreads), smem,
-                                   static_cast<cudaStream_t>(stream), cs, p, cs));
+    CTCSD_CUDA_CHECK(h, launch_pdl(evict_rows_kernel, dim3(cs, c.Hkv, c.B), dim3(kThreads), smem, s, cs, p, cs));
     h->launches++;
+    if (apart) {
+        CTCSD_CUDA_CHECK(h, launch_pdl(evict_move_kernel, dim3(2 * h->num_sms), dim3(kThreads), sizeof(long long) * (size_t)(pairs + 1), s, 1, p));
+        h->launches++;
+    }
     return CTCSD_OK;
 }

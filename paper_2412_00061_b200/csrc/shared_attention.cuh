@@ -35,7 +35,7 @@ struct SharedAttnParams {
     int* plan;              // workspace: header, row_off, tile_cum (written by CTA 0, read by the merge)
     float4* part_o;         // workspace: [span][2][D/4][TR]
     float2* part_ml;        // workspace: [span][2][TR] (reference in log2 units, sum)
-    int min_blocks;         // spans are not cut finer than this
+    int min_blocks, long_span;   // see span_map
 };
 
 constexpr int kSharedMaxB = 1024;              // sequences
@@ -146,10 +146,20 @@ __host__ __device__ inline SpanMap span_map_n(int per_head, int Hkv, int spans) 
     return m;
 }
 
-// As many spans as `max_spans` allows, none shorter than min_blocks unless it is the only one.
-__host__ __device__ inline SpanMap span_map(int per_head, int Hkv, int max_spans, int min_blocks) {
-    const long long want = (long long)per_head * Hkv / min_blocks;
-    return span_map_n(per_head, Hkv, want < 1 ? 1 : (want < max_spans ? (int)want : max_spans));
+// How many spans to cut the line into.  A span that crosses from one tile into the next pays for a second set of
+// queries and a second output, as much as several blocks.  So with few (kv head, tile) pairs every pair gets the same
+// number of spans, none shorter than min_blocks on average, and the cuts fall on the tiles' ends when
+// these have equal work; where spans are long (over `long_span` blocks) or the pairs outnumber them, balance counts more
+// and all max_spans are used.
+__host__ __device__ inline SpanMap span_map(int per_head, int tiles, int Hkv, int max_spans, int min_blocks, int long_span) {
+    const long long total = (long long)per_head * Hkv, pairs = (long long)tiles * Hkv;
+    if (pairs <= 0 || pairs >= max_spans || total >= (long long)max_spans * long_span) {
+        const long long fit = pairs <= 0 ? 1 : max_spans;
+        return span_map_n(per_head, Hkv, (int)fit);
+    }
+    const long long room = max_spans / pairs, want = total / (pairs * min_blocks);
+    const long long each = want < 1 ? 1 : (want < room ? want : room);
+    return span_map_n(per_head, Hkv, (int)(pairs * each));
 }
 
 // Tile that holds block x (0 <= x < tile_cum[tiles]) of a kv head.

@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(kSimpleThreads, 2) shared_attention_simple_ker
     pdl_wait();
     pdl_trigger();
     plan_build(pl, p, TR, KB, blockIdx.x == 0);
-    const SpanMap sp = span_map(pl.tile_cum[pl.tiles], p.Hkv, (int)gridDim.x, p.min_blocks);
+    const SpanMap sp = span_map(pl.tile_cum[pl.tiles], pl.tiles, p.Hkv, (int)gridDim.x, p.min_blocks, p.long_span);
     if (blockIdx.x == 0) plan_publish(pl, p, sp.spans);
     SpanWalk at;
 
@@ -428,7 +428,8 @@ extern "C" int ctcsd_tree_attention_shared(ctcsd_handle* hh, void* stream, void*
     p.plan = reinterpret_cast<int*>(ws + l.plan);
     p.part_ml = reinterpret_cast<float2*>(ws + l.ml);
     p.part_o = reinterpret_cast<float4*>(ws + l.o);
-    p.min_blocks = 4;
+    p.min_blocks = c.dtype == CTCSD_DTYPE_BF16 ? 3 : 1;
+    p.long_span = 16;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     int rc;
     if (c.dtype == CTCSD_DTYPE_BF16) rc = launch_shared_attention_tc(h, s, p);

@@ -220,7 +220,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
     pdl_wait();
     pdl_trigger();
     plan_build(pl, p, kTcRows, kKeys, blockIdx.x == 0);
-    const SpanMap sp = span_map(pl.tile_cum[pl.tiles], p.Hkv, (int)gridDim.x, p.min_blocks);
+    const SpanMap sp = span_map(pl.tile_cum[pl.tiles], pl.tiles, p.Hkv, (int)gridDim.x, p.min_blocks, p.long_span);
     if (blockIdx.x == 0) plan_publish(pl, p, sp.spans);
     bool failed = false;
     SpanWalk at;
