@@ -7,7 +7,7 @@
 // holds every row's position, which is what "newest" is decided on.
 //
 // One thread-block cluster per (kv head, sequence): radix selection of the threshold (11 + 11 + 10 bits, the
-// histograms added up through distributed shared memory), ranks by ballots, then the copies.  With few (kv head,
+// histograms added up through distributed shared memory), ranks by block scans, then the copies.  With few (kv head,
 // sequence) pairs their clusters leave most SMs idle, so the copies then are a second kernel's, spread evenly over all.
 #include "common.cuh"
 #include "tc_primitives.cuh"
@@ -22,6 +22,7 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kBins = 2048;
 constexpr int kCacheKeys = 8192;       // keys a CTA keeps in shared memory; a longer share is read again from L2
 constexpr int kMaxCluster = 8;
+constexpr int kMaxRun = 17;            // rows a thread looks after at a time (odd: its neighbours' rows lie in other banks)
 
 struct EvictParams {
     void* K; void* V;                  // [B,Hkv,Lcap,D]
@@ -39,15 +40,7 @@ __device__ __forceinline__ void cluster_sync(int cs) {
     if (cs == 1) __syncthreads();
     else asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ int ld_peer(const int* local, int rank) {
-    uint32_t a;
-    int v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tc::smem_u32(local)), "r"(rank));
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return v;
-}
-
-__device__ __forceinline__ int4 ld_peer4(const int* local, int rank) {
+__device__ __forceinline__ int4 ld_peer4(const void* local, int rank) {
     uint32_t a;
     int4 v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tc::smem_u32(local)), "r"(rank));
@@ -57,8 +50,12 @@ __device__ __forceinline__ int4 ld_peer4(const int* local, int rank) {
 
 // Copies pieces [i, n) in steps of `step`: piece k * chunks + c is 16 bytes (column c) of the k-th moving row, of K and
 // of V.  Four at a time, so that a thread has eight loads on their way.
-__device__ __forceinline__ void move_pieces(unsigned char* Kb, unsigned char* Vb, const int* hole_list, const int* mover_list,
-                                            int row_bytes, long long i, long long n, long long step) {
+__device__ __forceinline__ void move_pieces(const EvictParams& p, size_t row0, long long i, long long n, long long step) {
+    const int row_bytes = p.row_bytes;
+    unsigned char* Kb = static_cast<unsigned char*>(p.K) + row0 * row_bytes;
+    unsigned char* Vb = static_cast<unsigned char*>(p.V) + row0 * row_bytes;
+    const int* hole_list = p.lists + row0;
+    const int* mover_list = hole_list + p.Lcap / 2;
     const int chunks = row_bytes / 16;                                     // a power of two: 8, 16 or 32
     const int sh = 31 - __clz(chunks);
     constexpr int U = 4;
@@ -71,8 +68,9 @@ __device__ __forceinline__ void move_pieces(unsigned char* Kb, unsigned char* Vb
             src[u] = dst[u] = 0;
             if (x < n) {
                 const int k = (int)(x >> sh), c = (int)(x & (chunks - 1));
-                src[u] = (size_t)__ldcg(mover_list + k) * row_bytes + c * 16;
-                dst[u] = (size_t)__ldcg(hole_list + k) * row_bytes + c * 16;
+                const int from = __ldcg(mover_list + k), to = __ldcg(hole_list + k);
+                src[u] = (size_t)from * row_bytes + c * 16;
+                dst[u] = (size_t)to * row_bytes + c * 16;
             }
         }
 #pragma unroll
@@ -90,9 +88,11 @@ __device__ __forceinline__ void move_pieces(unsigned char* Kb, unsigned char* Vb
     }
 }
 
+constexpr unsigned kTopKey = 0xffffffffu;        // protected rows
+
 // Ranking key: larger is kept first.  Protected rows lead; then the weight, +0 and -0 alike, NaN last.
 __device__ __forceinline__ unsigned rank_key(float m, int pos, int sinks, int newest_from) {
-    if (pos < sinks || pos >= newest_from) return 0xffffffffu;
+    if (pos < sinks || pos >= newest_from) return kTopKey;
     if (m != m) return 0u;
     const unsigned u = __float_as_uint(m + 0.f);
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
@@ -100,10 +100,9 @@ __device__ __forceinline__ unsigned rank_key(float m, int pos, int sinks, int ne
 
 struct __align__(16) EvictShared {
     int hist[3][kBins];
-    int tot[kWarps];
-    int warp_cnt[3][kWarps];           // ties, dropped rows, moving rows per warp
-    int cta_cnt[3];
-    int pick[3];                       // digit, rows above it, rows in it
+    int scan[2][kWarps];               // warp totals of a block scan (two buffers: one barrier per scan)
+    int4 cta_cnt[2];                   // [0] ties; [1] dropped rows, moving rows
+    int pick[3][3];                    // per round: digit, rows above it, rows in it
 };
 
 __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, int cs) {
@@ -137,6 +136,28 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
         auto key_of = [&](int j) -> unsigned { return rank_key(mass[j], row_pos[j], p.sinks, newest_from); };
         auto key_at = [&](int j) -> unsigned { return cached ? cache[j - lo] : key_of(j); };
         __syncthreads();
+        int flip = 0;
+        // exclusive prefix over the block's threads, and the total
+        auto block_scan = [&](int v, int& total) -> int {
+            int incl = v;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += u;
+            }
+            if (lane == 31) sh->scan[flip][warp] = incl;
+            __syncthreads();
+            int below = 0;
+            total = 0;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const int x = sh->scan[flip][w];
+                below += w < warp ? x : 0;
+                total += x;
+            }
+            flip ^= 1;
+            return below + incl - v;
+        };
         // ---- threshold: the keep-th largest key, 11 + 11 + 10 bits from the top ----
         unsigned prefix = 0u;
         int shift = 32, left = keep;                                       // rows still to be found among the keys with this prefix
@@ -150,16 +171,18 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
                     int q[U];
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
-                        const int j = j0 + u * kThreads;
-                        m[u] = j < hi ? mass[j] : 0.f;
-                        q[u] = j < hi ? row_pos[j] : 0;
+                        const int j = min(j0 + u * kThreads, hi - 1);
+                        m[u] = mass[j];
+                        q[u] = row_pos[j];
                     }
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
                         const int j = j0 + u * kThreads;
-                        if (j >= hi) break;
+                        if (j >= hi) continue;
                         const unsigned key = rank_key(m[u], q[u], p.sinks, newest_from);
                         if (cached) cache[j - lo] = key;
+                        // (rows that go are overwritten by the moves, behind a barrier)
+                        if (!in_place && j < keep) { out_mass[j] = m[u]; out_pos[j] = q[u]; }
                         atomicAdd(&sh->hist[0][key >> shift], 1);
                     }
                 }
@@ -188,114 +211,125 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
                 }
             }
             const int sum = v[0] + v[1] + v[2] + v[3];
-            int incl = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int u = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += u;
-            }
-            if (lane == 31) sh->tot[warp] = incl;
-            __syncthreads();
-            int before = incl - sum;
-            for (int w = 0; w < warp; ++w) before += sh->tot[w];
+            int in_block;
+            int before = block_scan(sum, in_block);
 #pragma unroll
             for (int i = 0; i < kBins / kThreads; ++i) {
                 if (before < left && before + v[i] >= left) {              // exactly one bin of one thread
-                    sh->pick[0] = nb - 1 - (tid * (kBins / kThreads) + i);
-                    sh->pick[1] = before;
-                    sh->pick[2] = v[i];
+                    sh->pick[rd][0] = nb - 1 - (tid * (kBins / kThreads) + i);
+                    sh->pick[rd][1] = before;
+                    sh->pick[rd][2] = v[i];
                 }
                 before += v[i];
             }
             __syncthreads();
-            prefix = (prefix << bits) | (unsigned)sh->pick[0];
-            left -= sh->pick[1];
-            const bool all = sh->pick[2] == left;                          // the whole bin stays: no need to look closer
-            __syncthreads();
-            if (all) break;
+            prefix = (prefix << bits) | (unsigned)sh->pick[rd][0];
+            left -= sh->pick[rd][1];
+            if (sh->pick[rd][2] == left) break;                            // the whole bin stays: no need to look closer
         }
         // rows whose key's top bits are above the threshold stay; of those equal to it the first `left`
         const bool ties_split = shift == 0;
-        // every warp owns a contiguous run of rows, so that ranks follow row order
-        const int run = ((hi - lo + kWarps - 1) / kWarps + 31) / 32 * 32;
-        const int w0 = min(lo + warp * run, hi), w1 = min(w0 + run, hi);
-        int tie_base = 0;
-        if (ties_split) {
-            int cnt = 0;
-            for (int j = w0; j < w1; j += 32) {
-                const bool tie = j + lane < w1 && key_at(j + lane) == prefix;
-                cnt += __popc(__ballot_sync(0xffffffffu, tie));
-            }
-            if (lane == 0) sh->warp_cnt[0][warp] = cnt;
-            __syncthreads();
-            if (tid == 0) {
-                int s = 0;
-                for (int w = 0; w < kWarps; ++w) s += sh->warp_cnt[0][w];
-                sh->cta_cnt[0] = s;
-            }
-            cluster_sync(cs);
-            for (int c = 0; c < rank; ++c) tie_base += ld_peer(&sh->cta_cnt[0], c);
-            for (int w = 0; w < warp; ++w) tie_base += sh->warp_cnt[0][w];
-        }
-        // visits this warp's rows in order with (row, dropped before the new length, kept behind it)
-        auto visit = [&](auto&& f) {
-            int tie_rank = tie_base;
-            for (int j = w0; j < w1; j += 32) {
-                const int r = j + lane;
-                const bool in = r < w1;
-                const unsigned top = in ? key_at(r) >> shift : 0u;
-                bool kept = in && top > prefix;
-                const bool tie = in && top == prefix;
-                if (ties_split) {
-                    const unsigned m = __ballot_sync(0xffffffffu, tie);
-                    kept = kept || (tie && tie_rank + __popc(m & ((1u << lane) - 1u)) < left);
-                    tie_rank += __popc(m);
-                } else {
-                    kept = kept || tie;
-                }
-                f(r, in && !kept && r < keep, kept && r >= keep, kept && r < keep);
+        // every thread owns a run of rows, so that ranks follow row order; a share that is not in shared memory is
+        // looked at in several tiles, and again in every pass
+        const int n = hi - lo;
+        const int run = min((n + kThreads - 1) / kThreads | 1, kMaxRun), tile = run * kThreads;
+        auto classify = [&](int t0, unsigned& above, unsigned& ties) {     // bit i: row lo + t0 + tid * run + i
+            above = ties = 0u;
+            const int r0 = lo + t0 + tid * run;
+            for (int i = 0; i < run && r0 + i < hi; ++i) {
+                const unsigned top = key_at(r0 + i) >> shift;
+                above |= top > prefix ? 1u << i : 0u;
+                ties |= top == prefix ? 1u << i : 0u;
             }
         };
-        int holes = 0, movers = 0;
-        visit([&](int, bool hole, bool mover, bool) {
-            holes += __popc(__ballot_sync(0xffffffffu, hole));
-            movers += __popc(__ballot_sync(0xffffffffu, mover));
-        });
-        if (lane == 0) { sh->warp_cnt[1][warp] = holes; sh->warp_cnt[2][warp] = movers; }
-        __syncthreads();
-        if (tid < 2) {
-            int s = 0;
-            for (int w = 0; w < kWarps; ++w) s += sh->warp_cnt[1 + tid][w];
-            sh->cta_cnt[1 + tid] = s;
+        int tie_base = 0;
+        if (ties_split) {
+            int cnt = 0, total;
+            for (int t0 = 0; t0 < n; t0 += tile) {
+                unsigned above, ties;
+                classify(t0, above, ties);
+                cnt += __popc(ties);
+            }
+            block_scan(cnt, total);
+            if (cs > 1) {
+                if (tid == 0) sh->cta_cnt[0] = make_int4(total, 0, 0, 0);
+                cluster_sync(cs);
+                int4 q[kMaxCluster];
+#pragma unroll
+                for (int c = 0; c < kMaxCluster; ++c) q[c] = c < rank ? ld_peer4(&sh->cta_cnt[0], c) : make_int4(0, 0, 0, 0);
+#pragma unroll
+                for (int c = 0; c < kMaxCluster; ++c) tie_base += q[c].x;
+            }
         }
-        cluster_sync(cs);
-        int hole_at = 0, mover_at = 0, n_move = 0;
-        for (int c = 0; c < cs; ++c) {
-            const int x = ld_peer(&sh->cta_cnt[1], c), y = ld_peer(&sh->cta_cnt[2], c);
-            if (c < rank) { hole_at += x; mover_at += y; }
-            n_move += x;
+        // rows of the tile that are dropped before the new length, and that are kept behind it; `place`: how many of
+        // each (low and high half) come before this thread's in the tile, `sum`: in the whole tile
+        int tie_run = tie_base;
+        auto sort_out = [&](int t0, unsigned& holes, unsigned& movers, int& place, int& sum) {
+            unsigned above, ties;
+            classify(t0, above, ties);
+            if (ties_split) {
+                int total;
+                int allow = left - tie_run - block_scan(__popc(ties), total);
+                tie_run += total;
+                for (; ties != 0u && allow > 0; --allow) {
+                    above |= ties & (0u - ties);
+                    ties &= ties - 1u;
+                }
+            } else {
+                above |= ties;
+            }
+            const int r0 = lo + t0 + tid * run;
+            const int mine = max(0, min(run, hi - r0)), front = max(0, min(mine, keep - r0));
+            const unsigned all = (1u << mine) - 1u, before = (1u << front) - 1u;       // (mine <= 17)
+            holes = ~above & before;
+            movers = above & all & ~before;
+            place = block_scan(__popc(holes) | __popc(movers) << 16, sum);
+        };
+        unsigned holes = 0u, movers = 0u;
+        int place = 0, n_holes = 0, n_movers = 0;
+        for (int t0 = 0; t0 < n; t0 += tile) {
+            int sum;
+            sort_out(t0, holes, movers, place, sum);
+            n_holes += sum & 0xffff;
+            n_movers += sum >> 16;
         }
-        for (int w = 0; w < warp; ++w) { hole_at += sh->warp_cnt[1][w]; mover_at += sh->warp_cnt[2][w]; }
+        int hole_at = 0, mover_at = 0, n_move = n_holes;
+        if (cs > 1) {
+            if (tid == 0) sh->cta_cnt[1] = make_int4(n_holes, n_movers, 0, 0);
+            cluster_sync(cs);
+            int4 q[kMaxCluster];
+#pragma unroll
+            for (int c = 0; c < kMaxCluster; ++c) q[c] = c < cs ? ld_peer4(&sh->cta_cnt[1], c) : make_int4(0, 0, 0, 0);
+            n_move = 0;
+#pragma unroll
+            for (int c = 0; c < kMaxCluster; ++c) {
+                hole_at += c < rank ? q[c].x : 0;
+                mover_at += c < rank ? q[c].y : 0;
+                n_move += q[c].x;
+            }
+        }
         // as many rows move as there are holes, at most half of L: the lists share one array of L entries
         int* hole_list = p.lists + row0;
         int* mover_list = p.lists + row0 + p.Lcap / 2;
-        visit([&](int r, bool hole, bool mover, bool stays) {
-            const unsigned mh = __ballot_sync(0xffffffffu, hole), mm = __ballot_sync(0xffffffffu, mover);
-            const unsigned below = (1u << lane) - 1u;
-            if (hole && CTCSD_IN_BOUNDS(p.status, 61, hole_at + __popc(mh & below), p.Lcap / 2)) hole_list[hole_at + __popc(mh & below)] = r;
-            if (mover && CTCSD_IN_BOUNDS(p.status, 62, mover_at + __popc(mm & below), p.Lcap - p.Lcap / 2))
-                mover_list[mover_at + __popc(mm & below)] = r;
-            hole_at += __popc(mh);
-            mover_at += __popc(mm);
-            if (stays && !in_place) { out_mass[r] = mass[r]; out_pos[r] = row_pos[r]; }
-        });
+        tie_run = tie_base;
+        for (int t0 = 0; t0 < n; t0 += tile) {
+            int sum = 0;
+            if (n > tile) sort_out(t0, holes, movers, place, sum);         // (else they are still in registers)
+            const int r0 = lo + t0 + tid * run;
+            int h = hole_at + (place & 0xffff), m = mover_at + (place >> 16);
+            for (; holes != 0u; holes &= holes - 1u, ++h)
+                if (CTCSD_IN_BOUNDS(p.status, 61, h, p.Lcap / 2)) hole_list[h] = r0 + __ffs(holes) - 1;
+            for (; movers != 0u; movers &= movers - 1u, ++m)
+                if (CTCSD_IN_BOUNDS(p.status, 62, m, p.Lcap - p.Lcap / 2)) mover_list[m] = r0 + __ffs(movers) - 1;
+            hole_at += sum & 0xffff;
+            mover_at += sum >> 16;
+        }
         cluster_sync(cs);                                                  // the lists are complete; every weight has been read
         // ---- the moves: 16 bytes per thread and tensor, neighbours on one row ----
         if (p.n_move) {
             if (rank == 0 && tid == 0) p.n_move[b * p.Hkv + g] = n_move;
         } else {
-            move_pieces(static_cast<unsigned char*>(p.K) + row0 * p.row_bytes, static_cast<unsigned char*>(p.V) + row0 * p.row_bytes, hole_list,
-                        mover_list, p.row_bytes, (long long)rank * kThreads + tid, (long long)n_move * (p.row_bytes / 16), (long long)cs * kThreads);
+            move_pieces(p, row0, (long long)rank * kThreads + tid, (long long)n_move * (p.row_bytes / 16), (long long)cs * kThreads);
         }
         for (int k = rank * kThreads + tid; k < n_move; k += cs * kThreads) {
             const int src = __ldcg(mover_list + k), dst = __ldcg(hole_list + k);
@@ -342,10 +376,7 @@ __global__ void __launch_bounds__(kThreads) evict_move_kernel(EvictParams p) {
     for (int u = 0; u < units; ++u) {
         const long long from = x0 > cum[u] ? x0 : cum[u], to = x1 < cum[u + 1] ? x1 : cum[u + 1];
         if (from >= to) continue;
-        const size_t row0 = (size_t)u * p.Lcap;
-        const int* hole_list = p.lists + row0;
-        move_pieces(static_cast<unsigned char*>(p.K) + row0 * p.row_bytes, static_cast<unsigned char*>(p.V) + row0 * p.row_bytes, hole_list,
-                    hole_list + p.Lcap / 2, p.row_bytes, from - cum[u] + threadIdx.x, to - cum[u], kThreads);
+        move_pieces(p, (size_t)u * p.Lcap, from - cum[u] + threadIdx.x, to - cum[u], kThreads);
     }
 }
 
