@@ -122,9 +122,12 @@ def _ptr(t: Optional[torch.Tensor], dtype=None, numel: Optional[int] = None, nam
     return t.data_ptr()
 
 
-def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+def _stream_ptr(stream: Optional[torch.cuda.Stream], device_index: Optional[int] = None) -> int:
+    """The stream's handle; without one the current stream (of `device_index`, else of the current device).  The raw
+    query is what torch.cuda.current_stream() makes its object from, at a fortieth of its time."""
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device_index is None else device_index)
 
 
 class Handle:
@@ -137,6 +140,7 @@ class Handle:
             raise CtcsdError("ctcsd needs a CUDA device (B200); there is no CPU path")
         self.cfg = CConfig(B, H, V, T, k, beam, topN, max_nodes, Hq, Hkv, D, dtype, score_mode, max_draft_rows)
         self.device = torch.device(device)
+        self._dev = torch.cuda.current_device() if self.device.index is None else self.device.index
         self.act_dtype = torch.bfloat16 if dtype == DTYPE_BF16 else torch.float32
         self.M_draft_max = max_draft_rows or B
         nbytes = ctypes.c_size_t(0)
@@ -408,7 +412,7 @@ class Handle:
         W = (c.max_nodes + 63) // 64
         rows = c.B * c.max_nodes * c.Hq
         rc = self.lib.ctcsd_tree_attention_shared(
-            self._h, _stream_ptr(stream), sa["ws_ptr"], sa["ws_bytes"],
+            self._h, _stream_ptr(stream, self._dev), sa["ws_ptr"], sa["ws_bytes"],
             _ptr(Q, act, rows * c.D, "Q"), _ptr(Kp, act, c.Hkv * Pcap * c.D, "Kp"), _ptr(Vp, act, c.Hkv * Pcap * c.D, "Vp"),
             Pcap, _ptr(prefix_len, i32, c.B, "prefix_len"),
             _ptr(K, act, c.B * c.Hkv * Lcap * c.D, "K"), _ptr(V, act, c.B * c.Hkv * Lcap * c.D, "V"), Lcap,
@@ -426,7 +430,7 @@ class Handle:
         i32, f32 = torch.int32, torch.float32
         Lcap = K.shape[2]
         rc = self.lib.ctcsd_attention_mass(
-            self._h, _stream_ptr(stream),
+            self._h, _stream_ptr(stream, self._dev),
             _ptr(Q, self.act_dtype, c.B * c.max_nodes * c.Hq * c.D, "Q"),
             _ptr(K, self.act_dtype, c.B * c.Hkv * Lcap * c.D, "K"), Lcap,
             _ptr(kv_len, i32, c.B, "kv_len"), _ptr(acc_len, i32, c.B, "acc_len"), _ptr(acc_nodes, i32, c.B * c.T, "acc_nodes"),
@@ -452,7 +456,7 @@ class Handle:
         Lcap = K.shape[2]
         rows = c.B * c.Hkv * Lcap
         rc = self.lib.ctcsd_evict_rows(
-            self._h, _stream_ptr(stream), ev["ws_ptr"], ev["ws_bytes"],
+            self._h, _stream_ptr(stream, self._dev), ev["ws_ptr"], ev["ws_bytes"],
             _ptr(K, self.act_dtype, rows * c.D, "K"), _ptr(V, self.act_dtype, rows * c.D, "V"), Lcap,
             _ptr(mass, f32, rows, "mass"), _ptr(row_pos, i32, rows, "row_pos"), _ptr(kv_len, i32, c.B, "kv_len"),
             _ptr(n_evicted, i32, c.B, "n_evicted"), int(budget), int(sinks), int(recent),

@@ -327,7 +327,7 @@ int launch_mass(Handle* h, cudaStream_t s, const MassParams& p, bool bf16) {
         smem = sizeof(float) * (64 * (D + 4) + 64 * D + 64 + 4 * 64 + 64) + sizeof(int) * (p.B + 1);
     }
     auto kern = bf16 ? attention_mass_mma_kernel<D> : attention_mass_f32_kernel<D>;
-    CTCSD_CUDA_CHECK(h, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    CTCSD_CUDA_CHECK(h, prepare_kernel(h, bf16 ? kPrepMassMma : kPrepMassF32, kern));
     CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(h->num_sms * 2), dim3(kThreads), smem, s, 1, p));
     h->launches++;
     return CTCSD_OK;
@@ -354,6 +354,7 @@ extern "C" int ctcsd_attention_mass(ctcsd_handle* hh, void* stream, const void* 
     p.scale = scale; p.decay = decay;
     p.status = status_ptr(h);
     const bool bf16 = c.dtype == CTCSD_DTYPE_BF16;
+    const DeviceGuard on(h->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return c.D == 64 ? launch_mass<64>(h, s, p, bf16) : launch_mass<128>(h, s, p, bf16);
 }

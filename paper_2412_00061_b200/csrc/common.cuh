@@ -56,7 +56,34 @@ struct Handle {
     long long launches;
     const void* l2_hint_ptr;     // range that ctcsd_draft_logits asks L2 to fetch when it finishes
     size_t l2_hint_bytes;
+    unsigned prepared;           // kernels (bits kPrep*) whose shared-memory limit has been raised on the handle's device
 };
+
+// A call made while another device is current works on the handle's all the same.
+struct DeviceGuard {
+    int before, now;
+    explicit DeviceGuard(int device) : before(device), now(device) {
+        if (cudaGetDevice(&before) == cudaSuccess && before != now) cudaSetDevice(now);
+    }
+    ~DeviceGuard() {
+        if (before != now) cudaSetDevice(before);
+    }
+    DeviceGuard(const DeviceGuard&) = delete;
+    DeviceGuard& operator=(const DeviceGuard&) = delete;
+};
+
+enum { kPrepSharedTc = 1, kPrepSharedSimple = 2, kPrepMassMma = 4, kPrepMassF32 = 8, kPrepEvict = 16 };
+constexpr int kMaxDynamicSmem = 227 * 1024;
+
+// Lets `kernel` (no static shared memory) use all of an SM's shared memory; the limit is the same for every caller, so once per
+// handle is enough.
+template <typename K>
+inline cudaError_t prepare_kernel(Handle* h, unsigned bit, K kernel) {
+    if (h->prepared & bit) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynamicSmem);
+    if (e == cudaSuccess) h->prepared |= bit;
+    return e;
+}
 
 // Sampling acceptance: the token drawn after tree node i of sequence b is
 // argmax_v fma(y[v], inv_temp, noise[(b * rows_per_seq + depth[b,i]) * V + v]).  noise == null: plain arg-max.

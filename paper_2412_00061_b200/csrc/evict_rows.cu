@@ -427,8 +427,9 @@ extern "C" int ctcsd_evict_rows(ctcsd_handle* hh, void* stream, void* workspace,
     const bool apart = pairs * cs * 2 <= h->num_sms && movable > 0 && pairs * movable * p.row_bytes >= (4ll << 20);
     p.n_move = apart ? p.lists + (size_t)pairs * Lcap : nullptr;
     const size_t smem = sizeof(EvictShared) + sizeof(unsigned) * kCacheKeys;
+    const DeviceGuard on(h->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    CTCSD_CUDA_CHECK(h, cudaFuncSetAttribute(evict_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    CTCSD_CUDA_CHECK(h, prepare_kernel(h, kPrepEvict, evict_rows_kernel));
     CTCSD_CUDA_CHECK(h, launch_pdl(evict_rows_kernel, dim3(cs, c.Hkv, c.B), dim3(kThreads), smem, s, cs, p, cs));
     h->launches++;
     if (apart) {

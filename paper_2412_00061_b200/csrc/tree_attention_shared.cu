@@ -351,7 +351,7 @@ int launch_simple(Handle* h, cudaStream_t s, const SharedAttnParams& p) {
     const int max_tiles = (int)(((long long)p.B * p.max_nodes * (p.Hq / p.Hkv) + TR - 1) / TR);
     const size_t smem = sizeof(float) * (TR * (D + 4) + KB * (D + 4) + TR * (KB + 4)) + sizeof(int) * plan_ints(p.B, max_tiles);
     auto kern = shared_attention_simple_kernel<D>;
-    CTCSD_CUDA_CHECK(h, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    CTCSD_CUDA_CHECK(h, prepare_kernel(h, kPrepSharedSimple, kern));
     CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(h->num_sms * kSharedSpansPerSm), dim3(kSimpleThreads), smem, s, 1, p));
     h->launches++;
     return CTCSD_OK;
@@ -430,6 +430,7 @@ extern "C" int ctcsd_tree_attention_shared(ctcsd_handle* hh, void* stream, void*
     p.part_o = reinterpret_cast<float4*>(ws + l.o);
     p.min_blocks = c.dtype == CTCSD_DTYPE_BF16 ? 3 : 1;
     p.long_span = 16;
+    const DeviceGuard on(h->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     int rc;
     if (c.dtype == CTCSD_DTYPE_BF16) rc = launch_shared_attention_tc(h, s, p);

@@ -741,7 +741,7 @@ int launch_tc(Handle* h, cudaStream_t s, const SharedAttnParams& p) {
     const size_t smem = (size_t)2 * kHalf * D * 2 + (size_t)Shape<D>::kStages * 2 * kKeys * D * 2 + sizeof(SharedState) +
                         sizeof(int) * plan_ints(p.B, max_tiles);
     auto kern = shared_attention_tc_kernel<D>;
-    CTCSD_CUDA_CHECK(h, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    CTCSD_CUDA_CHECK(h, prepare_kernel(h, kPrepSharedTc, kern));
     CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(h->num_sms), dim3(kThreads), smem, s, 1, tmKp, tmVp, tmK, tmV, p));
     h->launches++;
     return CTCSD_OK;
