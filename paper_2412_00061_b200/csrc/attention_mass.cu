@@ -19,6 +19,8 @@ constexpr int kThreads = 256;
 constexpr int kMaxRows = 256;          // query rows held in shared memory at a time; more rows take another pass over K
 constexpr int kMassMaxB = 1024;
 
+template <int N> struct Count { static constexpr int value = N; };
+
 struct MassParams {
     const void* Q; const void* K;      // [B,max_nodes,Hq,D], [B,Hkv,Lcap,D]
     const int* kv_len; const int* acc_len; const int* acc_nodes;
@@ -175,28 +177,44 @@ __global__ void __launch_bounds__(kThreads, 2) attention_mass_mma_kernel(MassPar
                 if (writes && j1 < kv && (j1 < base || r0 > 0)) old1 = p.mass[krow0 + j1];
                 const bool tail = blk * KB + KB > base;                     // some key is not seen by every query
                 float w0 = 0.f, w1 = 0.f;
-                for (int rt = 0; rt < tiles; ++rt) {
-                    float c4[4] = {0.f, 0.f, 0.f, 0.f};
-                    const uint4* qf = Qf + rt * NC * 32 + lane;
+                // N row tiles at a time: an mma.sync that waits for the one before takes some 200 cycles here, so
+                // several chains run side by side (a lone tile is cut into two chains)
+                auto weigh = [&](auto count, int rt) {
+                    constexpr int N = decltype(count)::value, CH = N >= 4 ? 1 : 2;
+                    float c4[N][CH][4];
 #pragma unroll
-                    for (int c = 0; c < NC; ++c) {
-                        const uint4 q = qf[c * 32];
-                        mma_bf16(c4, cur[0][c].x, cur[1][c].x, cur[0][c].y, cur[1][c].y, q.x, q.y);
-                        mma_bf16(c4, cur[0][c].z, cur[1][c].z, cur[0][c].w, cur[1][c].w, q.z, q.w);
+                    for (int i = 0; i < N * CH * 4; ++i) c4[i / (CH * 4)][(i / 4) % CH][i % 4] = 0.f;
+#pragma unroll
+                    for (int c = 0; c < NC; ++c)
+#pragma unroll
+                        for (int i = 0; i < N; ++i) {
+                            const uint4 q = Qf[((rt + i) * NC + c) * 32 + lane];
+                            mma_bf16(c4[i][0], cur[0][c].x, cur[1][c].x, cur[0][c].y, cur[1][c].y, q.x, q.y);
+                            mma_bf16(c4[i][CH - 1], cur[0][c].z, cur[1][c].z, cur[0][c].w, cur[1][c].w, q.z, q.w);
+                        }
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        float s[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) s[x] = CH == 2 ? c4[i][0][x] + c4[i][CH - 1][x] : c4[i][0][x];
+                        const float2 ls = *reinterpret_cast<const float2*>(lse2 + (rt + i) * 8 + tig * 2);
+                        float e0 = exp2_fast(fmaf(s[0], sl2, -ls.x)), e1 = exp2_fast(fmaf(s[1], sl2, -ls.y));
+                        float e2 = exp2_fast(fmaf(s[2], sl2, -ls.x)), e3 = exp2_fast(fmaf(s[3], sl2, -ls.y));
+                        if (tail) {
+                            const int2 lm = *reinterpret_cast<const int2*>(lim + (rt + i) * 8 + tig * 2);
+                            e0 = lm.x >= 0 && j0 - base <= lm.x ? e0 : 0.f;
+                            e1 = lm.y >= 0 && j0 - base <= lm.y ? e1 : 0.f;
+                            e2 = lm.x >= 0 && j1 - base <= lm.x ? e2 : 0.f;
+                            e3 = lm.y >= 0 && j1 - base <= lm.y ? e3 : 0.f;
+                        }
+                        w0 += e0 + e1;
+                        w1 += e2 + e3;
                     }
-                    const float2 ls = *reinterpret_cast<const float2*>(lse2 + rt * 8 + tig * 2);
-                    float e0 = exp2_fast(fmaf(c4[0], sl2, -ls.x)), e1 = exp2_fast(fmaf(c4[1], sl2, -ls.y));
-                    float e2 = exp2_fast(fmaf(c4[2], sl2, -ls.x)), e3 = exp2_fast(fmaf(c4[3], sl2, -ls.y));
-                    if (tail) {
-                        const int2 lm = *reinterpret_cast<const int2*>(lim + rt * 8 + tig * 2);
-                        e0 = lm.x >= 0 && j0 - base <= lm.x ? e0 : 0.f;
-                        e1 = lm.y >= 0 && j0 - base <= lm.y ? e1 : 0.f;
-                        e2 = lm.x >= 0 && j1 - base <= lm.x ? e2 : 0.f;
-                        e3 = lm.y >= 0 && j1 - base <= lm.y ? e3 : 0.f;
-                    }
-                    w0 += e0 + e1;
-                    w1 += e2 + e3;
-                }
+                };
+                int rt = 0;
+                for (; rt + 4 <= tiles; rt += 4) weigh(Count<4>(), rt);
+                if (rt + 2 <= tiles) { weigh(Count<2>(), rt); rt += 2; }
+                if (rt < tiles) weigh(Count<1>(), rt);
 #pragma unroll
                 for (int o = 1; o < 4; o <<= 1) {
                     w0 += __shfl_xor_sync(0xffffffffu, w0, o);
