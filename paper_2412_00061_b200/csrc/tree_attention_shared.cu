@@ -249,31 +249,35 @@ template <> __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16*
     *reinterpret_cast<uint4*>(out) = *reinterpret_cast<uint4*>(w);
 }
 
-constexpr int kMergeThreads = 256;
-
+// A warp holds 8 columns of 32 rows: D / 8 warps.  The parts of a tile are taken four at a time, all their loads on the
+// way at once, against a reference that follows the largest so far.
 template <typename T, int D, int TR>
-__global__ void __launch_bounds__(kMergeThreads) shared_attention_merge_kernel(SharedAttnParams p, long long units) {
+__global__ void __launch_bounds__(D * 4) shared_attention_merge_kernel(SharedAttnParams p, long long units) {
+    constexpr int kWarps = D / 8, U = 4;
+    extern __shared__ int row_off[];                         // [B+1]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int grp = p.Hq / p.Hkv;
     pdl_wait();
     pdl_trigger();
-    const int rows = p.plan[0], tiles = p.plan[1];
-    const SpanMap sp = span_map_n(p.plan[2], p.Hkv, p.plan[3]);
-    const int* row_off = p.plan + kPlanHeader;
-    const int* tile_cum = row_off + p.B + 1;
-    const int max_rows = p.B * p.max_nodes * grp;            // packed rows if every node were live
+    const int* tile_cum = p.plan + kPlanHeader + p.B + 1;
+    const int rows = p.plan[0], per_head = p.plan[2], spans = p.plan[3];
+    for (int b = threadIdx.x; b <= p.B; b += kWarps * 32) row_off[b] = p.plan[kPlanHeader + b];
+    const SpanMap sp = span_map_n(per_head, p.Hkv, spans);
+    const int node_rows = p.max_nodes * grp;
+    const int max_rows = p.B * node_rows;                    // packed rows if every node were live
     const int chunks = (max_rows + 31) / 32;
+    __syncthreads();
     for (long long u = blockIdx.x; u < units; u += gridDim.x) {
         const int g = (int)(u / chunks), ch = (int)(u - (long long)g * chunks);
         {   // zero rows: output row (b, node, head of group g) for the nodes that are not used
             const int m = ch * 32 + lane;
             if (m < max_rows) {
-                const int b = m / (p.max_nodes * grp), o = m - b * p.max_nodes * grp;
+                const int b = m / node_rows, o = m - b * node_rows;
                 if (o >= row_off[b + 1] - row_off[b]) {
                     const int node = o / grp;
                     const size_t orow = ((size_t)b * p.max_nodes + node) * p.Hq + g * grp + (o - node * grp);
                     const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                    for (int c = warp; c < D / 8; c += kMergeThreads / 32) store8<T>(static_cast<T*>(p.O) + orow * D + 8 * c, z);
+                    store8<T>(static_cast<T*>(p.O) + orow * D + 8 * warp, z);
                     if (warp == 0 && p.lse) p.lse[orow] = -INFINITY;
                 }
             }
@@ -281,18 +285,49 @@ __global__ void __launch_bounds__(kMergeThreads) shared_attention_merge_kernel(S
         const int pr0 = ch * 32;
         if (pr0 >= rows) continue;
         const int t = pr0 / TR;                              // 32 divides TR: one tile for all lanes
-        const long long xs = (long long)g * sp.per_head + tile_cum[t], xe = (long long)g * sp.per_head + tile_cum[t + 1];
+        const long long xs = (long long)g * per_head + tile_cum[t], xe = (long long)g * per_head + tile_cum[t + 1];
         const int c0 = sp.span_of(xs), c1 = sp.span_of(xe - 1);
         if (c0 == c1) continue;                              // finished by its span
         const int pr = pr0 + lane;
         if (pr >= rows) continue;
         const int r = pr - t * TR;
-        float ref = -INFINITY, sum = 0.f;
-        for (int c = c0; c <= c1; ++c) {
-            const size_t part = (size_t)c * 2 + (sp.start(c) > xs ? 0 : 1);
-            ref = fmaxf(ref, p.part_ml[part * TR + r].x);
+        // only the first part can be one that a span begins (slot 1); the others continue a tile (slot 0)
+        float ref = -INFINITY, sum = 0.f, a[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] = 0.f;
+        for (int c = c0; c <= c1; c += U) {
+            float2 ml[U];
+            float4 o[U][2];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                // (the last part again past the end, with no weight)
+                const int cc = min(c + i, c1);
+                const size_t part = (size_t)cc * 2 + (cc == c0 ? 1 : 0);
+                ml[i] = p.part_ml[part * TR + r];
+                o[i][0] = p.part_o[(part * (D / 4) + 2 * warp) * TR + r];
+                o[i][1] = p.part_o[(part * (D / 4) + 2 * warp + 1) * TR + r];
+                if (c + i > c1) ml[i] = make_float2(-INFINITY, 0.f);
+            }
+            float top = ref;
+#pragma unroll
+            for (int i = 0; i < U; ++i) top = fmaxf(top, ml[i].x);
+            const float base = top == -INFINITY ? 0.f : top;
+            const float keep = exp2_fast(ref - base);
+            sum *= keep;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[e] *= keep;
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const float w = exp2_fast(ml[i].x - base);
+                sum = fmaf(w, ml[i].y, sum);
+                if (!(ml[i].y != 0.f)) continue;             // this part saw nothing: its output is not meaningful
+                a[0] = fmaf(w, o[i][0].x, a[0]); a[1] = fmaf(w, o[i][0].y, a[1]);
+                a[2] = fmaf(w, o[i][0].z, a[2]); a[3] = fmaf(w, o[i][0].w, a[3]);
+                a[4] = fmaf(w, o[i][1].x, a[4]); a[5] = fmaf(w, o[i][1].y, a[5]);
+                a[6] = fmaf(w, o[i][1].z, a[6]); a[7] = fmaf(w, o[i][1].w, a[7]);
+            }
+            ref = top;
         }
-        const float base = ref == -INFINITY ? 0.f : ref;
         int lo = 0, hi = p.B - 1;
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
@@ -300,36 +335,10 @@ __global__ void __launch_bounds__(kMergeThreads) shared_attention_merge_kernel(S
         }
         const int o = pr - row_off[lo], node = o / grp;
         const size_t orow = ((size_t)lo * p.max_nodes + node) * p.Hq + g * grp + (o - node * grp);
-        float a[(D / 8 + kMergeThreads / 32 - 1) / (kMergeThreads / 32)][8];
-        constexpr int NC = D / 8 / (kMergeThreads / 32);     // chunks of 8 columns per warp
-#pragma unroll
-        for (int k = 0; k < NC; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) a[k][e] = 0.f;
-        for (int c = c0; c <= c1; ++c) {
-            const size_t part = (size_t)c * 2 + (sp.start(c) > xs ? 0 : 1);
-            const float2 ml = p.part_ml[part * TR + r];
-            const float w = exp2_fast(ml.x - base);
-            sum = fmaf(w, ml.y, sum);
-            if (!(ml.y != 0.f)) continue;                    // this part saw nothing: its output is not meaningful
-#pragma unroll
-            for (int k = 0; k < NC; ++k) {
-                const int col = warp + k * (kMergeThreads / 32);
-                const float4 u0 = p.part_o[(part * (D / 4) + 2 * col) * TR + r];
-                const float4 u1 = p.part_o[(part * (D / 4) + 2 * col + 1) * TR + r];
-                a[k][0] = fmaf(w, u0.x, a[k][0]); a[k][1] = fmaf(w, u0.y, a[k][1]);
-                a[k][2] = fmaf(w, u0.z, a[k][2]); a[k][3] = fmaf(w, u0.w, a[k][3]);
-                a[k][4] = fmaf(w, u1.x, a[k][4]); a[k][5] = fmaf(w, u1.y, a[k][5]);
-                a[k][6] = fmaf(w, u1.z, a[k][6]); a[k][7] = fmaf(w, u1.w, a[k][7]);
-            }
-        }
         const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
 #pragma unroll
-        for (int k = 0; k < NC; ++k) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) a[k][e] *= inv;
-            store8<T>(static_cast<T*>(p.O) + orow * D + 8 * (warp + k * (kMergeThreads / 32)), a[k]);
-        }
+        for (int e = 0; e < 8; ++e) a[e] *= inv;
+        store8<T>(static_cast<T*>(p.O) + orow * D + 8 * warp, a);
         if (warp == 0 && p.lse) p.lse[orow] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
     }
 }
@@ -338,9 +347,9 @@ template <typename T, int D, int TR>
 int launch_merge(Handle* h, cudaStream_t s, const SharedAttnParams& p) {
     const long long max_rows = (long long)p.B * p.max_nodes * (p.Hq / p.Hkv);
     const long long units = (max_rows + 31) / 32 * p.Hkv;
-    const long long cap = (long long)h->num_sms * 64;
+    const long long cap = (long long)h->num_sms * 16;
     CTCSD_CUDA_CHECK(h, launch_pdl(shared_attention_merge_kernel<T, D, TR>, dim3((unsigned)(units < cap ? units : cap)),
-                                   dim3(kMergeThreads), 0, s, 1, p, units));
+                                   dim3(D * 4), sizeof(int) * (size_t)(p.B + 1), s, 1, p, units));
     h->launches++;
     return CTCSD_OK;
 }
