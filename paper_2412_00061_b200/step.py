@@ -71,12 +71,63 @@ class DraftVerifyStep:
             self.out["draft_logits_dbg"] = z(self.M, T, cfg.V + 1, dtype=f32)
             self.out["lm_logits_dbg"] = z(B * n, cfg.V, dtype=f32)
         self.inp: Dict[str, Optional[torch.Tensor]] = {}
+        self.shared = None       # workspace of the attention over a shared prefix
+        self.cache = None        # state of the cache budget (enable_cache_budget)
 
     def set_inputs(self, **tensors):
-        """x, Wd, blank_bias, row_seq, sel_row, base_tok, kv_len, Q, K, V, hn, Wl (device tensors)."""
+        """x, Wd, blank_bias, row_seq, sel_row, base_tok, kv_len, Q, K, V, hn, Wl (device tensors); Kp, Vp
+        [Hkv,Pcap,D] and prefix_len [B] when the sequences share a prefix: the attention then reads it once
+        for all of them, and tree positions start behind it."""
         self.inp.update(tensors)
+        if tensors.get("Kp") is not None and self.shared is None:
+            self._use_shared_attention()
         if "Wl" in tensors and self.cfg.dtype == "bf16" and self.L2_PREFETCH_BYTES > 0:
             self.h.set_l2_prefetch(tensors["Wl"], self.L2_PREFETCH_BYTES)
+
+    def _use_shared_attention(self):
+        self.shared = self.h.make_shared_attention()
+        z = lambda *s, dtype: torch.zeros(*s, dtype=dtype, device=self.device)
+        self.out["attn_lse"] = z(self.cfg.B, self.cfg.max_nodes, self.cfg.Hq, dtype=torch.float32)
+        self.pos_base = z(self.cfg.B, dtype=torch.int32)
+
+    def enable_cache_budget(self, budget: int, sinks: int = 4, recent: int = 64, decay: float = 1.0,
+                            Lcap: Optional[int] = None):
+        """Keeps every sequence's own cache within `budget` rows: after each history update the accepted path's
+        attention weights are added up per cached row, and rows beyond the budget that drew the least are
+        dropped (never the first `sinks` positions nor the newest `recent`).  Lcap: rows the K/V buffers hold."""
+        cfg, dev = self.cfg, self.device
+        Lcap = cfg.Lcap if Lcap is None else Lcap
+        if budget + cfg.max_nodes > Lcap:
+            raise ValueError("a cache of %d rows does not hold a budget of %d and %d tree rows" % (Lcap, budget, cfg.max_nodes))
+        if self.shared is None:
+            self._use_shared_attention()
+        self.cache = dict(budget=budget, sinks=sinks, recent=recent, decay=decay, ws=self.h.make_eviction(Lcap),
+                          mass=torch.zeros(cfg.B, cfg.Hkv, Lcap, dtype=torch.float32, device=dev),
+                          row_pos=torch.arange(Lcap, dtype=torch.int32, device=dev).repeat(cfg.B, cfg.Hkv, 1),
+                          n_evicted=torch.zeros(cfg.B, dtype=torch.int32, device=dev))
+
+    def _tree_base(self, stream=None):
+        """What tree positions count from: the cached rows, those dropped earlier and the shared prefix."""
+        i = self.inp
+        if self.shared is None:
+            return i["kv_len"]
+        with torch.cuda.stream(stream):                 # (None: the current one)
+            base = self.pos_base.copy_(i["kv_len"])
+            if i.get("prefix_len") is not None:
+                base.add_(i["prefix_len"])
+            if self.cache is not None:
+                base.add_(self.cache["n_evicted"])
+        return base
+
+    def _trim_cache(self, kv_len, stream=None):
+        """After the history update (kv_len: the new length, changed in place): weights, then eviction."""
+        i, o, c = self.inp, self.out, self.cache
+        if c is None:
+            return
+        self.h.attention_mass(i["Q"], i["K"], kv_len, o["acc_len"], o["acc_nodes"], o["attn_lse"], 1.0 / float(self.cfg.D) ** 0.5,
+                              c["mass"], c["row_pos"], c["n_evicted"], decay=c["decay"], stream=stream)
+        self.h.evict_rows(c["ws"], i["K"], i["V"], c["mass"], c["row_pos"], kv_len, c["n_evicted"], c["budget"], c["sinks"],
+                          c["recent"], c["mass"], c["row_pos"], kv_len, c["n_evicted"], stream=stream)
 
     PER_STEP_INPUTS = ("x", "base_tok", "kv_len", "Q", "hn")
 
@@ -151,16 +202,21 @@ class DraftVerifyStep:
     def tree(self, stream=None):
         i, o = self.inp, self.out
         if self.layout == "raw":
-            self.h.build_raw_tree(i["base_tok"], i["kv_len"], o["cand_tok"], o["n_cand"],
+            self.h.build_raw_tree(i["base_tok"], self._tree_base(stream), o["cand_tok"], o["n_cand"],
                                   o["node_tok"], o["parent"], o["depth"], o["pos"], o["mask"], o["retrieve"],
                                   o["n_nodes"], o["kept"], o["nka"], stream=stream)
             return
-        self.h.build_tree(i["base_tok"], i["kv_len"], o["cand_tok"], o["cand_len"], o["n_cand"],
+        self.h.build_tree(i["base_tok"], self._tree_base(stream), o["cand_tok"], o["cand_len"], o["n_cand"],
                           o["node_tok"], o["parent"], o["depth"], o["pos"], o["mask"], o["retrieve"], o["n_nodes"],
                           stream=stream)
 
     def attention(self, stream=None):
         i, o = self.inp, self.out
+        if self.shared is not None:
+            self.h.tree_attention_shared(self.shared, i["Q"], i.get("Kp"), i.get("Vp"), i.get("prefix_len"), i["K"], i["V"],
+                                         i["kv_len"], o["n_nodes"], o["mask"], 1.0 / float(self.cfg.D) ** 0.5, o["O"],
+                                         o["attn_lse"], stream=stream)
+            return
         self.h.tree_attention(i["Q"], i["K"], i["V"], i["kv_len"], o["n_nodes"], o["mask"],
                               1.0 / float(self.cfg.D) ** 0.5, o["O"], stream=stream)
 
@@ -184,10 +240,11 @@ class DraftVerifyStep:
                                      o["next_tok"], o.get("lm_logits_dbg"), stream=stream)
 
     def commit(self, stream=None):
-        """History update (not part of run(): it changes the K/V cache in place)."""
+        """History update (not part of run(): it changes the K/V cache in place), and the cache budget's upkeep."""
         i, o = self.inp, self.out
         self.h.commit_accepted(i["K"], i["V"], i["kv_len"], o["acc_len"], o["acc_nodes"],
                                o["new_kv_len"], o["next_sel_row"], stream=stream)
+        self._trim_cache(o["new_kv_len"], stream)
 
     def run(self, stream=None):
         """The whole hot path: five calls back to back on one stream, no host sync."""
@@ -259,6 +316,7 @@ class DraftVerifyStep:
         # the new length overwrites the old one in place; the next step drafts from out["next_sel_row"]
         self.h.commit_accepted(i["K"], i["V"], c["kv_len"], o["acc_len"], o["acc_nodes"], c["kv_len"],
                                o["next_sel_row"])
+        self._trim_cache(c["kv_len"])
         if c["rec"] is not None:
             o["new_kv_len"].copy_(c["kv_len"])
             for k, buf in c["rec"].items():
@@ -266,7 +324,7 @@ class DraftVerifyStep:
 
     def run_chain(self):
         """All steps of the chain back to back on the current stream: per step the five calls and
-        the history update, the next step reading its drafting row, root token and cache length
+        the history update (with the cache budget's upkeep, where one is set), the next step reading its drafting row, root token and cache length
         from what the previous one left on the device."""
         c = self.chain
         c["kv_len"].copy_(c["kv_len0"])

@@ -110,6 +110,8 @@ CASES = {   # B, Hq, Hkv, D, nodes, live nodes, prefix, cached
     "big_trees": (2, 8, 2, 128, 200, [200, 131], [257] * 2, [90, 33]),
     "odd_group": (3, 21, 3, 128, 40, [40, 39, 1], [333] * 3, [1, 2, 3]),
     "mqa": (2, 20, 1, 64, 30, [30, 29], [50, 20], [600, 0]),
+    "many_tokens": (300, 4, 2, 64, 2, [(i * 7) % 3 for i in range(300)], [150] * 300, [(13 * i) % 40 for i in range(300)]),
+    "many_spread": (1024, 2, 2, 64, 2, [1] * 1024, [(11 * i) % 130 for i in range(1024)], [i % 5 for i in range(1024)]),
     "long_split": (1, 4, 4, 128, 2, [2], [9001], [100]),
 }
 
