@@ -29,7 +29,7 @@ struct SharedAttnParams {
     const int* kv_len;      // [B]
     const int* n_nodes;     // [B]
     const unsigned long long* mask;   // [B,max_nodes,ceil(max_nodes/64)]
-    int B, Hq, Hkv, D, max_nodes, Lcap, Pcap;
+    int B, Hq, Hkv, D, max_nodes, Lcap, Pcap, grp;      // grp = Hq / Hkv
     float scale;
     int* status;
     int* plan;              // workspace: header, row_off, tile_cum (written by CTA 0, read by the merge)
@@ -127,6 +127,8 @@ struct SpanMap {
     __host__ __device__ long long start(int c) const { return each * c + (c < extra ? c : extra); }
     __host__ __device__ int span_of(long long x) const {
         const long long big = (each + 1) * extra;
+        if (total < (1ll << 31))                           // (the short division)
+            return x < big ? (int)((unsigned)x / (unsigned)(each + 1)) : extra + (int)((unsigned)(x - big) / (unsigned)each);
         return x < big ? (int)(x / (each + 1)) : extra + (int)((x - big) / each);
     }
 };
@@ -152,14 +154,13 @@ __host__ __device__ inline SpanMap span_map_n(int per_head, int Hkv, int spans) 
 // these have equal work; where spans are long (over `long_span` blocks) or the pairs outnumber them, balance counts more
 // and all max_spans are used.
 __host__ __device__ inline SpanMap span_map(int per_head, int tiles, int Hkv, int max_spans, int min_blocks, int long_span) {
-    const long long total = (long long)per_head * Hkv, pairs = (long long)tiles * Hkv;
-    if (pairs <= 0 || pairs >= max_spans || total >= (long long)max_spans * long_span) {
-        const long long fit = pairs <= 0 ? 1 : max_spans;
-        return span_map_n(per_head, Hkv, (int)fit);
-    }
-    const long long room = max_spans / pairs, want = total / (pairs * min_blocks);
-    const long long each = want < 1 ? 1 : (want < room ? want : room);
-    return span_map_n(per_head, Hkv, (int)(pairs * each));
+    const long long total = (long long)per_head * Hkv;
+    const int pairs = tiles * Hkv;                         // (below 2^31: 2^13 tiles at most, and Hkv of them fit no GPU's memory beyond)
+    if (pairs <= 0) return span_map_n(per_head, Hkv, 1);
+    if (pairs >= max_spans || total >= (long long)max_spans * long_span) return span_map_n(per_head, Hkv, max_spans);
+    const unsigned room = (unsigned)max_spans / (unsigned)pairs, want = (unsigned)total / (unsigned)(pairs * min_blocks);
+    const unsigned each = want < 1u ? 1u : (want < room ? want : room);
+    return span_map_n(per_head, Hkv, pairs * (int)each);
 }
 
 // Tile that holds block x (0 <= x < tile_cum[tiles]) of a kv head.
@@ -235,7 +236,7 @@ struct BlockIter {
 // would read outside its cache is reported (by the block that publishes) and takes no part.
 __device__ inline void plan_build(SharedPlan& p, const SharedAttnParams& a, int TR, int KB, bool publish) {
     const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31;
-    const int grp = a.Hq / a.Hkv;
+    const int grp = a.grp;
     if (tid < 32) {
         int rows = 0, blocks = 0, pmin = 0x7fffffff, pmax = 0;
         for (int b0 = 0; b0 < a.B; b0 += 32) {

@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(kSimpleThreads, 2) shared_attention_simple_ker
     SpanWalk at;
 
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-    const int grp = p.Hq / p.Hkv;
+    const int grp = p.grp;
     const int W = (p.max_nodes + 63) / 64;
     const float sl2 = p.scale * kLog2e;
     const float* Q = static_cast<const float*>(p.Q);
@@ -252,11 +252,11 @@ template <> __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16*
 // A warp holds 8 columns of 32 rows: D / 8 warps.  The parts of a tile are taken four at a time, all their loads on the
 // way at once, against a reference that follows the largest so far.
 template <typename T, int D, int TR>
-__global__ void __launch_bounds__(D * 4) shared_attention_merge_kernel(SharedAttnParams p, long long units) {
+__global__ void __launch_bounds__(D * 4) shared_attention_merge_kernel(SharedAttnParams p, unsigned units) {
     constexpr int kWarps = D / 8, U = 4;
     extern __shared__ int row_off[];                         // [B+1]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int grp = p.Hq / p.Hkv;
+    const int grp = p.grp;
     pdl_wait();
     pdl_trigger();
     const int* tile_cum = p.plan + kPlanHeader + p.B + 1;
@@ -267,8 +267,8 @@ __global__ void __launch_bounds__(D * 4) shared_attention_merge_kernel(SharedAtt
     const int max_rows = p.B * node_rows;                    // packed rows if every node were live
     const int chunks = (max_rows + 31) / 32;
     __syncthreads();
-    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
-        const int g = (int)(u / chunks), ch = (int)(u - (long long)g * chunks);
+    for (unsigned u = blockIdx.x; u < units; u += gridDim.x) {
+        const int g = (int)(u / (unsigned)chunks), ch = (int)(u - (unsigned)g * (unsigned)chunks);
         {   // zero rows: output row (b, node, head of group g) for the nodes that are not used
             const int m = ch * 32 + lane;
             if (m < max_rows) {
@@ -346,9 +346,9 @@ __global__ void __launch_bounds__(D * 4) shared_attention_merge_kernel(SharedAtt
 template <typename T, int D, int TR>
 int launch_merge(Handle* h, cudaStream_t s, const SharedAttnParams& p) {
     const long long max_rows = (long long)p.B * p.max_nodes * (p.Hq / p.Hkv);
-    const long long units = (max_rows + 31) / 32 * p.Hkv;
-    const long long cap = (long long)h->num_sms * 16;
-    CTCSD_CUDA_CHECK(h, launch_pdl(shared_attention_merge_kernel<T, D, TR>, dim3((unsigned)(units < cap ? units : cap)),
+    const unsigned units = (unsigned)((max_rows + 31) / 32) * (unsigned)p.Hkv;       // (at most 2^14 per kv head)
+    const unsigned cap = (unsigned)h->num_sms * 16u;
+    CTCSD_CUDA_CHECK(h, launch_pdl(shared_attention_merge_kernel<T, D, TR>, dim3(units < cap ? units : cap),
                                    dim3(D * 4), sizeof(int) * (size_t)(p.B + 1), s, 1, p, units));
     h->launches++;
     return CTCSD_OK;
@@ -430,7 +430,7 @@ extern "C" int ctcsd_tree_attention_shared(ctcsd_handle* hh, void* stream, void*
     SharedAttnParams p;
     p.Q = Q; p.Kp = Pcap > 0 ? Kp : nullptr; p.Vp = Pcap > 0 ? Vp : nullptr; p.K = K; p.V = V; p.O = out_O; p.lse = out_lse;
     p.prefix_len = Pcap > 0 ? prefix_len : nullptr; p.kv_len = kv_len; p.n_nodes = n_nodes; p.mask = mask;
-    p.B = c.B; p.Hq = c.Hq; p.Hkv = c.Hkv; p.D = c.D; p.max_nodes = c.max_nodes; p.Lcap = Lcap; p.Pcap = Pcap;
+    p.B = c.B; p.Hq = c.Hq; p.Hkv = c.Hkv; p.D = c.D; p.max_nodes = c.max_nodes; p.Lcap = Lcap; p.Pcap = Pcap; p.grp = c.Hq / c.Hkv;
     p.scale = scale;
     p.status = status_ptr(h);
     char* ws = static_cast<char*>(workspace);

@@ -400,7 +400,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
         const uint32_t lane_off = (uint32_t)(q * 32) << 16;
         const uint32_t tmem_s = tmem + (uint32_t)(half * 128) + lane_off;
         const uint32_t tmem_o = tmem + 256u + (uint32_t)(half * D) + lane_off;
-        const int grp = p.Hq / p.Hkv;
+        const int grp = p.grp;
         const int W = (p.max_nodes + 63) / 64;
         const float sl2 = p.scale * kLog2e;                    // scores are kept in log2 units
         const uint64_t sl22 = pair_of(sl2, sl2);
