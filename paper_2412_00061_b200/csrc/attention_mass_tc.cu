@@ -181,8 +181,7 @@ attention_mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, MassParams p, 
 #pragma unroll 1
                     for (int c0 = 0; c0 < cols; c0 += 16) {
                         uint32_t v[16];
-                        tc::tmem_ld16(tmem_s + (uint32_t)c0, v);
-                        tc::tmem_ld_wait(v);
+                        tc::tmem_read16(tmem_s + (uint32_t)c0, v);
 #pragma unroll
                         for (int i = 0; i < 16; i += 4) {
                             const float4 ls = *reinterpret_cast<const float4*>(nlse + c0 + i);

@@ -39,9 +39,6 @@ constexpr float kSlack = 8.f;          // log2 units: P stays below 2^8
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kNoteBits = 2048;
-constexpr int kPolyOf8 = 2;            // of 8 pairs of exponentials, how many the FMA pipe computes
-
-template <bool B> struct Flag { static constexpr bool value = B; };
 
 template <int D> struct Shape;
 template <> struct Shape<128> { static constexpr int kStages = 2; };
@@ -87,27 +84,6 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
     float r;
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
-}
-// 2^x of a pair on the FMA pipe.  x = i + f with i the nearest integer (taken from the low bits of x + 1.5 * 2^23)
-// and |f| <= 1/2; 2^f is the degree-4 polynomial of least relative error there (computed with the Remez
-// exchange; 2.7e-6 in float32, far below the rounding of P to bf16, and 1e-6 of a log-sum-exp at most);
-// i is added to the exponent field.  x is held at -126: what lies below is zero to any sum.
-__device__ __forceinline__ uint64_t exp2_poly2(uint64_t x) {
-    float a, b;
-    pair_split(x, a, b);
-    x = pair_of(fmaxf(a, -126.f), fmaxf(b, -126.f));
-    const float magic = 12582912.f;
-    const uint64_t t = add2(x, pair_of(magic, magic));
-    const uint64_t r = add2(t, pair_of(-magic, -magic));
-    const uint64_t f = fma2(r, pair_of(-1.f, -1.f), x);
-    uint64_t y = fma2(pair_of(0x1.3997d6p-7f, 0x1.3997d6p-7f), f, pair_of(0x1.ca1440p-5f, 0x1.ca1440p-5f));
-    y = fma2(y, f, pair_of(0x1.ec06dap-3f, 0x1.ec06dap-3f));
-    y = fma2(y, f, pair_of(0x1.62e0dcp-1f, 0x1.62e0dcp-1f));
-    y = fma2(y, f, pair_of(0x1.ffffe8p-1f, 0x1.ffffe8p-1f));
-    float ta, tb, ya, yb;
-    pair_split(t, ta, tb);
-    pair_split(y, ya, yb);
-    return pair_of(__int_as_float(__float_as_int(ya) + (__float_as_int(ta) << 23)), __int_as_float(__float_as_int(yb) + (__float_as_int(tb) << 23)));
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -478,31 +454,26 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                                 tc::tmem_st32(tmem_se, z);
                             }
                         } else {
-                            uint32_t v[2][32];
                             const bool open = __all_sync(0xffffffffu, !live || sees >= kStep);    // no row of the warp has anything masked
-                            tc::tmem_ld32(tmem_se, v[0]);
-                            tc::tmem_ld32(tmem_se + 32u, v[1]);
-                            tc::tmem_ld_wait(v[0]);            // (at once: a register with a load in flight must not be moved)
-                            tc::tmem_ld_wait(v[1]);
-                            if (!open) {
+                            uint32_t v[64];
+                            tc::tmem_read64(tmem_se, v);
+                            if (__builtin_expect(!open, 0)) {
 #pragma unroll
                                 for (int cc = 0; cc < 2; ++cc) {
                                     const uint32_t vis = visible32(it.seq, key + cc * 32);
 #pragma unroll
-                                    for (int j = 0; j < 32; ++j) v[cc][j] = ((vis >> j) & 1u) ? v[cc][j] : 0xff800000u;
+                                    for (int j = 0; j < 32; ++j) v[32 * cc + j] = ((vis >> j) & 1u) ? v[32 * cc + j] : 0xff800000u;
                                 }
                             }
                             float b4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                            for (int cc = 0; cc < 2; ++cc)
-#pragma unroll
-                                for (int j = 0; j < 32; j += 2)
-                                    b4[(j >> 1) & 3] = max3_nan(b4[(j >> 1) & 3], __uint_as_float(v[cc][j]), __uint_as_float(v[cc][j + 1]));
+                            for (int j = 0; j < 64; j += 2)
+                                b4[(j >> 1) & 3] = max3_nan(b4[(j >> 1) & 3], __uint_as_float(v[j]), __uint_as_float(v[j + 1]));
                             float bm = max3_nan(max3_nan(b4[0], b4[1], b4[2]), b4[3], -INFINITY);
                             poisoned = poisoned || !(bm < INFINITY);       // a NaN or +inf score: the row is not meaningful
                             bm *= sl2;
                             const bool move = bm > ref + kSlack;           // also the first visible key (ref = -inf)
-                            if (__any_sync(0xffffffffu, move)) {
+                            if (__builtin_expect(__any_sync(0xffffffffu, move), 0)) {
                                 const float corr = move ? exp2_fast(ref - bm) : 1.f;
                                 if (!first) {
                                     // O must be at rest: P V of the step before (older ones precede this step's scores)
@@ -511,8 +482,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
 #pragma unroll 1
                                     for (int c0 = 0; c0 < D; c0 += 32) {
                                         uint32_t o[32];
-                                        tc::tmem_ld32(tmem_o + (uint32_t)c0, o);
-                                        tc::tmem_ld_wait(o);
+                                        tc::tmem_read32(tmem_o + (uint32_t)c0, o);
 #pragma unroll
                                         for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * corr);
                                         tc::tmem_st32(tmem_o + (uint32_t)c0, o);
@@ -523,32 +493,35 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                             }
                             const float off = ref == -INFINITY ? 0.f : -ref;
                             const uint64_t off2 = pair_of(off, off);
-                            uint64_t s2[2] = {0ull, 0ull};
+                            // Eight pairs at a time, stage by stage: the pairs' chains (scale, exponential, sum, round) run side
+                            // by side.  (The exponential unit's 16 results a clock come to 2048 cycles a block, the tensor
+                            // core's time; a share of them as polynomials on the FMA pipe won 4 % on long prefixes and lost 8 % on
+                            // short calls, whose instructions then no longer stay in the caches near the schedulers.)
+                            uint64_t s2[4] = {0ull, 0ull, 0ull, 0ull};
                             uint32_t w[32];
-                            // the exponential unit does 16 results a clock: a share of them goes to the FMA pipe, which balances
-                            // the two (whole steps only: it does not make a masked score exactly zero)
-                            auto weigh = [&](auto mix) {
 #pragma unroll
-                                for (int j = 0; j < 32; ++j) {
-                                    uint64_t x = fma2(pair_of(__uint_as_float(v[j / 16][(2 * j) % 32]), __uint_as_float(v[j / 16][(2 * j) % 32 + 1])), sl22, off2);
-                                    float a, b;
-                                    if (decltype(mix)::value && (j % 8) >= 8 - kPolyOf8) {
-                                        x = exp2_poly2(x);
-                                        pair_split(x, a, b);
-                                    } else {
-                                        pair_split(x, a, b);
-                                        a = exp2_fast(a);
-                                        b = exp2_fast(b);
-                                        x = pair_of(a, b);
-                                    }
-                                    s2[j & 1] = add2(s2[j & 1], x);
-                                    w[j] = pack_bf16(a, b);
+                            for (int g0 = 0; g0 < 32; g0 += 8) {
+                                uint64_t x[8];
+                                float lo[8], hi[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    const int j = 2 * (g0 + i);
+                                    x[i] = fma2(pair_of(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), sl22, off2);
                                 }
-                            };
-                            if (open) weigh(Flag<true>()); else weigh(Flag<false>());
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    pair_split(x[i], lo[i], hi[i]);
+                                    lo[i] = exp2_fast(lo[i]);
+                                    hi[i] = exp2_fast(hi[i]);
+                                }
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) s2[i % 4] = add2(s2[i % 4], pair_of(lo[i], hi[i]));
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) w[g0 + i] = pack_bf16(lo[i], hi[i]);
+                            }
                             tc::tmem_st32(tmem_se, w);                     // over scores that have been read
                             float sa, sb;
-                            pair_split(add2(s2[0], s2[1]), sa, sb);
+                            pair_split(add2(add2(s2[0], s2[1]), add2(s2[2], s2[3])), sa, sb);
                             sum += sa + sb;
                         }
                         first = false;
@@ -605,8 +578,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
 #pragma unroll 1
                         for (int c0 = 0; c0 < D; c0 += 32) {
                             uint32_t o[32];
-                            tc::tmem_ld32(tmem_o + (uint32_t)c0, o);
-                            tc::tmem_ld_wait(o);
+                            tc::tmem_read32(tmem_o + (uint32_t)c0, o);
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
                                 *reinterpret_cast<uint4*>(join + rl * D + ((((c0 / 4) + j) ^ (rl & 7)) << 2)) =
@@ -637,8 +609,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                     float o[32];
                     if (!first) {
                         uint32_t u[32];
-                        tc::tmem_ld32(tmem_o + (uint32_t)c0, u);
-                        tc::tmem_ld_wait(u);
+                        tc::tmem_read32(tmem_o + (uint32_t)c0, u);
 #pragma unroll
                         for (int j = 0; j < 32; ++j) o[j] = __uint_as_float(u[j]) * mine;
                     } else {
