@@ -301,7 +301,7 @@ int ctcsd_commit_accepted(ctcsd_handle* h, void* stream, void* K, void* V, int L
  * included (rows behind the lengths, other branches of the tree, other sequences).  A row that does see
  * a NaN or infinite value is not meaningful.
  * workspace: device memory of ctcsd_tree_attention_shared_workspace_bytes(cfg) bytes, 256-byte aligned, owned by the
- *   caller, used only during the call (calls that overlap on the device need one each).
+ *   caller, used only during the call (calls on different handles that overlap on the device need one each).
  * Q, Kp, Vp, K, V, out_O 16-byte aligned.  A sequence whose lengths lie outside its arrays is treated as having no nodes and
  * CTCSD_ERR_INVALID_ARG is recorded in the device status word.  Needs B <= 1024 and B*max_nodes*Hq/Hkv <= 524288
  * (else CTCSD_ERR_UNSUPPORTED).

@@ -11,6 +11,9 @@
 // per CTA.  A tile inside one span is finished there; a tile that crosses a cut leaves (O, reference,
 // sum) of each part in the workspace and the merge kernel joins the parts.  A span has at most two such
 // parts: slot 0 continues a tile of the previous span, slot 1 begins a tile that the next one continues.
+//
+// Loops here stay rolled: they run a few times per call, and the kernels' code has to stay small, since the roles of a CTA
+// fetch theirs side by side (the bf16 kernel's: 135 KB, 88 KB with these and its own rare loops rolled).
 #pragma once
 
 #include "common.cuh"
@@ -75,6 +78,7 @@ __host__ __device__ inline void plan_carve(SharedPlan& p, int* at, int B) {
 // Sequence that owns packed row r (0 <= r < rows).
 __host__ __device__ inline int plan_seq_of_row(const SharedPlan& p, int B, int r) {
     int lo = 0, hi = B - 1;                    // smallest b with row_off[b+1] > r
+#pragma unroll 1
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (p.row_off[mid + 1] > r) hi = mid; else lo = mid + 1;
@@ -86,6 +90,7 @@ __host__ __device__ inline int plan_seq_of_row(const SharedPlan& p, int B, int r
 __host__ __device__ inline int plan_pre_max(const SharedPlan& p, int b0, int b1) {
     if (p.edge[0] == p.edge[1]) return p.edge[1];          // all alike
     int m = 0;
+#pragma unroll 1
     for (int b = b0; b <= b1; ++b) m = p.pre[b] > m ? p.pre[b] : m;
     return m;
 }
@@ -106,6 +111,7 @@ __host__ __device__ inline TileInfo plan_tile(const SharedPlan& p, int B, int TR
     ti.pmax = ti.pmin = p.edge[1];
     if (p.edge[0] != p.edge[1]) {
         ti.pmax = 0;
+#pragma unroll 1
         for (int b = ti.b0; b <= ti.b1; ++b) {
             if (p.own_len[b] == 0) continue;
             ti.pmax = p.pre[b] > ti.pmax ? p.pre[b] : ti.pmax;
@@ -166,6 +172,7 @@ __host__ __device__ inline SpanMap span_map(int per_head, int tiles, int Hkv, in
 // Tile that holds block x (0 <= x < tile_cum[tiles]) of a kv head.
 __host__ __device__ inline int plan_tile_of_block(const int* tile_cum, int tiles, int x) {
     int lo = 0, hi = tiles - 1;                // smallest t with tile_cum[t+1] > x
+#pragma unroll 1
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (tile_cum[mid + 1] > x) hi = mid; else lo = mid + 1;
@@ -214,6 +221,7 @@ struct BlockIter {
         if (blk < pb) { seq = -1; key0 = blk * KB; len = ti.pmax; return; }
         blk += p.own_cum[ti.b0] - pb;
         int lo = ti.b0, hi = ti.b1;            // smallest b with own_cum[b+1] > blk
+#pragma unroll 1
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
             if (p.own_cum[mid + 1] > blk) hi = mid; else lo = mid + 1;
@@ -225,6 +233,7 @@ struct BlockIter {
         key0 += KB;
         if (key0 < len) return;
         int b = seq < 0 ? ti.b0 : seq + 1;
+#pragma unroll 1
         while (b < ti.b1 && p.own_len[b] == 0) ++b;
         seq = b; key0 = 0; len = p.own_len[b];
     }
@@ -239,6 +248,7 @@ __device__ inline void plan_build(SharedPlan& p, const SharedAttnParams& a, int 
     const int grp = a.grp;
     if (tid < 32) {
         int rows = 0, blocks = 0, pmin = 0x7fffffff, pmax = 0;
+#pragma unroll 1
         for (int b0 = 0; b0 < a.B; b0 += 32) {
             const int b = b0 + lane;
             int n = 0, L = 0, P = 0;
@@ -287,11 +297,13 @@ __device__ inline void plan_build(SharedPlan& p, const SharedAttnParams& a, int 
         __syncthreads();
         return;
     }
+#pragma unroll 1
     for (int t = tid; t < p.tiles; t += nt) p.tile_cum[t + 1] = plan_tile_blocks(p, plan_tile(p, a.B, TR, t), KB);
     if (tid == 0) p.tile_cum[0] = 0;
     __syncthreads();
     if (tid < 32) {
         int run = 0;
+#pragma unroll 1
         for (int t0 = 0; t0 < p.tiles; t0 += 32) {
             int v = t0 + lane < p.tiles ? p.tile_cum[t0 + lane + 1] : 0;
 #pragma unroll
@@ -308,7 +320,9 @@ __device__ inline void plan_build(SharedPlan& p, const SharedAttnParams& a, int 
 
 // CTA 0 leaves what the merge kernel needs.
 __device__ inline void plan_publish(const SharedPlan& p, const SharedAttnParams& a, int spans) {
+#pragma unroll 1
     for (int b = threadIdx.x; b <= a.B; b += blockDim.x) a.plan[kPlanHeader + b] = p.row_off[b];
+#pragma unroll 1
     for (int t = threadIdx.x; t <= p.tiles; t += blockDim.x) a.plan[kPlanHeader + a.B + 1 + t] = p.tile_cum[t];
     if (threadIdx.x == 0) {
         a.plan[0] = p.rows;

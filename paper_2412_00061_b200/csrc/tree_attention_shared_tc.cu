@@ -89,6 +89,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t*>(&v);
 }
+__device__ __forceinline__ __nv_bfloat162 bf16_pair(uint32_t w) { return *reinterpret_cast<__nv_bfloat162*>(&w); }
 // A wait has run out: record it once and let every other role stop waiting.
 __device__ __forceinline__ void give_up(SharedState* sh, int* status, int site) {
     volatile int* f = &sh->abort_flag;
@@ -97,6 +98,8 @@ __device__ __forceinline__ void give_up(SharedState* sh, int* status, int site) 
 }
 // All softmax threads (both halves) meet here.
 __device__ __forceinline__ void halves_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+template <bool B> struct Flag { static constexpr bool value = B; };
 
 // What every role has to know of a part of the span.
 struct Piece {
@@ -278,7 +281,6 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                     if (e == 1) {
                         tc::mma_commit(&sh->v_empty[st]);
                         ++count;
-                        pend = -1;
                     }
                     return true;
                 };
@@ -303,25 +305,30 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                     return true;
                 };
                 ok = tc::mbar_wait_suspended(&sh->q_full, (uint32_t)piece & 1u, abort_flag);
-                for (int blk = c.blk0; blk < c.blk1 && ok; ++blk, ++fill) {
+                // (one more round than blocks: the last block's P V)
+                for (int blk = c.blk0; blk <= c.blk1 && ok; ++blk) {
                     const int st = fill % NS;
-                    if ((takers(c, it, blk) >> half) & 1u) {
-                        // a step's P is read by P V before the next S overwrites it: the tensor core works in issue order
-                        if (pend >= 0 && !issue_pv(0)) { ok = false; break; }
-                        if (!tc::mbar_wait_suspended(&sh->k_full[st], (uint32_t)(fill / NS) & 1u, abort_flag)) { ok = false; break; }
-                        tc::tc_fence_after_sync();
-                        issue_s(0, st);
-                        if (pend >= 0 && !issue_pv(1)) { ok = false; break; }
-                        issue_s(1, st);
-                        tc::mma_commit(&sh->k_empty[st]);
-                        pend = fill;
-                    } else {
-                        if (pend >= 0 && !(issue_pv(0) && issue_pv(1))) { ok = false; break; }
-                        ok = pass_k(fill) && pass_v(fill);
+                    const bool more_blocks = blk < c.blk1;
+                    const bool mine = more_blocks && ((takers(c, it, blk) >> half) & 1u);
+                    // a step's P is read by P V before the next S overwrites it: the tensor core works in issue order
+#pragma unroll 1
+                    for (int e = 0; e < 2 && ok; ++e) {
+                        if (pend >= 0) ok = issue_pv(e);
+                        if (ok && mine) {
+                            if (e == 0) {
+                                ok = tc::mbar_wait_suspended(&sh->k_full[st], (uint32_t)(fill / NS) & 1u, abort_flag);
+                                tc::tc_fence_after_sync();
+                            }
+                            if (ok) issue_s(e, st);
+                        }
                     }
+                    if (!ok || !more_blocks) break;
+                    pend = mine ? fill : -1;
+                    if (mine) tc::mma_commit(&sh->k_empty[st]);
+                    else ok = pass_k(fill) && pass_v(fill);
+                    ++fill;
                     if (blk + 1 < c.blk1) it.next(pl, c.ti, kKeys);
                 }
-                if (ok && pend >= 0) ok = issue_pv(0) && issue_pv(1);
                 if (ok) tc::mma_commit(&sh->o_full[half]);
             }
             if (!ok) give_up(sh, p.status, 32);
@@ -342,16 +349,22 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
 #pragma unroll 1
                     for (int rr = 0; rr < kKeys / 32; ++rr) {
                         unsigned char* row = Vs + (size_t)st * kTile + (rr * 32 + lane) * 128;
-                        uint32_t bad = 0u;
+                        // 0 * w is NaN for a NaN or an infinity and 0 otherwise
+                        __nv_bfloat162 z4[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) z4[i] = __float2bfloat162_rn(0.f);
+                        const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
 #pragma unroll
                         for (int i = 0; i < DH * 8; ++i) {
                             const uint4 w = *reinterpret_cast<const uint4*>(row + (i / 8) * (kKeys * 128) + (((i + lane) & 7) << 4));
-                            // an exponent of all ones carries into the sign's place
-                            bad |= ((w.x & 0x7f807f80u) + 0x00800080u) | ((w.y & 0x7f807f80u) + 0x00800080u) |
-                                   ((w.z & 0x7f807f80u) + 0x00800080u) | ((w.w & 0x7f807f80u) + 0x00800080u);
+                            z4[0] = __hfma2(bf16_pair(w.x), zero, z4[0]);
+                            z4[1] = __hfma2(bf16_pair(w.y), zero, z4[1]);
+                            z4[2] = __hfma2(bf16_pair(w.z), zero, z4[2]);
+                            z4[3] = __hfma2(bf16_pair(w.w), zero, z4[3]);
                         }
-                        if (bad & 0x80008000u) {
-#pragma unroll
+                        const float2 sum = __bfloat1622float2(__hadd2(__hadd2(z4[0], z4[1]), __hadd2(z4[2], z4[3])));
+                        if (sum.x + sum.y != 0.f) {
+#pragma unroll 1
                             for (int i = 0; i < DH * 8; ++i)
                                 *reinterpret_cast<uint4*>(row + (i / 8) * (kKeys * 128) + ((i & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
                             atomicOr(&sh->note[(fill % kNoteBits) >> 5], 1u << (fill & 31));
@@ -382,6 +395,14 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
         const uint64_t sl22 = pair_of(sl2, sl2);
         uint32_t s_count = 0u, steps = 0u;                     // blocks and steps of this half so far
         int fill0 = 0, piece = 0;
+        // After a wait that ran out, nothing is waited for any more: the loops run to their ends on meaningless scores,
+        // and no output is written.
+        auto wait = [&](uint64_t* bar, uint32_t parity, int site) {
+            if (!failed && !tc::mbar_wait_suspended(bar, parity, abort_flag)) {
+                failed = true;
+                give_up(sh, p.status, site);
+            }
+        };
         for (; more; more = at.next(pl), ++piece) {
             const Piece c = make_piece(pl, p.B, at);
             // ---- this thread's row ----
@@ -398,7 +419,8 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                 row_kv = pl.kv[seq];
                 row_n = pl.own_len[seq] - row_kv;
             }
-            auto out_row = [&]() -> size_t { return live ? ((size_t)seq * p.max_nodes + node) * p.Hq + head : 0; };
+            // (below 2^32: as many rows of 64 columns fill no GPU's memory)
+            auto out_row = [&]() -> unsigned { return live ? ((unsigned)seq * p.max_nodes + node) * p.Hq + head : 0u; };
             auto visible32 = [&](int src, int key) -> uint32_t {
                 return live ? visible32_of(src, key, seq, row_pre, row_kv, row_n, p.mask + ((size_t)seq * p.max_nodes + node) * W, W) : 0u;
             };
@@ -409,19 +431,20 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                 constexpr int LR = D / 8, RI = 32 / LR;         // lanes per row, rows per instruction
                 unsigned char* dst = Qs + half * kQHalf + (q * 32) * 128;
                 const int cc = lane % LR;
-                const unsigned long long orow = out_row();
-                const unsigned there = __ballot_sync(0xffffffffu, live);
-                uint4 w[LR];
+                const unsigned orow = out_row(), there = __ballot_sync(0xffffffffu, live);
+                const uint4* Qg = static_cast<const uint4*>(p.Q) + cc;
+#pragma unroll 1
+                for (int i0 = 0; i0 < LR; i0 += 8) {
+                    uint4 w[8];
 #pragma unroll
-                for (int i = 0; i < LR; ++i) {                  // (a row that is not there reads row 0)
-                    const unsigned long long src = __shfl_sync(0xffffffffu, orow, i * RI + lane / LR);
-                    w[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.Q) + src * D) + cc);
-                }
+                    for (int i = 0; i < 8; ++i)                 // (a row that is not there reads row 0)
+                        w[i] = __ldg(Qg + (size_t)__shfl_sync(0xffffffffu, orow, (i0 + i) * RI + lane / LR) * LR);
 #pragma unroll
-                for (int i = 0; i < LR; ++i) {
-                    const int rr = i * RI + lane / LR;
-                    if (!((there >> rr) & 1u)) w[i] = make_uint4(0u, 0u, 0u, 0u);
-                    *reinterpret_cast<uint4*>(dst + rr * 128 + (cc / 8) * (kHalf * 128) + (((cc % 8) ^ (rr & 7)) << 4)) = w[i];
+                    for (int i = 0; i < 8; ++i) {
+                        const int rr = (i0 + i) * RI + lane / LR;
+                        if (!((there >> rr) & 1u)) w[i] = make_uint4(0u, 0u, 0u, 0u);
+                        *reinterpret_cast<uint4*>(dst + rr * 128 + (cc / 8) * (kHalf * 128) + (((cc % 8) ^ (rr & 7)) << 4)) = w[i];
+                    }
                 }
                 tc::fence_proxy_async();
             }
@@ -430,120 +453,132 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
 
             float ref = -INFINITY, sum = 0.f;
             bool first = true, poisoned = false;
+            // One step of a block.  Open: every row of the warp sees all of its keys; else the rows' limits and masks are looked
+            // at.  (Two copies of the code: with the masks inside the loop of open blocks, which is most of them, its
+            // instructions take longer to fetch.)
+            auto step = [&](auto open_tag, int e, int src, int key) {
+                constexpr bool Open = decltype(open_tag)::value;
+                const uint32_t tmem_se = tmem_s + (uint32_t)(e * kStep);
+                bool none = false;                              // no row of the warp sees any of the step's keys
+                if constexpr (!Open) {
+                    const int sees = src < 0 ? row_pre : (src == seq ? row_kv + row_n : 0);
+                    none = __all_sync(0xffffffffu, !live || sees <= key);
+                }
+                wait(&sh->s_full[half][e], s_count & 1u, 35);
+                __syncwarp();
+                tc::tc_fence_after_sync();
+                if (!Open && none) {
+                    // nothing to see for this warp: P is zero (rows that are not there take no part at all)
+                    if (warp_live) {
+                        uint32_t z[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[j] = 0u;
+                        tc::tmem_st32(tmem_se, z);
+                    }
+                } else {
+                    uint32_t v[64];
+                    tc::tmem_read64(tmem_se, v);
+                    if constexpr (!Open) {
+#pragma unroll
+                        for (int cc = 0; cc < 2; ++cc) {
+                            const uint32_t vis = visible32(src, key + cc * 32);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[32 * cc + j] = ((vis >> j) & 1u) ? v[32 * cc + j] : 0xff800000u;
+                        }
+                    }
+                    float b4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int j = 0; j < 64; j += 2)
+                        b4[(j >> 1) & 3] = max3_nan(b4[(j >> 1) & 3], __uint_as_float(v[j]), __uint_as_float(v[j + 1]));
+                    float bm = max3_nan(max3_nan(b4[0], b4[1], b4[2]), b4[3], -INFINITY);
+                    poisoned = poisoned || !(bm < INFINITY);       // a NaN or +inf score: the row is not meaningful
+                    bm *= sl2;
+                    const bool move = bm > ref + kSlack;           // also the first visible key (ref = -inf)
+                    if (__builtin_expect(__any_sync(0xffffffffu, move), 0)) {
+                        const float corr = move ? exp2_fast(ref - bm) : 1.f;
+                        if (!first) {
+                            // O must be at rest: P V of the step before (older ones precede this step's scores)
+                            wait(&sh->pv_done[half], (steps - 1u) & 1u, 35);
+                            __syncwarp();
+                            tc::tc_fence_after_sync();
+#pragma unroll 1
+                            for (int c0 = 0; c0 < D; c0 += 32) {
+                                uint32_t o[32];
+                                tc::tmem_read32(tmem_o + (uint32_t)c0, o);
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * corr);
+                                tc::tmem_st32(tmem_o + (uint32_t)c0, o);
+                            }
+                        }
+                        sum *= corr;
+                        ref = move ? bm : ref;
+                    }
+                    const float off = ref == -INFINITY ? 0.f : -ref;
+                    const uint64_t off2 = pair_of(off, off);
+                    // Eight pairs at a time, stage by stage: the pairs' chains (scale, exponential, sum, round) run side
+                    // by side.  (The exponential unit's 16 results a clock come to 2048 cycles a block, the tensor
+                    // core's time; a share of them as polynomials on the FMA pipe won 4 % on long prefixes and lost 8 % on
+                    // short calls, whose instructions then no longer stay in the caches near the schedulers.)
+                    uint64_t s2[4] = {0ull, 0ull, 0ull, 0ull};
+                    uint32_t w[32];
+#pragma unroll
+                    for (int g0 = 0; g0 < 32; g0 += 8) {
+                        uint64_t x[8];
+                        float lo[8], hi[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int j = 2 * (g0 + i);
+                            x[i] = fma2(pair_of(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), sl22, off2);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            pair_split(x[i], lo[i], hi[i]);
+                            lo[i] = exp2_fast(lo[i]);
+                            hi[i] = exp2_fast(hi[i]);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) s2[i % 4] = add2(s2[i % 4], pair_of(lo[i], hi[i]));
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) w[g0 + i] = pack_bf16(lo[i], hi[i]);
+                    }
+                    tc::tmem_st32(tmem_se, w);                     // over scores that have been read
+                    float sa, sb;
+                    pair_split(add2(add2(s2[0], s2[1]), add2(s2[2], s2[3])), sa, sb);
+                    sum += sa + sb;
+                }
+                first = false;
+                ++steps;
+                tc::tmem_st_wait();
+                tc::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sh->p_full[half][e]);
+            };
             BlockIter it;
             it.init(pl, c.ti, kKeys, c.blk0);
             for (int blk = c.blk0; blk < c.blk1; ++blk) {
-                if ((takers(c, it, blk) >> half) & 1u) {
+                // whole blocks from here on that every row of the warp sees
+                int open = warp_live ? __reduce_min_sync(0xffffffffu, !live ? c.blk1 - blk : max((it.seq < 0 ? row_pre : (it.seq == seq ? row_kv : 0)) - it.key0, 0) / kKeys) : 0;
+                open = min(open, c.blk1 - blk);
+                if (open > 0) {
+                    // (the half takes them all, unless the halves take turns)
+                    const int by = c.split_keys ? 2 : 1;
 #pragma unroll 1
-                    for (int e = 0; e < 2; ++e) {
-                        const uint32_t tmem_se = tmem_s + (uint32_t)(e * kStep);
-                        if (!failed && !tc::mbar_wait_suspended(&sh->s_full[half][e], s_count & 1u, abort_flag)) failed = true;
-                        failed = __any_sync(0xffffffffu, failed);
-                        if (failed) break;
-                        tc::tc_fence_after_sync();
-                        const int key = it.key0 + e * kStep;
-                        // keys from here on that this row sees without a look at its mask, and whether there are others
-                        const int sees = !live ? 0 : (it.seq < 0 ? row_pre - key : (it.seq == seq ? row_kv - key : 0));
-                        const bool none = sees <= 0 && !(live && it.seq == seq && row_kv + row_n > key);
-                        if (__all_sync(0xffffffffu, none)) {
-                            // nothing to see for this warp: P is zero (rows that are not there take no part at all)
-                            if (warp_live) {
-                                uint32_t z[32];
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) z[j] = 0u;
-                                tc::tmem_st32(tmem_se, z);
-                            }
-                        } else {
-                            const bool open = __all_sync(0xffffffffu, !live || sees >= kStep);    // no row of the warp has anything masked
-                            uint32_t v[64];
-                            tc::tmem_read64(tmem_se, v);
-                            if (__builtin_expect(!open, 0)) {
-#pragma unroll
-                                for (int cc = 0; cc < 2; ++cc) {
-                                    const uint32_t vis = visible32(it.seq, key + cc * 32);
-#pragma unroll
-                                    for (int j = 0; j < 32; ++j) v[32 * cc + j] = ((vis >> j) & 1u) ? v[32 * cc + j] : 0xff800000u;
-                                }
-                            }
-                            float b4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                            for (int j = 0; j < 64; j += 2)
-                                b4[(j >> 1) & 3] = max3_nan(b4[(j >> 1) & 3], __uint_as_float(v[j]), __uint_as_float(v[j + 1]));
-                            float bm = max3_nan(max3_nan(b4[0], b4[1], b4[2]), b4[3], -INFINITY);
-                            poisoned = poisoned || !(bm < INFINITY);       // a NaN or +inf score: the row is not meaningful
-                            bm *= sl2;
-                            const bool move = bm > ref + kSlack;           // also the first visible key (ref = -inf)
-                            if (__builtin_expect(__any_sync(0xffffffffu, move), 0)) {
-                                const float corr = move ? exp2_fast(ref - bm) : 1.f;
-                                if (!first) {
-                                    // O must be at rest: P V of the step before (older ones precede this step's scores)
-                                    if (!tc::mbar_wait_suspended(&sh->pv_done[half], (steps - 1u) & 1u, abort_flag)) failed = true;
-                                    tc::tc_fence_after_sync();
+                    for (int i = c.split_keys ? (blk - c.blk0 + half) & 1 : 0; i < open; i += by, ++s_count)
 #pragma unroll 1
-                                    for (int c0 = 0; c0 < D; c0 += 32) {
-                                        uint32_t o[32];
-                                        tc::tmem_read32(tmem_o + (uint32_t)c0, o);
-#pragma unroll
-                                        for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * corr);
-                                        tc::tmem_st32(tmem_o + (uint32_t)c0, o);
-                                    }
-                                }
-                                sum *= corr;
-                                ref = move ? bm : ref;
-                            }
-                            const float off = ref == -INFINITY ? 0.f : -ref;
-                            const uint64_t off2 = pair_of(off, off);
-                            // Eight pairs at a time, stage by stage: the pairs' chains (scale, exponential, sum, round) run side
-                            // by side.  (The exponential unit's 16 results a clock come to 2048 cycles a block, the tensor
-                            // core's time; a share of them as polynomials on the FMA pipe won 4 % on long prefixes and lost 8 % on
-                            // short calls, whose instructions then no longer stay in the caches near the schedulers.)
-                            uint64_t s2[4] = {0ull, 0ull, 0ull, 0ull};
-                            uint32_t w[32];
-#pragma unroll
-                            for (int g0 = 0; g0 < 32; g0 += 8) {
-                                uint64_t x[8];
-                                float lo[8], hi[8];
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) {
-                                    const int j = 2 * (g0 + i);
-                                    x[i] = fma2(pair_of(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), sl22, off2);
-                                }
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) {
-                                    pair_split(x[i], lo[i], hi[i]);
-                                    lo[i] = exp2_fast(lo[i]);
-                                    hi[i] = exp2_fast(hi[i]);
-                                }
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) s2[i % 4] = add2(s2[i % 4], pair_of(lo[i], hi[i]));
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) w[g0 + i] = pack_bf16(lo[i], hi[i]);
-                            }
-                            tc::tmem_st32(tmem_se, w);                     // over scores that have been read
-                            float sa, sb;
-                            pair_split(add2(add2(s2[0], s2[1]), add2(s2[2], s2[3])), sa, sb);
-                            sum += sa + sb;
-                        }
-                        first = false;
-                        ++steps;
-                        tc::tmem_st_wait();
-                        tc::tc_fence_before_sync();
-                        __syncwarp();
-                        if (lane == 0) tc::mbar_arrive(&sh->p_full[half][e]);
-                    }
-                    if (failed) {
-                        if (lane == 0) give_up(sh, p.status, 35);
-                        break;
-                    }
+                        for (int e = 0; e < 2; ++e) step(Flag<true>(), e, 0, 0);
+                    blk += open - 1;
+                    it.key0 += (open - 1) * kKeys;
+                } else if ((takers(c, it, blk) >> half) & 1u) {
+#pragma unroll 1
+                    for (int e = 0; e < 2; ++e) step(Flag<false>(), e, it.seq, it.key0 + e * kStep);
                     ++s_count;
                 }
                 if (blk + 1 < c.blk1) it.next(pl, c.ti, kKeys);
             }
             if (poisoned) sum = __uint_as_float(0x7fc00000u);
             // ---- the half's output is complete ----
-            if (!failed && !tc::mbar_wait_suspended(&sh->o_full[half], (uint32_t)piece & 1u, abort_flag)) failed = true;
+            wait(&sh->o_full[half], (uint32_t)piece & 1u, 36);
             failed = __any_sync(0xffffffffu, failed);
-            if (failed && lane == 0) give_up(sh, p.status, 36);
             tc::tc_fence_after_sync();
             // a row that saw a V row that was cleared: NaN (rare: only if some block left a note)
             if (!failed && *(volatile int*)&sh->any_note != 0 && live) {
@@ -555,10 +590,12 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                     if (noted && ((takers(c, jt, blk) >> half) & 1u) && mixed(pl, c, jt)) {
                         const __nv_bfloat16* vb = jt.seq < 0 ? static_cast<const __nv_bfloat16*>(p.Vp) + (size_t)c.g * p.Pcap * D
                                                              : static_cast<const __nv_bfloat16*>(p.V) + ((size_t)jt.seq * p.Hkv + c.g) * (size_t)p.Lcap * D;
+#pragma unroll 1
                         for (int k = 0; k < kKeys; ++k) {
                             if (!((visible32(jt.seq, jt.key0 + (k & ~31)) >> (k & 31)) & 1u)) continue;
                             const uint32_t* vr = reinterpret_cast<const uint32_t*>(vb + (size_t)(jt.key0 + k) * D);
                             uint32_t bad = 0u;
+#pragma unroll 1
                             for (int d = 0; d < D / 2; ++d) bad |= (vr[d] & 0x7f807f80u) + 0x00800080u;
                             if (bad & 0x80008000u) sum = __uint_as_float(0x7fc00000u);
                         }
@@ -646,12 +683,11 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                     const int cc = lane % LR;
                     const unsigned char* from = c.split_keys ? Qs + q * 32 * (D * 4) : Qs + half * kQHalf + q * 32 * (D * 2);
                     const int stride = c.split_keys ? D * 4 : D * 2;
-                    const unsigned long long orow = out_row();
-                    const unsigned there = __ballot_sync(0xffffffffu, live);
-#pragma unroll 4
+                    const unsigned orow = out_row(), there = __ballot_sync(0xffffffffu, live);
+#pragma unroll 2
                     for (int i = 0; i < LR; ++i) {
                         const int rr = i * RI + lane / LR;
-                        const unsigned long long dst = __shfl_sync(0xffffffffu, orow, rr);
+                        const size_t dst = __shfl_sync(0xffffffffu, orow, rr);
                         const uint4 w = *reinterpret_cast<const uint4*>(from + rr * stride + ((cc ^ (rr & 7)) << 4));
                         if ((there >> rr) & 1u) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.O) + dst * D + 8 * cc) = w;
                     }
