@@ -453,16 +453,20 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
 
             float ref = -INFINITY, sum = 0.f;
             bool first = true, poisoned = false;
-            // One step of a block.  Open: every row of the warp sees all of its keys; else the rows' limits and masks are looked
-            // at.  (Two copies of the code: with the masks inside the loop of open blocks, which is most of them, its
-            // instructions take longer to fetch.)
+            // One step of a block.  Open: every row of the warp sees all of its keys; else the rows' limits are looked at, and
+            // their masks where a row sees some of the keys.  (Two copies of the code: with the masks inside the loop of
+            // open blocks, which is most of them, its instructions take longer to fetch.)
             auto step = [&](auto open_tag, int e, int src, int key) {
                 constexpr bool Open = decltype(open_tag)::value;
                 const uint32_t tmem_se = tmem_s + (uint32_t)(e * kStep);
                 bool none = false;                              // no row of the warp sees any of the step's keys
+                bool plain = true, sees = true;                 // every row sees all of them or none; this one does
                 if constexpr (!Open) {
-                    const int sees = src < 0 ? row_pre : (src == seq ? row_kv + row_n : 0);
-                    none = __all_sync(0xffffffffu, !live || sees <= key);
+                    const int all_to = src < 0 ? row_pre : (src == seq ? row_kv : 0);
+                    const bool hidden = !live || all_to + (src == seq ? row_n : 0) <= key;
+                    sees = live && all_to >= key + kStep;
+                    none = __all_sync(0xffffffffu, hidden);
+                    plain = __all_sync(0xffffffffu, hidden || sees);
                 }
                 wait(&sh->s_full[half][e], s_count & 1u, 35);
                 __syncwarp();
@@ -478,7 +482,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                 } else {
                     uint32_t v[64];
                     tc::tmem_read64(tmem_se, v);
-                    if constexpr (!Open) {
+                    if (!Open && !plain) {
 #pragma unroll
                         for (int cc = 0; cc < 2; ++cc) {
                             const uint32_t vis = visible32(src, key + cc * 32);
@@ -491,6 +495,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                     for (int j = 0; j < 64; j += 2)
                         b4[(j >> 1) & 3] = max3_nan(b4[(j >> 1) & 3], __uint_as_float(v[j]), __uint_as_float(v[j + 1]));
                     float bm = max3_nan(max3_nan(b4[0], b4[1], b4[2]), b4[3], -INFINITY);
+                    if (!Open && plain && !sees) bm = -INFINITY;
                     poisoned = poisoned || !(bm < INFINITY);       // a NaN or +inf score: the row is not meaningful
                     bm *= sl2;
                     const bool move = bm > ref + kSlack;           // also the first visible key (ref = -inf)
@@ -541,10 +546,16 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
 #pragma unroll
                         for (int i = 0; i < 8; ++i) w[g0 + i] = pack_bf16(lo[i], hi[i]);
                     }
-                    tc::tmem_st32(tmem_se, w);                     // over scores that have been read
                     float sa, sb;
                     pair_split(add2(add2(s2[0], s2[1]), add2(s2[2], s2[3])), sa, sb);
-                    sum += sa + sb;
+                    float more_sum = sa + sb;
+                    if (!Open && plain && !sees) {
+                        more_sum = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) w[j] = 0u;
+                    }
+                    tc::tmem_st32(tmem_se, w);                     // over scores that have been read
+                    sum += more_sum;
                 }
                 first = false;
                 ++steps;
