@@ -72,7 +72,7 @@ struct DeviceGuard {
     DeviceGuard& operator=(const DeviceGuard&) = delete;
 };
 
-enum { kPrepSharedTc = 1, kPrepSharedSimple = 2, kPrepMassTc = 4, kPrepMassF32 = 8, kPrepEvict = 16 };
+enum { kPrepSharedTc = 1, kPrepSharedSimple = 2, kPrepMassTc = 4, kPrepMassF32 = 8, kPrepEvict = 16, kPrepEvictAlone = 32 };
 constexpr int kMaxDynamicSmem = 227 * 1024;
 
 // Lets `kernel` (no static shared memory) use all of an SM's shared memory; the limit is the same for every caller, so once per

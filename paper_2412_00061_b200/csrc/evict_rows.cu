@@ -53,13 +53,16 @@ __device__ __forceinline__ int4 ld_peer4(const void* local, int rank) {
 }
 
 // Copies pieces [i, n) in steps of `step`: piece k * chunks + c is 16 bytes (column c) of the k-th moving row, of K and
-// of V.  Four at a time, so that a thread has eight loads on their way.
-__device__ __forceinline__ void move_pieces(const EvictParams& p, size_t row0, long long i, long long n, long long step) {
+// of V.  Four at a time, so that a thread has eight loads on their way.  The lists are the workspace's; Near: those
+// given, in shared memory.
+template <bool Near>
+__device__ __forceinline__ void move_pieces(const EvictParams& p, size_t row0, long long i, long long n, long long step, const int* near_holes = nullptr,
+                                            const int* near_movers = nullptr) {
     const int row_bytes = p.row_bytes;
     unsigned char* Kb = static_cast<unsigned char*>(p.K) + row0 * row_bytes;
     unsigned char* Vb = static_cast<unsigned char*>(p.V) + row0 * row_bytes;
-    const int* hole_list = p.lists + row0;
-    const int* mover_list = hole_list + p.Lcap / 2;
+    const int* hole_list = Near ? near_holes : p.lists + row0;
+    const int* mover_list = Near ? near_movers : hole_list + p.Lcap / 2;
     const int chunks = row_bytes / 16;                                     // a power of two: 8, 16 or 32
     const int sh = 31 - __clz(chunks);
     constexpr int U = 4;
@@ -72,7 +75,7 @@ __device__ __forceinline__ void move_pieces(const EvictParams& p, size_t row0, l
             src[u] = dst[u] = 0;
             if (x < n) {
                 const int k = (int)(x >> sh), c = (int)(x & (chunks - 1));
-                const int from = __ldcg(mover_list + k), to = __ldcg(hole_list + k);
+                const int from = Near ? mover_list[k] : __ldcg(mover_list + k), to = Near ? hole_list[k] : __ldcg(hole_list + k);
                 src[u] = (size_t)from * row_bytes + c * 16;
                 dst[u] = (size_t)to * row_bytes + c * 16;
             }
@@ -109,12 +112,15 @@ struct __align__(16) EvictShared {
     int pick[3][3];                    // per round: digit, rows above it, rows in it
 };
 
-__global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, int cs) {
+// Alone: a CTA by itself for each pair, which also copies (else a cluster of cs, or another kernel for the copies).
+template <bool Alone>
+__global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, int cs_) {
     extern __shared__ __align__(16) unsigned char dyn[];
     EvictShared* sh = reinterpret_cast<EvictShared*>(dyn);
     unsigned* cache = reinterpret_cast<unsigned*>(sh + 1);                 // [kCacheKeys]
     const int g = blockIdx.y, b = blockIdx.z, rank = blockIdx.x;           // a cluster is one row of the grid
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int cs = Alone ? 1 : cs_;
     pdl_wait();
     pdl_trigger();
     const int L = p.kv_len[b], ev = p.n_evicted[b];
@@ -246,8 +252,8 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
                 ties |= top == prefix ? 1u << i : 0u;
             }
         };
-        int tie_base = 0;
-        if (ties_split) {
+        int tie_base = 0;                                                  // ties in the CTAs before this one
+        if (ties_split && cs > 1) {
             int cnt = 0, total;
             for (int t0 = 0; t0 < n; t0 += tile) {
                 unsigned above, ties;
@@ -255,15 +261,13 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
                 cnt += __popc(ties);
             }
             block_scan(cnt, total);
-            if (cs > 1) {
-                if (tid == 0) sh->cta_cnt[0] = make_int4(total, 0, 0, 0);
-                cluster_sync(cs);
-                int4 q[kMaxCluster];
+            if (tid == 0) sh->cta_cnt[0] = make_int4(total, 0, 0, 0);
+            cluster_sync(cs);
+            int4 q[kMaxCluster];
 #pragma unroll
-                for (int c = 0; c < kMaxCluster; ++c) q[c] = c < rank ? ld_peer4(&sh->cta_cnt[0], c) : make_int4(0, 0, 0, 0);
+            for (int c = 0; c < kMaxCluster; ++c) q[c] = c < rank ? ld_peer4(&sh->cta_cnt[0], c) : make_int4(0, 0, 0, 0);
 #pragma unroll
-                for (int c = 0; c < kMaxCluster; ++c) tie_base += q[c].x;
-            }
+            for (int c = 0; c < kMaxCluster; ++c) tie_base += q[c].x;
         }
         // rows of the tile that are dropped before the new length, and that are kept behind it; `place`: how many of
         // each (low and high half) come before this thread's in the tile, `sum`: in the whole tile
@@ -312,9 +316,11 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
                 n_move += q[c].x;
             }
         }
-        // as many rows move as there are holes, at most half of L: the lists share one array of L entries
-        int* hole_list = p.lists + row0;
-        int* mover_list = p.lists + row0 + p.Lcap / 2;
+        // as many rows move as there are holes, at most half of L: the lists share one array of L entries; short ones of a CTA by
+        // itself stay with it, in the place of the histograms (batch-32 cut 57 -> 53 us)
+        const bool near = Alone && n_move <= kBins;
+        int* hole_list = near ? sh->hist[1] : p.lists + row0;
+        int* mover_list = near ? sh->hist[2] : p.lists + row0 + p.Lcap / 2;
         tie_run = tie_base;
         for (int t0 = 0; t0 < n; t0 += tile) {
             int sum = 0;
@@ -333,13 +339,18 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
         if (p.n_move) {
             if (rank == 0 && tid == 0) p.n_move[b * p.Hkv + g] = n_move;
         } else {
-            move_pieces(p, row0, (long long)rank * kThreads + tid, (long long)n_move * (p.row_bytes / 16), (long long)cs * kThreads);
+            const long long pieces = (long long)n_move * (p.row_bytes / 16);
+            if (near) move_pieces<true>(p, row0, tid, pieces, kThreads, sh->hist[1], sh->hist[2]);
+            else move_pieces<false>(p, row0, (long long)rank * kThreads + tid, pieces, (long long)cs * kThreads);
         }
-        for (int k = rank * kThreads + tid; k < n_move; k += cs * kThreads) {
-            const int src = __ldcg(mover_list + k), dst = __ldcg(hole_list + k);
+        auto move_mass = [&](int src, int dst) {
             out_mass[dst] = mass[src];
             out_pos[dst] = row_pos[src];
-        }
+        };
+        if (near)
+            for (int k = tid; k < n_move; k += kThreads) move_mass(sh->hist[2][k], sh->hist[1][k]);
+        else
+            for (int k = rank * kThreads + tid; k < n_move; k += cs * kThreads) move_mass(__ldcg(mover_list + k), __ldcg(hole_list + k));
     }
     if (p.n_move && rank == 0 && tid == 0 && (bad || L <= p.budget)) p.n_move[b * p.Hkv + g] = 0;
     // out_kv_len / out_n_evicted may be the very input arrays: the last kv head's cluster writes them, when
@@ -380,7 +391,7 @@ __global__ void __launch_bounds__(kThreads) evict_move_kernel(EvictParams p) {
     for (int u = 0; u < units; ++u) {
         const long long from = x0 > cum[u] ? x0 : cum[u], to = x1 < cum[u + 1] ? x1 : cum[u + 1];
         if (from >= to) continue;
-        move_pieces(p, (size_t)u * p.Lcap, from - cum[u] + threadIdx.x, to - cum[u], kThreads);
+        move_pieces<false>(p, (size_t)u * p.Lcap, from - cum[u] + threadIdx.x, to - cum[u], kThreads);
     }
 }
 
@@ -433,8 +444,10 @@ extern "C" int ctcsd_evict_rows(ctcsd_handle* hh, void* stream, void* workspace,
     const size_t smem = sizeof(EvictShared) + sizeof(unsigned) * kCacheKeys;
     const DeviceGuard on(h->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    CTCSD_CUDA_CHECK(h, prepare_kernel(h, kPrepEvict, evict_rows_kernel));
-    CTCSD_CUDA_CHECK(h, launch_pdl(evict_rows_kernel, dim3(cs, c.Hkv, c.B), dim3(kThreads), smem, s, cs, p, cs));
+    const bool alone = cs == 1 && !apart;
+    auto kern = alone ? evict_rows_kernel<true> : evict_rows_kernel<false>;
+    CTCSD_CUDA_CHECK(h, prepare_kernel(h, alone ? kPrepEvictAlone : kPrepEvict, kern));
+    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(cs, c.Hkv, c.B), dim3(kThreads), smem, s, cs, p, cs));
     h->launches++;
     if (apart) {
         CTCSD_CUDA_CHECK(h, launch_pdl(evict_move_kernel, dim3(2 * h->num_sms), dim3(kThreads), sizeof(long long) * (size_t)(pairs + 1), s, 1, p));
