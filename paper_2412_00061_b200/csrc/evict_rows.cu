@@ -10,9 +10,9 @@
 // histograms added up through distributed shared memory), ranks by block scans, then the copies.  With few (kv head,
 // sequence) pairs their clusters leave most SMs idle, so the copies then are a second kernel's, spread evenly over all.
 //
-// Measured: 256 pairs that lose 1-7 of 2055 rows 13.5 us (the passes of the selection; 9.5 MB, 1.5 us of HBM); 256 pairs cut from up to
-// 8192 rows to 1024 57 us for 219 MB (rows of 256 bytes, scattered both ways, 3.8 TB/s); 8 pairs cut from 65536 rows to 16384 55 us, 30 of
-// them the selection on 64 CTAs and 22 the moves (108 us with both in one kernel and loads one at a time).
+// Measured: 256 pairs that lose 1-7 of 2055 rows 12.0 us (the passes of the selection; 9.5 MB, 1.5 us of HBM); 256 pairs cut from up to
+// 8192 rows to 1024 52 us for 219 MB (rows of 256 bytes, scattered both ways, 4.2 TB/s); 8 pairs cut from 65536 rows to 16384 55 us, 28 of
+// them the selection on 64 CTAs and the rest the moves (108 us with both in one kernel and loads one at a time).
 #include "common.cuh"
 #include "tc_primitives.cuh"
 
