@@ -525,9 +525,9 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                     const float off = ref == -INFINITY ? 0.f : -ref;
                     const uint64_t off2 = pair_of(off, off);
                     // Eight pairs at a time, stage by stage: the pairs' chains (scale, exponential, sum, round) run side
-                    // by side.  (The exponential unit's 16 results a clock come to 2048 cycles a block, the tensor
-                    // core's time; a share of them as polynomials on the FMA pipe won 4 % on long prefixes and lost 8 % on
-                    // short calls, whose instructions then no longer stay in the caches near the schedulers.)
+                    // by side.  (The exponential unit's 16 results a clock come to 2048 cycles a block, the tensor core's time at
+                    // its best; with a share of them as polynomials on the FMA pipe an 8192-row prefix took 519-540 us
+                    // against 517.)
                     uint64_t s2[4] = {0ull, 0ull, 0ull, 0ull};
                     uint32_t w[32];
 #pragma unroll
