@@ -73,12 +73,16 @@ class DraftVerifyStep:
         self.inp: Dict[str, Optional[torch.Tensor]] = {}
         self.shared = None       # workspace of the attention over a shared prefix
         self.cache = None        # state of the cache budget (enable_cache_budget)
+        self.chain = None        # state of chained steps (setup_chain)
 
     def set_inputs(self, **tensors):
         """x, Wd, blank_bias, row_seq, sel_row, base_tok, kv_len, Q, K, V, hn, Wl (device tensors); Kp, Vp
         [Hkv,Pcap,D] and prefix_len [B] when the sequences share a prefix: the attention then reads it once
-        for all of them, and tree positions start behind it."""
+        for all of them, and tree positions start behind it.  With a cache budget, K and V of a new batch need
+        reset_cache() as well."""
         self.inp.update(tensors)
+        if "K" in tensors or "V" in tensors:
+            self._forget_chain_start()
         if tensors.get("Kp") is not None and self.shared is None:
             self._use_shared_attention()
         if "Wl" in tensors and self.cfg.dtype == "bf16" and self.L2_PREFETCH_BYTES > 0:
@@ -94,17 +98,42 @@ class DraftVerifyStep:
                             Lcap: Optional[int] = None):
         """Keeps every sequence's own cache within `budget` rows: after each history update the accepted path's
         attention weights are added up per cached row, and rows beyond the budget that drew the least are
-        dropped (never the first `sinks` positions nor the newest `recent`).  Lcap: rows the K/V buffers hold."""
+        dropped (never the first `sinks` positions nor the newest `recent`).  Lcap: rows the K/V buffers hold.
+        Called again, it starts afresh with the new limits; graphs captured before hold the old ones."""
         cfg, dev = self.cfg, self.device
         Lcap = cfg.Lcap if Lcap is None else Lcap
         if budget + cfg.max_nodes > Lcap:
             raise ValueError("a cache of %d rows does not hold a budget of %d and %d tree rows" % (Lcap, budget, cfg.max_nodes))
         if self.shared is None:
             self._use_shared_attention()
-        self.cache = dict(budget=budget, sinks=sinks, recent=recent, decay=decay, ws=self.h.make_eviction(Lcap),
-                          mass=torch.zeros(cfg.B, cfg.Hkv, Lcap, dtype=torch.float32, device=dev),
-                          row_pos=torch.arange(Lcap, dtype=torch.int32, device=dev).repeat(cfg.B, cfg.Hkv, 1),
-                          n_evicted=torch.zeros(cfg.B, dtype=torch.int32, device=dev))
+        state = {} if self.cache is None or self.cache["Lcap"] != Lcap else {k: self.cache[k] for k in ("ws",) + self.CACHE_STATE}
+        if not state:
+            state = dict(ws=self.h.make_eviction(Lcap),
+                         mass=torch.empty(cfg.B, cfg.Hkv, Lcap, dtype=torch.float32, device=dev),
+                         row_pos=torch.empty(cfg.B, cfg.Hkv, Lcap, dtype=torch.int32, device=dev),
+                         n_evicted=torch.empty(cfg.B, dtype=torch.int32, device=dev))
+        self.cache = dict(state, budget=budget, sinks=sinks, recent=recent, decay=decay, Lcap=Lcap)
+        self.reset_cache()
+
+    CACHE_STATE = ("mass", "row_pos", "n_evicted")
+
+    def reset_cache(self, sequences=None):
+        """Starts the cache budget's state afresh, in the same tensors (captured graphs go on using them): no weight
+        gathered, cache row j at position j, nothing dropped.  For a new batch, or for those `sequences` (indices) whose
+        place another one takes; K, V and kv_len are the caller's to refill.  Weights known from a prompt may be
+        written to cache["mass"] afterwards."""
+        k = self.cache
+        if k is None:
+            raise ValueError("reset_cache() needs a cache budget")
+        which = list(range(self.cfg.B)) if sequences is None else [int(b) for b in sequences]
+        if any(b < 0 or b >= self.cfg.B for b in which):
+            raise ValueError("sequences are 0..%d" % (self.cfg.B - 1))
+        ages = torch.arange(k["Lcap"], dtype=torch.int32, device=self.device)
+        for at in [slice(None)] if sequences is None else which:
+            k["mass"][at] = 0.0
+            k["row_pos"][at] = ages
+            k["n_evicted"][at] = 0
+        self._forget_chain_start()
 
     def _tree_base(self, stream=None):
         """What tree positions count from: the cached rows, those dropped earlier and the shared prefix."""
@@ -266,7 +295,7 @@ class DraftVerifyStep:
         [S,B,Hkv,max_nodes,D] tree-node keys/values, hntab [S,B*max_nodes,H] tree-node hidden states.
         K, V (the cache, updated in place), Wd, Wl, blank_bias come from set_inputs()."""
         cfg, dev = self.cfg, self.device
-        self.chain = dict(n=n_steps, x0=x0, base_tok0=base_tok0, kv_len0=kv_len0, Qtab=Qtab, Ktab=Ktab, Vtab=Vtab,
+        self.chain = dict(start=None, start_kept=False, n=n_steps, x0=x0, base_tok0=base_tok0, kv_len0=kv_len0, Qtab=Qtab, Ktab=Ktab, Vtab=Vtab,
                           hntab=hntab, kv_len=kv_len0.clone(), kv_before=None, rec=None,
                           node_off=torch.arange(cfg.max_nodes, device=dev, dtype=torch.int64))
         if record:
@@ -322,12 +351,53 @@ class DraftVerifyStep:
             for k, buf in c["rec"].items():
                 buf[s].copy_(o[k])
 
-    def run_chain(self):
-        """All steps of the chain back to back on the current stream: per step the five calls and
-        the history update (with the cache budget's upkeep, where one is set), the next step reading its drafting row, root token and cache length
-        from what the previous one left on the device."""
+    def _chain_state(self):
+        return [self.inp["K"], self.inp["V"]] + [self.cache[k] for k in self.CACHE_STATE]
+
+    def _forget_chain_start(self):
+        if self.chain is not None:
+            self.chain["start_kept"] = False
+
+    def save_chain_start(self):
+        """With a cache budget a chain drops and moves rows of K and V that were there before it, so that going back to
+        its start takes a copy of them and of the budget's state.  run_chain() and plant_chain_hidden() keep one by
+        themselves when they first run after setup_chain(), enable_cache_budget(), reset_cache() or a set_inputs()
+        of K or V, and go back to it from then on.  Needed by hand before run_chain() is captured without having run,
+        and before a graph that holds it is replayed on rows that were refilled.  Without a budget it does nothing."""
+        c = self.chain
+        if c is None:
+            raise ValueError("save_chain_start() needs a chain (setup_chain)")
+        if self.cache is None:
+            return
+        now = self._chain_state()
+        if c["start"] is None or any(a.shape != b.shape or a.dtype != b.dtype for a, b in zip(c["start"], now)):
+            c["start"] = [t.clone() for t in now]
+        else:
+            for kept, t in zip(c["start"], now):
+                kept.copy_(t)
+        c["start_kept"] = True
+
+    def _rewind_chain(self):
+        """Back to where the chain starts.  (Without a budget the rows before kv_len0 are still the start's.)"""
         c = self.chain
         c["kv_len"].copy_(c["kv_len0"])
+        if self.cache is None:
+            return
+        if c["start_kept"]:
+            for t, kept in zip(self._chain_state(), c["start"]):
+                t.copy_(kept)
+            return
+        if self.device.type == "cuda" and torch.cuda.is_current_stream_capturing():
+            raise binding.CtcsdError("run the chain once, or call save_chain_start(), before capturing it with a cache budget")
+        self.save_chain_start()
+
+    def run_chain(self):
+        """All steps of the chain back to back on the current stream: per step the five calls and
+        the history update (with the cache budget's upkeep, where one is set), the next step reading its drafting
+        row, root token and cache length from what the previous one left on the device.  Every run begins at
+        the chain's start, with a cache budget too (see save_chain_start)."""
+        c = self.chain
+        self._rewind_chain()
         for s in range(c["n"]):
             self.chain_head(s)
             self.chain_tail(s)
@@ -339,7 +409,7 @@ class DraftVerifyStep:
         round trip per step (set-up only; run_chain() then needs none)."""
         from . import synth
         c, cfg = self.chain, self.cfg
-        c["kv_len"].copy_(c["kv_len0"])
+        self._rewind_chain()
         for s in range(c["n"]):
             self.chain_head(s)
             self.check_status()
