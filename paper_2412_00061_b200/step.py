@@ -78,8 +78,10 @@ class DraftVerifyStep:
     def set_inputs(self, **tensors):
         """x, Wd, blank_bias, row_seq, sel_row, base_tok, kv_len, Q, K, V, hn, Wl (device tensors); Kp, Vp
         [Hkv,Pcap,D] and prefix_len [B] when the sequences share a prefix: the attention then reads it once
-        for all of them, and tree positions start behind it.  With a cache budget, K and V of a new batch need
-        reset_cache() as well."""
+        for all of them, and tree positions start behind it (Kp=None: no prefix any more, prefix_len goes with it).
+        With a cache budget, K and V of a new batch need reset_cache() as well."""
+        if "Kp" in tensors and tensors["Kp"] is None:
+            tensors.update(Vp=None, prefix_len=None)
         self.inp.update(tensors)
         if "K" in tensors or "V" in tensors:
             self._forget_chain_start()
@@ -142,7 +144,7 @@ class DraftVerifyStep:
             return i["kv_len"]
         with torch.cuda.stream(stream):                 # (None: the current one)
             base = self.pos_base.copy_(i["kv_len"])
-            if i.get("prefix_len") is not None:
+            if i.get("Kp") is not None and i["Kp"].shape[1] > 0 and i.get("prefix_len") is not None:
                 base.add_(i["prefix_len"])
             if self.cache is not None:
                 base.add_(self.cache["n_evicted"])
