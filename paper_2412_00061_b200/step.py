@@ -82,6 +82,8 @@ class DraftVerifyStep:
         With a cache budget, K and V of a new batch need reset_cache() as well."""
         if "Kp" in tensors and tensors["Kp"] is None:
             tensors.update(Vp=None, prefix_len=None)
+        if self.cache is not None:
+            self._check_cache_rows(tensors, self.cache["Lcap"])
         self.inp.update(tensors)
         if "K" in tensors or "V" in tensors:
             self._forget_chain_start()
@@ -100,10 +102,17 @@ class DraftVerifyStep:
                             Lcap: Optional[int] = None):
         """Keeps every sequence's own cache within `budget` rows: after each history update the accepted path's
         attention weights are added up per cached row, and rows beyond the budget that drew the least are
-        dropped (never the first `sinks` positions nor the newest `recent`).  Lcap: rows the K/V buffers hold.
-        Called again, it starts afresh with the new limits; graphs captured before hold the old ones."""
+        dropped (never the first `sinks` positions nor the newest `recent`).  Lcap: rows the K/V buffers hold
+        (default: what K has; before K is known, the configuration's).  Limits that a commit could not keep are refused here
+        (ValueError).  Called again, it starts afresh with the new limits; graphs captured before hold the old ones."""
         cfg, dev = self.cfg, self.device
-        Lcap = cfg.Lcap if Lcap is None else Lcap
+        if budget < 1 or sinks < 0 or recent < 0 or sinks + recent > budget:
+            raise ValueError("a budget of %d rows does not hold %d sinks and the newest %d" % (budget, sinks, recent))
+        if not 0.0 <= decay <= 1.0:
+            raise ValueError("decay lies in 0..1")
+        if Lcap is None:
+            Lcap = cfg.Lcap if self.inp.get("K") is None else self.inp["K"].shape[2]
+        self._check_cache_rows(self.inp, Lcap)
         if budget + cfg.max_nodes > Lcap:
             raise ValueError("a cache of %d rows does not hold a budget of %d and %d tree rows" % (Lcap, budget, cfg.max_nodes))
         if self.shared is None:
@@ -116,6 +125,12 @@ class DraftVerifyStep:
                          n_evicted=torch.empty(cfg.B, dtype=torch.int32, device=dev))
         self.cache = dict(state, budget=budget, sinks=sinks, recent=recent, decay=decay, Lcap=Lcap)
         self.reset_cache()
+
+    @staticmethod
+    def _check_cache_rows(tensors, Lcap):
+        for k in ("K", "V"):
+            if tensors.get(k) is not None and tensors[k].shape[2] != Lcap:
+                raise ValueError("%s holds %d rows a sequence, the cache budget is for %d" % (k, tensors[k].shape[2], Lcap))
 
     CACHE_STATE = ("mass", "row_pos", "n_evicted")
 

@@ -190,3 +190,33 @@ def test_enabling_the_budget_again_keeps_its_tensors(step):
 def test_reset_without_a_budget_is_refused(step):
     with pytest.raises(ValueError):
         step.reset_cache()
+
+
+@pytest.mark.parametrize("kw", [dict(budget=0), dict(sinks=-1), dict(recent=-1), dict(sinks=5, recent=4), dict(decay=1.5), dict(decay=-0.1),
+                                dict(decay=float("nan")), dict(Lcap=LCAP + 1), dict(budget=LCAP), dict(budget=16, sinks=4, recent=64)])
+def test_limits_that_no_commit_would_take_are_refused_at_once(step, kw):
+    """The library refuses these too, but only inside the first commit, behind the history update.  A refusal leaves a
+    budget that was set before as it is."""
+    args = dict(dict(budget=8, sinks=1, recent=2, decay=0.5, Lcap=LCAP), **kw)
+    with pytest.raises(ValueError):
+        step.enable_cache_budget(**args)
+    assert step.cache is None and step.shared is None
+    step.enable_cache_budget(8, sinks=1, recent=2, decay=0.5, Lcap=LCAP)
+    before = dict(step.cache)
+    with pytest.raises(ValueError):
+        step.enable_cache_budget(**args)
+    assert step.cache == before
+
+
+def test_the_caches_rows_are_taken_from_them(step):
+    step.enable_cache_budget(8, sinks=1, recent=2)
+    assert step.cache["Lcap"] == LCAP and step.cache["mass"].shape[2] == LCAP
+
+
+@pytest.mark.parametrize("name", ["K", "V"])
+def test_caches_of_another_size_are_refused(step, name):
+    step.enable_cache_budget(8, sinks=1, recent=2, Lcap=LCAP)
+    before = dict(step.inp)
+    with pytest.raises(ValueError):
+        step.set_inputs(**{name: torch.zeros(CFG.B, CFG.Hkv, LCAP + 2, CFG.D), "kv_len": None})
+    assert all(step.inp[k] is before[k] for k in before)
