@@ -332,8 +332,9 @@ int ctcsd_tree_attention_shared(ctcsd_handle* h, void* stream, void* workspace, 
  * Q [B,max_nodes,Hq,D] dtype, the tree's queries;  K [B,Hkv,Lcap,D] dtype, kv_len [B]: as AFTER
  * ctcsd_commit_accepted;  acc_len [B], acc_nodes [B,T] of that step;  lse [B,max_nodes,Hq] float32: the log-sum-exp
  * ctcsd_tree_attention_shared returned (entries of nodes off the path are not read; -inf: the query
- * adds nothing);  scale > 0;  0 <= decay <= 1;  n_evicted [B] int32 or NULL (zeros);  mass, row_pos updated IN PLACE.
- * Sums are formed in float32 in a fixed order.  A sequence whose acc_len, acc_nodes or kv_len lie outside their
+ * adds nothing, whatever its row of Q holds);  scale > 0;  0 <= decay <= 1;  n_evicted [B] int32 or NULL (zeros);  mass, row_pos updated IN PLACE.
+ * Sums are formed in float32 in a fixed order.  The weight of a cached row that holds a NaN or an infinity is not
+ * meaningful; other rows' weights do not depend on it.  A sequence whose acc_len, acc_nodes or kv_len lie outside their
  * arrays is left unchanged and CTCSD_ERR_INVALID_ARG is recorded in the device status word.
  * Needs B <= 1024 (else CTCSD_ERR_UNSUPPORTED); Q and K 16-byte aligned.
  */

@@ -70,8 +70,11 @@ __global__ void __launch_bounds__(kThreads, 2) attention_mass_mma_kernel(MassPar
         for (int i = tid; i < tiles * NC * 32; i += kThreads) {
             const int ln = i & 31, c = (i >> 5) % NC, r = (i >> 5) / NC * 8 + (ln >> 2);
             uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (r < R)
-                v = *(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.Q) + mass_query_row(p, m.b, m.g, grp, r) * D) + c * 4 + (ln & 3));
+            if (r < R) {
+                const size_t qr = mass_query_row(p, m.b, m.g, grp, r);
+                const uint4 q = *(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.Q) + qr * D) + c * 4 + (ln & 3));
+                if (mass_row_counts(p.lse[qr])) v = q;
+            }
             Qf[i] = v;
         }
         if (tid < RC) {
@@ -176,8 +179,11 @@ __global__ void __launch_bounds__(kThreads) attention_mass_f32_kernel(MassParams
                     for (int i = tid; i < nr4 * (D / 4); i += kThreads) {
                         const int r = i / (D / 4), c = i - r * (D / 4);
                         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (r < nr)
-                            v = reinterpret_cast<const float4*>(static_cast<const float*>(p.Q) + mass_query_row(p, m.b, m.g, grp, r0 + r) * D)[c];
+                        if (r < nr) {
+                            const size_t qr = mass_query_row(p, m.b, m.g, grp, r0 + r);
+                            const float4 q = reinterpret_cast<const float4*>(static_cast<const float*>(p.Q) + qr * D)[c];
+                            if (mass_row_counts(p.lse[qr])) v = q;
+                        }
                         *reinterpret_cast<float4*>(Qs + r * D + 4 * c) = v;
                     }
                     for (int r = tid; r < nr4; r += kThreads) {

@@ -89,8 +89,11 @@ __device__ __forceinline__ size_t mass_query_row(const MassParams& p, int b, int
 }
 
 // Log-sum-exp in log2 units.  A query that saw nothing (-inf) adds nothing, and so do the rows that fill up
-// a tile: an infinite value makes every weight 2^(-inf) = 0.
+// a tile: an infinite value makes every weight 2^(-inf) = 0.  Their scores must be finite for that: both are zero rows to
+// the products, since the attention looked at no query that saw nothing, and such a row of Q may hold anything.
 __device__ __forceinline__ float mass_row_lse2(float lse) { return lse == -INFINITY ? INFINITY : lse * kMassLog2e; }
+
+__device__ __forceinline__ bool mass_row_counts(float lse) { return lse != -INFINITY; }
 
 // Row j's weight of one pass: `first` pass applies the decay to the old mass and gives new rows (j >= base) their
 // position; a later pass (more query rows than fit) adds.

@@ -156,7 +156,11 @@ attention_mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, MassParams p, 
                 for (int i = et; i < cols * LR; i += 256) {
                     const int r = i / LR, cc = i % LR;
                     uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                    if (r < nr) w = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.Q) + mass_query_row(p, m.b, m.g, grp, r0 + r) * D) + cc);
+                    if (r < nr) {
+                        const size_t qr = mass_query_row(p, m.b, m.g, grp, r0 + r);
+                        const uint4 q = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.Q) + qr * D) + cc);
+                        if (mass_row_counts(p.lse[qr])) w = q;
+                    }
                     *reinterpret_cast<uint4*>(Qs + (size_t)(cc / 8) * rcap * 128 + r * 128 + (((cc % 8) ^ (r & 7)) << 4)) = w;
                 }
                 // rows that fill up the last 16 weigh 2^(-inf) = 0
