@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(kThreads) attention_mass_f32_kernel(MassParams
             }
             part[rg * KB + key] = w;
             __syncthreads();
-            if (rg == 0 && j < kv) {
+            if (rg == 0 && j < kv && CTCSD_IN_BOUNDS(p.status, 72, j, p.Lcap)) {
                 const float ws = (part[key] + part[KB + key]) + (part[2 * KB + key] + part[3 * KB + key]);
                 if (j >= base) {
                     p.mass[krow0 + j] = ws;

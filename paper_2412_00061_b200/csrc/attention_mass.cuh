@@ -98,7 +98,7 @@ __device__ __forceinline__ bool mass_row_counts(float lse) { return lse != -INFI
 // Row j's weight of one pass: `first` pass applies the decay to the old mass and gives new rows (j >= base) their
 // position; a later pass (more query rows than fit) adds.
 __device__ __forceinline__ void mass_put(const MassParams& p, int b, size_t krow0, int j, int kv, int base, float decay, float old, float w, bool first) {
-    if (j >= kv) return;
+    if (j >= kv || !CTCSD_IN_BOUNDS(p.status, 71, j, p.Lcap)) return;
     const bool fresh = first && j >= base;
     p.mass[krow0 + j] = fresh ? w : (first ? fmaf(decay, old, w) : old + w);
     if (fresh) p.row_pos[krow0 + j] = (p.n_evicted ? p.n_evicted[b] : 0) + j;

@@ -88,7 +88,7 @@ __device__ __forceinline__ void move_pieces(const EvictParams& p, size_t row0, l
             }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i + u * step < n) {
+            if (i + u * step < n && CTCSD_IN_BOUNDS(p.status, 63, dst[u], (size_t)p.Lcap * row_bytes)) {
                 *reinterpret_cast<uint4*>(Kb + dst[u]) = kk[u];
                 *reinterpret_cast<uint4*>(Vb + dst[u]) = vv[u];
             }
@@ -138,7 +138,8 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
 
     if (!bad && L <= p.budget) {
         if (!in_place)
-            for (int j = lo + tid; j < hi; j += kThreads) { out_mass[j] = mass[j]; out_pos[j] = row_pos[j]; }
+            for (int j = lo + tid; j < hi; j += kThreads)
+                if (CTCSD_IN_BOUNDS(p.status, 64, j, p.Lcap)) { out_mass[j] = mass[j]; out_pos[j] = row_pos[j]; }
     } else if (!bad) {
         const int newest_from = ev + L - p.recent;
         const bool cached = hi - lo <= kCacheKeys;
@@ -192,7 +193,7 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
                         const unsigned key = rank_key(m[u], q[u], p.sinks, newest_from);
                         if (cached) cache[j - lo] = key;
                         // (rows that go are overwritten by the moves, behind a barrier)
-                        if (!in_place && j < keep) { out_mass[j] = m[u]; out_pos[j] = q[u]; }
+                        if (!in_place && j < keep && CTCSD_IN_BOUNDS(p.status, 65, j, p.Lcap)) { out_mass[j] = m[u]; out_pos[j] = q[u]; }
                         atomicAdd(&sh->hist[0][key >> shift], 1);
                     }
                 }
@@ -344,6 +345,7 @@ __global__ void __launch_bounds__(kThreads, 2) evict_rows_kernel(EvictParams p, 
             else move_pieces<false>(p, row0, (long long)rank * kThreads + tid, pieces, (long long)cs * kThreads);
         }
         auto move_mass = [&](int src, int dst) {
+            if (!CTCSD_IN_BOUNDS(p.status, 66, dst, keep)) return;
             out_mass[dst] = mass[src];
             out_pos[dst] = row_pos[src];
         };

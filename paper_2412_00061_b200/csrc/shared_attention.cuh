@@ -244,6 +244,11 @@ inline int shared_sms(const Handle* h) { return h->num_sms < kSharedMaxSms ? h->
 
 #ifdef __CUDACC__
 
+// Tiles if every node were live: what the plan's arrays have room for.
+__device__ __forceinline__ int plan_max_tiles(const SharedAttnParams& a, int TR) { return (a.B * a.max_nodes * a.grp + TR - 1) / TR; }
+// Output rows, for the debug build's checks.
+__device__ __forceinline__ long long out_rows(const SharedAttnParams& a) { return (long long)a.B * a.max_nodes * a.Hq; }
+
 // Fills the plan's arrays; executed by the whole block, ends with a barrier.  A sequence whose lengths
 // would read outside its cache is reported (by the block that publishes) and takes no part.
 __device__ inline void plan_build(SharedPlan& p, const SharedAttnParams& a, int TR, int KB, bool publish) {
@@ -294,14 +299,15 @@ __device__ inline void plan_build(SharedPlan& p, const SharedAttnParams& a, int 
                 const int u = __shfl_up_sync(0xffffffffu, v, o);
                 if (lane >= o) v += u;
             }
-            if (lane < p.tiles) p.tile_cum[lane + 1] = v;
+            if (lane < p.tiles && CTCSD_IN_BOUNDS(a.status, 81, lane, plan_max_tiles(a, TR))) p.tile_cum[lane + 1] = v;
             if (lane == 0) p.tile_cum[0] = 0;
         }
         __syncthreads();
         return;
     }
 #pragma unroll 1
-    for (int t = tid; t < p.tiles; t += nt) p.tile_cum[t + 1] = plan_tile_blocks(p, plan_tile(p, a.B, TR, t), KB);
+    for (int t = tid; t < p.tiles; t += nt)
+        if (CTCSD_IN_BOUNDS(a.status, 81, t, plan_max_tiles(a, TR))) p.tile_cum[t + 1] = plan_tile_blocks(p, plan_tile(p, a.B, TR, t), KB);
     if (tid == 0) p.tile_cum[0] = 0;
     __syncthreads();
     if (tid < 32) {
@@ -322,11 +328,12 @@ __device__ inline void plan_build(SharedPlan& p, const SharedAttnParams& a, int 
 }
 
 // CTA 0 leaves what the merge kernel needs.
-__device__ inline void plan_publish(const SharedPlan& p, const SharedAttnParams& a, int spans) {
+__device__ inline void plan_publish(const SharedPlan& p, const SharedAttnParams& a, int TR, int spans) {
 #pragma unroll 1
     for (int b = threadIdx.x; b <= a.B; b += blockDim.x) a.plan[kPlanHeader + b] = p.row_off[b];
 #pragma unroll 1
-    for (int t = threadIdx.x; t <= p.tiles; t += blockDim.x) a.plan[kPlanHeader + a.B + 1 + t] = p.tile_cum[t];
+    for (int t = threadIdx.x; t <= p.tiles; t += blockDim.x)
+        if (CTCSD_IN_BOUNDS(a.status, 82, t, plan_max_tiles(a, TR) + 1)) a.plan[kPlanHeader + a.B + 1 + t] = p.tile_cum[t];
     if (threadIdx.x == 0) {
         a.plan[0] = p.rows;
         a.plan[1] = p.tiles;

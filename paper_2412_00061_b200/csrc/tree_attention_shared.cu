@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(kSimpleThreads, 2) shared_attention_simple_ker
     pdl_trigger();
     plan_build(pl, p, TR, KB, blockIdx.x == 0);
     const SpanMap sp = span_map(pl.tile_cum[pl.tiles], pl.tiles, p.Hkv, (int)gridDim.x, p.min_blocks, p.long_span);
-    if (blockIdx.x == 0) plan_publish(pl, p, sp.spans);
+    if (blockIdx.x == 0) plan_publish(pl, p, TR, sp.spans);
     SpanWalk at;
 
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
@@ -214,6 +214,7 @@ __global__ void __launch_bounds__(kSimpleThreads, 2) shared_attention_simple_ker
             const int r = ty + 16 * i;
             if (rseq[i] < 0) continue;
             if (whole) {
+                if (!CTCSD_IN_BOUNDS(p.status, 83, orow[i], out_rows(p))) continue;
                 const float inv = s > 0.f ? 1.f / s : (s == 0.f ? 0.f : s);      // a NaN sum stays a NaN
                 float* out = static_cast<float*>(p.O) + orow[i] * D;
 #pragma unroll
@@ -223,6 +224,7 @@ __global__ void __launch_bounds__(kSimpleThreads, 2) shared_attention_simple_ker
                 if (tx == 0 && p.lse) p.lse[orow[i]] = s == 0.f ? -INFINITY : (ref[i] + log2f(s)) * kLn2;
             } else {
                 const size_t part = (size_t)blockIdx.x * 2 + slot;
+                if (!CTCSD_IN_BOUNDS(p.status, 84, part * TR + r, 2ll * gridDim.x * TR)) continue;
 #pragma unroll
                 for (int c = 0; c < DC; ++c)
                     p.part_o[(part * (D / 4) + 16 * c + tx) * TR + r] =
@@ -280,8 +282,10 @@ __global__ void __launch_bounds__(D * 4) shared_attention_merge_kernel(SharedAtt
                     const int node = o / grp;
                     const size_t orow = ((size_t)b * p.max_nodes + node) * p.Hq + g * grp + (o - node * grp);
                     const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                    store8<T>(static_cast<T*>(p.O) + orow * D + 8 * warp, z);
-                    if (warp == 0 && p.lse) p.lse[orow] = -INFINITY;
+                    if (CTCSD_IN_BOUNDS(p.status, 85, orow, out_rows(p))) {
+                        store8<T>(static_cast<T*>(p.O) + orow * D + 8 * warp, z);
+                        if (warp == 0 && p.lse) p.lse[orow] = -INFINITY;
+                    }
                 }
             }
         }
@@ -338,6 +342,7 @@ __global__ void __launch_bounds__(D * 4) shared_attention_merge_kernel(SharedAtt
         }
         const int o = pr - row_off[lo], node = o / grp;
         const size_t orow = ((size_t)lo * p.max_nodes + node) * p.Hq + g * grp + (o - node * grp);
+        if (!CTCSD_IN_BOUNDS(p.status, 86, orow, out_rows(p))) continue;
         const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
 #pragma unroll
         for (int e = 0; e < 8; ++e) a[e] *= inv;

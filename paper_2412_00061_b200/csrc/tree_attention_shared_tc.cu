@@ -204,7 +204,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
     pdl_trigger();
     plan_build(pl, p, kTcRows, kKeys, blockIdx.x == 0);
     const SpanMap sp = span_map(pl.tile_cum[pl.tiles], pl.tiles, p.Hkv, (int)gridDim.x, p.min_blocks, p.long_span);
-    if (blockIdx.x == 0) plan_publish(pl, p, sp.spans);
+    if (blockIdx.x == 0) plan_publish(pl, p, kTcRows, sp.spans);
     bool failed = false;
     SpanWalk at;
     bool more = at.init(pl, sp, blockIdx.x);
@@ -686,7 +686,7 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                             w.w = pack_bf16(o[8 * j + 6] * inv, o[8 * j + 7] * inv);
                             *reinterpret_cast<uint4*>(stage + (((c0 / 8 + j) ^ (rl & 7)) << 4)) = w;
                         }
-                    } else if (live) {
+                    } else if (live && CTCSD_IN_BOUNDS(p.status, 87, part * kTcRows + rt, 2ll * gridDim.x * kTcRows)) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
                             p.part_o[(part * (D / 4) + c0 / 4 + j) * kTcRows + rt] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
@@ -704,12 +704,14 @@ shared_attention_tc_kernel(const __grid_constant__ CUtensorMap tmKp, const __gri
                         const int rr = i * RI + lane / LR;
                         const size_t dst = __shfl_sync(0xffffffffu, orow, rr);
                         const uint4 w = *reinterpret_cast<const uint4*>(from + rr * stride + ((cc ^ (rr & 7)) << 4));
-                        if ((there >> rr) & 1u) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.O) + dst * D + 8 * cc) = w;
+                        if (((there >> rr) & 1u) && CTCSD_IN_BOUNDS(p.status, 88, dst, out_rows(p))) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.O) + dst * D + 8 * cc) = w;
                     }
                 }
                 if (live) {
-                    if (!whole) p.part_ml[part * kTcRows + rt] = make_float2(ref, sum);
-                    else if (p.lse) p.lse[out_row()] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+                    if (!whole) {
+                        if (CTCSD_IN_BOUNDS(p.status, 89, part * kTcRows + rt, 2ll * gridDim.x * kTcRows)) p.part_ml[part * kTcRows + rt] = make_float2(ref, sum);
+                    } else if (p.lse && CTCSD_IN_BOUNDS(p.status, 90, out_row(), out_rows(p)))
+                        p.lse[out_row()] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
                 }
             }
             tc::tc_fence_before_sync();
