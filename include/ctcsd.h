@@ -303,8 +303,9 @@ int ctcsd_commit_accepted(ctcsd_handle* h, void* stream, void* K, void* V, int L
  * workspace: device memory of ctcsd_tree_attention_shared_workspace_bytes(cfg) bytes, 256-byte aligned, owned by the
  *   caller, used only during the call (calls on different handles that overlap on the device need one each).
  * Q, Kp, Vp, K, V, out_O 16-byte aligned.  A sequence whose lengths lie outside its arrays is treated as having no nodes and
- * CTCSD_ERR_INVALID_ARG is recorded in the device status word.  Needs B <= 1024 and B*max_nodes*Hq/Hkv <= 524288
- * (else CTCSD_ERR_UNSUPPORTED).
+ * CTCSD_ERR_INVALID_ARG is recorded in the device status word.  Needs B <= 1024, B*max_nodes*Hq/Hkv <= 524288, and
+ * tiles * ceil(Pcap/keys) + (tiles + B) * ceil(Lcap/keys) < 2^31, where a tile is 256 of those query rows and a block 128 keys (float32: 64
+ * and 64); a million rows of prefix and cache always do (else CTCSD_ERR_UNSUPPORTED).
  */
 int ctcsd_tree_attention_shared_workspace_bytes(const ctcsd_config* cfg, size_t* out_bytes);
 int ctcsd_tree_attention_shared(ctcsd_handle* h, void* stream, void* workspace, size_t workspace_bytes,

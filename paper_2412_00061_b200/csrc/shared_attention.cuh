@@ -52,7 +52,7 @@ constexpr int kSimpleKeys = 64;
 constexpr int kTcRows = 256;                   // of the tensor-core kernel (two 128-row halves)
 constexpr int kTcKeys = 128;
 
-// The plan's arrays in shared memory (kernels) or in host memory (tests).
+// The plan's arrays in shared memory (kernels) or in host memory (tests/shared_plan_host.cu).
 struct SharedPlan {
     int* row_off;    // [B+1] packed rows before each sequence
     int* own_cum;    // [B+1] blocks of own keys before each sequence
@@ -124,6 +124,18 @@ __host__ __device__ inline TileInfo plan_tile(const SharedPlan& p, int B, int TR
 
 __host__ __device__ inline int plan_tile_blocks(const SharedPlan& p, const TileInfo& ti, int KB) {
     return (ti.pmax + KB - 1) / KB + p.own_cum[ti.b1 + 1] - p.own_cum[ti.b0];
+}
+
+// At most this many key blocks a kv head's tiles have together: every tile the whole prefix, and a sequence's own blocks once for each
+// tile that holds rows of it (tiles + B such pairs, since rows of a sequence are neighbours).
+inline long long plan_most_blocks(int B, int max_nodes, int grp, int TR, int KB, int Pcap, int Lcap) {
+    const long long tiles = ((long long)B * max_nodes * grp + TR - 1) / TR;
+    return tiles * (((long long)Pcap + KB - 1) / KB) + (tiles + B) * (((long long)Lcap + KB - 1) / KB);
+}
+// The plan numbers a kv head's blocks in 32 bits.  (Capacities decide, since only the device knows the lengths; a million rows of prefix
+// and of each cache fit with the most query rows.)
+inline bool plan_fits(int B, int max_nodes, int grp, int TR, int KB, int Pcap, int Lcap) {
+    return plan_most_blocks(B, max_nodes, grp, TR, KB, Pcap, Lcap) < (1ll << 31);
 }
 
 // The line of blocks and its spans (their lengths differ by one at most).

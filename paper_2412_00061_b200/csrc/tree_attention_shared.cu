@@ -428,6 +428,8 @@ extern "C" int ctcsd_tree_attention_shared(ctcsd_handle* hh, void* stream, void*
     if (!shared_supported(c)) return CTCSD_ERR_UNSUPPORTED;
     if (Lcap < 1 || Pcap < 0) return CTCSD_ERR_INVALID_ARG;
     if (Pcap > 0 && (!Kp || !Vp || !prefix_len)) return CTCSD_ERR_INVALID_ARG;
+    const bool tc = c.dtype == CTCSD_DTYPE_BF16;
+    if (!plan_fits(c.B, c.max_nodes, c.Hq / c.Hkv, tc ? kTcRows : kSimpleRows, tc ? kTcKeys : kSimpleKeys, Pcap, Lcap)) return CTCSD_ERR_UNSUPPORTED;
     if (!(scale > 0.f) || isinf(scale)) return CTCSD_ERR_INVALID_ARG;      // the row maximum is taken before scaling
     const uintptr_t all = reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(Kp) | reinterpret_cast<uintptr_t>(Vp) |
                           reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V) | reinterpret_cast<uintptr_t>(out_O);
@@ -444,13 +446,13 @@ extern "C" int ctcsd_tree_attention_shared(ctcsd_handle* hh, void* stream, void*
     p.plan = reinterpret_cast<int*>(ws + l.plan);
     p.part_ml = reinterpret_cast<float2*>(ws + l.ml);
     p.part_o = reinterpret_cast<float4*>(ws + l.o);
-    p.min_blocks = c.dtype == CTCSD_DTYPE_BF16 ? 3 : 1;
+    p.min_blocks = tc ? 3 : 1;
     p.long_span = 16;
     const DeviceGuard on(h->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     int rc;
-    if (c.dtype == CTCSD_DTYPE_BF16) rc = launch_shared_attention_tc(h, s, p);
+    if (tc) rc = launch_shared_attention_tc(h, s, p);
     else rc = c.D == 64 ? launch_simple<64>(h, s, p) : launch_simple<128>(h, s, p);
     if (rc != CTCSD_OK) return rc;
-    return launch_shared_attention_merge(h, s, p, c.dtype == CTCSD_DTYPE_BF16 ? kTcRows : kSimpleRows);
+    return launch_shared_attention_merge(h, s, p, tc ? kTcRows : kSimpleRows);
 }
