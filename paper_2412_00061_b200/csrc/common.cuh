@@ -46,6 +46,10 @@ struct Layout {
 
 constexpr int kCounters = 64;
 
+// SMs that workspaces have room for: an upper bound that covers every B200 configuration and lets sizes be queried without a
+// device.  ctcsd_create refuses a GPU with more.
+constexpr int kLayoutSms = 160;
+
 struct Handle {
     ctcsd_config cfg;
     Layout lay;

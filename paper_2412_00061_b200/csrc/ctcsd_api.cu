@@ -68,10 +68,6 @@ Layout make_layout(const ctcsd_config& c, int num_sms) {
 
 using namespace ctcsd;
 
-// The workspace size depends on the SM count only through upper bounds; 160 covers every
-// B200 configuration and lets the size be queried without a device.
-static const int kLayoutSms = 160;
-
 extern "C" int ctcsd_workspace_bytes(const ctcsd_config* cfg, size_t* out_bytes) {
     if (!cfg || !out_bytes) return CTCSD_ERR_INVALID_ARG;
     int rc = validate_config(*cfg);

@@ -43,8 +43,7 @@ struct SharedAttnParams {
 
 constexpr int kSharedMaxB = 1024;              // sequences
 constexpr int kSharedMaxRows = 1 << 19;        // packed rows per kv head
-constexpr int kSharedSpansPerSm = 2;           // upper bound over the kernels
-constexpr int kSharedMaxSms = 160;         // SMs the workspace has parts for; a larger GPU's others stay idle
+constexpr int kSharedSpansPerSm = 2;           // of the kernel without tensor cores
 constexpr int kPlanHeader = 8;                 // ints: rows, tiles, blocks per kv head, spans
 
 constexpr int kSimpleRows = 64;                // tile and block of the kernel without tensor cores
@@ -251,8 +250,6 @@ struct BlockIter {
         seq = b; key0 = 0; len = p.own_len[b];
     }
 };
-
-inline int shared_sms(const Handle* h) { return h->num_sms < kSharedMaxSms ? h->num_sms : kSharedMaxSms; }
 
 #ifdef __CUDACC__
 

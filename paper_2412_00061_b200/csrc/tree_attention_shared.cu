@@ -369,7 +369,7 @@ int launch_simple(Handle* h, cudaStream_t s, const SharedAttnParams& p) {
     const size_t smem = sizeof(float) * (TR * (D + 4) + KB * (D + 4) + TR * (KB + 4)) + sizeof(int) * plan_ints(p.B, max_tiles);
     auto kern = shared_attention_simple_kernel<D>;
     CTCSD_CUDA_CHECK(h, prepare_kernel(h, kPrepSharedSimple, kern));
-    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(shared_sms(h) * kSharedSpansPerSm), dim3(kSimpleThreads), smem, s, 1, p));
+    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(h->num_sms * kSharedSpansPerSm), dim3(kSimpleThreads), smem, s, 1, p));
     h->launches++;
     return CTCSD_OK;
 }
@@ -380,7 +380,7 @@ struct SharedLayout { size_t plan, ml, o, total; };
 SharedLayout shared_layout(const ctcsd_config& c) {
     const bool tc = c.dtype == CTCSD_DTYPE_BF16;
     const int TR = tc ? kTcRows : kSimpleRows;
-    const size_t spans = (size_t)kSharedMaxSms * (tc ? 1 : kSharedSpansPerSm);
+    const size_t spans = (size_t)kLayoutSms * (tc ? 1 : kSharedSpansPerSm);
     const long long rows = (long long)c.B * c.max_nodes * (c.Hq / c.Hkv);
     SharedLayout l;
     l.plan = 0;

@@ -766,7 +766,7 @@ int launch_tc(Handle* h, cudaStream_t s, const SharedAttnParams& p) {
                         sizeof(int) * plan_ints(p.B, max_tiles);
     auto kern = shared_attention_tc_kernel<D>;
     CTCSD_CUDA_CHECK(h, prepare_kernel(h, kPrepSharedTc, kern));
-    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(shared_sms(h)), dim3(kThreads), smem, s, 1, tmKp, tmVp, tmK, tmV, p));
+    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(h->num_sms), dim3(kThreads), smem, s, 1, tmKp, tmVp, tmK, tmV, p));
     h->launches++;
     return CTCSD_OK;
 }
