@@ -8,8 +8,10 @@
 //   warp 1       MMAs, S alternating between two places in tensor memory;
 //   warps 4-11   epilogue, four warps per place; together they also bring the query rows of a (sequence, kv head)
 //                into shared memory.
-// HBM bounds it: a 128-key block costs 512 cycles of tensor core, about 4 R of exponentials, and 1400 of memory.
-// Measured: 179 MB (32 sequences, 8 kv heads, 7 x 8 query rows) in 37 us, 4.9 TB/s.
+// HBM bounds it while the rows are few: a 128-key block costs 512 cycles of tensor core, 8 R of exponentials (128 R at 16 a
+// clock) and 1400 of memory (700 at head dimension 64), so that from about 175 rows (90) on the exponentials do.
+// Measured: 179 MB (32 sequences, 8 kv heads, up to 7 x 8 query rows) in 36.5 us, 4.9 TB/s; 112 MB (8 sequences, 8 kv heads, up to 9 x 24 rows) in
+// 57.6 us, 1.9 TB/s.
 #include "attention_mass.cuh"
 #include "tc_primitives.cuh"
 

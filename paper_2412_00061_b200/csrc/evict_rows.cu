@@ -10,8 +10,9 @@
 // histograms added up through distributed shared memory), ranks by block scans, then the copies.  With few (kv head,
 // sequence) pairs their clusters leave most SMs idle, so the copies then are a second kernel's, spread evenly over all.
 //
-// Measured: 256 pairs that lose 1-7 of 2055 rows 12.0 us (the passes of the selection; 9.5 MB, 1.5 us of HBM); 256 pairs cut from up to
-// 8192 rows to 1024 52 us for 219 MB (rows of 256 bytes, scattered both ways, 4.2 TB/s); 8 pairs cut from 65536 rows to 16384 55 us, 28 of
+// Measured: 256 pairs that lose 1-7 of 2055 rows 11.8 us (the passes of the selection; 9.5 MB, 1.5 us of HBM); 256 pairs cut from up to
+// 8192 rows to 1024 50 us for 219 MB: all CTAs select at once, for 10 us at least (measured with nothing to move), while HBM idles, and then copy at
+// about 5.4 TB/s (rows of 256 bytes, scattered both ways); 8 pairs cut from 65536 rows to 16384 52 us, 28 of
 // them the selection on 64 CTAs and the rest the moves (108 us with both in one kernel and loads one at a time).
 #include "common.cuh"
 #include "tc_primitives.cuh"
@@ -24,7 +25,9 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kBins = 2048;
-constexpr int kCacheKeys = 8192;       // keys a CTA keeps in shared memory; a longer share is read again from L2
+// Keys a CTA keeps in shared memory; a longer share is read again from L2 in every pass (8 pairs cut to 16384 rows: from 65536 rows,
+// the most that eight CTAs keep, 52 us, from 81920 97, from 131072 125).
+constexpr int kCacheKeys = 8192;
 constexpr int kMaxCluster = 8;
 constexpr int kMaxRun = 17;            // rows a thread looks after at a time (odd: its neighbours' rows lie in other banks)
 
@@ -435,11 +438,16 @@ extern "C" int ctcsd_evict_rows(ctcsd_handle* hh, void* stream, void* workspace,
     p.seq_ticket = reinterpret_cast<unsigned*>(h->ws + h->lay.seq_ticket_off);
     p.status = status_ptr(h);
     // a cluster per (kv head, sequence): more CTAs while they all run at once (two fit on an SM) and each
-    // still has rows to look at
+    // still has rows to look at.  (Measured with 512 / 1024 / 2048 rows a CTA at least, in us: 32 heads of one sequence cut from 4096 rows to
+    // 1024 27.3 / 18.2 / 19.1; 8 heads, 32768 to 8192 31.1 / 32.4 / 31.3; 8192 to 2048 19.3 / 18.0 / 16.3; three rows leave 2051, 32 heads, 15.3 / 12.8 / 8.4,
+    // 8 heads, three leave 8195 16.8 / 17.0 / 14.6.)
     const long long pairs = (long long)c.B * c.Hkv;
     int cs = 1;
     while (cs < kMaxCluster && pairs * cs * 2 <= 2ll * h->num_sms && Lcap / (cs * 2) >= 1024) cs *= 2;
-    // the clusters cover less than half of the SMs, and there may be enough to copy: a kernel of its own for that
+    // the clusters cover less than half of the SMs, and there may be enough to copy: a kernel of its own for that.  The capacity decides,
+    // since only the device knows the lengths.  (Measured apart / in one kernel, in us, 8 heads: 65536 rows cut to 16384 52 / 66, 16384 to 4096 20.6 / 23.1, 8192
+    // to 2048, at the limit, 18.0 / 18.3, 4096 to 1024, below it, 15.8 / 16.1; three rows leave 2051 in a buffer of that size, below it, 15.4 / 12.8, in a buffer
+    // of 65048 rows 19.1 / 16.1.)
     const long long movable = budget < Lcap - budget ? budget : Lcap - budget;
     const bool apart = pairs * cs * 2 <= h->num_sms && movable > 0 && pairs * movable * p.row_bytes >= (4ll << 20);
     p.n_move = apart ? p.lists + (size_t)pairs * Lcap : nullptr;

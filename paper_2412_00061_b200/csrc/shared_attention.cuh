@@ -171,6 +171,10 @@ __host__ __device__ inline SpanMap span_map_n(int per_head, int Hkv, int spans) 
 // number of spans, none shorter than min_blocks on average, and the cuts fall on the tiles' ends when
 // these have equal work; where spans are long (over `long_span` blocks) or the pairs outnumber them, balance counts more
 // and all max_spans are used.
+// Measured, in us.  min_blocks of bf16 at 1 / 2 / 3 / 4 / 6: 32 heads, one 64-node tree, prefix 200, own 300: 20.4 / 21.5 / 18.9 / 19.0 / 19.0; prefix and own
+// 1024: 24.4 / 24.7 / 24.6 / 24.7 / 28.7; 12 heads on 3 of 64, four trees, prefix 3000: 27.4 / 27.6 / 27.5 / 28.6 / 31.3.  Of float32 at 1 / 2 / 3: 4 heads, prefix
+// and own 128: 15.5 / 29.0 / 38.1; 32 heads, 512: 58 / 67 / 83.  long_span at 4 / 8 / 16 / 32 / never: four tokens, 32 heads, prefix 4096: 41.5 / 41.0 /
+// 38.4 / 38.6 / 38.5; eight trees, 32 heads, prefix 2048: 85.6 / 85.5 / 85.4 / 93.6 / 93.5; eight tokens, prefix 8192: 70.5 / 70.3 / 70.2 / 70.7 / 76.4.
 __host__ __device__ inline SpanMap span_map(int per_head, int tiles, int Hkv, int max_spans, int min_blocks, int long_span) {
     const long long total = (long long)per_head * Hkv;
     const int pairs = tiles * Hkv;                         // (below 2^31: 2^13 tiles at most, and Hkv of them fit no GPU's memory beyond)

@@ -22,11 +22,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 
 // ---------------------------------------------------------------------------------------
-// float32: 64 packed rows x 64 keys per step, 256 threads.  The FP32 pipe bounds it (4 D flops per row
-// and key), so a thread computes 4 x 4 scores and 4 x D/16 outputs from 128-bit shared loads; rows and
-// keys are dealt 16 apart, which keeps the loads free of bank conflicts (row stride D + 4).
-// K and V take turns in one buffer so that two CTAs fit on an SM and hide each other's loads.  (Measured: eight trees of 64
-// nodes, 32 heads of 128, prefix 2048: 552 us, 31 TFLOP/s.)
+// float32: 64 packed rows x 64 keys per step, 256 threads.  A thread computes 4 x 4 scores and 4 x D/16 outputs from
+// 128-bit shared loads; rows and keys are dealt 16 apart, which keeps the loads free of bank conflicts (row stride D + 4).
+// K and V take turns in one buffer so that two CTAs fit on an SM and hide each other's loads.  Shared-memory reads bound it: eight
+// 128-bit loads feed 64 multiply-adds, their pipe is 72 % busy, the FMA pipe 49 %.  (Measured: eight trees of 64
+// nodes, 32 heads of 128, prefix 2048: 552 us, 31 TFLOP/s of the FP32 pipe's 74.)
 // ---------------------------------------------------------------------------------------
 constexpr int kSimpleThreads = 256;
 

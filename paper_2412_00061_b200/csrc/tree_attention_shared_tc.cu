@@ -15,6 +15,10 @@
 // (two warps share a scheduler's unit), storing P 115, hand-over and loop 200-300 - and the tensor core 720 for each half
 // (scores of 64 keys take it as long as scores of 128).  64 rows x 8 heads of 32 sequences on an 8192-row prefix: 517 us,
 // 1.07 PFLOP/s.  Batches of single tokens are bound by HBM: 319 MB in 71 us, 13 us of that set-up and merge.
+// P is rounded to bf16, by 2^-8 of a weight at most, because a tensor-core product takes both operands in one type and V is bf16:
+// weights in 32 bits would take V widened to tf32 (half the rate, twice the space) or P in two bf16 parts (twice the
+// products).  Scores, references, sums (of the unrounded weights), O and the parts are float32.  Against 64 bits the outputs are off
+// by 0.0020-0.0022 relative, 1.1-1.3 times what rounding them to bf16 alone costs; tree_attention_tc.cu does the same.
 // With at most 128 rows in a tile both halves work on the same rows, one on the even and one on the odd
 // blocks, and their outputs are joined at the end: short batches keep both pipes busy too.
 // ref, the exponent's reference, follows the row maximum lazily (only when it falls kSlack behind), so that O
