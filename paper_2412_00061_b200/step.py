@@ -84,9 +84,9 @@ class DraftVerifyStep:
             tensors.update(Vp=None, prefix_len=None)
         if self.cache is not None:
             self._check_cache_rows(tensors, self.cache["Lcap"])
-        self.inp.update(tensors)
-        if "K" in tensors or "V" in tensors:
+        if any(k in tensors and tensors[k] is not self.inp.get(k) for k in ("K", "V")):
             self._forget_chain_start()
+        self.inp.update(tensors)
         if tensors.get("Kp") is not None and self.shared is None:
             self._use_shared_attention()
         if "Wl" in tensors and self.cfg.dtype == "bf16" and self.L2_PREFETCH_BYTES > 0:
@@ -379,7 +379,7 @@ class DraftVerifyStep:
         """With a cache budget a chain drops and moves rows of K and V that were there before it, so that going back to
         its start takes a copy of them and of the budget's state.  run_chain() and plant_chain_hidden() keep one by
         themselves when they first run after setup_chain(), enable_cache_budget(), reset_cache() or a set_inputs()
-        of K or V, and go back to it from then on.  Needed by hand before run_chain() is captured without having run,
+        of another K or V, and go back to it from then on.  Needed by hand before run_chain() is captured without having run,
         and before a graph that holds it is replayed on rows that were refilled.  Without a budget it does nothing."""
         c = self.chain
         if c is None:

@@ -220,3 +220,15 @@ def test_caches_of_another_size_are_refused(step, name):
     with pytest.raises(ValueError):
         step.set_inputs(**{name: torch.zeros(CFG.B, CFG.Hkv, LCAP + 2, CFG.D), "kv_len": None})
     assert all(step.inp[k] is before[k] for k in before)
+
+
+def test_the_same_buffers_given_again_are_no_new_batch(step):
+    """set_inputs() with the tensors that are in use already, between two runs of a chain."""
+    step.enable_cache_budget(8, sinks=1, recent=2, Lcap=LCAP)
+    _chain(step)
+    step.run_chain()
+    got = _state(step)
+    step.set_inputs(K=step.inp["K"], V=step.inp["V"])
+    step.run_chain()
+    for a, b in zip(_state(step), got):
+        assert torch.equal(a, b)
