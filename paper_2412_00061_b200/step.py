@@ -103,8 +103,9 @@ class DraftVerifyStep:
         """Keeps every sequence's own cache within `budget` rows: after each history update the accepted path's
         attention weights are added up per cached row, and rows beyond the budget that drew the least are
         dropped (never the first `sinks` positions nor the newest `recent`).  Lcap: rows the K/V buffers hold
-        (default: what K has; before K is known, the configuration's).  Limits that a commit could not keep are refused here
-        (ValueError).  Called again, it starts afresh with the new limits; graphs captured before hold the old ones."""
+        (default: what K has; before K is known, the configuration's).  Limits that a commit could not keep are
+        refused here (ValueError).  Called again, it starts afresh with the new limits (a chain goes on beginning
+        at its own rows); graphs captured before hold the old ones."""
         cfg, dev = self.cfg, self.device
         if budget < 1 or sinks < 0 or recent < 0 or sinks + recent > budget:
             raise ValueError("a budget of %d rows does not hold %d sinks and the newest %d" % (budget, sinks, recent))
@@ -124,7 +125,12 @@ class DraftVerifyStep:
                          row_pos=torch.empty(cfg.B, cfg.Hkv, Lcap, dtype=torch.int32, device=dev),
                          n_evicted=torch.empty(cfg.B, dtype=torch.int32, device=dev))
         self.cache = dict(state, budget=budget, sinks=sinks, recent=recent, decay=decay, Lcap=Lcap)
+        kept = self.chain is not None and self.chain["start_kept"]
         self.reset_cache()
+        if kept:                 # the rows of a chain's start are those of its batch still; the rest starts afresh
+            for there, k in zip(self.chain["start"][2:], self.CACHE_STATE):
+                there.copy_(self.cache[k])
+            self.chain["start_kept"] = True
 
     @staticmethod
     def _check_cache_rows(tensors, Lcap):
@@ -378,8 +384,8 @@ class DraftVerifyStep:
     def save_chain_start(self):
         """With a cache budget a chain drops and moves rows of K and V that were there before it, so that going back to
         its start takes a copy of them and of the budget's state.  run_chain() and plant_chain_hidden() keep one by
-        themselves when they first run after setup_chain(), enable_cache_budget(), reset_cache() or a set_inputs()
-        of another K or V, and go back to it from then on.  Needed by hand before run_chain() is captured without having run,
+        themselves when they first run after setup_chain(), the first enable_cache_budget(), reset_cache() or a
+        set_inputs() of another K or V, and go back to it from then on.  Needed by hand before run_chain() is captured without having run,
         and before a graph that holds it is replayed on rows that were refilled.  Without a budget it does nothing."""
         c = self.chain
         if c is None:

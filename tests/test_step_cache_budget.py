@@ -232,3 +232,21 @@ def test_the_same_buffers_given_again_are_no_new_batch(step):
     step.run_chain()
     for a, b in zip(_state(step), got):
         assert torch.equal(a, b)
+
+
+def test_another_budget_for_the_same_chain(step):
+    """enable_cache_budget() between two runs: the chain still begins at its own start, with nothing dropped."""
+    K0, V0 = step.inp["K"].clone(), step.inp["V"].clone()
+    step.enable_cache_budget(8, sinks=1, recent=2, Lcap=LCAP)
+    _chain(step)
+    step.run_chain()
+    step.enable_cache_budget(6, sinks=1, recent=2, decay=0.5, Lcap=LCAP)
+    step.run_chain()
+
+    other = DraftVerifyStep(CFG, device="cpu")
+    other.set_inputs(K=K0, V=V0, Wd=None, Wl=None, base_tok=step.inp["base_tok"])
+    other.enable_cache_budget(6, sinks=1, recent=2, decay=0.5, Lcap=LCAP)
+    _chain(other)
+    other.run_chain()
+    for a, b in zip(_state(step), _state(other)):
+        assert torch.equal(a, b)
