@@ -98,6 +98,14 @@ class DraftVerifyStep:
         self.out["attn_lse"] = z(self.cfg.B, self.cfg.max_nodes, self.cfg.Hq, dtype=torch.float32)
         self.pos_base = z(self.cfg.B, dtype=torch.int32)
 
+    def _has_prefix(self):
+        return self.inp.get("Kp") is not None and self.inp["Kp"].shape[1] > 0
+
+    def _shared_in_use(self):
+        """Whether the attention takes the shared form: for a prefix, or for the log-sum-exp (out["attn_lse"]) that a
+        cache budget needs.  Otherwise ctcsd_tree_attention is faster."""
+        return self.cache is not None or self._has_prefix()
+
     def enable_cache_budget(self, budget: int, sinks: int = 4, recent: int = 64, decay: float = 1.0,
                             Lcap: Optional[int] = None):
         """Keeps every sequence's own cache within `budget` rows: after each history update the accepted path's
@@ -161,11 +169,11 @@ class DraftVerifyStep:
     def _tree_base(self, stream=None):
         """What tree positions count from: the cached rows, those dropped earlier and the shared prefix."""
         i = self.inp
-        if self.shared is None:
+        if not self._shared_in_use():
             return i["kv_len"]
         with torch.cuda.stream(stream):                 # (None: the current one)
             base = self.pos_base.copy_(i["kv_len"])
-            if i.get("Kp") is not None and i["Kp"].shape[1] > 0 and i.get("prefix_len") is not None:
+            if self._has_prefix() and i.get("prefix_len") is not None:
                 base.add_(i["prefix_len"])
             if self.cache is not None:
                 base.add_(self.cache["n_evicted"])
@@ -264,7 +272,7 @@ class DraftVerifyStep:
 
     def attention(self, stream=None):
         i, o = self.inp, self.out
-        if self.shared is not None:
+        if self._shared_in_use():
             self.h.tree_attention_shared(self.shared, i["Q"], i.get("Kp"), i.get("Vp"), i.get("prefix_len"), i["K"], i["V"],
                                          i["kv_len"], o["n_nodes"], o["mask"], 1.0 / float(self.cfg.D) ** 0.5, o["O"],
                                          o["attn_lse"], stream=stream)

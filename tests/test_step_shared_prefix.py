@@ -34,3 +34,21 @@ def test_lengths_alone_are_no_prefix(step):  # noqa: F811
 def test_an_empty_prefix_is_no_prefix(step):  # noqa: F811
     step.set_inputs(Kp=_prefix(0), Vp=_prefix(0), prefix_len=torch.tensor([6, 2], dtype=torch.int32))
     assert _base(step) == [4, 9]
+
+
+def test_the_attention_goes_back_to_its_own_form(step):  # noqa: F811
+    """Without a prefix and without a budget a step makes the calls of one that never had a prefix: the shared form is
+    slower there."""
+    def made():
+        step.h.calls.clear()
+        step.tree()
+        step.attention()
+        return step.h.calls[1:]
+    step.set_inputs(Q=None)
+    assert made() == ["tree_attention"]
+    step.set_inputs(Kp=_prefix(6), Vp=_prefix(6), prefix_len=torch.tensor([6, 2], dtype=torch.int32))
+    assert made() == ["tree_attention_shared"]
+    step.set_inputs(Kp=None)
+    assert made() == ["tree_attention"] and _base(step) == [4, 9]
+    step.enable_cache_budget(8, sinks=1, recent=2)
+    assert made() == ["tree_attention_shared"]
