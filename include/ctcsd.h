@@ -367,6 +367,83 @@ int ctcsd_evict_rows(ctcsd_handle* h, void* stream, void* workspace, size_t work
                      float* out_mass, int* out_row_pos, int* out_kv_len, int* out_n_evicted);
 
 /*
+ * Weights and cached rows in 4 bits (the paper has no counterpart: the draft head's weights and, for long contexts, the cache are
+ * what a step reads most of, and drafts are only proposals, which verification keeps from changing what is output).
+ *
+ * Format.  A row of n values is cut into groups; a group keeps two bfloat16 numbers, scale and origin (one 32-bit word, scale in
+ * the low half), and level q = 0..15 stands for
+ *   round( origin + scale * (16 + q) ),  rounded once, to the handle's dtype.
+ * Eight consecutive values share a 32-bit word: value 2i at bits 4i..4i+3, value 2i+1 at bits 16+4i..19+4i.
+ * Quantising, every step rounded to float32 (lo, hi: least and largest value of the group):
+ *   scale = bfloat16((hi - lo) / 15);  origin = bfloat16(lo - 16 scale);
+ *   q = (v - origin) / scale - 16, rounded half to even and clamped to 0..15;  0 where scale = 0.
+ * A group that holds a NaN or an infinity, or whose scale or origin would not be finite, stands for NaN (scale 0, origin NaN).
+ *
+ * ctcsd_quantize_weights_q4: Wd [T,V+1,H] dtype -> out_Wq, ctcsd_weights_q4_bytes(cfg, group) bytes; groups of 32, 64 or 128
+ * along H (the last one of a row may be shorter).  Done once.  Layout: panels of 16 consecutive classes of a slot (the last one
+ * filled up with rows of zeros), [T][ceil((V+1)/16)][ceil(H/128)] blocks of 1024 + 64 * (128 / group) bytes, for 128 elements of H each:
+ *   word 128 h + 16 g + 4 t + i (h < 2, g < 8, t < 4, i < 4): class 8h + g, values 32t + 8i .. 32t + 8i + 7 of the block;
+ *   then [16 classes][128 / group] words of scale and origin.
+ *
+ * ctcsd_draft_logits_q4: ctcsd_draft_logits over such weights, with the values they stand for.
+ * x [x_row_count,H] dtype;  x_rows NULL (draft row m reads x[m], x_row_count >= M) or [M] int32 as for ctcsd_draft_logits_rows (an entry
+ *   outside 0..x_row_count-1 records CTCSD_ERR_INVALID_ARG in the device status word and that row drafts from a zero vector);
+ * Wq, group as for the call above, not written by any kernel while the call runs or directly before it (ctcsd_quantize_weights_q4
+ *   itself may precede it);  everything else as for ctcsd_draft_logits.
+ * Needs H <= 10240 (else CTCSD_ERR_UNSUPPORTED).  The weights are read once per 16 rows (8 where H > 4096; float32: 4).
+ */
+int ctcsd_weights_q4_bytes(const ctcsd_config* cfg, int group, size_t* out_bytes);
+int ctcsd_quantize_weights_q4(ctcsd_handle* h, void* stream, const void* Wd, int group, void* out_Wq);
+int ctcsd_draft_logits_q4(ctcsd_handle* h, void* stream, int M, const void* x, int x_row_count, const int* x_rows,
+                          const void* Wq, int group, const int* row_seq, const float* blank_bias,
+                          int* out_topk_id, float* out_topk_lp, float* out_lse, float* out_logits_dbg);
+
+/*
+ * A cache in 4 bits.  K and V have two arrays each: levels Kq, Vq [B,Hkv,Lcap,D/2] bytes (D/8 words a row) and scales and origins
+ * Ks, Vs [B,Hkv,Lcap,D/32] words (groups of 32 along D), all 16-byte aligned.  A step's tree rows stay in full precision, in
+ * Kt, Vt [B,Hkv,max_nodes,D] dtype: node j's key and value at row j.
+ *
+ * ctcsd_store_rows_q4: rows 0..n_rows[b]-1 of K, V [B,Hkv,Lsrc,D] dtype (a prompt's) to cache rows at[b].. (at NULL: from 0).
+ * ctcsd_load_rows_q4: cache rows first[b] .. first[b]+n_rows[b]-1 (first NULL: from 0), as values, to rows 0.. of out_K, out_V
+ *   [B,Hkv,Lout,D] dtype; rows from n_rows[b] on become zero.
+ * ctcsd_commit_accepted_q4: ctcsd_commit_accepted for such a cache.  With L = kv_len[b], the root's row of Kt, Vt goes to cache row
+ *   L, that of accepted node acc_nodes[b,l] to row L + 1 + l;  out_kv_len [B] = L + 1 + acc_len (it may be the array kv_len);
+ *   out_sel_row [B] or NULL as there.
+ * A sequence whose rows would leave its arrays (or whose acc_len or acc_nodes do) is left unchanged (load: zeros) and
+ * CTCSD_ERR_INVALID_ARG is recorded in the device status word.
+ */
+int ctcsd_store_rows_q4(ctcsd_handle* h, void* stream, const void* K, const void* V, int Lsrc, const int* n_rows,
+                        const int* at, void* Kq, void* Ks, void* Vq, void* Vs, int Lcap);
+int ctcsd_load_rows_q4(ctcsd_handle* h, void* stream, const void* Kq, const void* Ks, const void* Vq, const void* Vs,
+                       int Lcap, const int* first, const int* n_rows, void* out_K, void* out_V, int Lout);
+int ctcsd_commit_accepted_q4(ctcsd_handle* h, void* stream, const void* Kt, const void* Vt, void* Kq, void* Ks, void* Vq,
+                             void* Vs, int Lcap, const int* kv_len, const int* acc_len, const int* acc_nodes,
+                             int* out_kv_len, int* out_sel_row);
+
+/*
+ * Tree attention over a cache in 4 bits: keys of sequence b = the values that rows 0..kv_len[b]-1 of its cache stand for, and
+ * the tree rows of node i's mask, from Kt, Vt;
+ *   O[b,i,h,:] = softmax_j( scale * q[b,i,h,:].k_j ) v_j;   lse[b,i,h] = log sum_j exp( scale * q.k_j ).
+ * Any batch from single tokens (n_nodes = 1) to full trees.
+ * Q [B,max_nodes,Hq,D] dtype;  kv_len [B] int32 in 0..Lcap;  n_nodes [B] int32 in 0..max_nodes;  mask as produced by
+ *   ctcsd_build_tree;  scale > 0;
+ * out_O [B,max_nodes,Hq,D] dtype;  out_lse [B,max_nodes,Hq] float32 or NULL.  Rows of unused nodes, and of nodes that see no key at
+ *   all, are written as 0 and -inf.
+ * What a row's mask hides does not reach it: rows behind the lengths and other branches of the tree may hold anything, NaN and
+ * infinities included.  A row that does see a NaN or infinite value is not meaningful.
+ * workspace: device memory of ctcsd_tree_attention_q4_workspace_bytes(cfg) bytes, 256-byte aligned, owned by the caller, used
+ *   only during the call (calls on different handles that overlap on the device need one each).
+ * All tensors 16-byte aligned.  A sequence whose lengths lie outside its arrays is treated as having no nodes and
+ * CTCSD_ERR_INVALID_ARG is recorded in the device status word.  Needs B <= 1024 and fewer than 2^31 key blocks (B times tiles of 16 query
+ * rows times blocks of 64 keys are an upper bound; else CTCSD_ERR_UNSUPPORTED).
+ */
+int ctcsd_tree_attention_q4_workspace_bytes(const ctcsd_config* cfg, size_t* out_bytes);
+int ctcsd_tree_attention_q4(ctcsd_handle* h, void* stream, void* workspace, size_t workspace_bytes, const void* Q,
+                            const void* Kq, const void* Ks, const void* Vq, const void* Vs, int Lcap,
+                            const void* Kt, const void* Vt, const int* kv_len, const int* n_nodes,
+                            const unsigned long long* mask, float scale, void* out_O, float* out_lse);
+
+/*
  * The paper's own verification layout (Sec. 3.3): instead of collapsing the slot paths before
  * the tree is built, the most probable RAW paths - blanks and repeats still in place - form the
  * token tree, and the CTC transform acts through the attention map: a position whose symbol the

@@ -765,3 +765,47 @@ def evict_rows(K: np.ndarray, Vc: np.ndarray, mass: np.ndarray, row_pos: np.ndar
         n_evicted[b] += L - budget
         kv_len[b] = budget
     return K, Vc, mass, row_pos, kv_len, n_evicted
+
+
+# --------------------------------------------------------------------------------------
+# Weights and cached rows in 4 bits (no counterpart in the paper)
+# --------------------------------------------------------------------------------------
+def round_to_bf16(a: np.ndarray) -> np.ndarray:
+    """Nearest bfloat16 (ties to even) of float64 values, as float64: 8 significant bits."""
+    a = np.asarray(a, dtype=np.float64)
+    m, e = np.frexp(a)
+    return np.ldexp(np.rint(m * 256.0), e - 8)
+
+
+def q4_quantize(v: np.ndarray, group: int) -> Tuple[np.ndarray, np.ndarray, np.ndarray]:
+    """Rows of v [...,n] in groups of `group` (the last may be shorter).  Returns levels [...,n] int64 and
+    per group scale, origin [...,ceil(n/group)] (float64 values that are bfloat16 numbers); a group that holds
+    a NaN or an infinity has scale 0, origin NaN, levels 0.  Every step is rounded to float32."""
+    f = np.asarray(v, dtype=np.float32)
+    n = f.shape[-1]
+    groups = (n + group - 1) // group
+    q = np.zeros(f.shape, dtype=np.int64)
+    scale = np.zeros(f.shape[:-1] + (groups,), dtype=np.float64)
+    origin = np.zeros_like(scale)
+    with np.errstate(all="ignore"):
+        for i in range(groups):
+            w = f[..., i * group:(i + 1) * group]
+            lo, hi = w.min(axis=-1), w.max(axis=-1)
+            s = round_to_bf16((hi - lo) / np.float32(15.0)).astype(np.float32)
+            o = round_to_bf16(lo - np.float32(16.0) * s).astype(np.float32)
+            bad = ~(np.isfinite(s) & np.isfinite(o))
+            s = np.where(bad, np.float32(0), s)
+            o = np.where(bad, np.float32(np.nan), o)
+            level = np.rint((w - o[..., None]) / s[..., None] - np.float32(16.0))
+            level = np.where((s > 0)[..., None], np.clip(level, 0, 15), 0)
+            q[..., i * group:(i + 1) * group] = level.astype(np.int64)
+            scale[..., i], origin[..., i] = s, o
+    return q, scale, origin
+
+
+def q4_values(q: np.ndarray, scale: np.ndarray, origin: np.ndarray, group: int, bf16: bool) -> np.ndarray:
+    """What levels stand for: origin + scale * (16 + q), rounded once to bfloat16 or float32 (as float64)."""
+    n = q.shape[-1]
+    at = np.arange(n) // group
+    v = origin[..., at] + scale[..., at] * (16.0 + q)
+    return round_to_bf16(v) if bf16 else v.astype(np.float32).astype(np.float64)

@@ -27,6 +27,8 @@ EXPORTS = [
     "ctcsd_verify_accept_sampled", "ctcsd_draft_module_workspace_bytes", "ctcsd_draft_module",
     "ctcsd_select_raw_paths", "ctcsd_build_raw_tree", "ctcsd_verify_accept_raw",
     "ctcsd_tree_attention_shared_workspace_bytes", "ctcsd_tree_attention_shared", "ctcsd_attention_mass", "ctcsd_evict_rows_workspace_bytes", "ctcsd_evict_rows",
+    "ctcsd_weights_q4_bytes", "ctcsd_quantize_weights_q4", "ctcsd_draft_logits_q4", "ctcsd_store_rows_q4", "ctcsd_load_rows_q4",
+    "ctcsd_commit_accepted_q4", "ctcsd_tree_attention_q4_workspace_bytes", "ctcsd_tree_attention_q4",
 ]
 
 
@@ -89,6 +91,14 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.ctcsd_attention_mass.argtypes = [vp, vp, vp, vp, ci, vp, vp, vp, vp, ctypes.c_float, ctypes.c_float, vp, vp, vp]
     lib.ctcsd_evict_rows_workspace_bytes.argtypes = [ctypes.POINTER(CConfig), ci, ctypes.POINTER(cs)]
     lib.ctcsd_evict_rows.argtypes = [vp, vp, vp, cs, vp, vp, ci, vp, vp, vp, vp, ci, ci, ci, vp, vp, vp, vp]
+    lib.ctcsd_weights_q4_bytes.argtypes = [ctypes.POINTER(CConfig), ci, ctypes.POINTER(cs)]
+    lib.ctcsd_quantize_weights_q4.argtypes = [vp, vp, vp, ci, vp]
+    lib.ctcsd_draft_logits_q4.argtypes = [vp, vp, ci, vp, ci, vp, vp, ci] + [vp] * 6
+    lib.ctcsd_store_rows_q4.argtypes = [vp, vp, vp, vp, ci] + [vp] * 6 + [ci]
+    lib.ctcsd_load_rows_q4.argtypes = [vp] * 6 + [ci] + [vp] * 4 + [ci]
+    lib.ctcsd_commit_accepted_q4.argtypes = [vp] * 8 + [ci] + [vp] * 5
+    lib.ctcsd_tree_attention_q4_workspace_bytes.argtypes = [ctypes.POINTER(CConfig), ctypes.POINTER(cs)]
+    lib.ctcsd_tree_attention_q4.argtypes = [vp, vp, vp, cs] + [vp] * 5 + [ci] + [vp] * 5 + [ctypes.c_float, vp, vp]
     lib.ctcsd_tree_attention_static.argtypes = [vp, ci, ci, ci, ci, ci, vp, vp, vp, ci, vp, vp, vp,
                                                 ctypes.c_float, vp, vp]
     for name in EXPORTS:
@@ -463,6 +473,122 @@ class Handle:
             _ptr(out_mass, f32, rows, "out_mass"), _ptr(out_row_pos, i32, rows, "out_row_pos"),
             _ptr(out_kv_len, i32, c.B, "out_kv_len"), _ptr(out_n_evicted, i32, c.B, "out_n_evicted"))
         self._check(rc, "evict_rows")
+
+    # ---- weights and caches in 4 bits ----
+    Q4_GROUP = 32                      # values of a cached row that share a scale
+
+    def quantize_weights_q4(self, Wd, group=128, stream=None):
+        """Packs the draft head's weights [T,V+1,H] in 4 bits, `group` (32, 64 or 128) neighbours along H to a scale.
+        Returns what draft_logits_q4 takes; Wd is not needed any more."""
+        c = self.cfg
+        n = ctypes.c_size_t(0)
+        self._check(self.lib.ctcsd_weights_q4_bytes(ctypes.byref(self.cfg), int(group), ctypes.byref(n)), "weights_q4_bytes")
+        w = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        rc = self.lib.ctcsd_quantize_weights_q4(
+            self._h, _stream_ptr(stream, self._dev), _ptr(Wd, self.act_dtype, c.T * (c.V + 1) * c.H, "Wd"), int(group),
+            _ptr(w, torch.uint8, n.value, "Wq"))
+        self._check(rc, "quantize_weights_q4")
+        if stream is not None:         # (allocated on the current stream, written on another)
+            w.record_stream(stream)
+        return dict(w=w, group=int(group))
+
+    def draft_logits_q4(self, x, x_rows, Wq, row_seq, blank_bias, out_topk_id, out_topk_lp, out_lse,
+                        out_logits_dbg=None, stream=None):
+        """draft_logits over 4-bit weights (quantize_weights_q4); x_rows None or an int32 row map as for draft_logits_rows."""
+        c = self.cfg
+        R = x.shape[0]
+        M = R if x_rows is None else x_rows.shape[0]
+        i32, f32 = torch.int32, torch.float32
+        rc = self.lib.ctcsd_draft_logits_q4(
+            self._h, _stream_ptr(stream, self._dev), M,
+            _ptr(x, self.act_dtype, R * c.H, "x"), R, _ptr(x_rows, i32, M, "x_rows"), self._q4_weights(Wq), Wq["group"],
+            _ptr(row_seq, i32, M, "row_seq"), _ptr(blank_bias, f32, c.B, "blank_bias"),
+            _ptr(out_topk_id, i32, M * c.T * c.k, "out_topk_id"), _ptr(out_topk_lp, f32, M * c.T * c.k, "out_topk_lp"),
+            _ptr(out_lse, f32, M * c.T, "out_lse"),
+            _ptr(out_logits_dbg, f32, M * c.T * (c.V + 1), "out_logits_dbg"))
+        self._check(rc, "draft_logits_q4")
+
+    def _q4_weights(self, Wq):
+        c, group = self.cfg, Wq["group"]
+        if group not in (32, 64, 128):
+            raise CtcsdError("group must be 32, 64 or 128, got %r" % (group,))
+        return _ptr(Wq["w"], torch.uint8, c.T * ((c.V + 16) // 16) * ((c.H + 127) // 128) * (1024 + 64 * (128 // group)), "Wq")
+
+    def make_q4_cache(self, Lcap):
+        """An empty 4-bit cache of Lcap rows a sequence: levels Kq, Vq [B,Hkv,Lcap,D/2] uint8, (scale, origin) Ks, Vs
+        [B,Hkv,Lcap,D/32,2] bfloat16."""
+        c = self.cfg
+        levels = lambda: torch.zeros(c.B, c.Hkv, Lcap, c.D // 2, dtype=torch.uint8, device=self.device)
+        pairs = lambda: torch.zeros(c.B, c.Hkv, Lcap, c.D // self.Q4_GROUP, 2, dtype=torch.bfloat16, device=self.device)
+        return dict(Kq=levels(), Ks=pairs(), Vq=levels(), Vs=pairs())
+
+    def _q4_cache(self, cache):
+        c = self.cfg
+        Lcap = cache["Kq"].shape[2]
+        rows = c.B * c.Hkv * Lcap
+        return [_ptr(cache["Kq"], torch.uint8, rows * (c.D // 2), "Kq"),
+                _ptr(cache["Ks"], torch.bfloat16, rows * (c.D // self.Q4_GROUP) * 2, "Ks"),
+                _ptr(cache["Vq"], torch.uint8, rows * (c.D // 2), "Vq"),
+                _ptr(cache["Vs"], torch.bfloat16, rows * (c.D // self.Q4_GROUP) * 2, "Vs")], Lcap
+
+    def store_rows_q4(self, cache, K, V, n_rows, at=None, stream=None):
+        """The first n_rows[b] rows of K, V [B,Hkv,Lsrc,D] to rows at[b].. of the cache (at None: from 0)."""
+        c = self.cfg
+        i32 = torch.int32
+        Lsrc = K.shape[2]
+        ptrs, Lcap = self._q4_cache(cache)
+        n = c.B * c.Hkv * Lsrc * c.D
+        rc = self.lib.ctcsd_store_rows_q4(
+            self._h, _stream_ptr(stream, self._dev), _ptr(K, self.act_dtype, n, "K"), _ptr(V, self.act_dtype, n, "V"), Lsrc,
+            _ptr(n_rows, i32, c.B, "n_rows"), _ptr(at, i32, c.B, "at"), *ptrs, Lcap)
+        self._check(rc, "store_rows_q4")
+
+    def load_rows_q4(self, cache, first, n_rows, out_K, out_V, stream=None):
+        """Cache rows first[b] .. first[b]+n_rows[b]-1 as values to out_K, out_V [B,Hkv,Lout,D], zeros behind them."""
+        c = self.cfg
+        i32 = torch.int32
+        Lout = out_K.shape[2]
+        ptrs, Lcap = self._q4_cache(cache)
+        n = c.B * c.Hkv * Lout * c.D
+        rc = self.lib.ctcsd_load_rows_q4(
+            self._h, _stream_ptr(stream, self._dev), *ptrs, Lcap, _ptr(first, i32, c.B, "first"), _ptr(n_rows, i32, c.B, "n_rows"),
+            _ptr(out_K, self.act_dtype, n, "out_K"), _ptr(out_V, self.act_dtype, n, "out_V"), Lout)
+        self._check(rc, "load_rows_q4")
+
+    def commit_accepted_q4(self, Kt, Vt, cache, kv_len, acc_len, acc_nodes, out_kv_len, out_sel_row=None, stream=None):
+        """commit_accepted for a 4-bit cache: the accepted rows of Kt, Vt [B,Hkv,max_nodes,D] join it."""
+        c = self.cfg
+        i32 = torch.int32
+        ptrs, Lcap = self._q4_cache(cache)
+        n = c.B * c.Hkv * c.max_nodes * c.D
+        rc = self.lib.ctcsd_commit_accepted_q4(
+            self._h, _stream_ptr(stream, self._dev), _ptr(Kt, self.act_dtype, n, "Kt"), _ptr(Vt, self.act_dtype, n, "Vt"), *ptrs, Lcap,
+            _ptr(kv_len, i32, c.B, "kv_len"), _ptr(acc_len, i32, c.B, "acc_len"), _ptr(acc_nodes, i32, c.B * c.T, "acc_nodes"),
+            _ptr(out_kv_len, i32, c.B, "out_kv_len"), _ptr(out_sel_row, i32, c.B, "out_sel_row"))
+        self._check(rc, "commit_accepted_q4")
+
+    def make_q4_attention(self):
+        """Allocates the workspace tree_attention_q4 needs."""
+        n = ctypes.c_size_t(0)
+        self._check(self.lib.ctcsd_tree_attention_q4_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(n)),
+                    "tree_attention_q4_workspace_bytes")
+        ws = torch.empty(n.value + 256, dtype=torch.uint8, device=self.device)
+        return dict(ws=ws, ws_ptr=(ws.data_ptr() + 255) // 256 * 256, ws_bytes=n.value)
+
+    def tree_attention_q4(self, qa, Q, cache, Kt, Vt, kv_len, n_nodes, mask, scale, out_O, out_lse=None, stream=None):
+        """Tree attention over a 4-bit cache; the tree's own keys and values in Kt, Vt [B,Hkv,max_nodes,D]."""
+        c = self.cfg
+        i32, act = torch.int32, self.act_dtype
+        W = (c.max_nodes + 63) // 64
+        rows = c.B * c.max_nodes * c.Hq
+        tree = c.B * c.Hkv * c.max_nodes * c.D
+        ptrs, Lcap = self._q4_cache(cache)
+        rc = self.lib.ctcsd_tree_attention_q4(
+            self._h, _stream_ptr(stream, self._dev), qa["ws_ptr"], qa["ws_bytes"], _ptr(Q, act, rows * c.D, "Q"), *ptrs, Lcap,
+            _ptr(Kt, act, tree, "Kt"), _ptr(Vt, act, tree, "Vt"), _ptr(kv_len, i32, c.B, "kv_len"), _ptr(n_nodes, i32, c.B, "n_nodes"),
+            _ptr(mask, torch.int64, c.B * c.max_nodes * W, "mask"), float(scale),
+            _ptr(out_O, act, rows * c.D, "out_O"), _ptr(out_lse, torch.float32, rows, "out_lse"))
+        self._check(rc, "tree_attention_q4")
 
 
 def tree_attention_static(Q, K, V, kv_len, n_nodes, mask, scale, out_O, out_status=None, stream=None):

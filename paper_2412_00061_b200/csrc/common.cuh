@@ -76,7 +76,8 @@ struct DeviceGuard {
     DeviceGuard& operator=(const DeviceGuard&) = delete;
 };
 
-enum { kPrepSharedTc = 1, kPrepSharedSimple = 2, kPrepMassTc = 4, kPrepMassF32 = 8, kPrepEvict = 16, kPrepEvictAlone = 32 };
+enum { kPrepSharedTc = 1, kPrepSharedSimple = 2, kPrepMassTc = 4, kPrepMassF32 = 8, kPrepEvict = 16, kPrepEvictAlone = 32,
+       kPrepDraftQ4 = 64, kPrepDraftQ4x2 = 128, kPrepDraftQ4F32 = 256, kPrepAttnQ4Simple = 512, kPrepAttnQ4Mma = 1024, kPrepAttnQ4Tc = 2048 };
 constexpr int kMaxDynamicSmem = 227 * 1024;
 
 // Lets `kernel` (no static shared memory) use all of an SM's shared memory; the limit is the same for every caller, so once per

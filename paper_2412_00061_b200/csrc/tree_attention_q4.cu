@@ -1,0 +1,405 @@
+// ctcsd_tree_attention_q4: tree attention over a cache held in 4 bits.
+//   O[b,i,h] = sum_j p_j v_j,  p = softmax_j(scale q.k_j),  j over the kv_len[b] cached rows (4 bits, q4.cuh) and the tree rows of
+//   node i's mask (full precision);  lse[b,i,h] = log sum_j exp(scale q.k_j).
+// The work is divided as q4_attention.cuh describes.  This file holds the entry points, the kernel without tensor cores (float32)
+// and the merge of tiles that were cut.
+#include "q4_attention.cuh"
+
+#include <math.h>
+
+namespace ctcsd {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// ---------------------------------------------------------------------------------------
+// Without tensor cores: 64 rows x 64 keys per step, 256 threads; a thread computes 4 x 4 scores and 4 x D/16 outputs from 128-bit
+// shared loads, rows and keys dealt 16 apart (row stride D + 4: no bank conflicts).  Levels become float32 values on the way
+// into shared memory.
+// ---------------------------------------------------------------------------------------
+constexpr int kSimpleThreads = 256;
+
+template <bool B> struct Flag { static constexpr bool value = B; };
+
+template <typename T> __device__ __forceinline__ float4 load4(const T* p);
+template <> __device__ __forceinline__ float4 load4<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
+template <> __device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16* p) {
+    const uint2 w = *reinterpret_cast<const uint2*>(p);
+    return make_float4(bf16lo(w.x), bf16hi(w.x), bf16lo(w.y), bf16hi(w.y));
+}
+template <typename T> __device__ __forceinline__ void store4(T* p, float4 v);
+template <> __device__ __forceinline__ void store4<float>(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* p, float4 v) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+template <typename T> __device__ __forceinline__ void values8(uint32_t w, uint32_t so, float (&v)[8]);
+template <> __device__ __forceinline__ void values8<float>(uint32_t w, uint32_t so, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = q4_value_f32(w, i, bf16lo(so), bf16hi(so));
+}
+template <> __device__ __forceinline__ void values8<__nv_bfloat16>(uint32_t w, uint32_t so, float (&v)[8]) {
+    const uint4 u = q4_values_bf16(w, so);
+    v[0] = bf16lo(u.x); v[1] = bf16hi(u.x); v[2] = bf16lo(u.y); v[3] = bf16hi(u.y);
+    v[4] = bf16lo(u.z); v[5] = bf16hi(u.z); v[6] = bf16lo(u.w); v[7] = bf16hi(u.w);
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kSimpleThreads, kAq4SimplePerSm) attention_q4_simple_kernel(AttnQ4Params p) {
+    constexpr int TR = kAq4SimpleRows, KB = kAq4SimpleKeys, ST = D + 4, PS = KB + 4, DC = D / 64, W = D / 8;
+    extern __shared__ __align__(16) float sm[];
+    float* Qs = sm;                      // [TR][ST]
+    float* Ts = Qs + TR * ST;            // [KB][ST]: a K block, then its V block
+    float* Ps = Ts + KB * ST;            // [TR][PS]
+    PlanQ4 pl;
+    pl.carve(reinterpret_cast<int*>(Ps + TR * PS), p.B);
+    pdl_wait();
+    pdl_trigger();
+    const SpansQ4 sp = plan_q4_build(pl, p, TR, KB, (int)gridDim.x);
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    const int MW = (p.max_nodes + 63) / 64;
+    const float sl2 = p.scale * kLog2e;
+    WalkQ4 at;
+    for (bool more = at.init(pl, sp, p.B, KB, blockIdx.x); more; more = at.next(pl, p.B, KB)) {
+        const int g = at.g, b = at.b, kv = pl.kv[b], n = pl.n[b], row0 = at.t * TR;
+        const int nrows = n * p.grp - row0 < TR ? n * p.grp - row0 : TR;
+        const size_t pair = (size_t)b * p.Hkv + g;
+        auto out_row = [&](int r) -> size_t {                                // row of the tile -> row of Q, O, lse
+            const int node = (row0 + r) / p.grp;
+            return ((size_t)b * p.max_nodes + node) * p.Hq + g * p.grp + (row0 + r - node * p.grp);
+        };
+        __syncthreads();                 // the previous tile's shared memory is free
+        for (int i = tid; i < TR * (D / 4); i += kSimpleThreads) {
+            const int r = i / (D / 4), c = i - r * (D / 4);
+            *reinterpret_cast<float4*>(Qs + r * ST + 4 * c) =
+                r < nrows ? load4(static_cast<const T*>(p.Q) + out_row(r) * D + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        float acc[4][4 * DC], ref[4], sum[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            ref[i] = -INFINITY; sum[i] = 0.f;
+#pragma unroll
+            for (int d = 0; d < 4 * DC; ++d) acc[i][d] = 0.f;
+        }
+        // keys key0 .. key0+nkey-1 of the cache (or of the tree) as values, zeros behind them
+        auto load_tile = [&](const uint32_t* q, const uint32_t* so, const void* tree, bool cached, int key0, int nkey) {
+            for (int i = tid; i < KB * W; i += kSimpleThreads) {
+                const int k = i / W, c = i - k * W;
+                float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                if (k < nkey) {
+                    if (cached) {
+                        const size_t a = (pair * p.Lcap + key0 + k) * W + c;
+                        values8<T>(q[a], so[a >> 2], v);
+                    } else {
+                        load8(static_cast<const T*>(tree) + ((pair * p.max_nodes + key0 + k) * W + c) * 8, v);
+                    }
+                }
+                float* dst = Ts + k * ST + 8 * c;
+                reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
+            }
+        };
+        for (int blk = at.blk0; blk < at.blk1; ++blk) {
+            const bool cached = blk < at.cached;
+            const int key0 = (cached ? blk : blk - at.cached) * KB, len = cached ? kv : n;
+            const int nkey = len - key0 < KB ? len - key0 : KB;
+            __syncthreads();             // V of the previous block has been read
+            load_tile(p.Kq, p.Ks, p.Kt, cached, key0, nkey);
+            __syncthreads();
+            float s[4][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+            for (int d = 0; d < D; d += 4) {
+                float4 q4[4], k4[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q4[i] = *reinterpret_cast<const float4*>(Qs + (ty + 16 * i) * ST + d);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) k4[j] = *reinterpret_cast<const float4*>(Ts + (tx + 16 * j) * ST + d);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s[i][j] = fmaf(q4[i].x, k4[j].x, s[i][j]);
+                        s[i][j] = fmaf(q4[i].y, k4[j].y, s[i][j]);
+                        s[i][j] = fmaf(q4[i].z, k4[j].z, s[i][j]);
+                        s[i][j] = fmaf(q4[i].w, k4[j].w, s[i][j]);
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = ty + 16 * i;
+                uint32_t lo = 0u, hi = 0u;                                   // keys of the block that the row sees
+                if (r < nrows) {
+                    if (cached) {
+                        lo = nkey >= 32 ? 0xffffffffu : (1u << nkey) - 1u;
+                        hi = nkey >= 64 ? 0xffffffffu : (nkey > 32 ? (1u << (nkey - 32)) - 1u : 0u);
+                    } else {
+                        const unsigned long long* mrow = p.mask + ((size_t)b * p.max_nodes + (row0 + r) / p.grp) * MW;
+                        lo = tree_bits32(mrow, MW, key0, n);
+                        hi = tree_bits32(mrow, MW, key0 + 32, n);
+                    }
+                }
+                // masked scores become -inf by selection, so a NaN there does not count
+                float bm = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int k = tx + 16 * j;
+                    const bool vis = ((k < 32 ? lo >> k : hi >> (k - 32)) & 1u) != 0u;
+                    s[i][j] = vis ? s[i][j] * sl2 : -INFINITY;
+                    bm = fmaxf(bm, s[i][j]);
+                }
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, o));
+                const float nref = fmaxf(ref[i], bm);
+                const float base = nref == -INFINITY ? 0.f : nref;
+                const float corr = exp2_q4(ref[i] - base);                   // 2^(-inf) = 0 before the first key
+                ref[i] = nref;
+                float ps = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float e = exp2_q4(s[i][j] - base);
+                    ps += e;
+                    Ps[r * PS + tx + 16 * j] = e;
+                }
+                sum[i] = sum[i] * corr + ps;
+#pragma unroll
+                for (int d = 0; d < 4 * DC; ++d) acc[i][d] *= corr;
+            }
+            __syncthreads();             // K has been read, P is complete
+            load_tile(p.Vq, p.Vs, p.Vt, cached, key0, nkey);
+            __syncthreads();
+            // Every row of the tile sees every cached row; of the tree's rows it sees some, and a weight of zero must not meet a NaN or an
+            // infinity there: such products are left out.
+            auto pv = [&](auto guarded) {
+#pragma unroll 2
+                for (int k = 0; k < KB; k += 4) {
+                    float4 p4[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p4[i] = *reinterpret_cast<const float4*>(Ps + (ty + 16 * i) * PS + k);
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+                        for (int c = 0; c < DC; ++c) {
+                            const float4 v = *reinterpret_cast<const float4*>(Ts + (k + kk) * ST + 64 * c + 4 * tx);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float w = kk == 0 ? p4[i].x : (kk == 1 ? p4[i].y : (kk == 2 ? p4[i].z : p4[i].w));
+                                if (!decltype(guarded)::value || w != 0.f) {
+                                    acc[i][4 * c + 0] = fmaf(w, v.x, acc[i][4 * c + 0]);
+                                    acc[i][4 * c + 1] = fmaf(w, v.y, acc[i][4 * c + 1]);
+                                    acc[i][4 * c + 2] = fmaf(w, v.z, acc[i][4 * c + 2]);
+                                    acc[i][4 * c + 3] = fmaf(w, v.w, acc[i][4 * c + 3]);
+                                }
+                            }
+                        }
+                }
+            };
+            if (cached) pv(Flag<false>()); else pv(Flag<true>());
+        }
+        const bool whole = at.whole();
+        const size_t part = (size_t)blockIdx.x * 2 + at.slot();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float s = sum[i];
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            const int r = ty + 16 * i;
+            if (r >= nrows) continue;
+            if (whole) {
+                const size_t orow = out_row(r);
+                if (!CTCSD_IN_BOUNDS(p.status, 132, orow, out_rows(p))) continue;
+                const float inv = s > 0.f ? 1.f / s : (s == 0.f ? 0.f : s);  // a NaN sum stays a NaN
+                T* out = static_cast<T*>(p.O) + orow * D;
+#pragma unroll
+                for (int c = 0; c < DC; ++c)
+                    store4(out + 64 * c + 4 * tx, make_float4(acc[i][4 * c] * inv, acc[i][4 * c + 1] * inv, acc[i][4 * c + 2] * inv, acc[i][4 * c + 3] * inv));
+                if (tx == 0 && p.lse) p.lse[orow] = s == 0.f ? -INFINITY : (ref[i] + log2f(s)) * kLn2;
+            } else if (CTCSD_IN_BOUNDS(p.status, 133, part * TR + r, 2ll * gridDim.x * TR)) {
+#pragma unroll
+                for (int c = 0; c < DC; ++c)
+                    p.part_o[(part * (D / 4) + 16 * c + tx) * TR + r] = make_float4(acc[i][4 * c], acc[i][4 * c + 1], acc[i][4 * c + 2], acc[i][4 * c + 3]);
+                if (tx == 0) p.part_ml[part * TR + r] = make_float2(ref[i], s);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Merge.  A block looks after 32 rows (lane = row, so that the transposed parts are read in whole lines; warps share the head
+// dimension) of a (kv head, sequence): rows of unused nodes become zero, rows of tiles that were cut are joined in span order,
+// four parts at a time; the result does not depend on timing.
+// ---------------------------------------------------------------------------------------
+template <typename T, int D>
+__global__ void __launch_bounds__(D * 4) attention_q4_merge_kernel(AttnQ4Params p, int TR, int KB, unsigned units) {
+    constexpr int U = 4;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;              // a warp: columns 8 warp .. 8 warp + 7
+    pdl_wait();
+    pdl_trigger();
+    const int per_head = p.plan[0], spans = p.plan[1];
+    const int* blk_off = p.plan + kAq4Header;
+    const SpansQ4 sp = spans_of(per_head, p.Hkv, spans);
+    const int seq_rows = p.max_nodes * p.grp;
+    const unsigned chunks = (unsigned)(seq_rows + 31) / 32u;
+    for (unsigned u = blockIdx.x; u < units; u += gridDim.x) {
+        const unsigned pairi = u / chunks;
+        const int r = (int)(u - pairi * chunks) * 32 + lane;                 // row of the sequence
+        const int b = (int)(pairi / (unsigned)p.Hkv), g = (int)(pairi - (unsigned)b * (unsigned)p.Hkv);
+        if (r >= seq_rows) continue;
+        const int off = blk_off[b], blocks = blk_off[b + 1] - off;
+        const int n = blocks > 0 ? p.n_nodes[b] : 0;
+        const int node = r / p.grp;
+        const size_t orow = ((size_t)b * p.max_nodes + node) * p.Hq + g * p.grp + (r - node * p.grp);
+        if (!CTCSD_IN_BOUNDS(p.status, 134, orow, out_rows(p))) continue;
+        T* out = static_cast<T*>(p.O) + orow * D + 8 * warp;
+        if (node >= n) {
+            store4(out, make_float4(0.f, 0.f, 0.f, 0.f));
+            store4(out + 4, make_float4(0.f, 0.f, 0.f, 0.f));
+            if (warp == 0 && p.lse) p.lse[orow] = -INFINITY;
+            continue;
+        }
+        const int tiles = (n * p.grp + TR - 1) / TR, nblk = blocks / tiles, t = r / TR, tr = r - t * TR;
+        const long long x0 = (long long)g * per_head + off + t * nblk;
+        const int c0 = sp.span_of(x0), c1 = sp.span_of(x0 + nblk - 1);
+        if (c0 == c1) continue;                                              // finished by its span
+        // only the first part can be one that a span begins (slot 1); the others continue a tile (slot 0)
+        float ref = -INFINITY, sum = 0.f, a[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] = 0.f;
+        for (int c = c0; c <= c1; c += U) {
+            float2 ml[U];
+            float4 o[U][2];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {                                    // (the last part again past the end, with no weight)
+                const int cc = min(c + i, c1);
+                // (a span whose cut falls on the tile's first block holds it as a tile it begins)
+                const size_t part = (size_t)cc * 2 + (cc == c0 ? 1 : 0);
+                ml[i] = p.part_ml[part * TR + tr];
+                o[i][0] = p.part_o[(part * (D / 4) + 2 * warp) * TR + tr];
+                o[i][1] = p.part_o[(part * (D / 4) + 2 * warp + 1) * TR + tr];
+                if (c + i > c1) ml[i] = make_float2(-INFINITY, 0.f);
+            }
+            float top = ref;
+#pragma unroll
+            for (int i = 0; i < U; ++i) top = fmaxf(top, ml[i].x);
+            const float base = top == -INFINITY ? 0.f : top;
+            const float keep = exp2_q4(ref - base);
+            sum *= keep;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[e] *= keep;
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const float w = exp2_q4(ml[i].x - base);
+                sum = fmaf(w, ml[i].y, sum);
+                if (!(ml[i].y != 0.f)) continue;                             // this part saw nothing
+                a[0] = fmaf(w, o[i][0].x, a[0]); a[1] = fmaf(w, o[i][0].y, a[1]);
+                a[2] = fmaf(w, o[i][0].z, a[2]); a[3] = fmaf(w, o[i][0].w, a[3]);
+                a[4] = fmaf(w, o[i][1].x, a[4]); a[5] = fmaf(w, o[i][1].y, a[5]);
+                a[6] = fmaf(w, o[i][1].z, a[6]); a[7] = fmaf(w, o[i][1].w, a[7]);
+            }
+            ref = top;
+        }
+        const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
+        store4(out, make_float4(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv));
+        store4(out + 4, make_float4(a[4] * inv, a[5] * inv, a[6] * inv, a[7] * inv));
+        if (warp == 0 && p.lse) p.lse[orow] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+    }
+}
+
+template <typename T, int D>
+int launch_merge(Handle* h, cudaStream_t s, const AttnQ4Params& p, int TR, int KB) {
+    const long long units = (long long)p.B * p.Hkv * ((p.max_nodes * p.grp + 31) / 32);
+    const long long cap = (long long)h->num_sms * 16;
+    CTCSD_CUDA_CHECK(h, launch_pdl(attention_q4_merge_kernel<T, D>, dim3((unsigned)(units < cap ? units : cap)), dim3(D * 4), 0, s, 1, p, TR, KB,
+                                   (unsigned)units));
+    h->launches++;
+    return CTCSD_OK;
+}
+
+template <typename T, int D>
+int launch_simple(Handle* h, cudaStream_t s, const AttnQ4Params& p) {
+    constexpr int TR = kAq4SimpleRows, KB = kAq4SimpleKeys;
+    const size_t smem = sizeof(float) * (TR * (D + 4) + KB * (D + 4) + TR * (KB + 4)) + sizeof(int) * PlanQ4::ints(p.B);
+    auto kern = attention_q4_simple_kernel<T, D>;
+    CTCSD_CUDA_CHECK(h, prepare_kernel(h, kPrepAttnQ4Simple, kern));
+    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(h->num_sms * kAq4SimplePerSm), dim3(kSimpleThreads), smem, s, 1, p));
+    h->launches++;
+    return CTCSD_OK;
+}
+
+// Which kernel serves a handle: its tile, block and largest grid.
+struct Form { int TR, KB, spans; };
+Form form_of(const ctcsd_config&) { return {kAq4SimpleRows, kAq4SimpleKeys, kLayoutSms * kAq4SimplePerSm}; }
+
+// Workspace: plan, part sums, part outputs.
+struct AttnLayout { size_t plan, ml, o, total; };
+AttnLayout attn_layout(const ctcsd_config& c) {
+    const Form f = form_of(c);
+    AttnLayout l;
+    l.plan = 0;
+    l.ml = align_up(sizeof(int) * (size_t)(kAq4Header + c.B + 1), 256);
+    l.o = align_up(l.ml + sizeof(float2) * f.spans * 2 * f.TR, 256);
+    l.total = align_up(l.o + sizeof(float) * f.spans * 2 * f.TR * (size_t)c.D, 256);
+    return l;
+}
+
+bool attn_supported(const ctcsd_config& c) {
+    return c.B <= kAq4MaxB && (long long)c.B * c.Hkv * ((c.max_nodes * (c.Hq / c.Hkv) + 31) / 32) < (1ll << 31);
+}
+
+}  // namespace
+}  // namespace ctcsd
+
+using namespace ctcsd;
+
+extern "C" int ctcsd_tree_attention_q4_workspace_bytes(const ctcsd_config* cfg, size_t* out_bytes) {
+    if (!cfg || !out_bytes) return CTCSD_ERR_INVALID_ARG;
+    const int rc = validate_config(*cfg);
+    if (rc != CTCSD_OK) return rc;
+    if (!attn_supported(*cfg)) return CTCSD_ERR_UNSUPPORTED;
+    *out_bytes = attn_layout(*cfg).total;
+    return CTCSD_OK;
+}
+
+extern "C" int ctcsd_tree_attention_q4(ctcsd_handle* hh, void* stream, void* workspace, size_t workspace_bytes, const void* Q,
+                                       const void* Kq, const void* Ks, const void* Vq, const void* Vs, int Lcap,
+                                       const void* Kt, const void* Vt, const int* kv_len, const int* n_nodes,
+                                       const unsigned long long* mask, float scale, void* out_O, float* out_lse) {
+    if (!hh || !Q || !Kq || !Ks || !Vq || !Vs || !Kt || !Vt || !kv_len || !n_nodes || !mask || !out_O) return CTCSD_ERR_INVALID_ARG;
+    Handle* h = &hh->h;
+    const ctcsd_config& c = h->cfg;
+    if (!attn_supported(c)) return CTCSD_ERR_UNSUPPORTED;
+    if (Lcap < 1 || !(scale > 0.f) || isinf(scale)) return CTCSD_ERR_INVALID_ARG;            // the row maximum is taken before scaling
+    const uintptr_t all = reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(Kq) | reinterpret_cast<uintptr_t>(Ks) |
+                          reinterpret_cast<uintptr_t>(Vq) | reinterpret_cast<uintptr_t>(Vs) | reinterpret_cast<uintptr_t>(Kt) |
+                          reinterpret_cast<uintptr_t>(Vt) | reinterpret_cast<uintptr_t>(out_O);
+    if (all & 15) return CTCSD_ERR_INVALID_ARG;
+    const Form f = form_of(c);
+    const int grp = c.Hq / c.Hkv;
+    if (!plan_q4_fits(c.B, c.max_nodes, grp, f.TR, f.KB, Lcap)) return CTCSD_ERR_UNSUPPORTED;
+    const AttnLayout l = attn_layout(c);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < l.total) return CTCSD_ERR_WORKSPACE;
+    AttnQ4Params p;
+    p.Q = Q; p.O = out_O; p.lse = out_lse; p.Kt = Kt; p.Vt = Vt;
+    p.Kq = static_cast<const uint32_t*>(Kq); p.Ks = static_cast<const uint32_t*>(Ks);
+    p.Vq = static_cast<const uint32_t*>(Vq); p.Vs = static_cast<const uint32_t*>(Vs);
+    p.kv_len = kv_len; p.n_nodes = n_nodes; p.mask = mask;
+    p.B = c.B; p.Hq = c.Hq; p.Hkv = c.Hkv; p.max_nodes = c.max_nodes; p.Lcap = Lcap; p.grp = grp;
+    p.scale = scale;
+    p.status = status_ptr(h);
+    char* ws = static_cast<char*>(workspace);
+    p.plan = reinterpret_cast<int*>(ws + l.plan);
+    p.part_ml = reinterpret_cast<float2*>(ws + l.ml);
+    p.part_o = reinterpret_cast<float4*>(ws + l.o);
+    const DeviceGuard on(h->device);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int rc;
+    if (c.dtype == CTCSD_DTYPE_BF16) rc = c.D == 64 ? launch_simple<__nv_bfloat16, 64>(h, s, p) : launch_simple<__nv_bfloat16, 128>(h, s, p);
+    else rc = c.D == 64 ? launch_simple<float, 64>(h, s, p) : launch_simple<float, 128>(h, s, p);
+    if (rc != CTCSD_OK) return rc;
+    if (c.dtype == CTCSD_DTYPE_BF16) return c.D == 64 ? launch_merge<__nv_bfloat16, 64>(h, s, p, f.TR, f.KB) : launch_merge<__nv_bfloat16, 128>(h, s, p, f.TR, f.KB);
+    return c.D == 64 ? launch_merge<float, 64>(h, s, p, f.TR, f.KB) : launch_merge<float, 128>(h, s, p, f.TR, f.KB);
+}
