@@ -21,7 +21,7 @@ struct AttnQ4Params {
     float* lse;                          // [B,max_nodes,Hq] or null
     const int* kv_len; const int* n_nodes;     // [B]
     const unsigned long long* mask;      // [B,max_nodes,ceil(max_nodes/64)]
-    int B, Hq, Hkv, max_nodes, Lcap, grp;      // grp = Hq / Hkv
+    int B, Hq, Hkv, D, max_nodes, Lcap, grp;      // grp = Hq / Hkv
     float scale;
     int* status;
     int* plan;                           // workspace: header, blk_off (written by CTA 0, read by the merge)
@@ -33,7 +33,6 @@ constexpr int kAq4MaxB = 1024;
 constexpr int kAq4Header = 4;            // ints: blocks per kv head, spans
 constexpr int kAq4SimpleRows = 64, kAq4SimpleKeys = 64, kAq4SimplePerSm = 2;
 constexpr int kAq4MmaRows = 16, kAq4MmaKeys = 128;
-constexpr int kAq4TcRows = 128, kAq4TcKeys = 128;
 
 // The plan in shared memory.
 struct PlanQ4 {
@@ -183,7 +182,7 @@ __device__ __forceinline__ long long out_rows(const AttnQ4Params& a) { return (l
 
 #endif  // __CUDACC__
 
+// bf16, up to 16 query rows of a kv head.
 int launch_attention_q4_mma(Handle* h, cudaStream_t s, const AttnQ4Params& p);
-int launch_attention_q4_tc(Handle* h, cudaStream_t s, const AttnQ4Params& p);
 
 }  // namespace ctcsd

@@ -330,9 +330,14 @@ int launch_simple(Handle* h, cudaStream_t s, const AttnQ4Params& p) {
     return CTCSD_OK;
 }
 
+bool few_rows(const ctcsd_config& c) { return c.dtype == CTCSD_DTYPE_BF16 && c.max_nodes * (c.Hq / c.Hkv) <= kAq4MmaRows; }
+
 // Which kernel serves a handle: its tile, block and largest grid.
 struct Form { int TR, KB, spans; };
-Form form_of(const ctcsd_config&) { return {kAq4SimpleRows, kAq4SimpleKeys, kLayoutSms * kAq4SimplePerSm}; }
+Form form_of(const ctcsd_config& c) {
+    if (few_rows(c)) return {kAq4MmaRows, kAq4MmaKeys, kLayoutSms};
+    return {kAq4SimpleRows, kAq4SimpleKeys, kLayoutSms * kAq4SimplePerSm};
+}
 
 // Workspace: plan, part sums, part outputs.
 struct AttnLayout { size_t plan, ml, o, total; };
@@ -387,7 +392,7 @@ extern "C" int ctcsd_tree_attention_q4(ctcsd_handle* hh, void* stream, void* wor
     p.Kq = static_cast<const uint32_t*>(Kq); p.Ks = static_cast<const uint32_t*>(Ks);
     p.Vq = static_cast<const uint32_t*>(Vq); p.Vs = static_cast<const uint32_t*>(Vs);
     p.kv_len = kv_len; p.n_nodes = n_nodes; p.mask = mask;
-    p.B = c.B; p.Hq = c.Hq; p.Hkv = c.Hkv; p.max_nodes = c.max_nodes; p.Lcap = Lcap; p.grp = grp;
+    p.B = c.B; p.Hq = c.Hq; p.Hkv = c.Hkv; p.D = c.D; p.max_nodes = c.max_nodes; p.Lcap = Lcap; p.grp = grp;
     p.scale = scale;
     p.status = status_ptr(h);
     char* ws = static_cast<char*>(workspace);
@@ -397,7 +402,8 @@ extern "C" int ctcsd_tree_attention_q4(ctcsd_handle* hh, void* stream, void* wor
     const DeviceGuard on(h->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     int rc;
-    if (c.dtype == CTCSD_DTYPE_BF16) rc = c.D == 64 ? launch_simple<__nv_bfloat16, 64>(h, s, p) : launch_simple<__nv_bfloat16, 128>(h, s, p);
+    if (few_rows(c)) rc = launch_attention_q4_mma(h, s, p);
+    else if (c.dtype == CTCSD_DTYPE_BF16) rc = c.D == 64 ? launch_simple<__nv_bfloat16, 64>(h, s, p) : launch_simple<__nv_bfloat16, 128>(h, s, p);
     else rc = c.D == 64 ? launch_simple<float, 64>(h, s, p) : launch_simple<float, 128>(h, s, p);
     if (rc != CTCSD_OK) return rc;
     if (c.dtype == CTCSD_DTYPE_BF16) return c.D == 64 ? launch_merge<__nv_bfloat16, 64>(h, s, p, f.TR, f.KB) : launch_merge<__nv_bfloat16, 128>(h, s, p, f.TR, f.KB);
