@@ -373,7 +373,8 @@ int ctcsd_evict_rows(ctcsd_handle* h, void* stream, void* workspace, size_t work
  * Format.  A row of n values is cut into groups; a group keeps two bfloat16 numbers, scale and origin (one 32-bit word, scale in
  * the low half), and level q = 0..15 stands for
  *   round( origin + scale * (16 + q) ),  rounded once, to the handle's dtype.
- * Eight consecutive values share a 32-bit word: value 2i at bits 4i..4i+3, value 2i+1 at bits 16+4i..19+4i.
+ * Eight consecutive values 0..7 share a 32-bit word: the levels of 0, 1, 2, 3, 4, 5, 7 begin at bits 3, 19, 7, 23, 11, 27, 15, and that of 6
+ * has its lowest bit at bit 31 and the others at bits 0..2.
  * Quantising, every step rounded to float32 (lo, hi: least and largest value of the group):
  *   scale = bfloat16((hi - lo) / 15);  origin = bfloat16(lo - 16 scale);
  *   q = (v - origin) / scale - 16, rounded half to even and clamped to 0..15;  0 where scale = 0.
@@ -390,7 +391,8 @@ int ctcsd_evict_rows(ctcsd_handle* h, void* stream, void* workspace, size_t work
  *   outside 0..x_row_count-1 records CTCSD_ERR_INVALID_ARG in the device status word and that row drafts from a zero vector);
  * Wq, group as for the call above, not written by any kernel while the call runs or directly before it (ctcsd_quantize_weights_q4
  *   itself may precede it);  everything else as for ctcsd_draft_logits.
- * Needs H <= 10240 (else CTCSD_ERR_UNSUPPORTED).  The weights are read once per 16 rows (8 where H > 4096; float32: 4).
+ * The weights are read once per 16 rows (float32: 4), of long rows once per as many as fit into shared memory (8 at H = 8192); a single row fits
+ * * up to H = 65536, float32: 32768 (beyond that CTCSD_ERR_UNSUPPORTED).
  */
 int ctcsd_weights_q4_bytes(const ctcsd_config* cfg, int group, size_t* out_bytes);
 int ctcsd_quantize_weights_q4(ctcsd_handle* h, void* stream, const void* Wd, int group, void* out_Wq);

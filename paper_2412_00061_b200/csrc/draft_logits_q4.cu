@@ -18,11 +18,8 @@
 namespace ctcsd {
 namespace {
 
-constexpr int kWarps = 8;                // warps that multiply: they share a panel's blocks
 constexpr int kPanel = 16;               // classes of a panel
 constexpr int kBlock = 128;              // hidden elements of a block
-constexpr int kMaxSlots = 16;            // ring slots
-constexpr int kDepth = 4;                // panels whose partial sums are on their way to the epilogue
 
 __host__ __device__ inline int block_bytes(int group) { return 1024 + kPanel * 4 * (kBlock / group); }
 
@@ -78,11 +75,9 @@ struct DraftQ4Params {
     int m0, mcount;                      // rows of this pass
     int H, classes, panels, blocks, group;   // panels per draft slot, blocks per panel
     int slots;                           // draft slots (T)
-    int piece_blocks, pieces;            // blocks of a piece, pieces of a panel
-    int slot_pieces, nring;              // pieces of a ring slot (whole panels, or a piece of one), ring slots
+    int piece, nring;                    // blocks of a ring slot, ring slots of a warp
     DraftPartial* part;                  // [rows of a pass][grid][2]
-    int* part_slot;                      // [grid][2]
-    unsigned* counter;
+    unsigned* counter;                   // [draft slots], zero between calls
     int k;
     int* out_topk_id;
     float* out_topk_lp;
@@ -91,11 +86,84 @@ struct DraftQ4Params {
     int* status;
 };
 
-struct __align__(8) RingState {
-    uint64_t full[kMaxSlots], empty[kMaxSlots];
-    uint64_t cfull[kDepth], cempty[kDepth];
-    int abort_flag, never_set, is_last;
+// The running state of an activation row in a lane: the k best logits in order, in a list of kTopSlots.
+struct BestQ4 {
+    RunState st;
+    float floor;                         // a logit has to be above it to be among the k best
+    __device__ __forceinline__ void init() { st.init(); floor = -INFINITY; }
+    // (a lane's classes come in rising order: an equal logit ranks behind)
+    __device__ __forceinline__ void push(float z, int v, int k) {
+        if (z > st.mx) {
+            st.sum = st.sum * __expf(st.mx - z) + 1.f;
+            st.mx = z;
+        } else {
+            st.sum += __expf(z - st.mx);
+        }
+        if (z > floor || st.id[0] == INT_MAX) {
+            topk_insert(st.val, st.id, z, v);
+#pragma unroll
+            for (int s = 0; s < kTopSlots; ++s) {
+                float f = st.val[s];
+                asm("" : "+f"(f));       // (else the compiler makes it a look-up by k, and the list leaves the registers)
+                if (s == k - 1) floor = f;
+            }
+        }
+    }
 };
+
+// Unsigned numbers in the order of the floats; 0 for an entry that is not there.
+__device__ __forceinline__ uint32_t rank_of(float v, int id) {
+    if (id == INT_MAX) return 0u;
+    const uint32_t u = __float_as_uint(v);
+    return (u >> 31) ? ~u : u | 0x80000000u;
+}
+// Combines the states of the lanes that differ in the bits of `over` (31: all of the warp; 28: the eight with the same lane % 4): maximum, sum, and
+// the k best (ties to the lower id) in each of them.
+template <int over> __device__ __forceinline__ void combine_best(RunState& st, int k) {
+    float gmx = st.mx;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        if (over & o) gmx = fmaxf(gmx, __shfl_xor_sync(0xffffffffu, gmx, o));
+    st.sum = st.mx == -INFINITY ? 0.f : st.sum * __expf(st.mx - gmx);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        if (over & o) st.sum += __shfl_xor_sync(0xffffffffu, st.sum, o);
+    st.mx = gmx;
+    float ov[kTopSlots];
+    int oi[kTopSlots];
+#pragma unroll
+    for (int r = 0; r < kTopSlots; ++r) {
+        ov[r] = -INFINITY;
+        oi[r] = INT_MAX;
+        if (r < k) {
+            const uint32_t mine = rank_of(st.val[0], st.id[0]);
+            uint32_t top = mine;
+            unsigned id;
+            if constexpr (over == 31) {
+                top = __reduce_max_sync(0xffffffffu, mine);
+                id = __reduce_min_sync(0xffffffffu, mine == top ? (unsigned)st.id[0] : 0x7fffffffu);
+            } else {
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1)
+                    if (over & o) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                id = mine == top ? (unsigned)st.id[0] : 0x7fffffffu;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1)
+                    if (over & o) id = min(id, __shfl_xor_sync(0xffffffffu, id, o));
+            }
+            oi[r] = (int)id;
+            if (top != 0u) ov[r] = __uint_as_float((top >> 31) ? top & 0x7fffffffu : ~top);
+            if ((unsigned)st.id[0] == id && id != 0x7fffffffu) {              // (an id stands in one lane's list only)
+#pragma unroll
+                for (int q = 0; q < kTopSlots - 1; ++q) { st.val[q] = st.val[q + 1]; st.id[q] = st.id[q + 1]; }
+                st.val[kTopSlots - 1] = -INFINITY;
+                st.id[kTopSlots - 1] = INT_MAX;
+            }
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < kTopSlots; ++q) { st.val[q] = ov[q]; st.id[q] = oi[q]; }
+}
 
 // D[16x8] += A[16x16] * B[16x8], bf16 operands, fp32 accumulators (warp-wide).
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -106,44 +174,78 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
 
 constexpr int kF32Rows = 4;              // activation rows of a float32 pass
 constexpr int kF32Chunk = 36;            // floats from one 32-element chunk of x to the next (four lanes read four chunks: no bank conflict)
+constexpr int kMaxRing = 4;              // ring slots of a warp
 
-template <typename T, int NT> struct XShape;
-// bfloat16: fragments of B, [block][tile][word][lane][16 bytes]; float32: [row][chunk][36 floats]
-template <int NT> struct XShape<__nv_bfloat16, NT> {
-    __host__ __device__ static size_t bytes(int blocks) { return (size_t)blocks * NT * 2048; }
+// Bytes of the activation rows of a pass in shared memory.
+//   bfloat16: the lanes' shares of operand B, [block][word][row][chunk t][16 bytes] (a column without a row reads the last row's: its sums are not used);
+//   float32: [row][chunk][36 floats].
+template <typename T> __host__ __device__ inline size_t x_bytes(int blocks, int rows) {
+    return sizeof(T) == 2 ? (size_t)blocks * rows * 256 : (size_t)rows * blocks * 4 * kF32Chunk * 4;
+}
+
+// Warps of a CTA: as many as leave a thread the registers for its states (one of 19 registers per activation row it looks after).
+template <typename T, int NT> struct Shape {
+    static constexpr int warps = NT == 1 ? 16 : 12;
+    static constexpr int states = sizeof(T) == 2 ? 2 * NT : 1;
 };
-template <int NT> struct XShape<float, NT> {
-    __host__ __device__ static size_t bytes(int blocks) { return (size_t)kF32Rows * blocks * 4 * kF32Chunk * 4; }
+
+struct __align__(8) RingState {
+    uint64_t full[16 * kMaxRing];
+    int abort_flag, never_set, merge[2];
 };
 
-template <int NT> struct Threads { static constexpr int value = (kWarps + 1 + 4 * NT) * 32; };
+// A warp's way through the CTA's panels: whole panels in turn with the other warps, and at the end, when fewer panels than warps are left,
+// a share of the blocks of one of those.
+struct PanelWalk {
+    int pan, blk, end;                   // panel, next block of it and the block behind the last
+    bool shared;                         // this is a share
+    int npan, whole, per, warps, warp, blocks;   // panels; panels that warps take whole; warps to a panel of the rest
+    __device__ __forceinline__ void init(int npan_, int warps_, int warp_, int blocks_) {
+        npan = npan_; warps = warps_; warp = warp_; blocks = blocks_;
+        whole = npan / warps * warps;
+        per = whole < npan ? warps / (npan - whole) : 1;
+        pan = warp; blk = 0; end = blocks; shared = false;
+        if (pan >= whole) share();
+    }
+    __device__ __forceinline__ void share() {
+        shared = true;
+        const int i = warp / per, j = warp - i * per;
+        pan = whole + i;
+        blk = blocks * j / per;
+        end = blocks * (j + 1) / per;
+        if (pan >= npan) end = blk;      // (nothing left for this warp)
+    }
+    __device__ __forceinline__ bool done() const { return shared && blk >= end; }
+    __device__ __forceinline__ void next_panel() {           // after the last block of a whole panel
+        pan += warps;
+        blk = 0;
+        if (pan >= whole) share();
+    }
+};
 
-// One CTA per SM with a contiguous range of panels.  Warp 8 streams them through a ring in shared memory with the bulk-copy engine.  Warps
-// 0..7 share the blocks of every panel: levels to values (one multiply-add for two), values times activations on the tensor
-// cores (bfloat16: 16 classes x 8 rows an instruction; float32: fused multiply-adds); the eight partial sums of a panel
-// go through a small ring to the epilogue warps, a thread per (class of the panel, row), which keep the running maximum, sum of
-// exponentials and best eight.  The CTA that ends last merges all states.
+// One CTA per SM with a contiguous range of panels.  Every warp streams panels of its own through a small ring in shared memory with the
+// bulk-copy engine (its first lane asks for the next piece when a slot has been read): levels to values (one multiply-add for
+// two), values times activations on the tensor cores (bfloat16: 16 classes x 8 rows an instruction; float32: fused
+// multiply-adds), and the lanes that hold a panel's logits keep the running maximum, sum of exponentials and best k.  Warps meet
+// at the end only.  (Sets of 4 or 8 warps that shared a panel and handed partial sums to epilogue warps took 93-113 us
+// at the 7B shape, half of it in hand-overs.)
 template <typename T, int NT>
-__global__ void __launch_bounds__(Threads<NT>::value, 1) draft_q4_kernel(DraftQ4Params p) {
+__global__ void __launch_bounds__(Shape<T, NT>::warps * 32, 1) draft_q4_kernel(DraftQ4Params p) {
     constexpr bool kMma = sizeof(T) == 2;
-    constexpr int kThreads = Threads<NT>::value;
-    constexpr int kRows = 8 * NT;
+    constexpr int kWarps = Shape<T, NT>::warps, kThreads = kWarps * 32, kStates = Shape<T, NT>::states;
+    constexpr int kRows = kMma ? 8 * NT : kF32Rows;
     extern __shared__ __align__(128) unsigned char dyn[];
     unsigned char* xs = dyn;
-    unsigned char* ring = xs + XShape<T, NT>::bytes(p.blocks);
-    const int bb = block_bytes(p.group);
-    const int piece_bytes = p.piece_blocks * bb, slot_bytes = p.slot_pieces * piece_bytes;
-    RingState* sh = reinterpret_cast<RingState*>(ring + (size_t)p.nring * slot_bytes);
-    float* cpart = reinterpret_cast<float*>(sh + 1);                         // [kDepth][kWarps][16][kRows]
-    DraftPartial* s_part = reinterpret_cast<DraftPartial*>(ring);            // [2][16][kRows], over the ring when it has been read
+    unsigned char* ring = xs + x_bytes<T>(p.blocks, p.mcount);
+    const int bb = block_bytes(p.group), slot_bytes = p.piece * bb;
+    RingState* sh = reinterpret_cast<RingState*>(ring + (size_t)kWarps * p.nring * slot_bytes);
+    DraftPartial* s_state = reinterpret_cast<DraftPartial*>(sh + 1);         // [2][warps][kRows]
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     volatile int* abort_flag = &sh->abort_flag;
     if (tid == 0) {
-        for (int s = 0; s < p.nring; ++s) { tc::mbar_init(&sh->full[s], 1); tc::mbar_init(&sh->empty[s], kWarps); }
-        for (int d = 0; d < kDepth; ++d) { tc::mbar_init(&sh->cfull[d], kWarps); tc::mbar_init(&sh->cempty[d], 4 * NT); }
+        for (int s = 0; s < kWarps * p.nring; ++s) tc::mbar_init(&sh->full[s], 1);
         sh->abort_flag = 0;
         sh->never_set = 0;
-        sh->is_last = 0;
         tc::fence_barrier_init();
     }
     __syncthreads();
@@ -153,43 +255,30 @@ __global__ void __launch_bounds__(Threads<NT>::value, 1) draft_q4_kernel(DraftQ4
     const int npan = (int)(p1 - p0);
     const int slot0 = (int)(p0 / p.panels);                                   // draft slot of the first panel
     const int n_seg0 = (int)(((long long)(slot0 + 1) * p.panels < p1 ? (long long)(slot0 + 1) * p.panels : p1) - p0);
-    // the CTA's stream of pieces: blocks piece_blocks * i .. of a panel (its last piece may be shorter)
-    const size_t panel_bytes = (size_t)p.blocks * bb;
-    const int npieces = npan * p.pieces;
-    const int nfill = (npieces + p.slot_pieces - 1) / p.slot_pieces;
-
+    const unsigned char* const W0 = p.W + (size_t)p0 * p.blocks * bb;
     const uint64_t policy = tc::policy_evict_first();
-    int prod_j = 0;
-    bool prod_ok = true;
-    // bytes of the CTA's stream before piece i
-    auto offset_of = [&](int i) -> size_t {
-        const int pan = i / p.pieces;
-        return (size_t)pan * panel_bytes + (size_t)(i - pan * p.pieces) * piece_bytes;
-    };
-    auto issue_fill = [&](int j) -> bool {
-        const int s = j % p.nring;
-        if (!tc::mbar_wait(&sh->empty[s], ((uint32_t)(j / p.nring) & 1u) ^ 1u, abort_flag)) return false;
-        const int i0 = j * p.slot_pieces, i1 = i0 + p.slot_pieces < npieces ? i0 + p.slot_pieces : npieces;
-        const size_t from = offset_of(i0), bytes = offset_of(i1) - from;
-        if (bytes == 0 || bytes > (size_t)slot_bytes || (bytes & 15) != 0) {  // never hand the copy engine a range outside the ring
-            report_error(p.status, CTCSD_ERR_INTERNAL, 41);
-            return false;
+    PanelWalk ahead;                                                          // of what is asked for
+    ahead.init(npan, kWarps, warp, p.blocks);
+    unsigned char* const my_ring = ring + (size_t)warp * p.nring * slot_bytes;
+    uint64_t* const my_full = sh->full + warp * p.nring;
+    // asks for the next piece (nothing where the warp's panels are done); all lanes follow the walk, the first asks
+    auto ask = [&](int s) {
+        if (ahead.done()) return;
+        const int nb = min(p.piece, ahead.end - ahead.blk);
+        if (lane == 0) {
+            const uint32_t bytes = (uint32_t)(nb * bb);
+            tc::mbar_arrive_expect_tx(my_full + s, bytes);
+            tc::bulk_load_1d(my_ring + s * slot_bytes, W0 + ((size_t)ahead.pan * p.blocks + ahead.blk) * bb, bytes, my_full + s, policy);
         }
-        tc::mbar_arrive_expect_tx(&sh->full[s], (uint32_t)bytes);
-        tc::bulk_load_1d(ring + (size_t)s * slot_bytes, p.W + (size_t)p0 * panel_bytes + from, (uint32_t)bytes, &sh->full[s], policy);
-        return true;
+        ahead.blk += nb;
+        if (!ahead.shared && ahead.blk == ahead.end) ahead.next_panel();
     };
     // (weights are not written while they are in use: the ring fills while the predecessor in the stream drains)
-    if (warp == kWarps && lane == 0)
-        while (prod_ok && prod_j < nfill && prod_j < p.nring) {
-            prod_ok = issue_fill(prod_j);
-            if (prod_ok) ++prod_j;
-        }
+    for (int s = 0; s < p.nring; ++s) ask(s);
     pdl_wait();
     pdl_trigger();
     // ---- activations to shared memory, in the order in which the lanes take them ----
     auto source_row = [&](int m) -> long long {                              // -1: none
-        if (m >= p.mcount) return -1;
         long long r = p.m0 + m;
         if (p.x_rows != nullptr) {
             r = p.x_rows[p.m0 + m];
@@ -199,18 +288,19 @@ __global__ void __launch_bounds__(Threads<NT>::value, 1) draft_q4_kernel(DraftQ4
     };
     if constexpr (kMma) {
         const int pieces16 = p.blocks * 16;                                  // 16-byte pieces of a row: [block][chunk t][word i]
-        for (int m = warp; m < kRows; m += kThreads / 32) {                  // (a warp, a row)
+        for (int m = 0; m < p.mcount; ++m) {
             const long long r = source_row(m);
-            for (int c = lane; c < pieces16; c += 32) {
+#pragma unroll 2
+            for (int c = tid; c < pieces16; c += kThreads) {
                 uint4 w = make_uint4(0u, 0u, 0u, 0u);
                 if (r >= 0 && c * 8 < p.H) w = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.x) + (size_t)r * p.H + c * 8);
                 const int kb = c >> 4, t = (c >> 2) & 3, i = c & 3;
-                *reinterpret_cast<uint4*>(xs + ((((size_t)kb * NT + (m >> 3)) * 4 + i) * 32 + (m & 7) * 4 + t) * 16) = w;
+                *reinterpret_cast<uint4*>(xs + (((size_t)(kb * 4 + i) * p.mcount + m) * 4 + t) * 16) = w;
             }
         }
     } else {
         const int chunks = p.blocks * 4;
-        for (int m = 0; m < kF32Rows; ++m) {
+        for (int m = 0; m < p.mcount; ++m) {
             const long long r = source_row(m);
             for (int c = tid; c < chunks * 8; c += kThreads) {               // four floats each
                 float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -221,219 +311,239 @@ __global__ void __launch_bounds__(Threads<NT>::value, 1) draft_q4_kernel(DraftQ4
     }
     __syncthreads();
 
-    bool failed = false;
-    RunState st;
-    st.init();
-    int cur_seg = 0;
-    const int ei = (warp - kWarps - 1) * 32 + lane;                          // epilogue: class of the panel, row of the pass
-    const int own_r = ei / kRows, own_m = ei - own_r * kRows;
-    const bool owner = warp > kWarps && own_m < p.mcount;
-    RunState first_seg;                                                      // (filled when the CTA's range enters the next draft slot)
-    first_seg.init();
-    if (warp == kWarps) {
-        // ---------------- producer ----------------
-        if (lane == 0) {
-            bool ok = prod_ok;
-            int j = prod_j;
-            while (ok && j < nfill) {
-                ok = issue_fill(j);
-                if (ok) ++j;
-            }
-            if (!ok) {
-                if (*abort_flag == 0) report_error(p.status, CTCSD_ERR_TIMEOUT, 42);
-                *abort_flag = 1;
-            }
-            if (*abort_flag != 0)                                            // copies in flight land before the CTA's memory is given back
-                for (int back = 1; back <= p.nring && back <= j; ++back) {
-                    const int q = j - back;
-                    tc::mbar_wait(&sh->full[q % p.nring], (uint32_t)(q / p.nring) & 1u, &sh->never_set, 1ll << 24);
-                }
-        }
-    } else if (warp < kWarps) {
-        // ---------------- products ----------------
-        const int g = lane >> 2, t = lane & 3;
-        const int gpb = kBlock / p.group, gi = t * 32 / p.group;             // groups of a block, this lane's
-        float acc[2][NT][4];
-        float facc[2][kF32Rows];
+    const int g = lane >> 2, t = lane & 3;
+    // the lane's activation rows (columns of the product), and their states
+    auto col_of = [&](int c) -> int { return kMma ? (c >> 1) * 8 + 2 * t + (c & 1) : t; };
+    BestQ4 best[kStates];
+    float bias[kStates];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+    for (int c = 0; c < kStates; ++c) {
+        best[c].init();
+        bias[c] = 0.f;
+        const int m = col_of(c);
+        if (m < p.mcount && p.blank_bias != nullptr) bias[c] = p.blank_bias[p.row_seq ? p.row_seq[p.m0 + m] : p.m0 + m];
+    }
+    // the warp's states of a draft slot, one for every row, to shared memory
+    auto put_states = [&](int seg) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < kStates; ++c) {
+            combine_best<28>(best[c].st, p.k);
+            if (g == 0 && col_of(c) < kRows) best[c].st.store(&s_state[(seg * kWarps + warp) * kRows + col_of(c)]);
+            best[c].init();
+        }
+    };
+    int cur_seg = 0;
+    // the panel's logits: z[c][u] is class g + 8u, row col_of(c)
+    auto push = [&](int pan, const float (&z)[kStates][2]) __attribute__((always_inline)) {
+        const int seg = pan >= n_seg0 ? 1 : 0, slot = slot0 + seg;
+        if (seg != cur_seg) { put_states(0); cur_seg = 1; }
+        const int v0 = (int)(p0 + pan - (long long)slot * p.panels) * kPanel + g;
+#pragma unroll
+        for (int c = 0; c < kStates; ++c) {
+            const int m = col_of(c);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int v = v0 + 8 * u;
+                if (m < p.mcount && v < p.classes) {
+                    const float zz = z[c][u] + (v == p.classes - 1 ? bias[c] : 0.f);
+                    if (p.logits_dbg) p.logits_dbg[((size_t)(p.m0 + m) * p.slots + slot) * p.classes + v] = zz;
+                    best[c].push(zz, v, p.k);
+                }
+            }
+        }
+    };
+
+    const int gpb = kBlock / p.group;                                        // groups of a block
+    const unsigned so_a = 1024u + (g * gpb + t * 32 / p.group) * 4, so_b = so_a + 8 * gpb * 4;
+    const unsigned xstep = (unsigned)p.mcount * 64u;                          // bytes from a word's activations to the next word's
+    const unsigned xblock = kMma ? 4u * xstep : 4u * kF32Chunk * 4u;
+    unsigned xrow[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) xrow[nt] = (nt * 8 + g < p.mcount ? nt * 8 + g : p.mcount - 1) * 64u + t * 16u;
+    constexpr int kChains = 2;                                               // sums that run side by side (an instruction waits for the one before it in its own)
+    float acc[kChains][NT][4];
+    float facc[2][kF32Rows];
+    auto clear = [&]() {
+#pragma unroll
+        for (int u = 0; u < kChains; ++u)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) acc[u][nt][q] = 0.f;
 #pragma unroll
-            for (int m = 0; m < kF32Rows; ++m) facc[u][m] = 0.f;
-        }
-        int pan = 0, part_of = 0;                                            // panel and piece of it
-        for (int j = 0; j < nfill && !failed; ++j) {
-            const int s = j % p.nring;
-            if (!tc::mbar_wait(&sh->full[s], (uint32_t)(j / p.nring) & 1u, abort_flag)) { failed = true; break; }
-            const int here = npieces - j * p.slot_pieces < p.slot_pieces ? npieces - j * p.slot_pieces : p.slot_pieces;
-            size_t at = 0;
-            for (int pc = 0; pc < here; ++pc) {
-                const int b0 = part_of * p.piece_blocks;
-                const int nb = p.blocks - b0 < p.piece_blocks ? p.blocks - b0 : p.piece_blocks;
-                const unsigned char* base = ring + (size_t)s * slot_bytes + at;
-                for (int kb = warp; kb < nb; kb += kWarps) {
-                    const unsigned char* blk = base + (size_t)kb * bb;
-                    const uint4 wa = *reinterpret_cast<const uint4*>(blk + lane * 16);
-                    const uint4 wb = *reinterpret_cast<const uint4*>(blk + 512 + lane * 16);
-                    const uint32_t sa = *reinterpret_cast<const uint32_t*>(blk + 1024 + (g * gpb + gi) * 4);
-                    const uint32_t sb = *reinterpret_cast<const uint32_t*>(blk + 1024 + ((g + 8) * gpb + gi) * 4);
-                    const uint32_t a4[4] = {wa.x, wa.y, wa.z, wa.w}, b4[4] = {wb.x, wb.y, wb.z, wb.w};
-                    if constexpr (kMma) {
-                        const uint4* xf = reinterpret_cast<const uint4*>(xs) + (size_t)(b0 + kb) * NT * 128 + lane;
+        for (int m = 0; m < kF32Rows; ++m) facc[0][m] = facc[1][m] = 0.f;
+    };
+    clear();
+    auto finish = [&](float (&z)[kStates][2]) __attribute__((always_inline)) {   // the sums as logits, and zero again
+        if constexpr (kMma) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint4 va = q4_values_bf16(a4[i], sa), vb = q4_values_bf16(b4[i], sb);
+            for (int c = 0; c < kStates; ++c)
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                const uint4 x = xf[(nt * 4 + i) * 32];
-                                mma_16816(acc[0][nt], va.x, vb.x, va.y, vb.y, x.x, x.y);
-                                mma_16816(acc[1][nt], va.z, vb.z, va.w, vb.w, x.z, x.w);
-                            }
-                        }
-                    } else {
-                        const float* xf = reinterpret_cast<const float*>(xs) + ((size_t)(b0 + kb) * 4 + t) * kF32Chunk;
-                        const size_t row = (size_t)p.blocks * 4 * kF32Chunk;
-                        const float s0 = bf16lo(sa), o0 = bf16hi(sa), s1 = bf16lo(sb), o1 = bf16hi(sb);
+                for (int u = 0; u < 2; ++u) z[c][u] = acc[0][c >> 1][2 * u + (c & 1)] + acc[1][c >> 1][2 * u + (c & 1)];
+        } else {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float va[8], vb[8];
+            for (int m = 0; m < kF32Rows; ++m)
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) { va[e] = q4_value_f32(a4[i], e, s0, o0); vb[e] = q4_value_f32(b4[i], e, s1, o1); }
-#pragma unroll
-                            for (int m = 0; m < kF32Rows; ++m) {
-                                float x[8];
-                                load8(xf + m * row + i * 8, x);
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) { facc[0][m] = fmaf(va[e], x[e], facc[0][m]); facc[1][m] = fmaf(vb[e], x[e], facc[1][m]); }
-                            }
-                        }
-                    }
+                for (int u = 0; u < 2; ++u) {
+                    facc[u][m] += __shfl_xor_sync(0xffffffffu, facc[u][m], 1);
+                    facc[u][m] += __shfl_xor_sync(0xffffffffu, facc[u][m], 2);
+                    if (t == m) z[0][u] = facc[u][m];
                 }
-                at += (size_t)nb * bb;
-                if (++part_of < p.pieces) continue;
-                // ---- the panel's partial sums ----
-                part_of = 0;
-                const int d = pan % kDepth;
-                if (!tc::mbar_wait(&sh->cempty[d], ((uint32_t)(pan / kDepth) & 1u) ^ 1u, abort_flag)) { failed = true; break; }
-                float* cp = cpart + (size_t)(d * kWarps + warp) * kPanel * kRows;
-                if constexpr (kMma) {
+        }
+        clear();
+    };
+
+    PanelWalk at;
+    at.init(npan, kWarps, warp, p.blocks);
+    bool failed = false;
+    uint32_t phase = 0u;
+    for (int s = 0; !at.done();) {
+        if (!tc::mbar_wait(my_full + s, phase, abort_flag)) { failed = true; break; }
+        const int nb = min(p.piece, at.end - at.blk);
+        const unsigned char* blk = my_ring + s * slot_bytes;
+        const unsigned char* xb = xs + (unsigned)at.blk * xblock;
+        for (int kb = 0; kb < nb; ++kb, blk += bb, xb += xblock) {
+            const uint4 wa = *reinterpret_cast<const uint4*>(blk + lane * 16);
+            const uint4 wb = *reinterpret_cast<const uint4*>(blk + 512 + lane * 16);
+            const uint32_t sa = *reinterpret_cast<const uint32_t*>(blk + so_a);
+            const uint32_t sb = *reinterpret_cast<const uint32_t*>(blk + so_b);
+            const uint32_t a4[4] = {wa.x, wa.y, wa.z, wa.w}, b4[4] = {wb.x, wb.y, wb.z, wb.w};
+            if constexpr (kMma) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 va = q4_values_bf16(a4[i], sa), vb = q4_values_bf16(b4[i], sb);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        *reinterpret_cast<float2*>(cp + g * kRows + nt * 8 + 2 * t) = make_float2(acc[0][nt][0] + acc[1][nt][0], acc[0][nt][1] + acc[1][nt][1]);
-                        *reinterpret_cast<float2*>(cp + (g + 8) * kRows + nt * 8 + 2 * t) = make_float2(acc[0][nt][2] + acc[1][nt][2], acc[0][nt][3] + acc[1][nt][3]);
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) acc[0][nt][q] = acc[1][nt][q] = 0.f;
-                    }
-                } else {
-#pragma unroll
-                    for (int m = 0; m < kF32Rows; ++m) {
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            facc[u][m] += __shfl_xor_sync(0xffffffffu, facc[u][m], 1);
-                            facc[u][m] += __shfl_xor_sync(0xffffffffu, facc[u][m], 2);
-                            if (t == 0) cp[(g + 8 * u) * kRows + m] = facc[u][m];
-                            facc[u][m] = 0.f;
-                        }
+                        const uint4 x = *reinterpret_cast<const uint4*>(xb + i * xstep + xrow[nt]);
+                        mma_16816(acc[0][nt], va.x, vb.x, va.y, vb.y, x.x, x.y);
+                        mma_16816(acc[1][nt], va.z, vb.z, va.w, vb.w, x.z, x.w);
                     }
                 }
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(&sh->cfull[d]);
-                ++pan;
-            }
-            __syncwarp();
-            if (lane == 0 && !failed) tc::mbar_arrive(&sh->empty[s]);
-        }
-        if (failed && lane == 0) {
-            if (*abort_flag == 0) report_error(p.status, CTCSD_ERR_TIMEOUT, 43);
-            *abort_flag = 1;
-        }
-    } else {
-        // ---------------- epilogue ----------------
-        float bias = 0.f;
-        if (owner && p.blank_bias != nullptr) bias = p.blank_bias[p.row_seq ? p.row_seq[p.m0 + own_m] : p.m0 + own_m];
-        for (int pan = 0; pan < npan; ++pan) {
-            const int d = pan % kDepth;
-            if (!tc::mbar_wait(&sh->cfull[d], (uint32_t)(pan / kDepth) & 1u, abort_flag)) { failed = true; break; }
-            float z = 0.f;
-            if (owner) {
-                const float* cp = cpart + (size_t)d * kWarps * kPanel * kRows + own_r * kRows + own_m;
+            } else {
+                const float* xf = reinterpret_cast<const float*>(xb) + t * kF32Chunk;
+                const unsigned row = (unsigned)p.blocks * 4 * kF32Chunk;
+                const float s0 = bf16lo(sa), o0 = bf16hi(sa), s1 = bf16lo(sb), o1 = bf16hi(sb);
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) z += cp[w * kPanel * kRows];
-            }
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&sh->cempty[d]);
-            const int seg = pan >= n_seg0 ? 1 : 0, slot = slot0 + seg;
-            const int v = (int)(p0 + pan - (long long)slot * p.panels) * kPanel + own_r;
-            if (owner && v < p.classes) {
-                if (seg != cur_seg) { first_seg = st; st.init(); cur_seg = 1; }
-                if (v == p.classes - 1) z += bias;
-                if (p.logits_dbg) p.logits_dbg[((size_t)(p.m0 + own_m) * p.slots + slot) * p.classes + v] = z;
-                st.push(z, v);
+                for (int i = 0; i < 4; ++i) {
+                    float va[8], vb[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) { va[e] = q4_value_f32(a4[i], e, s0, o0); vb[e] = q4_value_f32(b4[i], e, s1, o1); }
+#pragma unroll
+                    for (int m = 0; m < kF32Rows; ++m) {
+                        if (m >= p.mcount) break;
+                        float x[8];
+                        load8(xf + m * row + i * 8, x);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) { facc[0][m] = fmaf(va[e], x[e], facc[0][m]); facc[1][m] = fmaf(vb[e], x[e], facc[1][m]); }
+                    }
+                }
             }
         }
-        if (failed && lane == 0) {
-            if (*abort_flag == 0) report_error(p.status, CTCSD_ERR_TIMEOUT, 44);
-            *abort_flag = 1;
-        }
+        at.blk += nb;
+        __syncwarp();                                                        // the slot has been read
+        ask(s);
+        if (++s == p.nring) { s = 0; phase ^= 1u; }
+        if (at.shared || at.blk < at.end) continue;
+        float z[kStates][2];
+        finish(z);
+        push(at.pan, z);
+        at.next_panel();
     }
-    __syncthreads();                                                         // the ring has been read (or, after a failure, has landed)
+    if (failed && lane == 0) {
+        if (*abort_flag == 0) report_error(p.status, CTCSD_ERR_TIMEOUT, 43);
+        *abort_flag = 1;
+        // copies in flight land before the CTA's memory is given back (both parities: the newest fill of a slot has one of them)
+        for (int s = 0; s < p.nring; ++s)
+            for (uint32_t q = 0; q < 2; ++q) tc::mbar_wait_suspended(my_full + s, q, &sh->never_set, 1ll << 20);
+    }
+    __syncthreads();                                                         // all rings have been read
     if (*abort_flag != 0) return;                                            // (uniform: set before the barrier or not at all)
-    if (owner) {
-        RunState none;
-        none.init();
-        (cur_seg == 0 ? st : first_seg).store(&s_part[own_r * kRows + own_m]);
-        (cur_seg == 0 ? none : st).store(&s_part[(kPanel + own_r) * kRows + own_m]);
+    // ---- the panels that were shared: partial sums through the rings' memory, one warp adds a panel's up ----
+    if (at.whole < npan) {
+        float* sums = reinterpret_cast<float*>(ring);                        // [warps][kStates * 2][32 lanes]
+        float z[kStates][2];
+        finish(z);
+#pragma unroll
+        for (int c = 0; c < kStates; ++c)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) sums[(warp * kStates * 2 + 2 * c + u) * 32 + lane] = z[c][u];
+        __syncthreads();
+        const int rest = npan - at.whole;
+        if (warp < rest) {
+#pragma unroll
+            for (int c = 0; c < kStates; ++c)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    z[c][u] = 0.f;
+                    for (int w = 0; w < at.per; ++w) z[c][u] += sums[((warp * at.per + w) * kStates * 2 + 2 * c + u) * 32 + lane];
+                }
+            push(at.whole + warp, z);
+        }
     }
+    const int segs = npan > n_seg0 ? 2 : 1;
+#pragma unroll 1
+    for (int seg = cur_seg; seg < segs; ++seg) put_states(seg);
     __syncthreads();
-    // fold the CTA's states: a warp, a (segment, row) at a time
-    for (int i = warp; i < 2 * p.mcount; i += kThreads / 32) {
+    // fold the warps' states: a warp, a (segment, row) at a time
+    for (int i = warp; i < segs * p.mcount; i += kWarps) {
         const int seg = i / p.mcount, m = i - seg * p.mcount;
         RunState ms;
         ms.init();
-        if (lane < kPanel) ms.absorb(s_part[(seg * kPanel + lane) * kRows + m]);
-        warp_combine(ms);
+        if (lane < kWarps) ms.absorb(s_state[(seg * kWarps + lane) * kRows + m]);
+        combine_best<31>(ms, p.k);
         if (lane == 0) ms.store(p.part + ((size_t)m * gridDim.x + blockIdx.x) * 2 + seg);
     }
-    if (tid < 2) p.part_slot[blockIdx.x * 2 + tid] = (tid == 0 ? n_seg0 : npan - n_seg0) > 0 ? slot0 + tid : -1;
     __threadfence();
     __syncthreads();
-    if (tid == 0) sh->is_last = atomicAdd(p.counter, 1u) == gridDim.x - 1;
+    // the CTAs whose panels touch a draft slot are neighbours; the one among them that ends last merges their states
+    auto first_cta = [&](int slot) -> int {                                  // the first whose panels reach beyond the slot's first
+        const long long n = gridDim.x, lo = (long long)slot * p.panels;
+        long long c = lo * n / total;
+        while (c > 0 && total * c / n > lo) --c;
+        while (total * (c + 1) / n <= lo) ++c;
+        return (int)c;
+    };
+    auto last_cta = [&](int slot) -> int {                                   // the last whose panels begin before the slot's end
+        const long long n = gridDim.x, hi = (long long)(slot + 1) * p.panels;
+        long long c = hi * n / total;
+        if (c > n - 1) c = n - 1;
+        while (total * c / n >= hi) --c;
+        while (c < n - 1 && total * (c + 1) / n < hi) ++c;
+        return (int)c;
+    };
+    if (tid < segs) {
+        const int slot = slot0 + tid, touch = last_cta(slot) - first_cta(slot) + 1;
+        const bool mine = atomicAdd(p.counter + slot, 1u) == (unsigned)touch - 1u;
+        if (mine) p.counter[slot] = 0u;
+        sh->merge[tid] = mine ? 1 : 0;
+    }
     __syncthreads();
-    if (!sh->is_last) return;
     __threadfence();
-    for (int task = warp; task < p.mcount * p.slots; task += kThreads / 32) {
-        const int m = task / p.slots, slot = task - m * p.slots;
-        RunState fs;
-        fs.init();
-        // the CTAs whose panels touch this draft slot are neighbours
-        const long long n = gridDim.x, lo = (long long)slot * p.panels, hi = lo + p.panels;
-        long long c0 = lo * n / total, c1 = hi * n / total;
-        while (c0 > 0 && total * c0 / n > lo) --c0;
-        if (c1 > n - 1) c1 = n - 1;
-        for (long long c = c0 + lane; c <= c1; c += 32) {
-            const int seg = slot - (int)((total * c / n) / p.panels);
-            if (seg < 0 || seg > 1) continue;
-            const int e = (int)(2 * c + seg);
-            if (__ldcg(p.part_slot + e) == slot) fs.absorb(load_partial_cg(p.part + (size_t)m * n * 2 + e));
-        }
-        warp_combine(fs);
-        if (lane == 0) {
-            const int row = p.m0 + m;
-            const float lse = fs.mx + logf(fs.sum);
-            p.out_lse[(size_t)row * p.slots + slot] = lse;
+    for (int seg = 0; seg < segs; ++seg) {
+        if (!sh->merge[seg]) continue;
+        const int slot = slot0 + seg, c0 = first_cta(slot), c1 = last_cta(slot);
+        for (int m = warp; m < p.mcount; m += kWarps) {
+            RunState fs;
+            fs.init();
+            for (int c = c0 + lane; c <= c1; c += 32) {
+                const int which = slot - (int)(total * c / gridDim.x / p.panels);          // the slot is the CTA's first or second
+                fs.absorb(load_partial_cg(p.part + ((size_t)m * gridDim.x + c) * 2 + which));
+            }
+            combine_best<31>(fs, p.k);
+            if (lane == 0) {
+                const int row = p.m0 + m;
+                const float lse = fs.mx + logf(fs.sum);
+                p.out_lse[(size_t)row * p.slots + slot] = lse;
 #pragma unroll
-            for (int j = 0; j < kTopSlots; ++j)
-                if (j < p.k) {
-                    const size_t o = ((size_t)row * p.slots + slot) * p.k + j;
-                    p.out_topk_id[o] = fs.id[j];
-                    p.out_topk_lp[o] = fs.val[j] - lse;
-                }
+                for (int j = 0; j < kTopSlots; ++j)
+                    if (j < p.k) {
+                        const size_t o = ((size_t)row * p.slots + slot) * p.k + j;
+                        p.out_topk_id[o] = fs.id[j];
+                        p.out_topk_lp[o] = fs.val[j] - lse;
+                    }
+            }
         }
     }
-    if (tid == 0) *p.counter = 0u;
 }
 
 int panels_of(const ctcsd_config& c) { return (c.V + 1 + kPanel - 1) / kPanel; }
@@ -442,48 +552,34 @@ int blocks_of(const ctcsd_config& c) { return (c.H + kBlock - 1) / kBlock; }
 constexpr size_t kSmemBudget = kMaxDynamicSmem - 1024;                       // (1 KB of every CTA is the system's)
 
 template <typename T, int NT>
-size_t fixed_smem(int blocks) {
-    return XShape<T, NT>::bytes(blocks) + sizeof(RingState) + sizeof(float) * kDepth * kWarps * kPanel * 8 * NT;
+size_t fixed_smem(int blocks, int rows) {
+    return x_bytes<T>(blocks, rows) + sizeof(RingState) + sizeof(DraftPartial) * 2 * Shape<T, NT>::warps * (sizeof(T) == 2 ? 8 * NT : kF32Rows);
 }
 
-// Ring geometry: pieces of a panel and pieces of a slot.  False where not even two slots fit.
+// Ring geometry: blocks of a slot, slots of a warp.  False where there is no room for two blocks a warp.
 template <typename T, int NT>
 bool ring_shape(DraftQ4Params& p) {
-    const size_t fixed = fixed_smem<T, NT>(p.blocks);
-    const size_t state = sizeof(DraftPartial) * 2 * kPanel * 8 * NT;         // the states at the end lie over the ring
-    if (fixed + state > kSmemBudget) return false;
-    const size_t room = kSmemBudget - fixed;
-    const size_t bb = (size_t)block_bytes(p.group), panel = bb * p.blocks;
-    // slots of about a third of the room, at most 40 KB: whole panels where they are smaller, else equal parts of one
-    size_t want = room / 3 < 40 * 1024 ? room / 3 : 40 * 1024;
-    if (panel <= want) {
-        p.pieces = 1;
-        p.piece_blocks = p.blocks;
-        p.slot_pieces = (int)(want / panel);
-    } else {
-        p.pieces = (int)((panel + want - 1) / want);
-        p.piece_blocks = (p.blocks + p.pieces - 1) / p.pieces;
-        p.pieces = (p.blocks + p.piece_blocks - 1) / p.piece_blocks;
-        p.slot_pieces = 1;
-    }
-    const size_t slot = (size_t)p.slot_pieces * p.piece_blocks * bb;
-    size_t n = room / slot;
-    if (n > kMaxSlots) n = kMaxSlots;
-    while (n * slot < state && n < kMaxSlots) ++n;                           // (tiny panels: the states need the room)
-    if (n < 2 || n * slot < state || n * slot > room) return false;
-    p.nring = (int)n;
+    constexpr size_t warps = Shape<T, NT>::warps;
+    const size_t fixed = fixed_smem<T, NT>(p.blocks, p.mcount);
+    if (fixed > kSmemBudget) return false;
+    const size_t bb = (size_t)block_bytes(p.group), most = (kSmemBudget - fixed) / (warps * bb);        // blocks there is room for, a warp
+    if (most < 2) return false;
+    // two slots, of 8 blocks at most; three where they are small then
+    p.piece = (int)(most / 2 < 8 ? most / 2 : 8);
+    if (p.piece > p.blocks) p.piece = p.blocks;
+    p.nring = (int)(most / p.piece < kMaxRing ? most / p.piece : kMaxRing);
     return true;
 }
 
 template <typename T, int NT>
 int launch_pass(Handle* h, cudaStream_t s, DraftQ4Params& p) {
     if (!ring_shape<T, NT>(p)) return CTCSD_ERR_UNSUPPORTED;
-    const size_t smem = fixed_smem<T, NT>(p.blocks) + (size_t)p.nring * p.slot_pieces * p.piece_blocks * block_bytes(p.group);
+    const size_t smem = fixed_smem<T, NT>(p.blocks, p.mcount) + (size_t)Shape<T, NT>::warps * p.nring * p.piece * block_bytes(p.group);
     auto kern = draft_q4_kernel<T, NT>;
     CTCSD_CUDA_CHECK(h, prepare_kernel(h, sizeof(T) == 4 ? kPrepDraftQ4F32 : (NT == 1 ? kPrepDraftQ4 : kPrepDraftQ4x2), kern));
     const long long total = (long long)p.panels * p.slots;
     const unsigned grid = (unsigned)(total < h->num_sms ? total : h->num_sms);        // (total >= slots: a range touches two slots at most)
-    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(grid), dim3(Threads<NT>::value), smem, s, 1, p));
+    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(grid), dim3(Shape<T, NT>::warps * 32), smem, s, 1, p));
     h->launches++;
     return CTCSD_OK;
 }
@@ -537,16 +633,21 @@ extern "C" int ctcsd_draft_logits_q4(ctcsd_handle* hh, void* stream, int M, cons
     p.row_seq = row_seq; p.blank_bias = blank_bias;
     p.H = c.H; p.classes = c.V + 1; p.panels = panels_of(c); p.blocks = blocks_of(c); p.group = group; p.slots = c.T;
     p.part = reinterpret_cast<DraftPartial*>(h->ws + h->lay.draft_part_off);
-    p.part_slot = reinterpret_cast<int*>(h->ws + h->lay.part_slot_off);
     p.counter = counter_ptr(h);
     p.k = c.k; p.out_topk_id = out_topk_id; p.out_topk_lp = out_topk_lp; p.out_lse = out_lse; p.logits_dbg = out_logits_dbg;
     p.status = status_ptr(h);
     const DeviceGuard on(h->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool bf16 = c.dtype == CTCSD_DTYPE_BF16;
-    DraftQ4Params probe = p;
-    const bool wide = bf16 && M > 8 && ring_shape<__nv_bfloat16, 2>(probe);
-    const int per_pass = bf16 ? (wide ? 16 : 8) : kF32Rows;
+    // rows of a pass: 16 (float32: 4), or as many as leave the ring room
+    auto fits = [&](int rows) {
+        DraftQ4Params q = p;
+        q.mcount = rows;
+        return !bf16 ? ring_shape<float, 1>(q) : (rows > 8 ? ring_shape<__nv_bfloat16, 2>(q) : ring_shape<__nv_bfloat16, 1>(q));
+    };
+    int per_pass = bf16 ? 16 : kF32Rows;
+    if (per_pass > M) per_pass = M;
+    while (per_pass > 1 && !fits(per_pass)) per_pass = (per_pass + 1) / 2;
     for (int m0 = 0; m0 < M; m0 += per_pass) {
         p.m0 = m0;
         p.mcount = M - m0 < per_pass ? M - m0 : per_pass;

@@ -6,8 +6,8 @@
 // one and-or, two levels at a time, and one packed multiply-add makes it the value.  (Levels from 0 took a
 // subtraction more; the origin is then farther from the values, by 16 scales, and rounding it to 8 bits moves all levels of a group
 // together by 1/16 of a level at most where the group spans zero.)
-// Eight consecutive values share a 32-bit word: value 2i at bits 4i, value 2i + 1 at bits 16 + 4i, so that the pairs that come
-// out of a word are neighbours.
+// Eight consecutive values share a 32-bit word, at the nibbles that begin at bits 3, 19, 7, 23, 11, 27, 31 (and 0..2), 15: a pair's two
+// lie 16 bits apart and three shifts bring all pairs to bits 3..6 and 19..22, where a bfloat16 number takes them.
 #pragma once
 
 #include "common.cuh"
@@ -18,13 +18,38 @@ constexpr int kQ4Group = 32;                   // values of a cached row that sh
 
 #ifdef __CUDACC__
 
+// (a & mask) | base as one instruction: an instruction takes one constant of its own, so both are kept in registers (as
+// constants the two steps stay apart, and the draft head at the 7B shape took 113 us in place of 86).
+__device__ __forceinline__ uint32_t q4_level_bits(uint32_t a) {
+    uint32_t mask, base, r;
+    asm("mov.b32 %0, 0x00780078;" : "=r"(mask));
+    asm("mov.b32 %0, 0x41804180;" : "=r"(base));
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(mask), "r"(base));
+    return r;
+}
 // The eight levels of a word as four pairs of bfloat16 numbers 16..31: pair i = values 2i, 2i + 1.
 __device__ __forceinline__ void q4_pairs(uint32_t w, uint32_t (&c)[4]) {
-    c[0] = ((w << 3) & 0x00780078u) | 0x41804180u;
-    c[1] = ((w >> 1) & 0x00780078u) | 0x41804180u;
-    c[2] = ((w >> 5) & 0x00780078u) | 0x41804180u;
-    c[3] = ((w >> 9) & 0x00780078u) | 0x41804180u;
+    c[0] = q4_level_bits(w);
+    c[1] = q4_level_bits(w >> 4);
+    c[2] = q4_level_bits(w >> 8);
+    c[3] = q4_level_bits(__funnelshift_l(w, w, 4));
 }
+// The same for two words of two rows at once: pair i of `even` / `odd` = values 2i / 2i + 1 of the rows a and b.
+__device__ __forceinline__ void q4_pairs2(uint32_t a, uint32_t b, uint32_t (&even)[4], uint32_t (&odd)[4]) {
+    // (turned so that nibbles do not cross the halves: the low one holds values 0, 2, 4, 7, the high one 1, 3, 5, 6)
+    const uint32_t ra = __funnelshift_r(a, a, 3), rb = __funnelshift_r(b, b, 3);
+    const uint32_t lo = __byte_perm(ra, rb, 0x5410), hi = __byte_perm(ra, rb, 0x7632);
+    even[0] = q4_level_bits(lo << 3);
+    even[1] = q4_level_bits(lo >> 1);
+    even[2] = q4_level_bits(lo >> 5);
+    odd[3] = q4_level_bits(lo >> 9);
+    odd[0] = q4_level_bits(hi << 3);
+    odd[1] = q4_level_bits(hi >> 1);
+    odd[2] = q4_level_bits(hi >> 5);
+    even[3] = q4_level_bits(hi >> 9);
+}
+// First bit of value i (0..7) of a word.
+__host__ __device__ constexpr int q4_bit(int i) { return (i < 6 ? 3 + 4 * (i >> 1) + 16 * (i & 1) : (i == 6 ? 31 : 15)); }
 __device__ __forceinline__ uint32_t q4_fma2(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t d;
     asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
@@ -43,7 +68,7 @@ __device__ __forceinline__ uint4 q4_values_bf16(uint32_t w, uint32_t so) {
 }
 // Value i (0..7) of a word in float32.
 __device__ __forceinline__ float q4_value_f32(uint32_t w, int i, float scale, float origin) {
-    const uint32_t q = (w >> (4 * (i >> 1) + 16 * (i & 1))) & 15u;
+    const uint32_t q = __funnelshift_r(w, w, q4_bit(i)) & 15u;
     return __fmaf_rn(__uint_as_float(0x41800000u | (q << 19)), scale, origin);
 }
 
@@ -78,7 +103,10 @@ __device__ __forceinline__ uint32_t q4_word(const float (&v)[8], uint32_t so) {
     const float s = bf16lo(so), o = bf16hi(so);
     uint32_t w = 0u;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w |= q4_level(v[i], s, o) << (4 * (i >> 1) + 16 * (i & 1));
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t q = q4_level(v[i], s, o);
+        w |= __funnelshift_l(q, q, q4_bit(i)) & (i == 6 ? 0x80000007u : 15u << (q4_bit(i) & 31));
+    }
     return w;
 }
 

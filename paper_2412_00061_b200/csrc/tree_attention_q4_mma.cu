@@ -247,27 +247,35 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
                 const long long grow = (long long)pair * p.Lcap + (long long)blk * kKeys;
                 const uint32_t* Kso = RawQ4<D>::pairs(Kside, kKeys, grow);
                 const uint32_t* Vso = RawQ4<D>::pairs(Vside, kKeys, grow);
-                float s[2][4];
+                // scores, in two sums that run side by side for each tile of 8 keys (an instruction waits for the one before it in its own)
+                float s[2][4], s2[2][4];
+                uint32_t kw[2][LW], kso[2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const int key = warp * 16 + j * 8 + g;
-                    uint32_t w[LW];
                     if constexpr (LW == 4) {
                         const uint4 u = *reinterpret_cast<const uint4*>(Kside + key * RawQ4<D>::kLevels + t * 16);
-                        w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+                        kw[j][0] = u.x; kw[j][1] = u.y; kw[j][2] = u.z; kw[j][3] = u.w;
                     } else {
                         const uint2 u = *reinterpret_cast<const uint2*>(Kside + key * RawQ4<D>::kLevels + t * 8);
-                        w[0] = u.x; w[1] = u.y;
+                        kw[j][0] = u.x; kw[j][1] = u.y;
                     }
-                    const uint32_t so = Kso[key * (D / 32) + t * (D / 32) / 4];
+                    kso[j] = Kso[key * (D / 32) + t * (D / 32) / 4];
                     s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < LW; ++i) {
-                        const uint4 k = q4_values_bf16(w[i], so);
-                        mma_16816(s[j], qa[i].x, qb[i].x, qa[i].y, qb[i].y, k.x, k.y);
-                        mma_16816(s[j], qa[i].z, qb[i].z, qa[i].w, qb[i].w, k.z, k.w);
-                    }
+                    s2[j][0] = s2[j][1] = s2[j][2] = s2[j][3] = 0.f;
                 }
+#pragma unroll
+                for (int i = 0; i < LW; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint4 k = q4_values_bf16(kw[j][i], kso[j]);
+                        mma_16816(s[j], qa[i].x, qb[i].x, qa[i].y, qb[i].y, k.x, k.y);
+                        mma_16816(s2[j], qa[i].z, qb[i].z, qa[i].w, qb[i].w, k.z, k.w);
+                    }
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) s[j][q] += s2[j][q];
                 if (left < 16) {
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
@@ -301,10 +309,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
                     // even and odd columns of the two keys of a pair, in the halves of a word
                     uint32_t ev[2][4], od[2][4];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        q4_pairs(__byte_perm(w[2 * h][i], w[2 * h + 1][i], 0x5410), ev[h]);
-                        q4_pairs(__byte_perm(w[2 * h][i], w[2 * h + 1][i], 0x7632), od[h]);
-                    }
+                    for (int h = 0; h < 2; ++h) q4_pairs2(w[2 * h][i], w[2 * h + 1][i], ev[h], od[h]);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         mma_16816(o[8 * i + 2 * c], pa[0], pa[1], pa[2], pa[3], q4_fma2(ev[0][c], sc[0], og[0]), q4_fma2(ev[1][c], sc[1], og[1]));

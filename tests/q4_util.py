@@ -6,6 +6,7 @@ from oracle import ctcsd_oracle as orc
 from paper_2412_00061_b200 import binding
 
 DEV = "cuda:0"
+WORD_BITS = (3, 19, 7, 23, 11, 27, 31, 15)
 
 
 def act_of(dtype):
@@ -28,12 +29,12 @@ def stands_for(v, group, dtype):
 
 
 def levels_of(words, n):
-    """Levels [...,n] from stored bytes [...,n/2]: per 32-bit word value 2i at bits 4i, value 2i + 1 at bits 16 + 4i."""
+    """Levels [...,n] from stored bytes [...,n/2]: a word's values 0..7 at the bits of WORD_BITS (turned by a word's length)."""
     w = np.ascontiguousarray(words.cpu().numpy()).view("<u4")
     out = np.zeros(w.shape + (8,), dtype=np.int64)
-    for i in range(4):
-        out[..., 2 * i] = (w >> (4 * i)) & 15
-        out[..., 2 * i + 1] = (w >> (16 + 4 * i)) & 15
+    w = w.astype(np.uint64)
+    for i, bit in enumerate(WORD_BITS):
+        out[..., i] = ((w | (w << np.uint64(32))) >> np.uint64(bit)) & np.uint64(15)
     return out.reshape(*w.shape[:-1], -1)[..., :n]
 
 
