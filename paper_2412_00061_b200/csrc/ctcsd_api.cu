@@ -60,6 +60,14 @@ Layout make_layout(const ctcsd_config& c, int num_sms) {
         l.lm_rows_off = off;    off = align_up(off + (size_t)l.lm_key_count * c.H * 2, 256);
         l.lm_rowmap_off = off;  off = align_up(off + sizeof(int) * ((size_t)l.lm_key_count + 1), 256);
     }
+    l.q4_rows_off = l.q4_part_off = off;
+    {
+        const int rows = c.max_draft_rows > 0 ? c.max_draft_rows : c.B;
+        if (rows > 8 && c.dtype == CTCSD_DTYPE_BF16) {
+            l.q4_rows_off = off;  off = align_up(off + (size_t)rows * c.H * 2, 256);
+            l.q4_part_off = off;  off = align_up(off + sizeof(DraftPartial) * 128 * (size_t)num_sms * 2, 256);
+        }
+    }
     l.total = off;
     return l;
 }

@@ -4,12 +4,12 @@
 //
 // Packed weights.  Sixteen neighbouring classes of a slot are a panel (the last one of a slot filled up with zero rows), 128
 // hidden elements of a panel a block, blocks of a panel follow one another:
-//   block = levels [2][32 lanes][16 bytes], lane 4g + t of half h: class 8h + g, elements 32t .. 32t + 31, four words (q4.cuh);
+//   block = levels [2][32 lanes][16 bytes], lane 4g + t of half h: class 8h + g, elements 32t .. 32t + 31, four words (q4.cuh), for t >= 2 in
+//           the order 2, 3, 0, 1 (the lanes of a warp that write values to a tensor-core tile then meet in no bank);
 //           pairs  [16 classes][128 / group] (scale, origin).
 // This is the order in which the lanes of a warp hold the operand A of mma.m16n8k16 (with the hidden index permuted alike for x),
 // so a lane takes its share of a block by two 16-byte reads without bank conflicts, and a panel is one piece of memory.
-#include "q4.cuh"
-#include "run_state.cuh"
+#include "draft_q4.cuh"
 #include "tc_primitives.cuh"
 
 #include <limits.h>
@@ -17,11 +17,6 @@
 
 namespace ctcsd {
 namespace {
-
-constexpr int kPanel = 16;               // classes of a panel
-constexpr int kBlock = 128;              // hidden elements of a block
-
-__host__ __device__ inline int block_bytes(int group) { return 1024 + kPanel * 4 * (kBlock / group); }
 
 struct PackParams {
     const void* W;                       // [T,V+1,H]
@@ -34,11 +29,11 @@ template <typename T>
 __global__ void __launch_bounds__(256) quantize_weights_q4_kernel(PackParams p) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int kb = blockIdx.x, t = blockIdx.z;
-    const int bytes = block_bytes(p.group), per = p.group / 8;                // lanes of a group
+    const int bytes = q4_block_bytes(p.group), per = p.group / 8;                // lanes of a group
     for (int panel = blockIdx.y; panel < p.panels; panel += gridDim.y) {
         unsigned char* blk = p.out + (((size_t)t * p.panels + panel) * p.blocks + kb) * bytes;
         const int r = warp * 2 + (lane >> 4), e = (lane & 15) * 8;            // class of the panel, first element of the block
-        const int cls = panel * kPanel + r, k = kb * kBlock + e;
+        const int cls = panel * kQ4Panel + r, k = kb * kQ4Block + e;
         const bool in = cls < p.classes && k < p.H;                           // (H is a multiple of 8)
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         float lo = INFINITY, hi = -INFINITY;
@@ -53,11 +48,11 @@ __global__ void __launch_bounds__(256) quantize_weights_q4_kernel(PackParams p) 
             hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
         }
         // (a group without elements: zeros)
-        const bool some = cls < p.classes && kb * kBlock + e / p.group * p.group < p.H;
+        const bool some = cls < p.classes && kb * kQ4Block + e / p.group * p.group < p.H;
         const uint32_t so = some ? q4_scale_origin(lo, hi) : 0u;
         const uint32_t w = in ? q4_word(v, so) : 0u;
-        reinterpret_cast<uint32_t*>(blk)[(r >> 3) * 128 + ((r & 7) * 4 + (e >> 5)) * 4 + ((e >> 3) & 3)] = w;
-        if ((lane & 15) % per == 0) reinterpret_cast<uint32_t*>(blk + 1024)[r * (kBlock / p.group) + e / p.group] = so;
+        reinterpret_cast<uint32_t*>(blk)[(r >> 3) * 128 + ((r & 7) * 4 + (e >> 5)) * 4 + (((e >> 3) & 3) ^ ((e >> 6) << 1))] = w;
+        if ((lane & 15) % per == 0) reinterpret_cast<uint32_t*>(blk + 1024)[r * (kQ4Block / p.group) + e / p.group] = so;
     }
 }
 
@@ -65,32 +60,12 @@ __global__ void __launch_bounds__(256) quantize_weights_q4_kernel(PackParams p) 
 // before its predecessor in the stream has ended, and that must not be the kernel that writes them.
 __global__ void order_kernel() {}
 
-struct DraftQ4Params {
-    const void* x;                       // [x_row_count,H]
-    const int* x_rows;                   // [M] or null
-    int x_row_count;
-    const unsigned char* W;              // packed
-    const int* row_seq;
-    const float* blank_bias;
-    int m0, mcount;                      // rows of this pass
-    int H, classes, panels, blocks, group;   // panels per draft slot, blocks per panel
-    int slots;                           // draft slots (T)
-    int piece, nring;                    // blocks of a ring slot, ring slots of a warp
-    DraftPartial* part;                  // [rows of a pass][grid][2]
-    unsigned* counter;                   // [draft slots], zero between calls
-    int k;
-    int* out_topk_id;
-    float* out_topk_lp;
-    float* out_lse;
-    float* logits_dbg;
-    int* status;
-};
-
 // The running state of an activation row in a lane: the k best logits in order, in a list of kTopSlots.
 struct BestQ4 {
     RunState st;
-    float floor;                         // a logit has to be above it to be among the k best
-    __device__ __forceinline__ void init() { st.init(); floor = -INFINITY; }
+    float floor;                         // a logit has to be above it to be among the k best,
+    int have;                            // unless the list holds fewer
+    __device__ __forceinline__ void init() { st.init(); floor = -INFINITY; have = 0; }
     // (a lane's classes come in rising order: an equal logit ranks behind)
     __device__ __forceinline__ void push(float z, int v, int k) {
         if (z > st.mx) {
@@ -99,8 +74,9 @@ struct BestQ4 {
         } else {
             st.sum += __expf(z - st.mx);
         }
-        if (z > floor || st.id[0] == INT_MAX) {
+        if (z > floor || have < k) {
             topk_insert(st.val, st.id, z, v);
+            have += z == z ? 1 : 0;
 #pragma unroll
             for (int s = 0; s < kTopSlots; ++s) {
                 float f = st.val[s];
@@ -110,60 +86,6 @@ struct BestQ4 {
         }
     }
 };
-
-// Unsigned numbers in the order of the floats; 0 for an entry that is not there.
-__device__ __forceinline__ uint32_t rank_of(float v, int id) {
-    if (id == INT_MAX) return 0u;
-    const uint32_t u = __float_as_uint(v);
-    return (u >> 31) ? ~u : u | 0x80000000u;
-}
-// Combines the states of the lanes that differ in the bits of `over` (31: all of the warp; 28: the eight with the same lane % 4): maximum, sum, and
-// the k best (ties to the lower id) in each of them.
-template <int over> __device__ __forceinline__ void combine_best(RunState& st, int k) {
-    float gmx = st.mx;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        if (over & o) gmx = fmaxf(gmx, __shfl_xor_sync(0xffffffffu, gmx, o));
-    st.sum = st.mx == -INFINITY ? 0.f : st.sum * __expf(st.mx - gmx);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        if (over & o) st.sum += __shfl_xor_sync(0xffffffffu, st.sum, o);
-    st.mx = gmx;
-    float ov[kTopSlots];
-    int oi[kTopSlots];
-#pragma unroll
-    for (int r = 0; r < kTopSlots; ++r) {
-        ov[r] = -INFINITY;
-        oi[r] = INT_MAX;
-        if (r < k) {
-            const uint32_t mine = rank_of(st.val[0], st.id[0]);
-            uint32_t top = mine;
-            unsigned id;
-            if constexpr (over == 31) {
-                top = __reduce_max_sync(0xffffffffu, mine);
-                id = __reduce_min_sync(0xffffffffu, mine == top ? (unsigned)st.id[0] : 0x7fffffffu);
-            } else {
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1)
-                    if (over & o) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                id = mine == top ? (unsigned)st.id[0] : 0x7fffffffu;
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1)
-                    if (over & o) id = min(id, __shfl_xor_sync(0xffffffffu, id, o));
-            }
-            oi[r] = (int)id;
-            if (top != 0u) ov[r] = __uint_as_float((top >> 31) ? top & 0x7fffffffu : ~top);
-            if ((unsigned)st.id[0] == id && id != 0x7fffffffu) {              // (an id stands in one lane's list only)
-#pragma unroll
-                for (int q = 0; q < kTopSlots - 1; ++q) { st.val[q] = st.val[q + 1]; st.id[q] = st.id[q + 1]; }
-                st.val[kTopSlots - 1] = -INFINITY;
-                st.id[kTopSlots - 1] = INT_MAX;
-            }
-        }
-    }
-#pragma unroll
-    for (int q = 0; q < kTopSlots; ++q) { st.val[q] = ov[q]; st.id[q] = oi[q]; }
-}
 
 // D[16x8] += A[16x16] * B[16x8], bf16 operands, fp32 accumulators (warp-wide).
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -184,9 +106,9 @@ template <typename T> __host__ __device__ inline size_t x_bytes(int blocks, int 
 }
 
 // Warps of a CTA: as many as leave a thread the registers for its states (one of 19 registers per activation row it looks after).
-template <typename T, int NT> struct Shape {
-    static constexpr int warps = NT == 1 ? 16 : 12;
-    static constexpr int states = sizeof(T) == 2 ? 2 * NT : 1;
+template <typename T> struct Shape {
+    static constexpr int warps = 16;
+    static constexpr int states = sizeof(T) == 2 ? 2 : 1;
 };
 
 struct __align__(8) RingState {
@@ -229,15 +151,15 @@ struct PanelWalk {
 // multiply-adds), and the lanes that hold a panel's logits keep the running maximum, sum of exponentials and best k.  Warps meet
 // at the end only.  (Sets of 4 or 8 warps that shared a panel and handed partial sums to epilogue warps took 93-113 us
 // at the 7B shape, half of it in hand-overs.)
-template <typename T, int NT>
-__global__ void __launch_bounds__(Shape<T, NT>::warps * 32, 1) draft_q4_kernel(DraftQ4Params p) {
+template <typename T>
+__global__ void __launch_bounds__(Shape<T>::warps * 32, 1) draft_q4_kernel(DraftQ4Params p) {
     constexpr bool kMma = sizeof(T) == 2;
-    constexpr int kWarps = Shape<T, NT>::warps, kThreads = kWarps * 32, kStates = Shape<T, NT>::states;
-    constexpr int kRows = kMma ? 8 * NT : kF32Rows;
+    constexpr int kWarps = Shape<T>::warps, kThreads = kWarps * 32, kStates = Shape<T>::states;
+    constexpr int kRows = kMma ? 8 : kF32Rows;
     extern __shared__ __align__(128) unsigned char dyn[];
     unsigned char* xs = dyn;
     unsigned char* ring = xs + x_bytes<T>(p.blocks, p.mcount);
-    const int bb = block_bytes(p.group), slot_bytes = p.piece * bb;
+    const int bb = q4_block_bytes(p.group), slot_bytes = p.piece * bb;
     RingState* sh = reinterpret_cast<RingState*>(ring + (size_t)kWarps * p.nring * slot_bytes);
     DraftPartial* s_state = reinterpret_cast<DraftPartial*>(sh + 1);         // [2][warps][kRows]
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -294,7 +216,7 @@ __global__ void __launch_bounds__(Shape<T, NT>::warps * 32, 1) draft_q4_kernel(D
             for (int c = tid; c < pieces16; c += kThreads) {
                 uint4 w = make_uint4(0u, 0u, 0u, 0u);
                 if (r >= 0 && c * 8 < p.H) w = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.x) + (size_t)r * p.H + c * 8);
-                const int kb = c >> 4, t = (c >> 2) & 3, i = c & 3;
+                const int kb = c >> 4, t = (c >> 2) & 3, i = (c & 3) ^ ((t >> 1) << 1);   // (in the order of the weights' words)
                 *reinterpret_cast<uint4*>(xs + (((size_t)(kb * 4 + i) * p.mcount + m) * 4 + t) * 16) = w;
             }
         }
@@ -313,7 +235,7 @@ __global__ void __launch_bounds__(Shape<T, NT>::warps * 32, 1) draft_q4_kernel(D
 
     const int g = lane >> 2, t = lane & 3;
     // the lane's activation rows (columns of the product), and their states
-    auto col_of = [&](int c) -> int { return kMma ? (c >> 1) * 8 + 2 * t + (c & 1) : t; };
+    auto col_of = [&](int c) -> int { return kMma ? 2 * t + c : t; };
     BestQ4 best[kStates];
     float bias[kStates];
 #pragma unroll
@@ -337,7 +259,7 @@ __global__ void __launch_bounds__(Shape<T, NT>::warps * 32, 1) draft_q4_kernel(D
     auto push = [&](int pan, const float (&z)[kStates][2]) __attribute__((always_inline)) {
         const int seg = pan >= n_seg0 ? 1 : 0, slot = slot0 + seg;
         if (seg != cur_seg) { put_states(0); cur_seg = 1; }
-        const int v0 = (int)(p0 + pan - (long long)slot * p.panels) * kPanel + g;
+        const int v0 = (int)(p0 + pan - (long long)slot * p.panels) * kQ4Panel + g;
 #pragma unroll
         for (int c = 0; c < kStates; ++c) {
             const int m = col_of(c);
@@ -353,23 +275,19 @@ __global__ void __launch_bounds__(Shape<T, NT>::warps * 32, 1) draft_q4_kernel(D
         }
     };
 
-    const int gpb = kBlock / p.group;                                        // groups of a block
+    const int gpb = kQ4Block / p.group;                                        // groups of a block
     const unsigned so_a = 1024u + (g * gpb + t * 32 / p.group) * 4, so_b = so_a + 8 * gpb * 4;
     const unsigned xstep = (unsigned)p.mcount * 64u;                          // bytes from a word's activations to the next word's
     const unsigned xblock = kMma ? 4u * xstep : 4u * kF32Chunk * 4u;
-    unsigned xrow[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) xrow[nt] = (nt * 8 + g < p.mcount ? nt * 8 + g : p.mcount - 1) * 64u + t * 16u;
+    const unsigned xrow = (g < p.mcount ? g : p.mcount - 1) * 64u + t * 16u;
     constexpr int kChains = 2;                                               // sums that run side by side (an instruction waits for the one before it in its own)
-    float acc[kChains][NT][4];
+    float acc[kChains][4];
     float facc[2][kF32Rows];
     auto clear = [&]() {
 #pragma unroll
         for (int u = 0; u < kChains; ++u)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) acc[u][nt][q] = 0.f;
+            for (int q = 0; q < 4; ++q) acc[u][q] = 0.f;
 #pragma unroll
         for (int m = 0; m < kF32Rows; ++m) facc[0][m] = facc[1][m] = 0.f;
     };
@@ -379,7 +297,7 @@ __global__ void __launch_bounds__(Shape<T, NT>::warps * 32, 1) draft_q4_kernel(D
 #pragma unroll
             for (int c = 0; c < kStates; ++c)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) z[c][u] = acc[0][c >> 1][2 * u + (c & 1)] + acc[1][c >> 1][2 * u + (c & 1)];
+                for (int u = 0; u < 2; ++u) z[c][u] = acc[0][2 * u + c] + acc[1][2 * u + c];
         } else {
 #pragma unroll
             for (int m = 0; m < kF32Rows; ++m)
@@ -412,12 +330,9 @@ __global__ void __launch_bounds__(Shape<T, NT>::warps * 32, 1) draft_q4_kernel(D
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint4 va = q4_values_bf16(a4[i], sa), vb = q4_values_bf16(b4[i], sb);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const uint4 x = *reinterpret_cast<const uint4*>(xb + i * xstep + xrow[nt]);
-                        mma_16816(acc[0][nt], va.x, vb.x, va.y, vb.y, x.x, x.y);
-                        mma_16816(acc[1][nt], va.z, vb.z, va.w, vb.w, x.z, x.w);
-                    }
+                    const uint4 x = *reinterpret_cast<const uint4*>(xb + i * xstep + xrow);
+                    mma_16816(acc[0], va.x, vb.x, va.y, vb.y, x.x, x.y);
+                    mma_16816(acc[1], va.z, vb.z, va.w, vb.w, x.z, x.w);
                 }
             } else {
                 const float* xf = reinterpret_cast<const float*>(xb) + t * kF32Chunk;
@@ -432,7 +347,7 @@ __global__ void __launch_bounds__(Shape<T, NT>::warps * 32, 1) draft_q4_kernel(D
                     for (int m = 0; m < kF32Rows; ++m) {
                         if (m >= p.mcount) break;
                         float x[8];
-                        load8(xf + m * row + i * 8, x);
+                        load8(xf + m * row + (i ^ ((t >> 1) << 1)) * 8, x);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) { facc[0][m] = fmaf(va[e], x[e], facc[0][m]); facc[1][m] = fmaf(vb[e], x[e], facc[1][m]); }
                     }
@@ -493,76 +408,26 @@ __global__ void __launch_bounds__(Shape<T, NT>::warps * 32, 1) draft_q4_kernel(D
         combine_best<31>(ms, p.k);
         if (lane == 0) ms.store(p.part + ((size_t)m * gridDim.x + blockIdx.x) * 2 + seg);
     }
-    __threadfence();
-    __syncthreads();
-    // the CTAs whose panels touch a draft slot are neighbours; the one among them that ends last merges their states
-    auto first_cta = [&](int slot) -> int {                                  // the first whose panels reach beyond the slot's first
-        const long long n = gridDim.x, lo = (long long)slot * p.panels;
-        long long c = lo * n / total;
-        while (c > 0 && total * c / n > lo) --c;
-        while (total * (c + 1) / n <= lo) ++c;
-        return (int)c;
-    };
-    auto last_cta = [&](int slot) -> int {                                   // the last whose panels begin before the slot's end
-        const long long n = gridDim.x, hi = (long long)(slot + 1) * p.panels;
-        long long c = hi * n / total;
-        if (c > n - 1) c = n - 1;
-        while (total * c / n >= hi) --c;
-        while (c < n - 1 && total * (c + 1) / n < hi) ++c;
-        return (int)c;
-    };
-    if (tid < segs) {
-        const int slot = slot0 + tid, touch = last_cta(slot) - first_cta(slot) + 1;
-        const bool mine = atomicAdd(p.counter + slot, 1u) == (unsigned)touch - 1u;
-        if (mine) p.counter[slot] = 0u;
-        sh->merge[tid] = mine ? 1 : 0;
-    }
-    __syncthreads();
-    __threadfence();
-    for (int seg = 0; seg < segs; ++seg) {
-        if (!sh->merge[seg]) continue;
-        const int slot = slot0 + seg, c0 = first_cta(slot), c1 = last_cta(slot);
-        for (int m = warp; m < p.mcount; m += kWarps) {
-            RunState fs;
-            fs.init();
-            for (int c = c0 + lane; c <= c1; c += 32) {
-                const int which = slot - (int)(total * c / gridDim.x / p.panels);          // the slot is the CTA's first or second
-                fs.absorb(load_partial_cg(p.part + ((size_t)m * gridDim.x + c) * 2 + which));
-            }
-            combine_best<31>(fs, p.k);
-            if (lane == 0) {
-                const int row = p.m0 + m;
-                const float lse = fs.mx + logf(fs.sum);
-                p.out_lse[(size_t)row * p.slots + slot] = lse;
-#pragma unroll
-                for (int j = 0; j < kTopSlots; ++j)
-                    if (j < p.k) {
-                        const size_t o = ((size_t)row * p.slots + slot) * p.k + j;
-                        p.out_topk_id[o] = fs.id[j];
-                        p.out_topk_lp[o] = fs.val[j] - lse;
-                    }
-            }
-        }
-    }
+    draft_q4_finish(p, p.panels, 0, 1, slot0, segs, sh->merge);
 }
 
-int panels_of(const ctcsd_config& c) { return (c.V + 1 + kPanel - 1) / kPanel; }
-int blocks_of(const ctcsd_config& c) { return (c.H + kBlock - 1) / kBlock; }
+int panels_of(const ctcsd_config& c) { return (c.V + 1 + kQ4Panel - 1) / kQ4Panel; }
+int blocks_of(const ctcsd_config& c) { return (c.H + kQ4Block - 1) / kQ4Block; }
 
 constexpr size_t kSmemBudget = kMaxDynamicSmem - 1024;                       // (1 KB of every CTA is the system's)
 
-template <typename T, int NT>
+template <typename T>
 size_t fixed_smem(int blocks, int rows) {
-    return x_bytes<T>(blocks, rows) + sizeof(RingState) + sizeof(DraftPartial) * 2 * Shape<T, NT>::warps * (sizeof(T) == 2 ? 8 * NT : kF32Rows);
+    return x_bytes<T>(blocks, rows) + sizeof(RingState) + sizeof(DraftPartial) * 2 * Shape<T>::warps * (sizeof(T) == 2 ? 8 : kF32Rows);
 }
 
 // Ring geometry: blocks of a slot, slots of a warp.  False where there is no room for two blocks a warp.
-template <typename T, int NT>
+template <typename T>
 bool ring_shape(DraftQ4Params& p) {
-    constexpr size_t warps = Shape<T, NT>::warps;
-    const size_t fixed = fixed_smem<T, NT>(p.blocks, p.mcount);
+    constexpr size_t warps = Shape<T>::warps;
+    const size_t fixed = fixed_smem<T>(p.blocks, p.mcount);
     if (fixed > kSmemBudget) return false;
-    const size_t bb = (size_t)block_bytes(p.group), most = (kSmemBudget - fixed) / (warps * bb);        // blocks there is room for, a warp
+    const size_t bb = (size_t)q4_block_bytes(p.group), most = (kSmemBudget - fixed) / (warps * bb);        // blocks there is room for, a warp
     if (most < 2) return false;
     // two slots, of 8 blocks at most; three where they are small then
     p.piece = (int)(most / 2 < 8 ? most / 2 : 8);
@@ -571,15 +436,15 @@ bool ring_shape(DraftQ4Params& p) {
     return true;
 }
 
-template <typename T, int NT>
+template <typename T>
 int launch_pass(Handle* h, cudaStream_t s, DraftQ4Params& p) {
-    if (!ring_shape<T, NT>(p)) return CTCSD_ERR_UNSUPPORTED;
-    const size_t smem = fixed_smem<T, NT>(p.blocks, p.mcount) + (size_t)Shape<T, NT>::warps * p.nring * p.piece * block_bytes(p.group);
-    auto kern = draft_q4_kernel<T, NT>;
-    CTCSD_CUDA_CHECK(h, prepare_kernel(h, sizeof(T) == 4 ? kPrepDraftQ4F32 : (NT == 1 ? kPrepDraftQ4 : kPrepDraftQ4x2), kern));
+    if (!ring_shape<T>(p)) return CTCSD_ERR_UNSUPPORTED;
+    const size_t smem = fixed_smem<T>(p.blocks, p.mcount) + (size_t)Shape<T>::warps * p.nring * p.piece * q4_block_bytes(p.group);
+    auto kern = draft_q4_kernel<T>;
+    CTCSD_CUDA_CHECK(h, prepare_kernel(h, sizeof(T) == 4 ? kPrepDraftQ4F32 : kPrepDraftQ4, kern));
     const long long total = (long long)p.panels * p.slots;
     const unsigned grid = (unsigned)(total < h->num_sms ? total : h->num_sms);        // (total >= slots: a range touches two slots at most)
-    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(grid), dim3(Shape<T, NT>::warps * 32), smem, s, 1, p));
+    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(grid), dim3(Shape<T>::warps * 32), smem, s, 1, p));
     h->launches++;
     return CTCSD_OK;
 }
@@ -595,7 +460,7 @@ extern "C" int ctcsd_weights_q4_bytes(const ctcsd_config* cfg, int group, size_t
     if (!cfg || !out_bytes || !group_ok(group)) return CTCSD_ERR_INVALID_ARG;
     const int rc = validate_config(*cfg);
     if (rc != CTCSD_OK) return rc;
-    *out_bytes = (size_t)cfg->T * panels_of(*cfg) * blocks_of(*cfg) * block_bytes(group);
+    *out_bytes = (size_t)cfg->T * panels_of(*cfg) * blocks_of(*cfg) * q4_block_bytes(group);
     return CTCSD_OK;
 }
 
@@ -639,21 +504,29 @@ extern "C" int ctcsd_draft_logits_q4(ctcsd_handle* hh, void* stream, int M, cons
     const DeviceGuard on(h->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool bf16 = c.dtype == CTCSD_DTYPE_BF16;
-    // rows of a pass: 16 (float32: 4), or as many as leave the ring room
+    // more than 8 rows: the tensor memory's kernel, whose cost hardly depends on the rows (7B shape: 8 rows 108 us here, 16 rows 185 us there)
+    if (bf16 && M > 8 && c.H >= 64) {
+        for (int m0 = 0; m0 < M; m0 += kDraftQ4TcRows) {
+            p.m0 = m0;
+            p.mcount = M - m0 < kDraftQ4TcRows ? M - m0 : kDraftQ4TcRows;
+            const int rc = launch_draft_q4_tc(h, s, p);
+            if (rc != CTCSD_OK) return rc;
+        }
+        return CTCSD_OK;
+    }
+    // rows of a pass: 8 (float32: 4), or as many as leave the rings room
     auto fits = [&](int rows) {
         DraftQ4Params q = p;
         q.mcount = rows;
-        return !bf16 ? ring_shape<float, 1>(q) : (rows > 8 ? ring_shape<__nv_bfloat16, 2>(q) : ring_shape<__nv_bfloat16, 1>(q));
+        return bf16 ? ring_shape<__nv_bfloat16>(q) : ring_shape<float>(q);
     };
-    int per_pass = bf16 ? 16 : kF32Rows;
+    int per_pass = bf16 ? 8 : kF32Rows;
     if (per_pass > M) per_pass = M;
     while (per_pass > 1 && !fits(per_pass)) per_pass = (per_pass + 1) / 2;
     for (int m0 = 0; m0 < M; m0 += per_pass) {
         p.m0 = m0;
         p.mcount = M - m0 < per_pass ? M - m0 : per_pass;
-        int rc;
-        if (!bf16) rc = launch_pass<float, 1>(h, s, p);
-        else rc = p.mcount > 8 ? launch_pass<__nv_bfloat16, 2>(h, s, p) : launch_pass<__nv_bfloat16, 1>(h, s, p);
+        const int rc = bf16 ? launch_pass<__nv_bfloat16>(h, s, p) : launch_pass<float>(h, s, p);
         if (rc != CTCSD_OK) return rc;
     }
     return CTCSD_OK;

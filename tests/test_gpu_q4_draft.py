@@ -78,7 +78,8 @@ def test_logits_selection_and_lse(dtype, M, H, V, T, k, group):
 
 
 @pytest.mark.parametrize("dtype,M,H,V,group", [("bf16", 2, 10240, 200, 32), ("bf16", 12, 5120, 300, 64), ("bf16", 20, 8192, 64, 128), ("fp32", 5, 8192, 60, 64),
-                                               ("fp32", 2, 10240, 40, 32), ("bf16", 33, 1536, 2500, 128)])
+                                               ("fp32", 2, 10240, 40, 32), ("bf16", 33, 1536, 2500, 128), ("bf16", 70, 1088, 777, 64),
+                                               ("bf16", 130, 72, 400, 32), ("bf16", 9, 64, 3, 32), ("bf16", 64, 4096, 3000, 128)])
 def test_long_rows_and_several_passes(dtype, M, H, V, group):
     c = _Case(dtype, M, H, V, 2, 4, group, mapped=True)
     c.run()
@@ -110,7 +111,7 @@ def test_packed_weights_are_laid_out_as_described():
         for v in range(32):
             for h0 in range(0, 256, 8):
                 panel, r, kb, e = v // 16, v % 16, h0 // 128, h0 % 128
-                w = int(words[t, panel, kb, 128 * (r // 8) + 16 * (r % 8) + 4 * (e // 32) + e % 32 // 8])
+                w = int(words[t, panel, kb, 128 * (r // 8) + 16 * (r % 8) + 4 * (e // 32) + (e % 32 // 8 ^ (2 if e >= 64 else 0))])
                 got = [((w | w << 32) >> bit) & 15 for bit in u.WORD_BITS]
                 want = list(q[t, v, h0:h0 + 8]) if v <= V and h0 < H else [0] * 8
                 assert got == want
