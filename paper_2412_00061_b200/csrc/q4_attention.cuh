@@ -33,6 +33,7 @@ constexpr int kAq4MaxB = 1024;
 constexpr int kAq4Header = 4;            // ints: blocks per kv head, spans
 constexpr int kAq4SimpleRows = 64, kAq4SimpleKeys = 64, kAq4SimplePerSm = 2;
 constexpr int kAq4MmaRows = 16, kAq4MmaKeys = 128;
+constexpr int kAq4TcKeys = 128;
 
 // The plan in shared memory.
 struct PlanQ4 {
@@ -184,5 +185,7 @@ __device__ __forceinline__ long long out_rows(const AttnQ4Params& a) { return (l
 
 // bf16, up to 16 query rows of a kv head.
 int launch_attention_q4_mma(Handle* h, cudaStream_t s, const AttnQ4Params& p);
+// bf16, more: tiles of TR (128 or 256) rows.
+int launch_attention_q4_tc(Handle* h, cudaStream_t s, const AttnQ4Params& p, int TR);
 
 }  // namespace ctcsd

@@ -22,30 +22,14 @@ constexpr int kSimpleThreads = 256;
 
 template <bool B> struct Flag { static constexpr bool value = B; };
 
-template <typename T> __device__ __forceinline__ float4 load4(const T* p);
-template <> __device__ __forceinline__ float4 load4<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
-template <> __device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16* p) {
-    const uint2 w = *reinterpret_cast<const uint2*>(p);
-    return make_float4(bf16lo(w.x), bf16hi(w.x), bf16lo(w.y), bf16hi(w.y));
-}
 template <typename T> __device__ __forceinline__ void store4(T* p, float4 v);
 template <> __device__ __forceinline__ void store4<float>(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
 template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* p, float4 v) {
     const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
     *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
-template <typename T> __device__ __forceinline__ void values8(uint32_t w, uint32_t so, float (&v)[8]);
-template <> __device__ __forceinline__ void values8<float>(uint32_t w, uint32_t so, float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = q4_value_f32(w, i, bf16lo(so), bf16hi(so));
-}
-template <> __device__ __forceinline__ void values8<__nv_bfloat16>(uint32_t w, uint32_t so, float (&v)[8]) {
-    const uint4 u = q4_values_bf16(w, so);
-    v[0] = bf16lo(u.x); v[1] = bf16hi(u.x); v[2] = bf16lo(u.y); v[3] = bf16hi(u.y);
-    v[4] = bf16lo(u.z); v[5] = bf16hi(u.z); v[6] = bf16lo(u.w); v[7] = bf16hi(u.w);
-}
 
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kSimpleThreads, kAq4SimplePerSm) attention_q4_simple_kernel(AttnQ4Params p) {
     constexpr int TR = kAq4SimpleRows, KB = kAq4SimpleKeys, ST = D + 4, PS = KB + 4, DC = D / 64, W = D / 8;
     extern __shared__ __align__(16) float sm[];
@@ -73,7 +57,7 @@ __global__ void __launch_bounds__(kSimpleThreads, kAq4SimplePerSm) attention_q4_
         for (int i = tid; i < TR * (D / 4); i += kSimpleThreads) {
             const int r = i / (D / 4), c = i - r * (D / 4);
             *reinterpret_cast<float4*>(Qs + r * ST + 4 * c) =
-                r < nrows ? load4(static_cast<const T*>(p.Q) + out_row(r) * D + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
+                r < nrows ? *reinterpret_cast<const float4*>(static_cast<const float*>(p.Q) + out_row(r) * D + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
         float acc[4][4 * DC], ref[4], sum[4];
 #pragma unroll
@@ -90,9 +74,11 @@ __global__ void __launch_bounds__(kSimpleThreads, kAq4SimplePerSm) attention_q4_
                 if (k < nkey) {
                     if (cached) {
                         const size_t a = (pair * p.Lcap + key0 + k) * W + c;
-                        values8<T>(q[a], so[a >> 2], v);
+                        const uint32_t w = q[a], pr = so[a >> 2];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = q4_value_f32(w, e, bf16lo(pr), bf16hi(pr));
                     } else {
-                        load8(static_cast<const T*>(tree) + ((pair * p.max_nodes + key0 + k) * W + c) * 8, v);
+                        load8(static_cast<const float*>(tree) + ((pair * p.max_nodes + key0 + k) * W + c) * 8, v);
                     }
                 }
                 float* dst = Ts + k * ST + 8 * c;
@@ -213,7 +199,7 @@ __global__ void __launch_bounds__(kSimpleThreads, kAq4SimplePerSm) attention_q4_
                 const size_t orow = out_row(r);
                 if (!CTCSD_IN_BOUNDS(p.status, 132, orow, out_rows(p))) continue;
                 const float inv = s > 0.f ? 1.f / s : (s == 0.f ? 0.f : s);  // a NaN sum stays a NaN
-                T* out = static_cast<T*>(p.O) + orow * D;
+                float* out = static_cast<float*>(p.O) + orow * D;
 #pragma unroll
                 for (int c = 0; c < DC; ++c)
                     store4(out + 64 * c + 4 * tx, make_float4(acc[i][4 * c] * inv, acc[i][4 * c + 1] * inv, acc[i][4 * c + 2] * inv, acc[i][4 * c + 3] * inv));
@@ -319,11 +305,11 @@ int launch_merge(Handle* h, cudaStream_t s, const AttnQ4Params& p, int TR, int K
     return CTCSD_OK;
 }
 
-template <typename T, int D>
+template <int D>
 int launch_simple(Handle* h, cudaStream_t s, const AttnQ4Params& p) {
     constexpr int TR = kAq4SimpleRows, KB = kAq4SimpleKeys;
     const size_t smem = sizeof(float) * (TR * (D + 4) + KB * (D + 4) + TR * (KB + 4)) + sizeof(int) * PlanQ4::ints(p.B);
-    auto kern = attention_q4_simple_kernel<T, D>;
+    auto kern = attention_q4_simple_kernel<D>;
     CTCSD_CUDA_CHECK(h, prepare_kernel(h, kPrepAttnQ4Simple, kern));
     CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(h->num_sms * kAq4SimplePerSm), dim3(kSimpleThreads), smem, s, 1, p));
     h->launches++;
@@ -336,6 +322,7 @@ bool few_rows(const ctcsd_config& c) { return c.dtype == CTCSD_DTYPE_BF16 && c.m
 struct Form { int TR, KB, spans; };
 Form form_of(const ctcsd_config& c) {
     if (few_rows(c)) return {kAq4MmaRows, kAq4MmaKeys, kLayoutSms};
+    if (c.dtype == CTCSD_DTYPE_BF16) return {c.max_nodes * (c.Hq / c.Hkv) <= 128 ? 128 : 256, kAq4TcKeys, kLayoutSms};
     return {kAq4SimpleRows, kAq4SimpleKeys, kLayoutSms * kAq4SimplePerSm};
 }
 
@@ -403,8 +390,8 @@ extern "C" int ctcsd_tree_attention_q4(ctcsd_handle* hh, void* stream, void* wor
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     int rc;
     if (few_rows(c)) rc = launch_attention_q4_mma(h, s, p);
-    else if (c.dtype == CTCSD_DTYPE_BF16) rc = c.D == 64 ? launch_simple<__nv_bfloat16, 64>(h, s, p) : launch_simple<__nv_bfloat16, 128>(h, s, p);
-    else rc = c.D == 64 ? launch_simple<float, 64>(h, s, p) : launch_simple<float, 128>(h, s, p);
+    else if (c.dtype == CTCSD_DTYPE_BF16) rc = launch_attention_q4_tc(h, s, p, f.TR);
+    else rc = c.D == 64 ? launch_simple<64>(h, s, p) : launch_simple<128>(h, s, p);
     if (rc != CTCSD_OK) return rc;
     if (c.dtype == CTCSD_DTYPE_BF16) return c.D == 64 ? launch_merge<__nv_bfloat16, 64>(h, s, p, f.TR, f.KB) : launch_merge<__nv_bfloat16, 128>(h, s, p, f.TR, f.KB);
     return c.D == 64 ? launch_merge<float, 64>(h, s, p, f.TR, f.KB) : launch_merge<float, 128>(h, s, p, f.TR, f.KB);
