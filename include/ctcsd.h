@@ -376,7 +376,7 @@ int ctcsd_evict_rows(ctcsd_handle* h, void* stream, void* workspace, size_t work
  * Eight consecutive values 0..7 share a 32-bit word: the levels of 0, 1, 2, 3, 4, 5, 7 begin at bits 3, 19, 7, 23, 11, 27, 15, and that of 6
  * has its lowest bit at bit 31 and the others at bits 0..2.
  * Quantising, every step rounded to float32 (lo, hi: least and largest value of the group):
- *   scale = bfloat16((hi - lo) / 15);  origin = bfloat16(lo - 16 scale);
+ *   scale = bfloat16((hi - lo) * (1/15));  origin = bfloat16(lo - 16 scale);
  *   q = (v - origin) / scale - 16, rounded half to even and clamped to 0..15;  0 where scale = 0.
  * A group that holds a NaN or an infinity, or whose scale or origin would not be finite, stands for NaN (scale 0, origin NaN).
  *

@@ -791,7 +791,7 @@ def q4_quantize(v: np.ndarray, group: int) -> Tuple[np.ndarray, np.ndarray, np.n
         for i in range(groups):
             w = f[..., i * group:(i + 1) * group]
             lo, hi = w.min(axis=-1), w.max(axis=-1)
-            s = round_to_bf16((hi - lo) / np.float32(15.0)).astype(np.float32)
+            s = round_to_bf16((hi - lo) * np.float32(1.0 / 15.0)).astype(np.float32)
             o = round_to_bf16(lo - np.float32(16.0) * s).astype(np.float32)
             bad = ~(np.isfinite(s) & np.isfinite(o))
             s = np.where(bad, np.float32(0), s)

@@ -87,7 +87,7 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 // Scale and origin of a group with the limits lo, hi (float32 steps, each rounded to nearest).  A group that holds a NaN or an
 // infinity, or whose range leaves the type: scale 0, origin NaN.
 __device__ __forceinline__ uint32_t q4_scale_origin(float lo, float hi) {
-    const float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f)));
+    const float s = __bfloat162float(__float2bfloat16_rn(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f)));
     const float o = __bfloat162float(__float2bfloat16_rn(__fsub_rn(lo, __fmul_rn(16.f, s))));
     if (!(fabsf(s) < INFINITY) || !(fabsf(o) < INFINITY)) return 0x7fc00000u;
     return (__float_as_uint(s) >> 16) | (__float_as_uint(o) & 0xffff0000u);

@@ -24,13 +24,13 @@ struct AttnQ4Params {
     int B, Hq, Hkv, D, max_nodes, Lcap, grp;      // grp = Hq / Hkv
     float scale;
     int* status;
-    int* plan;                           // workspace: header, blk_off (written by CTA 0, read by the merge)
+    int4* cuts;                          // workspace: [span] (written by its CTA, read by the merge): kv head, sequence, tile and last span of the tile
+                                         // that the span continues from the one before it, -1 if there is none or a span further back began it
     float2* part_ml;                     // workspace: [span][2][TR] (reference in log2 units, sum)
     float4* part_o;                      // workspace: [span][2][D/4][TR]
 };
 
 constexpr int kAq4MaxB = 1024;
-constexpr int kAq4Header = 4;            // ints: blocks per kv head, spans
 constexpr int kAq4SimpleRows = 64, kAq4SimpleKeys = 64, kAq4SimplePerSm = 2;
 constexpr int kAq4MmaRows = 16, kAq4MmaKeys = 128;
 constexpr int kAq4TcKeys = 128;
@@ -121,8 +121,8 @@ inline bool plan_q4_fits(int B, int max_nodes, int grp, int TR, int KB, int Lcap
 
 #ifdef __CUDACC__
 
-// Fills the plan; executed by the whole block, ends with a barrier.  Block 0 also leaves it for the merge kernel.  A sequence whose
-// lengths would read outside its arrays is reported (by block 0) and takes no part.
+// Fills the plan; executed by the whole block, ends with a barrier.  A sequence whose lengths would read outside its arrays is
+// reported (by block 0) and takes no part.
 __device__ inline SpansQ4 plan_q4_build(PlanQ4& p, const AttnQ4Params& a, int TR, int KB, int spans) {
     const int lane = threadIdx.x & 31;
     if (threadIdx.x < 32) {
@@ -154,14 +154,35 @@ __device__ inline SpansQ4 plan_q4_build(PlanQ4& p, const AttnQ4Params& a, int TR
         if (lane == 0) p.blk_off[0] = 0;
     }
     __syncthreads();
-    const SpansQ4 m = spans_of(p.blk_off[a.B], a.Hkv, spans);
-    if (blockIdx.x == 0) {
+    return spans_of(p.blk_off[a.B], a.Hkv, spans);
+}
+
+// What the block does besides its span: the rows of unused nodes become 0 and -inf (all heads of a node are neighbours), and the merge
+// is told whether the span continues a tile.  `at`: the span's first part.
+template <typename T, int D>
+__device__ inline void attn_q4_sides(const AttnQ4Params& a, const PlanQ4& p, const SpansQ4& m, const WalkQ4& at, bool more) {
+    constexpr int E = 16 / (int)sizeof(T);
+    const int words = a.Hq * D / E;
 #pragma unroll 1
-        for (int b = threadIdx.x; b <= a.B; b += blockDim.x)
-            if (CTCSD_IN_BOUNDS(a.status, 131, b, kAq4MaxB + 1)) a.plan[kAq4Header + b] = p.blk_off[b];
-        if (threadIdx.x == 0) { a.plan[0] = m.per_head; a.plan[1] = m.count; }
+    for (int i = blockIdx.x; i < a.B * a.max_nodes; i += gridDim.x) {
+        const int b = i / a.max_nodes;
+        if (i - b * a.max_nodes < p.n[b]) continue;
+        uint4* out = reinterpret_cast<uint4*>(static_cast<T*>(a.O) + (size_t)i * a.Hq * D);
+#pragma unroll 1
+        for (int w = threadIdx.x; w < words; w += blockDim.x)
+            if (CTCSD_IN_BOUNDS(a.status, 131, (long long)i * words + w, (long long)a.B * a.max_nodes * words)) out[w] = make_uint4(0u, 0u, 0u, 0u);
+        if (a.lse)
+#pragma unroll 1
+            for (int h = threadIdx.x; h < a.Hq; h += blockDim.x) a.lse[(size_t)i * a.Hq + h] = -INFINITY;
     }
-    return m;
+    if (threadIdx.x == 0) {
+        int4 cut = make_int4(-1, 0, 0, 0);
+        if (more && at.blk0 > 0) {
+            const long long x0 = (long long)at.g * m.per_head + p.blk_off[at.b] + at.t * at.nblk;
+            if (m.span_of(x0) == (int)blockIdx.x - 1) cut = make_int4(at.g, at.b, at.t, m.span_of(x0 + at.nblk - 1));
+        }
+        a.cuts[blockIdx.x] = cut;
+    }
 }
 
 __device__ __forceinline__ float exp2_q4(float x) {

@@ -19,25 +19,27 @@ template <int D> struct RawQ4 {
         if (D == 128 || !(past & 1)) return past;
         return past == rows ? past - 1 : past + 1;
     }
-    __device__ static __forceinline__ uint32_t copied(long long row0, int n, long long rows) {
-        const long long f = first(row0), e = end(row0, n, rows);
-        return (uint32_t)n * kLevels + (e > f ? (uint32_t)(e - f) * kPairs : 0u);
-    }
     // The pairs of row 0 of the block, behind levels for `keys` rows.
     __device__ static __forceinline__ const uint32_t* pairs(const unsigned char* dst, int keys, long long row0) {
         return reinterpret_cast<const uint32_t*>(dst + keys * kLevels + (D == 64 && (row0 & 1) ? kPairs : 0));
     }
-    // Asks for the block.  One thread, which has announced the bytes of copied() and arrives on the barrier afterwards.
-    __device__ static __forceinline__ void request(unsigned char* dst, const uint32_t* levels, const uint32_t* so, int keys, long long row0,
-                                                   int n, long long rows, uint64_t* bar, uint64_t policy) {
+    // Asks for the block's levels, or its pairs.  One thread each; an arrival on the barrier is part of it.
+    __device__ static __forceinline__ void request_levels(unsigned char* dst, const uint32_t* levels, long long row0, int n, uint64_t* bar, uint64_t policy) {
+        tc::mbar_arrive_expect_tx(bar, (uint32_t)n * kLevels);
         tc::bulk_load_1d(dst, levels + row0 * (kLevels / 4), (uint32_t)n * kLevels, bar, policy);
+    }
+    __device__ static __forceinline__ void request_pairs(unsigned char* dst, const uint32_t* so, int keys, long long row0, int n, long long rows,
+                                                         uint64_t* bar, uint64_t policy) {
         const long long f = first(row0), e = end(row0, n, rows);
-        if (e > f) tc::bulk_load_1d(dst + keys * kLevels, so + f * (kPairs / 4), (uint32_t)(e - f) * kPairs, bar, policy);
+        const uint32_t bytes = e > f ? (uint32_t)(e - f) * kPairs : 0u;
+        tc::mbar_expect_tx(bar, bytes);
+        if (bytes) tc::bulk_load_1d(dst + keys * kLevels, so + f * (kPairs / 4), bytes, bar, policy);
         if (D == 64 && e < row0 + n) {                                       // the array's last row, which stands alone
             const uint2 w = *reinterpret_cast<const uint2*>(so + e * (kPairs / 4));
             *reinterpret_cast<uint2*>(dst + keys * kLevels + (e - f) * kPairs) = w;
             tc::fence_proxy_async();                                         // (the engine writes there again)
         }
+        tc::mbar_arrive(bar);
     }
 };
 

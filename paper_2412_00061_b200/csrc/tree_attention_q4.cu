@@ -45,7 +45,9 @@ __global__ void __launch_bounds__(kSimpleThreads, kAq4SimplePerSm) attention_q4_
     const int MW = (p.max_nodes + 63) / 64;
     const float sl2 = p.scale * kLog2e;
     WalkQ4 at;
-    for (bool more = at.init(pl, sp, p.B, KB, blockIdx.x); more; more = at.next(pl, p.B, KB)) {
+    bool more = at.init(pl, sp, p.B, KB, blockIdx.x);
+    attn_q4_sides<float, D>(p, pl, sp, at, more);
+    for (; more; more = at.next(pl, p.B, KB)) {
         const int g = at.g, b = at.b, kv = pl.kv[b], n = pl.n[b], row0 = at.t * TR;
         const int nrows = n * p.grp - row0 < TR ? n * p.grp - row0 : TR;
         const size_t pair = (size_t)b * p.Hkv + g;
@@ -215,42 +217,24 @@ __global__ void __launch_bounds__(kSimpleThreads, kAq4SimplePerSm) attention_q4_
 }
 
 // ---------------------------------------------------------------------------------------
-// Merge.  A block looks after 32 rows (lane = row, so that the transposed parts are read in whole lines; warps share the head
-// dimension) of a (kv head, sequence): rows of unused nodes become zero, rows of tiles that were cut are joined in span order,
-// four parts at a time; the result does not depend on timing.
+// Merge of tiles that were cut.  A block for a span and 32 columns: if the span is the second of a tile's, the block joins the tile's parts in span
+// order, four at a time (the result does not depend on timing), else it has nothing to do.  A thread holds eight columns of a row;
+// neighbours take neighbouring rows, so that the transposed parts are read in whole lines.
 // ---------------------------------------------------------------------------------------
+constexpr int kMergeThreads = 256;
+
 template <typename T, int D>
-__global__ void __launch_bounds__(D * 4) attention_q4_merge_kernel(AttnQ4Params p, int TR, int KB, unsigned units) {
+__global__ void __launch_bounds__(kMergeThreads) attention_q4_merge_kernel(AttnQ4Params p, int TR) {
     constexpr int U = 4;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;              // a warp: columns 8 warp .. 8 warp + 7
     pdl_wait();
     pdl_trigger();
-    const int per_head = p.plan[0], spans = p.plan[1];
-    const int* blk_off = p.plan + kAq4Header;
-    const SpansQ4 sp = spans_of(per_head, p.Hkv, spans);
-    const int seq_rows = p.max_nodes * p.grp;
-    const unsigned chunks = (unsigned)(seq_rows + 31) / 32u;
-    for (unsigned u = blockIdx.x; u < units; u += gridDim.x) {
-        const unsigned pairi = u / chunks;
-        const int r = (int)(u - pairi * chunks) * 32 + lane;                 // row of the sequence
-        const int b = (int)(pairi / (unsigned)p.Hkv), g = (int)(pairi - (unsigned)b * (unsigned)p.Hkv);
-        if (r >= seq_rows) continue;
-        const int off = blk_off[b], blocks = blk_off[b + 1] - off;
-        const int n = blocks > 0 ? p.n_nodes[b] : 0;
-        const int node = r / p.grp;
-        const size_t orow = ((size_t)b * p.max_nodes + node) * p.Hq + g * p.grp + (r - node * p.grp);
-        if (!CTCSD_IN_BOUNDS(p.status, 134, orow, out_rows(p))) continue;
-        T* out = static_cast<T*>(p.O) + orow * D + 8 * warp;
-        if (node >= n) {
-            store4(out, make_float4(0.f, 0.f, 0.f, 0.f));
-            store4(out + 4, make_float4(0.f, 0.f, 0.f, 0.f));
-            if (warp == 0 && p.lse) p.lse[orow] = -INFINITY;
-            continue;
-        }
-        const int tiles = (n * p.grp + TR - 1) / TR, nblk = blocks / tiles, t = r / TR, tr = r - t * TR;
-        const long long x0 = (long long)g * per_head + off + t * nblk;
-        const int c0 = sp.span_of(x0), c1 = sp.span_of(x0 + nblk - 1);
-        if (c0 == c1) continue;                                              // finished by its span
+    const int4 cut = p.cuts[blockIdx.x];
+    if (cut.x < 0) return;
+    const int g = cut.x, b = cut.y, row0 = cut.z * TR, c0 = (int)blockIdx.x - 1, c1 = cut.w;
+    const int left = p.n_nodes[b] * p.grp - row0, nrows = left < TR ? left : TR;
+    for (int i = threadIdx.x; i < TR * 4; i += kMergeThreads) {
+        const int tr = i % TR, c8 = blockIdx.y * 4 + i / TR;                 // row of the tile, columns 8 c8 ..
+        if (tr >= nrows) continue;
         // only the first part can be one that a span begins (slot 1); the others continue a tile (slot 0)
         float ref = -INFINITY, sum = 0.f, a[8];
 #pragma unroll
@@ -259,48 +243,48 @@ __global__ void __launch_bounds__(D * 4) attention_q4_merge_kernel(AttnQ4Params 
             float2 ml[U];
             float4 o[U][2];
 #pragma unroll
-            for (int i = 0; i < U; ++i) {                                    // (the last part again past the end, with no weight)
-                const int cc = min(c + i, c1);
-                // (a span whose cut falls on the tile's first block holds it as a tile it begins)
+            for (int k = 0; k < U; ++k) {                                    // (the last part again past the end, with no weight)
+                const int cc = min(c + k, c1);
                 const size_t part = (size_t)cc * 2 + (cc == c0 ? 1 : 0);
-                ml[i] = p.part_ml[part * TR + tr];
-                o[i][0] = p.part_o[(part * (D / 4) + 2 * warp) * TR + tr];
-                o[i][1] = p.part_o[(part * (D / 4) + 2 * warp + 1) * TR + tr];
-                if (c + i > c1) ml[i] = make_float2(-INFINITY, 0.f);
+                ml[k] = p.part_ml[part * TR + tr];
+                o[k][0] = p.part_o[(part * (D / 4) + 2 * c8) * TR + tr];
+                o[k][1] = p.part_o[(part * (D / 4) + 2 * c8 + 1) * TR + tr];
+                if (c + k > c1) ml[k] = make_float2(-INFINITY, 0.f);
             }
             float top = ref;
 #pragma unroll
-            for (int i = 0; i < U; ++i) top = fmaxf(top, ml[i].x);
+            for (int k = 0; k < U; ++k) top = fmaxf(top, ml[k].x);
             const float base = top == -INFINITY ? 0.f : top;
             const float keep = exp2_q4(ref - base);
             sum *= keep;
 #pragma unroll
             for (int e = 0; e < 8; ++e) a[e] *= keep;
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const float w = exp2_q4(ml[i].x - base);
-                sum = fmaf(w, ml[i].y, sum);
-                if (!(ml[i].y != 0.f)) continue;                             // this part saw nothing
-                a[0] = fmaf(w, o[i][0].x, a[0]); a[1] = fmaf(w, o[i][0].y, a[1]);
-                a[2] = fmaf(w, o[i][0].z, a[2]); a[3] = fmaf(w, o[i][0].w, a[3]);
-                a[4] = fmaf(w, o[i][1].x, a[4]); a[5] = fmaf(w, o[i][1].y, a[5]);
-                a[6] = fmaf(w, o[i][1].z, a[6]); a[7] = fmaf(w, o[i][1].w, a[7]);
+            for (int k = 0; k < U; ++k) {
+                const float w = exp2_q4(ml[k].x - base);
+                sum = fmaf(w, ml[k].y, sum);
+                if (!(ml[k].y != 0.f)) continue;                             // this part saw nothing
+                a[0] = fmaf(w, o[k][0].x, a[0]); a[1] = fmaf(w, o[k][0].y, a[1]);
+                a[2] = fmaf(w, o[k][0].z, a[2]); a[3] = fmaf(w, o[k][0].w, a[3]);
+                a[4] = fmaf(w, o[k][1].x, a[4]); a[5] = fmaf(w, o[k][1].y, a[5]);
+                a[6] = fmaf(w, o[k][1].z, a[6]); a[7] = fmaf(w, o[k][1].w, a[7]);
             }
             ref = top;
         }
+        const int node = (row0 + tr) / p.grp;
+        const size_t orow = ((size_t)b * p.max_nodes + node) * p.Hq + g * p.grp + (row0 + tr - node * p.grp);
+        if (!CTCSD_IN_BOUNDS(p.status, 134, orow, out_rows(p))) continue;
         const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
+        T* out = static_cast<T*>(p.O) + orow * D + 8 * c8;
         store4(out, make_float4(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv));
         store4(out + 4, make_float4(a[4] * inv, a[5] * inv, a[6] * inv, a[7] * inv));
-        if (warp == 0 && p.lse) p.lse[orow] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+        if (c8 == 0 && p.lse) p.lse[orow] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * kLn2;
     }
 }
 
 template <typename T, int D>
-int launch_merge(Handle* h, cudaStream_t s, const AttnQ4Params& p, int TR, int KB) {
-    const long long units = (long long)p.B * p.Hkv * ((p.max_nodes * p.grp + 31) / 32);
-    const long long cap = (long long)h->num_sms * 16;
-    CTCSD_CUDA_CHECK(h, launch_pdl(attention_q4_merge_kernel<T, D>, dim3((unsigned)(units < cap ? units : cap)), dim3(D * 4), 0, s, 1, p, TR, KB,
-                                   (unsigned)units));
+int launch_merge(Handle* h, cudaStream_t s, const AttnQ4Params& p, int TR, int spans) {
+    CTCSD_CUDA_CHECK(h, launch_pdl(attention_q4_merge_kernel<T, D>, dim3(spans, D / 32), dim3(kMergeThreads), 0, s, 1, p, TR));
     h->launches++;
     return CTCSD_OK;
 }
@@ -326,20 +310,20 @@ Form form_of(const ctcsd_config& c) {
     return {kAq4SimpleRows, kAq4SimpleKeys, kLayoutSms * kAq4SimplePerSm};
 }
 
-// Workspace: plan, part sums, part outputs.
-struct AttnLayout { size_t plan, ml, o, total; };
+// Workspace: cuts, part sums, part outputs.
+struct AttnLayout { size_t cuts, ml, o, total; };
 AttnLayout attn_layout(const ctcsd_config& c) {
     const Form f = form_of(c);
     AttnLayout l;
-    l.plan = 0;
-    l.ml = align_up(sizeof(int) * (size_t)(kAq4Header + c.B + 1), 256);
+    l.cuts = 0;
+    l.ml = align_up(sizeof(int4) * (size_t)f.spans, 256);
     l.o = align_up(l.ml + sizeof(float2) * f.spans * 2 * f.TR, 256);
     l.total = align_up(l.o + sizeof(float) * f.spans * 2 * f.TR * (size_t)c.D, 256);
     return l;
 }
 
 bool attn_supported(const ctcsd_config& c) {
-    return c.B <= kAq4MaxB && (long long)c.B * c.Hkv * ((c.max_nodes * (c.Hq / c.Hkv) + 31) / 32) < (1ll << 31);
+    return c.B <= kAq4MaxB;
 }
 
 }  // namespace
@@ -383,7 +367,7 @@ extern "C" int ctcsd_tree_attention_q4(ctcsd_handle* hh, void* stream, void* wor
     p.scale = scale;
     p.status = status_ptr(h);
     char* ws = static_cast<char*>(workspace);
-    p.plan = reinterpret_cast<int*>(ws + l.plan);
+    p.cuts = reinterpret_cast<int4*>(ws + l.cuts);
     p.part_ml = reinterpret_cast<float2*>(ws + l.ml);
     p.part_o = reinterpret_cast<float4*>(ws + l.o);
     const DeviceGuard on(h->device);
@@ -393,6 +377,7 @@ extern "C" int ctcsd_tree_attention_q4(ctcsd_handle* hh, void* stream, void* wor
     else if (c.dtype == CTCSD_DTYPE_BF16) rc = launch_attention_q4_tc(h, s, p, f.TR);
     else rc = c.D == 64 ? launch_simple<64>(h, s, p) : launch_simple<128>(h, s, p);
     if (rc != CTCSD_OK) return rc;
-    if (c.dtype == CTCSD_DTYPE_BF16) return c.D == 64 ? launch_merge<__nv_bfloat16, 64>(h, s, p, f.TR, f.KB) : launch_merge<__nv_bfloat16, 128>(h, s, p, f.TR, f.KB);
-    return c.D == 64 ? launch_merge<float, 64>(h, s, p, f.TR, f.KB) : launch_merge<float, 128>(h, s, p, f.TR, f.KB);
+    const int spans = c.dtype == CTCSD_DTYPE_BF16 ? h->num_sms : h->num_sms * kAq4SimplePerSm;
+    if (c.dtype == CTCSD_DTYPE_BF16) return c.D == 64 ? launch_merge<__nv_bfloat16, 64>(h, s, p, f.TR, spans) : launch_merge<__nv_bfloat16, 128>(h, s, p, f.TR, spans);
+    return c.D == 64 ? launch_merge<float, 64>(h, s, p, f.TR, spans) : launch_merge<float, 128>(h, s, p, f.TR, spans);
 }

@@ -7,7 +7,7 @@
 //   O += P V    a lane's S fragment is its P fragment; the V operand pairs two keys of a column, and a lane takes the same bytes
 //               of four rows and joins halves of words, D/8 columns of its own (the order of columns is free as well).
 // One shift-and-or and half a multiply-add per value.  A warp takes 16 keys of every block and keeps maximum, sum and O of its own;
-// the eight warps' are joined when a tile ends.  One warp brings the blocks in by bulk copies, ten of them (200 KB) ahead.
+// the eight warps' are joined when a tile ends.  Four warps bring the blocks in by bulk copies, up to seven of them (140 KB) ahead.
 #include "q4_ring.cuh"
 
 #include <math.h>
@@ -16,7 +16,8 @@ namespace ctcsd {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kThreads = (kWarps + 1) * 32;
+constexpr int kProducers = 4;            // of K's levels and pairs, V's levels and pairs
+constexpr int kThreads = (kWarps + kProducers) * 32;
 constexpr int kRows = kAq4MmaRows;
 constexpr int kKeys = kAq4MmaKeys;
 constexpr int kMaxStages = 16;
@@ -66,7 +67,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     volatile int* abort_flag = &sh->abort_flag;
     if (tid == 0) {
-        for (int s = 0; s < nstages; ++s) { tc::mbar_init(&sh->full[s], 1); tc::mbar_init(&sh->empty[s], kWarps); }
+        for (int s = 0; s < nstages; ++s) { tc::mbar_init(&sh->full[s], kProducers); tc::mbar_init(&sh->empty[s], kWarps); }
         sh->abort_flag = 0;
         sh->never_set = 0;
         tc::fence_barrier_init();
@@ -77,8 +78,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
     const SpansQ4 sp = plan_q4_build(pl, p, kRows, kKeys, (int)gridDim.x);
     WalkQ4 at;
     bool more = at.init(pl, sp, p.B, kKeys, blockIdx.x);
-    if (warp == kWarps) {
-        // ---------------- producer ----------------
+    attn_q4_sides<__nv_bfloat16, D>(p, pl, sp, at, more);
+    if (warp >= kWarps) {
+        // ---------------- producers ----------------
+        // (a thread spends some 600 cycles on a request: one for all four arrays took as long as the block's copies, 281 us for 13B tokens
+        // over 16001-32767 rows)
+        const int what = warp - kWarps;
         if (lane == 0) {
             const uint64_t pol = tc::policy_evict_first();
             const long long rows = (long long)p.B * p.Hkv * p.Lcap;
@@ -93,10 +98,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
                     const long long row0 = base + (long long)blk * kKeys;
                     const int n = kv - blk * kKeys < kKeys ? kv - blk * kKeys : kKeys;
                     unsigned char* dst = ring + (size_t)s * 2 * kSide;
-                    tc::mbar_expect_tx(&sh->full[s], 2 * RawQ4<D>::copied(row0, n, rows));
-                    RawQ4<D>::request(dst, p.Kq, p.Ks, kKeys, row0, n, rows, &sh->full[s], pol);
-                    RawQ4<D>::request(dst + kSide, p.Vq, p.Vs, kKeys, row0, n, rows, &sh->full[s], pol);
-                    tc::mbar_arrive(&sh->full[s]);
+                    if (what & 1) RawQ4<D>::request_pairs(dst + (what >> 1) * kSide, what >> 1 ? p.Vs : p.Ks, kKeys, row0, n, rows, &sh->full[s], pol);
+                    else RawQ4<D>::request_levels(dst + (what >> 1) * kSide, what >> 1 ? p.Vq : p.Kq, row0, n, &sh->full[s], pol);
                 }
             }
             if (failed) {
@@ -126,15 +129,20 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
             return ((size_t)b * p.max_nodes + node) * p.Hq + at.g * p.grp + (row0 + r - node * p.grp);
         };
         // Q as operand A: rows g and g + 8, elements D/4 t .. of the head
-        uint4 qa[LW], qb[LW];
+        uint32_t qf[2 * LW][4];
         {
             const uint4 z = make_uint4(0u, 0u, 0u, 0u);
             const uint4* Qg = static_cast<const uint4*>(p.Q);
 #pragma unroll
             for (int i = 0; i < LW; ++i) {
-                qa[i] = g < nrows ? __ldg(Qg + out_row(g) * (D / 8) + t * LW + i) : z;
-                qb[i] = g + 8 < nrows ? __ldg(Qg + out_row(g + 8) * (D / 8) + t * LW + i) : z;
+                const uint4 a = g < nrows ? __ldg(Qg + out_row(g) * (D / 8) + t * LW + i) : z;
+                const uint4 b8 = g + 8 < nrows ? __ldg(Qg + out_row(g + 8) * (D / 8) + t * LW + i) : z;
+                qf[2 * i][0] = a.x; qf[2 * i][1] = b8.x; qf[2 * i][2] = a.y; qf[2 * i][3] = b8.y;
+                qf[2 * i + 1][0] = a.z; qf[2 * i + 1][1] = b8.z; qf[2 * i + 1][2] = a.w; qf[2 * i + 1][3] = b8.w;
             }
+            // (they stay in the order of the operand's registers: as loaded they would be moved there for every product)
+#pragma unroll
+            for (int i = 0; i < 2 * LW; ++i) asm volatile("" : "+r"(qf[i][0]), "+r"(qf[i][1]), "+r"(qf[i][2]), "+r"(qf[i][3]));
         }
         float o[NT][4], ref[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
 #pragma unroll
@@ -190,8 +198,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
 #pragma unroll
                         for (int i = 0; i < LW; ++i) {
                             const uint4 k = key < n ? __ldg(Kt + (size_t)key * (D / 8) + t * LW + i) : make_uint4(0u, 0u, 0u, 0u);
-                            mma_16816(s[j], qa[i].x, qb[i].x, qa[i].y, qb[i].y, k.x, k.y);
-                            mma_16816(s[j], qa[i].z, qb[i].z, qa[i].w, qb[i].w, k.z, k.w);
+                            mma_16816(s[j], qf[2 * i][0], qf[2 * i][1], qf[2 * i][2], qf[2 * i][3], k.x, k.y);
+                            mma_16816(s[j], qf[2 * i + 1][0], qf[2 * i + 1][1], qf[2 * i + 1][2], qf[2 * i + 1][3], k.z, k.w);
                         }
                     }
                     uint32_t vis[2];
@@ -269,8 +277,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const uint4 k = q4_values_bf16(kw[j][i], kso[j]);
-                        mma_16816(s[j], qa[i].x, qb[i].x, qa[i].y, qb[i].y, k.x, k.y);
-                        mma_16816(s2[j], qa[i].z, qb[i].z, qa[i].w, qb[i].w, k.z, k.w);
+                        mma_16816(s[j], qf[2 * i][0], qf[2 * i][1], qf[2 * i][2], qf[2 * i][3], k.x, k.y);
+                        mma_16816(s2[j], qf[2 * i + 1][0], qf[2 * i + 1][1], qf[2 * i + 1][2], qf[2 * i + 1][3], k.z, k.w);
                     }
 #pragma unroll
                 for (int j = 0; j < 2; ++j)

@@ -12,7 +12,7 @@
 // rescaled.  P is rounded to bf16, by 2^-8 of a weight at most, because a product takes both operands in one type and V is bf16; scores,
 // references, sums (of the unrounded weights), O and the parts are float32.
 //
-// Warp 0 brings levels in by bulk copies, warps 1 and 2 issue the products of one half each, warps 4-7 and 8-11 are the softmax warps of the
+// Warps 0 and 3 bring levels in by bulk copies, warps 1 and 2 issue the products of one half each, warps 4-7 and 8-11 are the softmax warps of the
 // halves, 12-15 make the tiles.  The softmax warps take the registers that the others give up (setmaxnreg).
 //
 // A weight of zero does not cancel a NaN.  Cached rows are seen by every row of the tile, and those behind the last are made zeros; a
@@ -84,18 +84,21 @@ __device__ __forceinline__ void halves_barrier() { asm volatile("bar.sync 1, 256
 
 template <bool B> struct Flag { static constexpr bool value = B; };
 
+// Levels of a side come in whole blocks, or in halves where shared memory has room for three blocks' only.
+template <int D, int TR> __host__ __device__ constexpr int raw_parts() { return D == 128 && TR == 256 ? 2 : 1; }
+
 template <int D, int TR>
 __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Params p, int nraw) {
     constexpr int DH = D / 64;
     constexpr int kQHalf = kHalf * D * 2;
     constexpr int kTile = kKeys * D * 2;
-    constexpr int kSide = RawQ4<D>::bytes(kKeys);
+    constexpr int kParts = raw_parts<D, TR>(), kPart = kKeys / kParts, kSlot = RawQ4<D>::bytes(kPart);
     extern __shared__ __align__(1024) unsigned char dyn[];
     unsigned char* Qs = dyn;                                   // [TR / 128][DH][128 rows][128 B]
     unsigned char* Ks = Qs + TR / kHalf * kQHalf;              // [kStages][DH][128 keys][128 B]
     unsigned char* Vs = Ks + kStages * kTile;
-    unsigned char* raw = Vs + kStages * kTile;                 // [nraw][one side of a block]
-    TcShared* sh = reinterpret_cast<TcShared*>(raw + nraw * kSide);
+    unsigned char* raw = Vs + kStages * kTile;                 // [side][nraw][kPart rows]
+    TcShared* sh = reinterpret_cast<TcShared*>(raw + 2 * nraw * kSlot);
     PlanQ4 pl;
     pl.carve(reinterpret_cast<int*>(sh + 1), p.B);
     if ((tc::smem_u32(dyn) & 1023u) != 0u) {                   // uniform over the CTA
@@ -106,10 +109,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
     volatile int* abort_flag = &sh->abort_flag;
     if (tid == 0) {
         tc::mbar_init(&sh->q_full, 8);
-        for (int s = 0; s < nraw; ++s) { tc::mbar_init(&sh->raw_full[s], 1); tc::mbar_init(&sh->raw_empty[s], 4); }
+        for (int s = 0; s < 2 * nraw; ++s) { tc::mbar_init(&sh->raw_full[s], 2); tc::mbar_init(&sh->raw_empty[s], 2); }
         for (int s = 0; s < kStages; ++s) {
-            tc::mbar_init(&sh->k_full[s], 4); tc::mbar_init(&sh->k_empty[s], 2);
-            tc::mbar_init(&sh->v_full[s], 4); tc::mbar_init(&sh->v_empty[s], 2);
+            tc::mbar_init(&sh->k_full[s], 2); tc::mbar_init(&sh->k_empty[s], 2);
+            tc::mbar_init(&sh->v_full[s], 2); tc::mbar_init(&sh->v_empty[s], 2);
         }
         for (int s = 0; s < 2; ++s) {
             for (int e = 0; e < 2; ++e) { tc::mbar_init(&sh->s_full[s][e], 1); tc::mbar_init(&sh->p_full[s][e], 4); }
@@ -134,39 +137,36 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
     bool failed = false;
     WalkQ4 at;
     bool more = at.init(pl, sp, p.B, kKeys, blockIdx.x);
+    attn_q4_sides<__nv_bfloat16, D>(p, pl, sp, at, more);
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsAux));
-        if (warp == 0) {
-            // ---------------- levels ----------------
+        if (warp == 0 || warp == 3) {
+            // ---------------- levels: of K and of V ----------------
             if (lane == 0) {
+                const int side = warp == 0 ? 0 : 1;
                 const uint64_t pol = tc::policy_evict_last();
                 const long long rows = (long long)p.B * p.Hkv * p.Lcap;
+                unsigned char* ring = raw + side * nraw * kSlot;
+                uint64_t *full = sh->raw_full + side * nraw, *empty = sh->raw_empty + side * nraw;
                 int s = 0, fill = 0;
                 uint32_t phase = 1u;
                 for (; more && !failed; more = at.next(pl, p.B, kKeys)) {
                     const long long base = ((long long)at.b * p.Hkv + at.g) * p.Lcap;
                     const int kv = pl.kv[at.b];
-                    for (int blk = at.blk0; blk < at.blk1 && blk < at.cached && !failed; ++blk) {
-                        const long long row0 = base + (long long)blk * kKeys;
-                        const int n = kv - blk * kKeys < kKeys ? kv - blk * kKeys : kKeys;
-                        const uint32_t bytes = RawQ4<D>::copied(row0, n, rows);
-#pragma unroll
-                        for (int side = 0; side < 2; ++side) {
-                            if (!tc::mbar_wait_suspended(&sh->raw_empty[s], phase, abort_flag)) { failed = true; break; }
-                            tc::mbar_expect_tx(&sh->raw_full[s], bytes);
-                            RawQ4<D>::request(raw + s * kSide, side ? p.Vq : p.Kq, side ? p.Vs : p.Ks, kKeys, row0, n, rows, &sh->raw_full[s], pol);
-                            tc::mbar_arrive(&sh->raw_full[s]);
-                            ++fill;
-                            if (++s == nraw) { s = 0; phase ^= 1u; }
-                        }
+                    for (int row = at.blk0 * kKeys; row < at.blk1 * kKeys && row < kv; row += kPart, ++fill) {
+                        const int n = kv - row < kPart ? kv - row : kPart;
+                        if (!tc::mbar_wait_suspended(empty + s, phase, abort_flag)) { failed = true; break; }
+                        RawQ4<D>::request_levels(ring + s * kSlot, side ? p.Vq : p.Kq, base + row, n, full + s, pol);
+                        RawQ4<D>::request_pairs(ring + s * kSlot, side ? p.Vs : p.Ks, kPart, base + row, n, rows, full + s, pol);
+                        if (++s == nraw) { s = 0; phase ^= 1u; }
                     }
                 }
                 if (failed) {
                     give_up(sh, p.status, 62);
                     for (int back = 1; back <= nraw && back <= fill; ++back) {              // copies in flight land before the exit
                         const int j = fill - back;
-                        tc::mbar_wait_suspended(&sh->raw_full[j % nraw], (uint32_t)(j / nraw) & 1u, &sh->never_set, 1ll << 24);
+                        tc::mbar_wait_suspended(full + j % nraw, (uint32_t)(j / nraw) & 1u, &sh->never_set, 1ll << 24);
                     }
                 }
             }
@@ -254,14 +254,17 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
     } else if (warp >= 12) {
         // ---------------- tiles of values ----------------
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsMaker));
-        const int mw = warp - 12;
-        // levels: a lane takes chunk c (32 values) of a row, 8 rows (D = 64: 16) of the warp's 32 at a time.  Its four words go to four 16-byte places of
-        // the row; lanes of the upper 64 columns begin with word 2, so that a store's lanes meet in no bank.
+        // Two warps make K's tiles, two V's.
+        const int mw = (warp - 12) & 1, side = (warp - 12) >> 1;
+        // levels: a lane takes chunk c (32 values) of a row, 8 rows (D = 64: 16) at a time.  Its four words go to four 16-byte places of the row; lanes of
+        // the upper 64 columns begin with word 2, so that a store's lanes meet in no bank.
         constexpr int CH = D / 32, RI = 32 / CH;               // chunks of a row, rows an instruction
-        const int c = lane % CH, r0 = mw * 32 + lane / CH, turn = (c >> 1) << 1;
+        const int c = lane % CH, r0 = mw * (kPart / 2) + lane / CH, turn = (c >> 1) << 1;
         unsigned put[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) put[i] = (c >> 1) * (kKeys * 128) + (((((c & 1) << 2) | (i ^ turn)) ^ (r0 & 7)) << 4);
+        const unsigned char* ring = raw + side * nraw * kSlot;
+        uint64_t *full = sh->raw_full + side * nraw, *empty = sh->raw_empty + side * nraw;
         int s = 0, fill = 0, piece = 0;
         uint32_t phase = 0u;
         for (; more && !failed; more = at.next(pl, p.B, kKeys), ++piece) {
@@ -270,31 +273,46 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
             for (int blk = at.blk0; blk < at.blk1 && !failed; ++blk, ++fill) {
                 const int st = fill % kStages;
                 const uint32_t ph = ((uint32_t)(fill / kStages) & 1u) ^ 1u;
-                const bool cached = blk < at.cached;
+                unsigned char* tile = (side ? Vs : Ks) + st * kTile;
+                if (!tc::mbar_wait_suspended(side ? &sh->v_empty[st] : &sh->k_empty[st], ph, abort_flag)) failed = true;
+                if (blk < at.cached) {
 #pragma unroll 1
-                for (int side = 0; side < 2; ++side) {
-                    unsigned char* tile = (side ? Vs : Ks) + st * kTile;
-                    if (cached && !tc::mbar_wait_suspended(&sh->raw_full[s], phase, abort_flag)) failed = true;
-                    if (!failed && !tc::mbar_wait_suspended(side ? &sh->v_empty[st] : &sh->k_empty[st], ph, abort_flag)) failed = true;
-                    failed = __any_sync(0xffffffffu, failed);
-                    if (failed) break;
-                    if (cached) {
-                        const unsigned char* from = raw + s * kSide;
-                        const uint32_t* so = RawQ4<D>::pairs(from, kKeys, (long long)pair * p.Lcap + (long long)blk * kKeys);
-                        const int left = kv - blk * kKeys;     // rows there are
+                    for (int part = 0; part < kParts; ++part) {
+                        const int row = blk * kKeys + part * kPart, left = kv - row;       // rows there are
+                        if (!failed && left > 0 && !tc::mbar_wait_suspended(full + s, phase, abort_flag)) failed = true;
+                        failed = __any_sync(0xffffffffu, failed);
+                        if (failed) break;
+                        const unsigned char* from = ring + s * kSlot;
+                        const uint32_t* so = RawQ4<D>::pairs(from, kPart, (long long)pair * p.Lcap + row);
+                        unsigned char* to = tile + part * (kPart * 128);
 #pragma unroll
-                        for (int i0 = 0; i0 < 32; i0 += RI) {
+                        for (int i0 = 0; i0 < kPart / 2; i0 += RI) {
                             const int r = r0 + i0;
-                            const uint4 u = *reinterpret_cast<const uint4*>(from + r * RawQ4<D>::kLevels + c * 16);
-                            uint32_t pr = so[r * CH + c];
-                            if (r >= left) pr = 0u;            // (behind the last row: zeros, whatever stands there)
+                            uint4 u = make_uint4(0u, 0u, 0u, 0u);
+                            uint32_t pr = 0u;                  // (behind the last row: zeros, whatever stands there)
+                            if (r < left) {
+                                u = *reinterpret_cast<const uint4*>(from + r * RawQ4<D>::kLevels + c * 16);
+                                pr = so[r * CH + c];
+                            }
                             const uint32_t w[4] = {turn ? u.z : u.x, turn ? u.w : u.y, turn ? u.x : u.z, turn ? u.y : u.w};
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(tile + r * 128 + put[i]) = q4_values_bf16(w[i], pr);
+                            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(to + r * 128 + put[i]) = q4_values_bf16(w[i], pr);
                         }
-                    } else {
-                        // the tree's own rows, one a lane
-                        const int tb = blk - at.cached, r = mw * 32 + lane, row = tb * kKeys + r;
+                        __syncwarp();
+                        if (left > 0) {
+                            if (lane == 0) tc::mbar_arrive(empty + s);
+                            if (++s == nraw) { s = 0; phase ^= 1u; }
+                        }
+                    }
+                    if (failed) break;
+                } else {
+                    failed = __any_sync(0xffffffffu, failed);
+                    if (failed) break;
+                    // the tree's own rows, one a lane
+                    const int tb = blk - at.cached;
+#pragma unroll 1
+                    for (int i32 = mw * 2; i32 < mw * 2 + 2; ++i32) {
+                        const int r = i32 * 32 + lane, row = tb * kKeys + r;
                         const uint4* src = static_cast<const uint4*>(side ? p.Vt : p.Kt) + (pair * p.max_nodes + (row < n ? row : 0)) * (D / 8);
                         bool is_bad = false;
 #pragma unroll 1
@@ -317,17 +335,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
                                 for (int i = 0; i < DH * 8; ++i)
                                     *reinterpret_cast<uint4*>(tile + (i >> 3) * (kKeys * 128) + r * 128 + ((i & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
                             const unsigned word = __ballot_sync(0xffffffffu, is_bad);
-                            if (lane == 0) sh->bad[piece & 3][tb * 4 + mw] = word;
+                            if (lane == 0) sh->bad[piece & 3][tb * 4 + i32] = word;
                         }
                     }
-                    tc::fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0) {
-                        tc::mbar_arrive(side ? &sh->v_full[st] : &sh->k_full[st]);
-                        if (cached) tc::mbar_arrive(&sh->raw_empty[s]);
-                    }
-                    if (cached && ++s == nraw) { s = 0; phase ^= 1u; }
                 }
+                tc::fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(side ? &sh->v_full[st] : &sh->k_full[st]);
             }
         }
         if (failed && lane == 0) give_up(sh, p.status, 64);
@@ -596,9 +610,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
 template <int D, int TR>
 int launch_tc(Handle* h, cudaStream_t s, const AttnQ4Params& p) {
     const size_t fixed = (size_t)TR * D * 2 + (size_t)kStages * 2 * kKeys * D * 2 + sizeof(TcShared) + sizeof(int) * PlanQ4::ints(p.B);
-    const size_t side = RawQ4<D>::bytes(kKeys);
-    size_t n = (kMaxDynamicSmem - 1024 - fixed) / side;
-    if (n > kMaxRaw) n = kMaxRaw;
+    const size_t slots = 2 * (size_t)RawQ4<D>::bytes(kKeys / raw_parts<D, TR>());      // one of each side
+    size_t n = (kMaxDynamicSmem - 1024 - fixed) / slots;
+    if (n > kMaxRaw / 2) n = kMaxRaw / 2;
     if (n < 1) return CTCSD_ERR_UNSUPPORTED;
     auto kern = attention_q4_tc_kernel<D, TR>;
     if (!(h->prepared & kPrepAttnQ4Tc)) {
@@ -608,7 +622,7 @@ int launch_tc(Handle* h, cudaStream_t s, const AttnQ4Params& p) {
         if (fa.numRegs < 128) return CTCSD_ERR_INTERNAL;
     }
     CTCSD_CUDA_CHECK(h, prepare_kernel(h, kPrepAttnQ4Tc, kern));
-    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(h->num_sms), dim3(kThreads), fixed + n * side, s, 1, p, (int)n));
+    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(h->num_sms), dim3(kThreads), fixed + n * slots, s, 1, p, (int)n));
     h->launches++;
     return CTCSD_OK;
 }
