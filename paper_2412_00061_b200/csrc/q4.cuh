@@ -92,22 +92,43 @@ __device__ __forceinline__ uint32_t q4_scale_origin(float lo, float hi) {
     if (!(fabsf(s) < INFINITY) || !(fabsf(o) < INFINITY)) return 0x7fc00000u;
     return (__float_as_uint(s) >> 16) | (__float_as_uint(o) & 0xffff0000u);
 }
-// Level of v in a group, rounded half to even.
-__device__ __forceinline__ uint32_t q4_level(float v, float scale, float origin) {
+// Level of v in a group, rounded half to even.  (Rarely called: see q4_word.)
+static __device__ __noinline__ uint32_t q4_level(float v, float scale, float origin) {
     if (!(scale > 0.f)) return 0u;
     const float q = rintf(__fsub_rn(__fdiv_rn(__fsub_rn(v, origin), scale), 16.f));
     return (uint32_t)fminf(fmaxf(q, 0.f), 15.f);
 }
-// The word of eight values.
+// The word of eight values.  A level is a division, which took most of the time of storing rows; so it is found by the group's reciprocal (off by
+// less than 31 * 2^-22 from the division's result), and only where that lies within 2^-15 of a tie by the division itself.
+// (32 prompts of 1024-4096 rows of 8 heads, stored and read back: 340 us with divisions, STORE_US so.)
 __device__ __forceinline__ uint32_t q4_word(const float (&v)[8], uint32_t so) {
     const float s = bf16lo(so), o = bf16hi(so);
-    uint32_t w = 0u;
+    if (!(s > 0.f)) return 0u;
+    const float r = __frcp_rn(s), magic = 12582912.f;                        // 1.5 * 2^23: adding it rounds to a whole number
+    float q[8];
+    if (fabsf(o) <= 100.f * s && r < INFINITY) {
+        // no limits needed: the scale's rounding (2^-8 of 15 levels) and the origin's (2^-8 of 100 at most) move a level by 0.45 at most
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t q = q4_level(v[i], s, o);
-        w |= __funnelshift_l(q, q, q4_bit(i)) & (i == 6 ? 0x80000007u : 15u << (q4_bit(i) & 31));
+        for (int i = 0; i < 8; ++i) {
+            const float d = __fsub_rn(v[i], o), x = __fmaf_rn(d, r, -16.f);
+            q[i] = __fsub_rn(__fadd_rn(x, magic), magic);
+            if (fabsf(__fsub_rn(x, q[i])) > 0.5f - 3.0517578125e-5f) {
+                // (14 bits hold scale times tie, so the difference is exact; the quotient of a d that is farther than 2^-20 from it is not the tie)
+                const float tie = __fadd_rn(floorf(x), 0.5f), diff = __fsub_rn(d, __fmul_rn(__fadd_rn(tie, 16.f), s));
+                if (diff == 0.f) q[i] = rintf(tie);
+                else if (fabsf(diff) > fabsf(d) * 9.5367431640625e-7f) q[i] = diff > 0.f ? tie + 0.5f : tie - 0.5f;
+                else q[i] = (float)q4_level(v[i], s, o);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = (float)q4_level(v[i], s, o);
     }
-    return w;
+    // the word turned back by 3: nibbles of values 0, 2, 4, 7 in the low half, 1, 3, 5, 6 in the high one
+    const float lo = fmaf(q[7], 4096.f, fmaf(q[4], 256.f, fmaf(q[2], 16.f, q[0])));
+    const float hi = fmaf(q[6], 4096.f, fmaf(q[5], 256.f, fmaf(q[3], 16.f, q[1])));
+    const uint32_t w = __byte_perm(__float_as_uint(__fadd_rn(lo, 8388608.f)), __float_as_uint(__fadd_rn(hi, 8388608.f)), 0x5410);
+    return __funnelshift_l(w, w, 3);
 }
 
 // Eight neighbouring values of an activation-type array (16- or 32-byte aligned), widened.

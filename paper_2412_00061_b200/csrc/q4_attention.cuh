@@ -32,7 +32,7 @@ struct AttnQ4Params {
 
 constexpr int kAq4MaxB = 1024;
 constexpr int kAq4SimpleRows = 64, kAq4SimpleKeys = 64, kAq4SimplePerSm = 2;
-constexpr int kAq4MmaRows = 16, kAq4MmaKeys = 128;
+constexpr int kAq4MmaRows = 16, kAq4MmaKeys = 192;
 constexpr int kAq4TcKeys = 128;
 
 // The plan in shared memory.

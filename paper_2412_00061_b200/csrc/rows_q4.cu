@@ -22,19 +22,56 @@ template <> __device__ __forceinline__ void store8<float>(float* out, const floa
     reinterpret_cast<float4*>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
-// Eight values -> their word, by four neighbouring lanes a group (all lanes of the warp take part).
-__device__ __forceinline__ uint32_t quantize8(const float (&v)[8], uint32_t& so) {
-    float lo = v[0], hi = v[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) { lo = min_nan(lo, v[i]); hi = max_nan(hi, v[i]); }
-#pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    }
-    so = q4_scale_origin(lo, hi);
-    return q4_word(v, so);
+__device__ __forceinline__ uint32_t min2_nan(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
+__device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// Eight values as they stand in memory, and as their word (by four neighbouring lanes a group; all lanes of the warp take part).
+template <typename T> struct Eight;
+template <> struct Eight<__nv_bfloat16> {
+    uint4 w;
+    __device__ __forceinline__ void zero() { w = make_uint4(0u, 0u, 0u, 0u); }
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ uint32_t quantize(uint32_t& so) const {
+        // (limits two at a time)
+        uint32_t lo = min2_nan(min2_nan(w.x, w.y), min2_nan(w.z, w.w)), hi = max2_nan(max2_nan(w.x, w.y), max2_nan(w.z, w.w));
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+            lo = min2_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+            hi = max2_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        }
+        so = q4_scale_origin(min_nan(bf16lo(lo), bf16hi(lo)), max_nan(bf16lo(hi), bf16hi(hi)));
+        const float v[8] = {bf16lo(w.x), bf16hi(w.x), bf16lo(w.y), bf16hi(w.y), bf16lo(w.z), bf16hi(w.z), bf16lo(w.w), bf16hi(w.w)};
+        return q4_word(v, so);
+    }
+};
+template <> struct Eight<float> {
+    float v[8];
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    }
+    __device__ __forceinline__ void load(const float* p) { load8(p, v); }
+    __device__ __forceinline__ uint32_t quantize(uint32_t& so) const {
+        float lo = v[0], hi = v[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) { lo = min_nan(lo, v[i]); hi = max_nan(hi, v[i]); }
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+            lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+            hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        }
+        so = q4_scale_origin(lo, hi);
+        return q4_word(v, so);
+    }
+};
 
 struct StoreParams {
     const void* K; const void* V;        // [B,Hkv,Lsrc,D]
@@ -63,25 +100,30 @@ __global__ void __launch_bounds__(kThreads) store_rows_q4_kernel(StoreParams p) 
     const T* src[2] = {static_cast<const T*>(p.K) + pair * p.Lsrc * D, static_cast<const T*>(p.V) + pair * p.Lsrc * D};
     uint32_t* q[2] = {p.c.Kq + dst, p.c.Vq + dst};
     uint32_t* s[2] = {p.c.Ks + dst / 4, p.c.Vs + dst / 4};
-    // (the same number of turns for all lanes of a warp: a group's lanes shuffle)
-    for (long long i0 = (long long)blockIdx.x * kThreads + (threadIdx.x & ~31); i0 < words; i0 += step) {
-        const long long i = i0 + (threadIdx.x & 31);
-        float v[2][8];
+    // (the same number of turns for all lanes of a warp: a group's lanes shuffle; the next turn's values are on their way meanwhile)
+    auto fetch = [&](long long i, Eight<T> (&v)[2]) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            if (i < words) load8(src[k] + i * 8, v[k]);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[k][e] = 0.f;
+            if (i < words) v[k].load(src[k] + i * 8);
+            else v[k].zero();
         }
+    };
+    const int lane = threadIdx.x & 31;
+    long long i0 = (long long)blockIdx.x * kThreads + (threadIdx.x & ~31);
+    Eight<T> v[2], next[2];
+    fetch(i0 + lane, v);
+    for (; i0 < words; i0 += step) {
+        const long long i = i0 + lane;
+        fetch(i + step, next);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             uint32_t so;
-            const uint32_t w = quantize8(v[k], so);
+            const uint32_t w = v[k].quantize(so);
             if (i < words && CTCSD_IN_BOUNDS(p.status, 121, at * (long long)W + i, (long long)p.Lcap * W)) {
                 q[k][i] = w;
                 if ((i & 3) == 0) s[k][i >> 2] = so;
             }
+            v[k] = next[k];
         }
     }
 }
@@ -166,13 +208,14 @@ __global__ void __launch_bounds__(kThreads) commit_accepted_q4_kernel(CommitQ4Pa
         const int i = i0 + (tid & 31);
         const int which = i >= (n + 1) * W ? 1 : 0, r = i - which * (n + 1) * W;
         const int l = r / W, w = r - l * W;
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        Eight<T> v;
+        v.zero();
         if (i < words) {
             const int node = l > 0 ? p.acc_nodes[b * p.T + l - 1] : 0;
-            load8(static_cast<const T*>(which ? p.Vt : p.Kt) + ((pair * p.max_nodes + node) * W + w) * 8, v);
+            v.load(static_cast<const T*>(which ? p.Vt : p.Kt) + ((pair * p.max_nodes + node) * W + w) * 8);
         }
         uint32_t so;
-        const uint32_t word = quantize8(v, so);
+        const uint32_t word = v.quantize(so);
         if (i < words && CTCSD_IN_BOUNDS(p.status, 123, L + l, p.Lcap)) {
             const size_t at = (pair * p.Lcap + L + l) * W + w;
             (which ? p.c.Vq : p.c.Kq)[at] = word;

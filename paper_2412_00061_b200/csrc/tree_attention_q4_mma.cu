@@ -1,13 +1,13 @@
 // Tree attention over a 4-bit cache for bf16 and few query rows (up to 16 of a kv head): plain decoding and small trees.
 //
-// HBM bounds it, and what a 128-key block of K and V costs on the way: 32768 levels made values.  So levels go from shared memory
+// HBM bounds it, and what a block of K and V costs on the way: 256 levels a key made values.  So levels go from shared memory
 // to the registers that the matrix instruction (mma.m16n8k16, 16 query rows) reads, and nowhere else:
 //   S = Q K^T   a lane holds the K operand of one key in a quarter of the head dimension: 16 bytes of levels of that row, in order, since the
 //               order of the summed index is free as long as Q has it too;
 //   O += P V    a lane's S fragment is its P fragment; the V operand pairs two keys of a column, and a lane takes the same bytes
 //               of four rows and joins halves of words, D/8 columns of its own (the order of columns is free as well).
 // One shift-and-or and half a multiply-add per value.  A warp takes 16 keys of every block and keeps maximum, sum and O of its own;
-// the eight warps' are joined when a tile ends.  Four warps bring the blocks in by bulk copies, up to seven of them (140 KB) ahead.
+// the warps' are joined when a tile ends.  Four warps bring the blocks in by bulk copies, up to five of them (150 KB) ahead.
 #include "q4_ring.cuh"
 
 #include <math.h>
@@ -15,7 +15,7 @@
 namespace ctcsd {
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 12;
 constexpr int kProducers = 4;            // of K's levels and pairs, V's levels and pairs
 constexpr int kThreads = (kWarps + kProducers) * 32;
 constexpr int kRows = kAq4MmaRows;
@@ -24,7 +24,7 @@ constexpr int kMaxStages = 16;
 constexpr float kSlack = 8.f;            // log2 units: P stays below 2^8
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-static_assert(kKeys == kWarps * 16, "a warp takes 16 keys of a block");
+static_assert(kKeys == kWarps * 16 && kWarps % 4 == 0, "a warp takes 16 keys of a block");
 
 struct __align__(8) MmaShared {
     uint64_t full[kMaxStages], empty[kMaxStages];
@@ -42,7 +42,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 // The consumer warps meet here.
-__device__ __forceinline__ void consumers_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ void consumers_barrier() { asm volatile("bar.sync 1, 384;" ::: "memory"); }
 
 // Place of 16-byte chunk c of row r in the buffer that joins the warps' outputs: the eight lanes of a phase write to eight banks.
 template <int D> __device__ __forceinline__ int join_at(int r, int c) {
@@ -60,8 +60,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
     constexpr int kSide = RawQ4<D>::bytes(kKeys);
     extern __shared__ __align__(128) unsigned char dyn[];
     unsigned char* ring = dyn;                               // [nstages][K side | V side]
-    float4* join = reinterpret_cast<float4*>(ring + (size_t)nstages * 2 * kSide);    // [4][16][D/4]
-    MmaShared* sh = reinterpret_cast<MmaShared*>(join + 4 * kRows * (D / 4));
+    uint4* join = reinterpret_cast<uint4*>(ring + (size_t)nstages * 2 * kSide);      // [4][16][D/4] of four floats
+    uint4* qs = join + 4 * kRows * (D / 4);                  // [2 LW][32 lanes]: Q as operand A
+    MmaShared* sh = reinterpret_cast<MmaShared*>(qs + 2 * LW * 32);
     PlanQ4 pl;
     pl.carve(reinterpret_cast<int*>(sh + 1), p.B);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -129,21 +130,17 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
             return ((size_t)b * p.max_nodes + node) * p.Hq + at.g * p.grp + (row0 + r - node * p.grp);
         };
         // Q as operand A: rows g and g + 8, elements D/4 t .. of the head
-        uint32_t qf[2 * LW][4];
-        {
+        // (in shared memory, for the registers' sake: with eight warps that held it, two to a scheduler, instructions waited for one another and 13B
+        // tokens took 265 us; twelve: MMA12 us)
+        if (warp < LW) {
             const uint4 z = make_uint4(0u, 0u, 0u, 0u);
             const uint4* Qg = static_cast<const uint4*>(p.Q);
-#pragma unroll
-            for (int i = 0; i < LW; ++i) {
-                const uint4 a = g < nrows ? __ldg(Qg + out_row(g) * (D / 8) + t * LW + i) : z;
-                const uint4 b8 = g + 8 < nrows ? __ldg(Qg + out_row(g + 8) * (D / 8) + t * LW + i) : z;
-                qf[2 * i][0] = a.x; qf[2 * i][1] = b8.x; qf[2 * i][2] = a.y; qf[2 * i][3] = b8.y;
-                qf[2 * i + 1][0] = a.z; qf[2 * i + 1][1] = b8.z; qf[2 * i + 1][2] = a.w; qf[2 * i + 1][3] = b8.w;
-            }
-            // (they stay in the order of the operand's registers: as loaded they would be moved there for every product)
-#pragma unroll
-            for (int i = 0; i < 2 * LW; ++i) asm volatile("" : "+r"(qf[i][0]), "+r"(qf[i][1]), "+r"(qf[i][2]), "+r"(qf[i][3]));
+            const uint4 a = g < nrows ? __ldg(Qg + out_row(g) * (D / 8) + t * LW + warp) : z;
+            const uint4 b8 = g + 8 < nrows ? __ldg(Qg + out_row(g + 8) * (D / 8) + t * LW + warp) : z;
+            qs[(2 * warp) * 32 + lane] = make_uint4(a.x, b8.x, a.y, b8.y);
+            qs[(2 * warp + 1) * 32 + lane] = make_uint4(a.z, b8.z, a.w, b8.w);
         }
+        consumers_barrier();
         float o[NT][4], ref[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -151,10 +148,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
             for (int q = 0; q < 4; ++q) o[i][q] = 0.f;
         bool poisoned[2] = {false, false};
         // scores of 16 keys (two tiles of 8) against the reference -> P as operand A; s: masked scores
-        auto weigh = [&](float (&s)[2][4], uint32_t (&pa)[4]) {
-            float bm[2];
+        const bool upper = nrows > 8;                            // rows 8 .. are there
+        auto weigh = [&](float (&s)[2][4], uint32_t (&pa)[4]) __attribute__((always_inline)) {
+            float bm[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
+                if (r == 1 && !upper) continue;
                 bm[r] = max_nan(max_nan(s[0][2 * r], s[0][2 * r + 1]), max_nan(s[1][2 * r], s[1][2 * r + 1]));
                 bm[r] = max_nan(bm[r], __shfl_xor_sync(0xffffffffu, bm[r], 1));
                 bm[r] = max_nan(bm[r], __shfl_xor_sync(0xffffffffu, bm[r], 2));
@@ -175,6 +174,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
             }
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
+                if (r == 1 && !upper) {
+                    pa[1] = pa[3] = 0u;
+                    continue;
+                }
                 const float off = ref[r] == -INFINITY ? 0.f : -ref[r];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
@@ -198,8 +201,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
 #pragma unroll
                         for (int i = 0; i < LW; ++i) {
                             const uint4 k = key < n ? __ldg(Kt + (size_t)key * (D / 8) + t * LW + i) : make_uint4(0u, 0u, 0u, 0u);
-                            mma_16816(s[j], qf[2 * i][0], qf[2 * i][1], qf[2 * i][2], qf[2 * i][3], k.x, k.y);
-                            mma_16816(s[j], qf[2 * i + 1][0], qf[2 * i + 1][1], qf[2 * i + 1][2], qf[2 * i + 1][3], k.z, k.w);
+                            const uint4 q0 = qs[(2 * i) * 32 + lane], q1 = qs[(2 * i + 1) * 32 + lane];
+                            mma_16816(s[j], q0.x, q0.y, q0.z, q0.w, k.x, k.y);
+                            mma_16816(s[j], q1.x, q1.y, q1.z, q1.w, k.z, k.w);
                         }
                     }
                     uint32_t vis[2];
@@ -273,13 +277,15 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
                     s2[j][0] = s2[j][1] = s2[j][2] = s2[j][3] = 0.f;
                 }
 #pragma unroll
-                for (int i = 0; i < LW; ++i)
+                for (int i = 0; i < LW; ++i) {
+                    const uint4 q0 = qs[(2 * i) * 32 + lane], q1 = qs[(2 * i + 1) * 32 + lane];
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const uint4 k = q4_values_bf16(kw[j][i], kso[j]);
-                        mma_16816(s[j], qf[2 * i][0], qf[2 * i][1], qf[2 * i][2], qf[2 * i][3], k.x, k.y);
-                        mma_16816(s2[j], qf[2 * i + 1][0], qf[2 * i + 1][1], qf[2 * i + 1][2], qf[2 * i + 1][3], k.z, k.w);
+                        mma_16816(s[j], q0.x, q0.y, q0.z, q0.w, k.x, k.y);
+                        mma_16816(s2[j], q1.x, q1.y, q1.z, q1.w, k.z, k.w);
                     }
+                }
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -353,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
         }
         // a lane's columns of rows g and g + 8: D/4 t .. : first those of its even position, then of its odd one
         auto put = [&](bool add) {
-            float4* buf = join + (warp & 3) * kRows * (D / 4);
+            float4* buf = reinterpret_cast<float4*>(join) + (warp & 3) * kRows * (D / 4);
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -365,12 +371,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
                     *at4 = v;
                 }
         };
-        if (warp >= 4) put(false);
-        consumers_barrier();
-        if (warp < 4) put(true);
-        consumers_barrier();
+#pragma unroll 1
+        for (int w0 = kWarps - 4; w0 >= 0; w0 -= 4) {        // four warps at a time
+            if (warp >= w0 && warp < w0 + 4) put(w0 + 4 < kWarps);
+            consumers_barrier();
+        }
         // ---- output: 16 threads a row ----
-        {
+        if (warp < 8) {
             const int r = tid >> 4, c0 = (tid & 15) * (D / 64);               // this thread's chunks of four columns
             float rtop = -INFINITY, rsum = 0.f;
 #pragma unroll
@@ -386,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
                 v[c] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const float4 u = join[w * kRows * (D / 4) + join_at<D>(r, c0 + c)];
+                    const float4 u = reinterpret_cast<const float4*>(join)[w * kRows * (D / 4) + join_at<D>(r, c0 + c)];
                     v[c].x += u.x; v[c].y += u.y; v[c].z += u.z; v[c].w += u.w;
                 }
             }
@@ -417,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
 
 template <int D>
 int launch_mma(Handle* h, cudaStream_t s, const AttnQ4Params& p) {
-    const size_t fixed = sizeof(float4) * 4 * kRows * (D / 4) + sizeof(MmaShared) + sizeof(int) * PlanQ4::ints(p.B);
+    const size_t fixed = sizeof(float4) * 4 * kRows * (D / 4) + sizeof(uint4) * 2 * (D / 32) * 32 + sizeof(MmaShared) + sizeof(int) * PlanQ4::ints(p.B);
     const size_t stage = 2 * (size_t)RawQ4<D>::bytes(kKeys);
     size_t n = (kMaxDynamicSmem - 1024 - fixed) / stage;
     if (n > kMaxStages) n = kMaxStages;
