@@ -73,13 +73,20 @@ class DraftVerifyStep:
         self.inp: Dict[str, Optional[torch.Tensor]] = {}
         self.shared = None       # workspace of the attention over a shared prefix
         self.cache = None        # state of the cache budget (enable_cache_budget)
+        self.q4 = None           # 4-bit cache and the workspace of the attention over it (use_q4_cache)
         self.chain = None        # state of chained steps (setup_chain)
 
     def set_inputs(self, **tensors):
         """x, Wd, blank_bias, row_seq, sel_row, base_tok, kv_len, Q, K, V, hn, Wl (device tensors); Kp, Vp
         [Hkv,Pcap,D] and prefix_len [B] when the sequences share a prefix: the attention then reads it once
         for all of them, and tree positions start behind it (Kp=None: no prefix any more, prefix_len goes with it).
-        With a cache budget, K and V of a new batch need reset_cache() as well."""
+        With a cache budget, K and V of a new batch need reset_cache() as well.  Kt, Vt [B,Hkv,max_nodes,D]: the tree's keys and
+        values of a step over a 4-bit cache (use_q4_cache).  Wd_q4: packed weights that the draft head reads in place
+        of Wd (quantize_draft_weights()); weights given as Wd afterwards put them aside."""
+        if self.q4 is not None and tensors.get("Kp") is not None:
+            raise ValueError("a 4-bit cache has no shared prefix beside it")
+        if tensors.get("Wd") is not None and "Wd_q4" not in tensors:
+            tensors["Wd_q4"] = None
         if "Kp" in tensors and tensors["Kp"] is None:
             tensors.update(Vp=None, prefix_len=None)
         if self.cache is not None:
@@ -115,6 +122,8 @@ class DraftVerifyStep:
         refused here (ValueError).  Called again, it starts afresh with the new limits (a chain goes on beginning
         at its own rows); graphs captured before hold the old ones."""
         cfg, dev = self.cfg, self.device
+        if self.q4 is not None:
+            raise ValueError("a 4-bit cache has no budget (its rows are not evicted)")
         if budget < 1 or sinks < 0 or recent < 0 or sinks + recent > budget:
             raise ValueError("a budget of %d rows does not hold %d sinks and the newest %d" % (budget, sinks, recent))
         if not 0.0 <= decay <= 1.0:
@@ -165,6 +174,54 @@ class DraftVerifyStep:
             k["row_pos"][at] = ages
             k["n_evicted"][at] = 0
         self._forget_chain_start()
+
+    # weights and cache in 4 bits --------------------------------------------------------
+    def quantize_draft_weights(self, group: int = 128, stream=None):
+        """Packs the draft head's weights in 4 bits (`group` neighbours along the hidden axis share a scale), once; the draft head reads
+        them from then on, and inp["Wd"] may be let go with set_inputs(Wd=None)."""
+        if self.inp.get("Wd") is None:
+            raise ValueError("quantize_draft_weights() needs the weights (set_inputs(Wd=...))")
+        self.inp["Wd_q4"] = self.h.quantize_weights_q4(self.inp["Wd"], group, stream=stream)
+        return self.inp["Wd_q4"]
+
+    def use_q4_cache(self, Lcap: Optional[int] = None):
+        """Keeps the sequences' caches in 4 bits: an empty cache of Lcap rows (default: the configuration's), which store_prompt() fills,
+        the attention reads and the history update extends; the inputs K and V are not looked at any more.  A step's tree
+        keys and values come as inputs Kt and Vt.  Called again, it starts with an empty cache."""
+        if self.cache is not None or self.inp.get("Kp") is not None:
+            raise ValueError("a 4-bit cache has no shared prefix and no budget beside it")
+        Lcap = self.cfg.Lcap if Lcap is None else Lcap
+        if Lcap < 1:
+            raise ValueError("a cache holds a row at least")
+        self.q4 = dict(cache=self.h.make_q4_cache(Lcap), ws=self.h.make_q4_attention())
+        self.out["attn_lse"] = torch.zeros(self.cfg.B, self.cfg.max_nodes, self.cfg.Hq, dtype=torch.float32, device=self.device)
+        return self.q4["cache"]
+
+    def store_prompt(self, K, V, n_rows, at=None, stream=None):
+        """The first n_rows[b] rows of K, V [B,Hkv,L,D] to the 4-bit cache, from row at[b] (None: 0) on; kv_len is the caller's to set."""
+        if self.q4 is None:
+            raise ValueError("store_prompt() needs a 4-bit cache (use_q4_cache)")
+        self.h.store_rows_q4(self.q4["cache"], K, V, n_rows, at, stream=stream)
+
+    def _draft_rows(self, x, x_rows, row_seq=None, dbg=None, stream=None):
+        """The draft head on rows x, or on the rows of x that a map picks."""
+        i, o = self.inp, self.out
+        outs = (o["topk_id"], o["topk_lp"], o["lse"])
+        if i.get("Wd_q4") is not None:
+            self.h.draft_logits_q4(x, x_rows, i["Wd_q4"], row_seq, i.get("blank_bias"), *outs, dbg, stream=stream)
+        elif x_rows is None:
+            self.h.draft_logits(x, i["Wd"], row_seq, i.get("blank_bias"), *outs, dbg, stream=stream)
+        else:
+            self.h.draft_logits_rows(x, x_rows, i["Wd"], row_seq, i.get("blank_bias"), *outs, dbg, stream=stream)
+
+    def _commit_rows(self, kv_len, out_kv_len, stream=None):
+        """The accepted path joins the cache."""
+        i, o = self.inp, self.out
+        if self.q4 is not None:
+            self.h.commit_accepted_q4(i["Kt"], i["Vt"], self.q4["cache"], kv_len, o["acc_len"], o["acc_nodes"], out_kv_len,
+                                      o["next_sel_row"], stream=stream)
+            return
+        self.h.commit_accepted(i["K"], i["V"], kv_len, o["acc_len"], o["acc_nodes"], out_kv_len, o["next_sel_row"], stream=stream)
 
     def _tree_base(self, stream=None):
         """What tree positions count from: the cached rows, those dropped earlier and the shared prefix."""
@@ -246,9 +303,7 @@ class DraftVerifyStep:
 
     # individual stages ----------------------------------------------------------------
     def draft(self, stream=None):
-        i, o = self.inp, self.out
-        self.h.draft_logits(i["x"], i["Wd"], i.get("row_seq"), i.get("blank_bias"),
-                            o["topk_id"], o["topk_lp"], o["lse"], o.get("draft_logits_dbg"), stream=stream)
+        self._draft_rows(self.inp["x"], None, self.inp.get("row_seq"), self.out.get("draft_logits_dbg"), stream=stream)
 
     def collapse(self, stream=None):
         i, o = self.inp, self.out
@@ -272,6 +327,10 @@ class DraftVerifyStep:
 
     def attention(self, stream=None):
         i, o = self.inp, self.out
+        if self.q4 is not None:
+            self.h.tree_attention_q4(self.q4["ws"], i["Q"], self.q4["cache"], i["Kt"], i["Vt"], i["kv_len"], o["n_nodes"], o["mask"],
+                                     1.0 / float(self.cfg.D) ** 0.5, o["O"], o["attn_lse"], stream=stream)
+            return
         if self._shared_in_use():
             self.h.tree_attention_shared(self.shared, i["Q"], i.get("Kp"), i.get("Vp"), i.get("prefix_len"), i["K"], i["V"],
                                          i["kv_len"], o["n_nodes"], o["mask"], 1.0 / float(self.cfg.D) ** 0.5, o["O"],
@@ -301,10 +360,8 @@ class DraftVerifyStep:
 
     def commit(self, stream=None):
         """History update (not part of run(): it changes the K/V cache in place), and the cache budget's upkeep."""
-        i, o = self.inp, self.out
-        self.h.commit_accepted(i["K"], i["V"], i["kv_len"], o["acc_len"], o["acc_nodes"],
-                               o["new_kv_len"], o["next_sel_row"], stream=stream)
-        self._trim_cache(o["new_kv_len"], stream)
+        self._commit_rows(self.inp["kv_len"], self.out["new_kv_len"], stream)
+        self._trim_cache(self.out["new_kv_len"], stream)
 
     def run(self, stream=None):
         """The whole hot path: five calls back to back on one stream, no host sync."""
@@ -324,7 +381,8 @@ class DraftVerifyStep:
         in between).  x0 [B,H], base_tok0 [B], kv_len0 [B]: where the chain starts.  The per-step
         tables stand in for the base model: Qtab [S,B,max_nodes,Hq,D] tree-node queries, Ktab/Vtab
         [S,B,Hkv,max_nodes,D] tree-node keys/values, hntab [S,B*max_nodes,H] tree-node hidden states.
-        K, V (the cache, updated in place), Wd, Wl, blank_bias come from set_inputs()."""
+        K, V (the cache, updated in place), Wd, Wl, blank_bias come from set_inputs().  With a 4-bit cache a step's tables are its
+        tree rows themselves; with 4-bit weights the draft head reads those."""
         cfg, dev = self.cfg, self.device
         self.chain = dict(start=None, start_kept=False, n=n_steps, x0=x0, base_tok0=base_tok0, kv_len0=kv_len0, Qtab=Qtab, Ktab=Ktab, Vtab=Vtab,
                           hntab=hntab, kv_len=kv_len0.clone(), kv_before=None, rec=None,
@@ -342,6 +400,9 @@ class DraftVerifyStep:
         """Stand-in for the base model's key/value projection of step s: node j's key and value go
         to cache row kv_len[b]+j (device-side indices, no host work)."""
         c, cfg = self.chain, self.cfg
+        if self.q4 is not None:
+            self.inp["Kt"], self.inp["Vt"] = c["Ktab"][s], c["Vtab"][s]
+            return
         rows = c["kv_len"].to(torch.int64)[:, None] + c["node_off"][None, :]                    # [B,n]
         idx = rows[:, None, :, None].expand(cfg.B, cfg.Hkv, cfg.max_nodes, cfg.D)
         self.inp["K"].scatter_(2, idx, c["Ktab"][s])
@@ -354,11 +415,10 @@ class DraftVerifyStep:
         i["sel_row"] = None
         if s == 0:
             i["base_tok"] = c["base_tok0"]
-            self.h.draft_logits(c["x0"], i["Wd"], None, i.get("blank_bias"), o["topk_id"], o["topk_lp"], o["lse"])
+            self._draft_rows(c["x0"], None)
         else:
             i["base_tok"] = o["next_tok"]              # the previous step's bonus token is this step's root
-            self.h.draft_logits_rows(c["hntab"][s - 1], o["next_sel_row"], i["Wd"], None, i.get("blank_bias"),
-                                     o["topk_id"], o["topk_lp"], o["lse"])
+            self._draft_rows(c["hntab"][s - 1], o["next_sel_row"])
         self.collapse()
         self.tree()
 
@@ -374,8 +434,7 @@ class DraftVerifyStep:
         if c["kv_before"] is not None:
             c["kv_before"][s].copy_(c["kv_len"])
         # the new length overwrites the old one in place; the next step drafts from out["next_sel_row"]
-        self.h.commit_accepted(i["K"], i["V"], c["kv_len"], o["acc_len"], o["acc_nodes"], c["kv_len"],
-                               o["next_sel_row"])
+        self._commit_rows(c["kv_len"], c["kv_len"])
         self._trim_cache(c["kv_len"])
         if c["rec"] is not None:
             o["new_kv_len"].copy_(c["kv_len"])
