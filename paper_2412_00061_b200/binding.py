@@ -140,6 +140,27 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream], device_index: Optional[int]
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device_index is None else device_index)
 
 
+class Q4Cache(dict):
+    """A 4-bit cache: levels Kq, Vq [B,Hkv,Lcap,D/2] uint8, (scale, origin) Ks, Vs [B,Hkv,Lcap,D/32,2] bfloat16.  Its tensors are checked
+    when they are put in, not again by every call."""
+
+    def __init__(self, handle, **tensors):
+        super().__init__(**tensors)
+        self.handle = handle
+        self._check()
+
+    def _check(self):
+        self.ptrs, self.Lcap = self.handle._q4_check(self)
+
+    def __setitem__(self, name, tensor):
+        super().__setitem__(name, tensor)
+        self._check()
+
+    def update(self, *args, **kw):
+        super().update(*args, **kw)
+        self._check()
+
+
 class Handle:
     """Owns a ctcsd handle and its device workspace (a torch uint8 tensor)."""
 
@@ -515,14 +536,18 @@ class Handle:
         return _ptr(Wq["w"], torch.uint8, c.T * ((c.V + 16) // 16) * ((c.H + 127) // 128) * (1024 + 64 * (128 // group)), "Wq")
 
     def make_q4_cache(self, Lcap):
-        """An empty 4-bit cache of Lcap rows a sequence: levels Kq, Vq [B,Hkv,Lcap,D/2] uint8, (scale, origin) Ks, Vs
-        [B,Hkv,Lcap,D/32,2] bfloat16."""
+        """An empty 4-bit cache (Q4Cache) of Lcap rows a sequence."""
         c = self.cfg
         levels = lambda: torch.zeros(c.B, c.Hkv, Lcap, c.D // 2, dtype=torch.uint8, device=self.device)
         pairs = lambda: torch.zeros(c.B, c.Hkv, Lcap, c.D // self.Q4_GROUP, 2, dtype=torch.bfloat16, device=self.device)
-        return dict(Kq=levels(), Ks=pairs(), Vq=levels(), Vs=pairs())
+        return Q4Cache(self, Kq=levels(), Ks=pairs(), Vq=levels(), Vs=pairs())
 
     def _q4_cache(self, cache):
+        if type(cache) is Q4Cache and cache.handle is self:
+            return cache.ptrs, cache.Lcap
+        return self._q4_check(cache)
+
+    def _q4_check(self, cache):
         c = self.cfg
         Lcap = cache["Kq"].shape[2]
         rows = c.B * c.Hkv * Lcap

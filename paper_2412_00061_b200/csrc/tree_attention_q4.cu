@@ -217,11 +217,14 @@ __global__ void __launch_bounds__(kSimpleThreads, kAq4SimplePerSm) attention_q4_
 }
 
 // ---------------------------------------------------------------------------------------
-// Merge of tiles that were cut.  A block for a span and 32 columns: if the span is the second of a tile's, the block joins the tile's parts in span
-// order, four at a time (the result does not depend on timing), else it has nothing to do.  A thread holds eight columns of a row;
-// neighbours take neighbouring rows, so that the transposed parts are read in whole lines.
+// Merge of tiles that were cut.  A block for a span and a share of the columns: if the span is the second of a tile's, the block joins the tile's parts
+// in span order, four at a time (the result does not depend on timing), else it has nothing to do.  A thread holds eight columns
+// of a row; neighbours take neighbouring rows, so that the transposed parts are read in whole lines.  Latency bounds it: one round of loads for the cut and
+// one for every four parts.
 // ---------------------------------------------------------------------------------------
-constexpr int kMergeThreads = 256;
+constexpr int kMergeThreads = 512;
+// Eights of columns of a block: as many as give every thread one.
+__host__ __device__ constexpr int merge_eights(int D, int TR) { return kMergeThreads / TR < D / 8 ? kMergeThreads / TR : D / 8; }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kMergeThreads) attention_q4_merge_kernel(AttnQ4Params p, int TR) {
@@ -232,9 +235,9 @@ __global__ void __launch_bounds__(kMergeThreads) attention_q4_merge_kernel(AttnQ
     if (cut.x < 0) return;
     const int g = cut.x, b = cut.y, row0 = cut.z * TR, c0 = (int)blockIdx.x - 1, c1 = cut.w;
     const int left = p.n_nodes[b] * p.grp - row0, nrows = left < TR ? left : TR;
-    for (int i = threadIdx.x; i < TR * 4; i += kMergeThreads) {
-        const int tr = i % TR, c8 = blockIdx.y * 4 + i / TR;                 // row of the tile, columns 8 c8 ..
-        if (tr >= nrows) continue;
+    const int eights = merge_eights(D, TR), i = threadIdx.x;
+    const int tr = i % TR, c8 = blockIdx.y * eights + i / TR;                // row of the tile, columns 8 c8 ..
+    if (i < TR * eights && tr < nrows) {
         // only the first part can be one that a span begins (slot 1); the others continue a tile (slot 0)
         float ref = -INFINITY, sum = 0.f, a[8];
 #pragma unroll
@@ -273,7 +276,7 @@ __global__ void __launch_bounds__(kMergeThreads) attention_q4_merge_kernel(AttnQ
         }
         const int node = (row0 + tr) / p.grp;
         const size_t orow = ((size_t)b * p.max_nodes + node) * p.Hq + g * p.grp + (row0 + tr - node * p.grp);
-        if (!CTCSD_IN_BOUNDS(p.status, 134, orow, out_rows(p))) continue;
+        if (!CTCSD_IN_BOUNDS(p.status, 134, orow, out_rows(p))) return;
         const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
         T* out = static_cast<T*>(p.O) + orow * D + 8 * c8;
         store4(out, make_float4(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv));
@@ -284,7 +287,7 @@ __global__ void __launch_bounds__(kMergeThreads) attention_q4_merge_kernel(AttnQ
 
 template <typename T, int D>
 int launch_merge(Handle* h, cudaStream_t s, const AttnQ4Params& p, int TR, int spans) {
-    CTCSD_CUDA_CHECK(h, launch_pdl(attention_q4_merge_kernel<T, D>, dim3(spans, D / 32), dim3(kMergeThreads), 0, s, 1, p, TR));
+    CTCSD_CUDA_CHECK(h, launch_pdl(attention_q4_merge_kernel<T, D>, dim3(spans, D / 8 / merge_eights(D, TR)), dim3(kMergeThreads), 0, s, 1, p, TR));
     h->launches++;
     return CTCSD_OK;
 }

@@ -13,7 +13,13 @@
 // references, sums (of the unrounded weights), O and the parts are float32.
 //
 // Warps 0 and 3 bring levels in by bulk copies, warps 1 and 2 issue the products of one half each, warps 4-7 and 8-11 are the softmax warps of the
-// halves, 12-15 make the tiles.  The softmax warps take the registers that the others give up (setmaxnreg).
+// halves, 12-15 make the tiles.  All have 128 registers (168 for the softmax warps, taken from the others with setmaxnreg: 64 us in place of 62 for
+// case B below).
+//
+// What bounds it: the round of a block from the makers through S, the softmax, P V and back, about 3100 cycles where the products alone
+// take 2100 (D = 128, TR = 256); then a piece's beginning and end (6500 cycles), which short sequences pay often.
+//   A: 16 sequences of 4096 cached rows, 64 nodes, 64 query heads on 8 kv heads    235 us, 574 TFLOP/s (bfloat16 rows: 247 us)
+//   B: 4 sequences of 2048 rows, 64 nodes, 32 heads of their own                    62 us with the merge (bfloat16 rows: 42 us)
 //
 // A weight of zero does not cancel a NaN.  Cached rows are seen by every row of the tile, and those behind the last are made zeros; a
 // tree row whose value holds a NaN or an infinity is made zeros too and noted, and a row that does see it becomes NaN at the end.
@@ -33,9 +39,6 @@ constexpr int kMaxRaw = 16;
 constexpr float kSlack = 8.f;          // log2 units: P stays below 2^8
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-// registers of a thread: launched with 128; 128 x 64 + 256 x 168 + 128 x 112 = 512 x 128
-constexpr int kRegsAux = 64, kRegsSoftmax = 168, kRegsMaker = 112;
-static_assert(128 * kRegsAux + 256 * kRegsSoftmax + 128 * kRegsMaker <= kThreads * 128, "registers of the launch");
 
 struct __align__(8) TcShared {
     uint64_t q_full;
@@ -140,7 +143,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
     attn_q4_sides<__nv_bfloat16, D>(p, pl, sp, at, more);
 
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsAux));
         if (warp == 0 || warp == 3) {
             // ---------------- levels: of K and of V ----------------
             if (lane == 0) {
@@ -253,7 +255,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
         }
     } else if (warp >= 12) {
         // ---------------- tiles of values ----------------
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsMaker));
         // Two warps make K's tiles, two V's.
         const int mw = (warp - 12) & 1, side = (warp - 12) >> 1;
         // levels: a lane takes chunk c (32 values) of a row, 8 rows (D = 64: 16) at a time.  Its four words go to four 16-byte places of the row; lanes of
@@ -285,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
                         const unsigned char* from = ring + s * kSlot;
                         const uint32_t* so = RawQ4<D>::pairs(from, kPart, (long long)pair * p.Lcap + row);
                         unsigned char* to = tile + part * (kPart * 128);
-#pragma unroll
+#pragma unroll 2
                         for (int i0 = 0; i0 < kPart / 2; i0 += RI) {
                             const int r = r0 + i0;
                             uint4 u = make_uint4(0u, 0u, 0u, 0u);
@@ -348,7 +349,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
     } else {
         // ---------------- softmax: one thread per query row of a half ----------------
         // Every softmax thread executes every barrier of the halves, also after a wait has failed.
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         const int half = (warp - 4) >> 2;
         const int q = warp & 3;                                // TMEM lane quarter this warp may read
         const int rl = q * 32 + lane;
