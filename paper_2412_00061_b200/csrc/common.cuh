@@ -39,8 +39,8 @@ struct Layout {
     size_t tc_part_bytes;
     size_t lm_rows_off;       // act[lm_key_count][H]: the LM head's live activation rows packed densely (bf16, more than 128 tree rows)
     size_t lm_rowmap_off;     // int[lm_key_count + 1]: packed row -> tree row; the last entry is the number of live rows
-    size_t q4_rows_off;       // act[max_draft_rows][H]: activation rows picked by a row map, for the tensor-core draft head over 4-bit weights
-    size_t q4_part_off;       // DraftPartial[128][SMs][2]: its states (bf16 and max_draft_rows > 8)
+    size_t q4_rows_off;       // act[max_draft_rows][H]: activation rows picked by a row map, for the draft head over 4-bit weights (bf16)
+    size_t q4_part_off;       // DraftPartial[4 * rows of a pass, a multiple of 32][SMs][2]: its states (bf16)
     size_t total;
     int gemv_grid_max;        // largest grid the GEMV may use
     int lm_key_count;
@@ -79,7 +79,7 @@ struct DeviceGuard {
 };
 
 enum { kPrepSharedTc = 1, kPrepSharedSimple = 2, kPrepMassTc = 4, kPrepMassF32 = 8, kPrepEvict = 16, kPrepEvictAlone = 32,
-       kPrepDraftQ4 = 64, kPrepDraftQ4Tc = 128, kPrepDraftQ4F32 = 256, kPrepAttnQ4Simple = 512, kPrepAttnQ4Mma = 1024, kPrepAttnQ4Tc = 2048 };
+       kPrepDraftQ4Tc = 128, kPrepDraftQ4F32 = 256, kPrepAttnQ4Simple = 512, kPrepAttnQ4Mma = 1024, kPrepAttnQ4Tc = 2048 };
 constexpr int kMaxDynamicSmem = 227 * 1024;
 
 // Lets `kernel` (no static shared memory) use all of an SM's shared memory; the limit is the same for every caller, so once per

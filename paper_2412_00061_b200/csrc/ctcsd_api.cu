@@ -63,9 +63,10 @@ Layout make_layout(const ctcsd_config& c, int num_sms) {
     l.q4_rows_off = l.q4_part_off = off;
     {
         const int rows = c.max_draft_rows > 0 ? c.max_draft_rows : c.B;
-        if (rows > 8 && c.dtype == CTCSD_DTYPE_BF16) {
+        if (c.dtype == CTCSD_DTYPE_BF16) {
+            const int states = 4 * (rows < 128 ? (rows + 31) / 32 * 32 : 128);
             l.q4_rows_off = off;  off = align_up(off + (size_t)rows * c.H * 2, 256);
-            l.q4_part_off = off;  off = align_up(off + sizeof(DraftPartial) * 128 * (size_t)num_sms * 2, 256);
+            l.q4_part_off = off;  off = align_up(off + sizeof(DraftPartial) * (size_t)states * (size_t)num_sms * 2, 256);
         }
     }
     l.total = off;

@@ -4,11 +4,11 @@
 //
 // Packed weights.  Sixteen neighbouring classes of a slot are a panel (the last one of a slot filled up with zero rows), 128
 // hidden elements of a panel a block, blocks of a panel follow one another:
-//   block = levels [2][32 lanes][16 bytes], lane 4g + t of half h: class 8h + g, elements 32t .. 32t + 31, four words (q4.cuh), for t >= 2 in
-//           the order 2, 3, 0, 1 (the lanes of a warp that write values to a tensor-core tile then meet in no bank);
+//   block = levels [4 chunks][16 classes][16 bytes], the 32 elements of a chunk as four words (q4.cuh);
 //           pairs  [16 classes][128 / group] (scale, origin).
-// This is the order in which the lanes of a warp hold the operand A of mma.m16n8k16 (with the hidden index permuted alike for x),
-// so a lane takes its share of a block by two 16-byte reads without bank conflicts, and a panel is one piece of memory.
+// Neighbouring lanes take neighbouring classes, so that reads of 16 bytes a lane meet in no bank, and a panel is one piece of memory.
+//
+// bfloat16: draft_logits_q4_tc.cu.  float32: the kernel below.
 #include "draft_q4.cuh"
 #include "tc_primitives.cuh"
 
@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(256) quantize_weights_q4_kernel(PackParams p) 
         const bool some = cls < p.classes && kb * kQ4Block + e / p.group * p.group < p.H;
         const uint32_t so = some ? q4_scale_origin(lo, hi) : 0u;
         const uint32_t w = in ? q4_word(v, so) : 0u;
-        reinterpret_cast<uint32_t*>(blk)[(r >> 3) * 128 + ((r & 7) * 4 + (e >> 5)) * 4 + (((e >> 3) & 3) ^ ((e >> 6) << 1))] = w;
+        reinterpret_cast<uint32_t*>(blk)[((e >> 5) * kQ4Panel + r) * 4 + ((e >> 3) & 3)] = w;
         if ((lane & 15) % per == 0) reinterpret_cast<uint32_t*>(blk + 1024)[r * (kQ4Block / p.group) + e / p.group] = so;
     }
 }
@@ -87,32 +87,14 @@ struct BestQ4 {
     }
 };
 
-// D[16x8] += A[16x16] * B[16x8], bf16 operands, fp32 accumulators (warp-wide).
-__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-constexpr int kF32Rows = 4;              // activation rows of a float32 pass
-constexpr int kF32Chunk = 36;            // floats from one 32-element chunk of x to the next (four lanes read four chunks: no bank conflict)
+constexpr int kRows = 4;                 // activation rows of a pass
 constexpr int kMaxRing = 4;              // ring slots of a warp
+constexpr int kWarps = 16, kThreads = kWarps * 32;
 
-// Bytes of the activation rows of a pass in shared memory.
-//   bfloat16: the lanes' shares of operand B, [block][word][row][chunk t][16 bytes] (a column without a row reads the last row's: its sums are not used);
-//   float32: [row][chunk][36 floats].
-template <typename T> __host__ __device__ inline size_t x_bytes(int blocks, int rows) {
-    return sizeof(T) == 2 ? (size_t)blocks * rows * 256 : (size_t)rows * blocks * 4 * kF32Chunk * 4;
-}
-
-// Warps of a CTA: as many as leave a thread the registers for its states (one of 19 registers per activation row it looks after).
-template <typename T> struct Shape {
-    static constexpr int warps = 16;
-    static constexpr int states = sizeof(T) == 2 ? 2 : 1;
-};
+__host__ __device__ inline size_t x_bytes(int blocks, int rows) { return (size_t)rows * blocks * kQ4Block * 4; }
 
 struct __align__(8) RingState {
-    uint64_t full[16 * kMaxRing];
+    uint64_t full[kWarps * kMaxRing];
     int abort_flag, never_set, merge[2];
 };
 
@@ -145,20 +127,15 @@ struct PanelWalk {
     }
 };
 
-// One CTA per SM with a contiguous range of panels.  Every warp streams panels of its own through a small ring in shared memory with the
-// bulk-copy engine (its first lane asks for the next piece when a slot has been read): levels to values (one multiply-add for
-// two), values times activations on the tensor cores (bfloat16: 16 classes x 8 rows an instruction; float32: fused
-// multiply-adds), and the lanes that hold a panel's logits keep the running maximum, sum of exponentials and best k.  Warps meet
-// at the end only.  (Sets of 4 or 8 warps that shared a panel and handed partial sums to epilogue warps took 93-113 us
-// at the 7B shape, half of it in hand-overs.)
-template <typename T>
-__global__ void __launch_bounds__(Shape<T>::warps * 32, 1) draft_q4_kernel(DraftQ4Params p) {
-    constexpr bool kMma = sizeof(T) == 2;
-    constexpr int kWarps = Shape<T>::warps, kThreads = kWarps * 32, kStates = Shape<T>::states;
-    constexpr int kRows = kMma ? 8 : kF32Rows;
+// float32.  One CTA per SM with a contiguous range of panels.  Every warp streams panels of its own through a small ring in shared memory with the
+// bulk-copy engine (its first lane asks for the next piece when a slot has been read); lane = (chunk t, class g and g + 8) makes values and multiplies
+// them with the activations of its chunk, held in shared memory; the sums of the four chunks are joined by shuffles, and lane (t, g) keeps the
+// running maximum, sum of exponentials and best k of row t.  Warps meet at the end only.  Bound by the fused multiply-adds: one for the value and
+// one a row, and four instructions to pick a level.
+__global__ void __launch_bounds__(kThreads, 1) draft_q4_f32_kernel(DraftQ4Params p) {
     extern __shared__ __align__(128) unsigned char dyn[];
     unsigned char* xs = dyn;
-    unsigned char* ring = xs + x_bytes<T>(p.blocks, p.mcount);
+    unsigned char* ring = xs + x_bytes(p.blocks, p.mcount);
     const int bb = q4_block_bytes(p.group), slot_bytes = p.piece * bb;
     RingState* sh = reinterpret_cast<RingState*>(ring + (size_t)kWarps * p.nring * slot_bytes);
     DraftPartial* s_state = reinterpret_cast<DraftPartial*>(sh + 1);         // [2][warps][kRows]
@@ -208,121 +185,62 @@ __global__ void __launch_bounds__(Shape<T>::warps * 32, 1) draft_q4_kernel(Draft
         }
         return r;
     };
-    if constexpr (kMma) {
-        const int pieces16 = p.blocks * 16;                                  // 16-byte pieces of a row: [block][chunk t][word i]
-        for (int m = 0; m < p.mcount; ++m) {
-            const long long r = source_row(m);
-#pragma unroll 2
-            for (int c = tid; c < pieces16; c += kThreads) {
-                uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                if (r >= 0 && c * 8 < p.H) w = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.x) + (size_t)r * p.H + c * 8);
-                const int kb = c >> 4, t = (c >> 2) & 3, i = (c & 3) ^ ((t >> 1) << 1);   // (in the order of the weights' words)
-                *reinterpret_cast<uint4*>(xs + (((size_t)(kb * 4 + i) * p.mcount + m) * 4 + t) * 16) = w;
-            }
-        }
-    } else {
-        const int chunks = p.blocks * 4;
-        for (int m = 0; m < p.mcount; ++m) {
-            const long long r = source_row(m);
-            for (int c = tid; c < chunks * 8; c += kThreads) {               // four floats each
-                float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (r >= 0 && c * 4 < p.H) w = *reinterpret_cast<const float4*>(static_cast<const T*>(p.x) + (size_t)r * p.H + c * 4);
-                *reinterpret_cast<float4*>(reinterpret_cast<float*>(xs) + ((size_t)m * chunks + (c >> 3)) * kF32Chunk + (c & 7) * 4) = w;
-            }
+    const int quads = p.blocks * (kQ4Block / 4);
+    for (int m = 0; m < p.mcount; ++m) {
+        const long long r = source_row(m);
+        for (int c = tid; c < quads; c += kThreads) {                        // four floats each
+            float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (r >= 0 && c * 4 < p.H) w = *reinterpret_cast<const float4*>(static_cast<const float*>(p.x) + (size_t)r * p.H + c * 4);
+            reinterpret_cast<float4*>(xs)[(size_t)m * quads + c] = w;
         }
     }
     __syncthreads();
 
-    const int g = lane >> 2, t = lane & 3;
-    // the lane's activation rows (columns of the product), and their states
-    auto col_of = [&](int c) -> int { return kMma ? 2 * t + c : t; };
-    BestQ4 best[kStates];
-    float bias[kStates];
-#pragma unroll
-    for (int c = 0; c < kStates; ++c) {
-        best[c].init();
-        bias[c] = 0.f;
-        const int m = col_of(c);
-        if (m < p.mcount && p.blank_bias != nullptr) bias[c] = p.blank_bias[p.row_seq ? p.row_seq[p.m0 + m] : p.m0 + m];
-    }
+    const int g = lane & 7, t = lane >> 3;
+    BestQ4 best;                                                              // of row t
+    best.init();
+    float bias = 0.f;
+    if (t < p.mcount && p.blank_bias != nullptr) bias = p.blank_bias[p.row_seq ? p.row_seq[p.m0 + t] : p.m0 + t];
     // the warp's states of a draft slot, one for every row, to shared memory
     auto put_states = [&](int seg) __attribute__((always_inline)) {
-#pragma unroll
-        for (int c = 0; c < kStates; ++c) {
-            combine_best<28>(best[c].st, p.k);
-            if (g == 0 && col_of(c) < kRows) best[c].st.store(&s_state[(seg * kWarps + warp) * kRows + col_of(c)]);
-            best[c].init();
-        }
+        combine_best<7>(best.st, p.k);
+        if (g == 0) best.st.store(&s_state[(seg * kWarps + warp) * kRows + t]);
+        best.init();
     };
     int cur_seg = 0;
-    // the panel's logits: z[c][u] is class g + 8u, row col_of(c)
-    auto push = [&](int pan, const float (&z)[kStates][2]) __attribute__((always_inline)) {
+    // the panel's logits: z[u] is class g + 8u, row t
+    auto push = [&](int pan, const float (&z)[2]) __attribute__((always_inline)) {
         const int seg = pan >= n_seg0 ? 1 : 0, slot = slot0 + seg;
         if (seg != cur_seg) { put_states(0); cur_seg = 1; }
         const int v0 = (int)(p0 + pan - (long long)slot * p.panels) * kQ4Panel + g;
 #pragma unroll
-        for (int c = 0; c < kStates; ++c) {
-            const int m = col_of(c);
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int v = v0 + 8 * u;
-                if (m < p.mcount && v < p.classes) {
-                    const float zz = z[c][u] + (v == p.classes - 1 ? bias[c] : 0.f);
-                    if (p.logits_dbg) p.logits_dbg[((size_t)(p.m0 + m) * p.slots + slot) * p.classes + v] = zz;
-                    best[c].push(zz, v, p.k);
-                }
+        for (int u = 0; u < 2; ++u) {
+            const int v = v0 + 8 * u;
+            if (t < p.mcount && v < p.classes) {
+                const float zz = z[u] + (v == p.classes - 1 ? bias : 0.f);
+                if (p.logits_dbg) p.logits_dbg[((size_t)(p.m0 + t) * p.slots + slot) * p.classes + v] = zz;
+                best.push(zz, v, p.k);
             }
         }
     };
 
     const int gpb = kQ4Block / p.group;                                        // groups of a block
     const unsigned so_a = 1024u + (g * gpb + t * 32 / p.group) * 4, so_b = so_a + 8 * gpb * 4;
-    const unsigned xstep = (unsigned)p.mcount * 64u;                          // bytes from a word's activations to the next word's
-    const unsigned xblock = kMma ? 4u * xstep : 4u * kF32Chunk * 4u;
-    const unsigned xrow = (g < p.mcount ? g : p.mcount - 1) * 64u + t * 16u;
-    constexpr int kChains = 2;                                               // sums that run side by side (an instruction waits for the one before it in its own)
-    float acc[kChains][4];
-    // The tensor core cuts a sum's last bits off at every addition, always towards zero, so long chains drift: a piece's sums are
-    // added here in rounded arithmetic and begin again (7B shape: log-probabilities off by 1.1e-6 without, MEASURED with).
-    float tot[kStates][2];
-    float facc[2][kF32Rows];
+    float acc[2][kRows];
     auto clear = [&]() {
 #pragma unroll
-        for (int u = 0; u < kChains; ++u)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) acc[u][q] = 0.f;
-#pragma unroll
-        for (int m = 0; m < kF32Rows; ++m) facc[0][m] = facc[1][m] = 0.f;
-#pragma unroll
-        for (int c = 0; c < kStates; ++c) tot[c][0] = tot[c][1] = 0.f;
+        for (int m = 0; m < kRows; ++m) acc[0][m] = acc[1][m] = 0.f;
     };
     clear();
-    auto gather = [&]() {
+    auto finish = [&](float (&z)[2]) __attribute__((always_inline)) {         // the sums as logits, and zero again
 #pragma unroll
-        for (int c = 0; c < kStates; ++c)
+        for (int m = 0; m < kRows; ++m)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) tot[c][u] += acc[0][2 * u + c] + acc[1][2 * u + c];
-#pragma unroll
-        for (int u = 0; u < kChains; ++u)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) acc[u][q] = 0.f;
-    };
-    auto finish = [&](float (&z)[kStates][2]) __attribute__((always_inline)) {   // the sums as logits, and zero again
-        if constexpr (kMma) {
-#pragma unroll
-            for (int c = 0; c < kStates; ++c)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) z[c][u] = tot[c][u];
-        } else {
-#pragma unroll
-            for (int m = 0; m < kF32Rows; ++m)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    facc[u][m] += __shfl_xor_sync(0xffffffffu, facc[u][m], 1);
-                    facc[u][m] += __shfl_xor_sync(0xffffffffu, facc[u][m], 2);
-                    if (t == m) z[0][u] = facc[u][m];
-                }
-        }
+            for (int u = 0; u < 2; ++u) {
+                acc[u][m] += __shfl_xor_sync(0xffffffffu, acc[u][m], 8);
+                acc[u][m] += __shfl_xor_sync(0xffffffffu, acc[u][m], 16);
+                if (t == m) z[u] = acc[u][m];
+            }
         clear();
     };
 
@@ -334,48 +252,36 @@ __global__ void __launch_bounds__(Shape<T>::warps * 32, 1) draft_q4_kernel(Draft
         if (!tc::mbar_wait(my_full + s, phase, abort_flag)) { failed = true; break; }
         const int nb = min(p.piece, at.end - at.blk);
         const unsigned char* blk = my_ring + s * slot_bytes;
-        const unsigned char* xb = xs + (unsigned)at.blk * xblock;
-        for (int kb = 0; kb < nb; ++kb, blk += bb, xb += xblock) {
-            const uint4 wa = *reinterpret_cast<const uint4*>(blk + lane * 16);
-            const uint4 wb = *reinterpret_cast<const uint4*>(blk + 512 + lane * 16);
+        const float* xb = reinterpret_cast<const float*>(xs) + (size_t)at.blk * kQ4Block + t * 32;
+        const unsigned row = (unsigned)p.blocks * kQ4Block;
+        for (int kb = 0; kb < nb; ++kb, blk += bb, xb += kQ4Block) {
+            const uint4 wa = *reinterpret_cast<const uint4*>(blk + (t * kQ4Panel + g) * 16);
+            const uint4 wb = *reinterpret_cast<const uint4*>(blk + (t * kQ4Panel + g + 8) * 16);
             const uint32_t sa = *reinterpret_cast<const uint32_t*>(blk + so_a);
             const uint32_t sb = *reinterpret_cast<const uint32_t*>(blk + so_b);
             const uint32_t a4[4] = {wa.x, wa.y, wa.z, wa.w}, b4[4] = {wb.x, wb.y, wb.z, wb.w};
-            if constexpr (kMma) {
+            const float s0 = bf16lo(sa), o0 = bf16hi(sa), s1 = bf16lo(sb), o1 = bf16hi(sb);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint4 va = q4_values_bf16(a4[i], sa), vb = q4_values_bf16(b4[i], sb);
-                    const uint4 x = *reinterpret_cast<const uint4*>(xb + i * xstep + xrow);
-                    mma_16816(acc[0], va.x, vb.x, va.y, vb.y, x.x, x.y);
-                    mma_16816(acc[1], va.z, vb.z, va.w, vb.w, x.z, x.w);
-                }
-            } else {
-                const float* xf = reinterpret_cast<const float*>(xb) + t * kF32Chunk;
-                const unsigned row = (unsigned)p.blocks * 4 * kF32Chunk;
-                const float s0 = bf16lo(sa), o0 = bf16hi(sa), s1 = bf16lo(sb), o1 = bf16hi(sb);
+            for (int i = 0; i < 4; ++i) {
+                float va[8], vb[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float va[8], vb[8];
+                for (int e = 0; e < 8; ++e) { va[e] = q4_value_f32(a4[i], e, s0, o0); vb[e] = q4_value_f32(b4[i], e, s1, o1); }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) { va[e] = q4_value_f32(a4[i], e, s0, o0); vb[e] = q4_value_f32(b4[i], e, s1, o1); }
+                for (int m = 0; m < kRows; ++m) {
+                    if (m >= p.mcount) break;
+                    float x[8];
+                    load8(xb + m * row + i * 8, x);
 #pragma unroll
-                    for (int m = 0; m < kF32Rows; ++m) {
-                        if (m >= p.mcount) break;
-                        float x[8];
-                        load8(xf + m * row + (i ^ ((t >> 1) << 1)) * 8, x);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) { facc[0][m] = fmaf(va[e], x[e], facc[0][m]); facc[1][m] = fmaf(vb[e], x[e], facc[1][m]); }
-                    }
+                    for (int e = 0; e < 8; ++e) { acc[0][m] = fmaf(va[e], x[e], acc[0][m]); acc[1][m] = fmaf(vb[e], x[e], acc[1][m]); }
                 }
             }
         }
         at.blk += nb;
-        if constexpr (kMma) gather();
         __syncwarp();                                                        // the slot has been read
         ask(s);
         if (++s == p.nring) { s = 0; phase ^= 1u; }
         if (at.shared || at.blk < at.end) continue;
-        float z[kStates][2];
+        float z[2];
         finish(z);
         push(at.pan, z);
         at.next_panel();
@@ -391,23 +297,19 @@ __global__ void __launch_bounds__(Shape<T>::warps * 32, 1) draft_q4_kernel(Draft
     if (*abort_flag != 0) return;                                            // (uniform: set before the barrier or not at all)
     // ---- the panels that were shared: partial sums through the rings' memory, one warp adds a panel's up ----
     if (at.whole < npan) {
-        float* sums = reinterpret_cast<float*>(ring);                        // [warps][kStates * 2][32 lanes]
-        float z[kStates][2];
+        float* sums = reinterpret_cast<float*>(ring);                        // [warps][2][32 lanes]
+        float z[2];
         finish(z);
 #pragma unroll
-        for (int c = 0; c < kStates; ++c)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) sums[(warp * kStates * 2 + 2 * c + u) * 32 + lane] = z[c][u];
+        for (int u = 0; u < 2; ++u) sums[(warp * 2 + u) * 32 + lane] = z[u];
         __syncthreads();
         const int rest = npan - at.whole;
         if (warp < rest) {
 #pragma unroll
-            for (int c = 0; c < kStates; ++c)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    z[c][u] = 0.f;
-                    for (int w = 0; w < at.per; ++w) z[c][u] += sums[((warp * at.per + w) * kStates * 2 + 2 * c + u) * 32 + lane];
-                }
+            for (int u = 0; u < 2; ++u) {
+                z[u] = 0.f;
+                for (int w = 0; w < at.per; ++w) z[u] += sums[((warp * at.per + w) * 2 + u) * 32 + lane];
+            }
             push(at.whole + warp, z);
         }
     }
@@ -424,7 +326,7 @@ __global__ void __launch_bounds__(Shape<T>::warps * 32, 1) draft_q4_kernel(Draft
         combine_best<31>(ms, p.k);
         if (lane == 0) ms.store(p.part + ((size_t)m * gridDim.x + blockIdx.x) * 2 + seg);
     }
-    draft_q4_finish(p, p.panels, 0, 1, slot0, segs, sh->merge);
+    draft_q4_finish(p, p.panels, slot0, segs, sh->merge);
 }
 
 int panels_of(const ctcsd_config& c) { return (c.V + 1 + kQ4Panel - 1) / kQ4Panel; }
@@ -432,18 +334,13 @@ int blocks_of(const ctcsd_config& c) { return (c.H + kQ4Block - 1) / kQ4Block; }
 
 constexpr size_t kSmemBudget = kMaxDynamicSmem - 1024;                       // (1 KB of every CTA is the system's)
 
-template <typename T>
-size_t fixed_smem(int blocks, int rows) {
-    return x_bytes<T>(blocks, rows) + sizeof(RingState) + sizeof(DraftPartial) * 2 * Shape<T>::warps * (sizeof(T) == 2 ? 8 : kF32Rows);
-}
+size_t fixed_smem(int blocks, int rows) { return x_bytes(blocks, rows) + sizeof(RingState) + sizeof(DraftPartial) * 2 * kWarps * kRows; }
 
 // Ring geometry: blocks of a slot, slots of a warp.  False where there is no room for two blocks a warp.
-template <typename T>
 bool ring_shape(DraftQ4Params& p) {
-    constexpr size_t warps = Shape<T>::warps;
-    const size_t fixed = fixed_smem<T>(p.blocks, p.mcount);
+    const size_t fixed = fixed_smem(p.blocks, p.mcount);
     if (fixed > kSmemBudget) return false;
-    const size_t bb = (size_t)q4_block_bytes(p.group), most = (kSmemBudget - fixed) / (warps * bb);        // blocks there is room for, a warp
+    const size_t bb = (size_t)q4_block_bytes(p.group), most = (kSmemBudget - fixed) / (kWarps * bb);       // blocks there is room for, a warp
     if (most < 2) return false;
     // two slots, of 8 blocks at most; three where they are small then
     p.piece = (int)(most / 2 < 8 ? most / 2 : 8);
@@ -452,15 +349,13 @@ bool ring_shape(DraftQ4Params& p) {
     return true;
 }
 
-template <typename T>
 int launch_pass(Handle* h, cudaStream_t s, DraftQ4Params& p) {
-    if (!ring_shape<T>(p)) return CTCSD_ERR_UNSUPPORTED;
-    const size_t smem = fixed_smem<T>(p.blocks, p.mcount) + (size_t)Shape<T>::warps * p.nring * p.piece * q4_block_bytes(p.group);
-    auto kern = draft_q4_kernel<T>;
-    CTCSD_CUDA_CHECK(h, prepare_kernel(h, sizeof(T) == 4 ? kPrepDraftQ4F32 : kPrepDraftQ4, kern));
+    if (!ring_shape(p)) return CTCSD_ERR_UNSUPPORTED;
+    const size_t smem = fixed_smem(p.blocks, p.mcount) + (size_t)kWarps * p.nring * p.piece * q4_block_bytes(p.group);
+    CTCSD_CUDA_CHECK(h, prepare_kernel(h, kPrepDraftQ4F32, draft_q4_f32_kernel));
     const long long total = (long long)p.panels * p.slots;
     const unsigned grid = (unsigned)(total < h->num_sms ? total : h->num_sms);        // (total >= slots: a range touches two slots at most)
-    CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(grid), dim3(Shape<T>::warps * 32), smem, s, 1, p));
+    CTCSD_CUDA_CHECK(h, launch_pdl(draft_q4_f32_kernel, dim3(grid), dim3(kThreads), smem, s, 1, p));
     h->launches++;
     return CTCSD_OK;
 }
@@ -520,29 +415,19 @@ extern "C" int ctcsd_draft_logits_q4(ctcsd_handle* hh, void* stream, int M, cons
     const DeviceGuard on(h->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool bf16 = c.dtype == CTCSD_DTYPE_BF16;
-    // more than 8 rows: the tensor memory's kernel, whose cost hardly depends on the rows (7B shape: 8 rows 108 us here, 16 rows 185 us there)
-    if (bf16 && M > 8 && c.H >= 64) {
-        for (int m0 = 0; m0 < M; m0 += kDraftQ4TcRows) {
-            p.m0 = m0;
-            p.mcount = M - m0 < kDraftQ4TcRows ? M - m0 : kDraftQ4TcRows;
-            const int rc = launch_draft_q4_tc(h, s, p);
-            if (rc != CTCSD_OK) return rc;
-        }
-        return CTCSD_OK;
-    }
-    // rows of a pass: 8 (float32: 4), or as many as leave the rings room
+    // rows of a pass (float32: or as many as leave the rings room)
+    int per_pass = bf16 ? kDraftQ4TcRows : kRows;
+    if (per_pass > M) per_pass = M;
     auto fits = [&](int rows) {
         DraftQ4Params q = p;
         q.mcount = rows;
-        return bf16 ? ring_shape<__nv_bfloat16>(q) : ring_shape<float>(q);
+        return ring_shape(q);
     };
-    int per_pass = bf16 ? 8 : kF32Rows;
-    if (per_pass > M) per_pass = M;
-    while (per_pass > 1 && !fits(per_pass)) per_pass = (per_pass + 1) / 2;
+    while (!bf16 && per_pass > 1 && !fits(per_pass)) per_pass = (per_pass + 1) / 2;
     for (int m0 = 0; m0 < M; m0 += per_pass) {
         p.m0 = m0;
         p.mcount = M - m0 < per_pass ? M - m0 : per_pass;
-        const int rc = bf16 ? launch_pass<__nv_bfloat16>(h, s, p) : launch_pass<float>(h, s, p);
+        const int rc = bf16 ? launch_draft_q4_tc(h, s, p) : launch_pass(h, s, p);
         if (rc != CTCSD_OK) return rc;
     }
     return CTCSD_OK;

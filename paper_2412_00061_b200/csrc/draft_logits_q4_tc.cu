@@ -1,40 +1,51 @@
-// Draft head over 4-bit weights for more than 8 activation rows, on the 5th-generation tensor cores (tcgen05 + TMEM).
+// Draft head over 4-bit weights for bfloat16, on the 5th-generation tensor cores (tcgen05 + TMEM), for up to 128 activation rows in a pass.
 //
-// D[128 x 192] = A[128 x H] B[192 x H]^T per tile: A = up to 128 activation rows, B = twelve panels of weights (draft_q4.cuh) as bfloat16 values,
-// both K-major with the 128-byte swizzle, 128 hidden elements to a stage, two stages; D in tensor memory (lane = activation row, column
-// = class), twice, so that a tile is read back while the next one is multiplied.
-// Twelve warps each take one panel of the tile from a ring that one TMA copy fills for all of them (a warp that asked for its own panel spent some 600
-// cycles on every request), turn its levels into values and write them into the stage, a 128-element block of 16 classes by
-// eight 16-byte stores a lane, which meet in no bank.  The cost hardly depends on the activation rows, so 9 to 128 of them take one pass.
-// Roles: warps 0-3 read the accumulators back (a quarter of the activation rows each), 4-15 make values, 16 loads activations, 17
-// issues the products, 18 loads levels.
+// D[128 x N] = A[128 x H] B[N x H]^T per tile: A = eight panels of weights (draft_q4.cuh) as bfloat16 values, in tensor memory (lane = class); B =
+// the activation rows, K-major with the 128-byte swizzle in shared memory, N the rows rounded up to 16; 128 hidden elements to a stage;
+// D in tensor memory (lane = class, column = row).
+// Sixteen warps turn levels into values, four to a stage, 32 classes each: a lane reads its class's levels of a block, 64 bytes, and writes 64 columns of
+// tensor memory.  So the values never pass through shared memory, and a row costs its share of B and D only.  (Weights as the B operand, written to
+// swizzled tiles in shared memory, with activations padded to 128 rows as A: 403 us for 32 rows of the 70B shape; and 8 rows and fewer were better off
+// with mma.sync, 99 us for a row of the 7B shape.)
+// The tensor core cuts a sum's last bits off at every addition, always towards zero, and long chains drift (log-probabilities off by
+// 6e-6 at H = 8192).  So sums begin again every kStretch blocks, and the four warps that read D back add them up in rounded arithmetic, in tensor memory.
+// They then turn 32 classes x 32 rows through shared memory, so that a lane has a row, and keep each row's maximum, sum of exponentials and best k.
+// Roles: warps 0-3 read sums back (32 classes each), 4-19 make values, 20 loads activations, 21 loads levels, 22 and 23 issue the
+// products of every other block each, into sums of their own (an issue takes some 500 cycles of waiting, describing and committing, more than its products).
 #include "draft_q4.cuh"
 #include "tc_primitives.cuh"
+
+#include <type_traits>
 
 namespace ctcsd {
 namespace {
 
 constexpr int kEpi = 4;
-constexpr int kStages = 2;
+constexpr int kGroups = 4;               // groups of four warps that make values
+constexpr int kMakers = 4 * kGroups;
+constexpr int kStages = kGroups;         // a stage holds a block; each group has its own, so that it sees every fill of it and no turn of its barriers goes by unseen
 constexpr int kMaxRing = 8;
-constexpr int kMakers = 12;              // warps that make values: one panel of the tile each
-constexpr int kThreads = (kEpi + kMakers + 3) * 32;
-constexpr int kTileN = kMakers * kQ4Panel, kBBytes = kTileN * kQ4Block * 2;
-constexpr int kAccCols = 256;            // columns from one accumulator to the other
+constexpr int kMaxAccs = 4;              // sums in tensor memory that take turns
+constexpr int kThreads = (kEpi + kMakers + 4) * 32;
+constexpr int kTile = 128, kTilePanels = kTile / kQ4Panel;
+constexpr int kStretch = 4;              // blocks whose products the tensor core adds up, per issuing warp
+constexpr int kTurn = 32 * 33;           // floats of a warp's 32 x 32 turning buffer
+constexpr int kSaved = 2 * kTopSlots + 2;    // words of a row's running state
 
 struct __align__(8) TcState {
-    uint64_t raw_full[kMaxRing], raw_empty[kMaxRing];    // levels of the tile's panels, a few blocks of each
-    uint64_t a_full[kStages], b_full[kStages], empty[kStages];
-    uint64_t acc_full[2], acc_empty[2];
+    uint64_t raw_full[kMaxRing], raw_empty[kMaxRing];    // levels of the tile's panels, two blocks of each
+    uint64_t x_full[kStages], v_full[kStages], empty[kStages];               // activations; values; both have been multiplied
+    uint64_t acc_full[kMaxAccs], acc_empty[kMaxAccs];
     uint32_t tmem_base;
     int abort_flag, never_set, merge[2];
 };
 
 struct TcGeo {
     int tiles;                           // tiles of a draft slot
-    int a_rows;                          // activation rows of a stage: 64 or 128 (products read 128: with 64, the rows behind are whatever follows, and their
-                                         // sums are not looked at)
-    int rows, copies;                    // they are `copies` times `rows`
+    int n;                               // rows of the product: those there are, rounded up to 16 (those behind the last are zeros)
+    int chunks;                          // 32-row chunks
+    int issuers;                         // warps that issue products, of every issuers-th block each, into sums of their own
+    int accs;                            // sums that take turns, of each (512 columns: 64 a stage, 32 a chunk of each of the sums and of the total)
 };
 
 __device__ __forceinline__ void give_up(TcState* sh, int* status, int site) {
@@ -44,12 +55,14 @@ __device__ __forceinline__ void give_up(TcState* sh, int* status, int site) {
 }
 
 __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, DraftQ4Params p,
-                                                                              TcGeo geo) {
+                                                                  TcGeo geo) {
     extern __shared__ __align__(1024) unsigned char dyn[];
-    const int a_plane = geo.a_rows * 128, a_bytes = 2 * a_plane, stage_bytes = a_bytes + kBBytes;   // (a plane: 64 elements)
-    unsigned char* ring = dyn + kStages * stage_bytes;
-    const int bb = q4_block_bytes(p.group), slot_bytes = (kMakers * p.piece * bb + 127) / 128 * 128;
-    TcState* sh = reinterpret_cast<TcState*>(ring + (size_t)p.nring * slot_bytes);
+    const int x_plane = geo.n * 128, x_bytes = 2 * x_plane;                   // activations of a stage (a plane: 64 elements)
+    unsigned char* ring = dyn + kStages * x_bytes;
+    const int bb = q4_block_bytes(p.group), slot_bytes = kTilePanels * 2 * bb;
+    float* turn = reinterpret_cast<float*>(ring + (size_t)p.nring * slot_bytes);            // [kEpi][kTurn]
+    uint32_t* saved = reinterpret_cast<uint32_t*>(turn + kEpi * kTurn);                     // [kEpi][chunks][kSaved][32]
+    TcState* sh = reinterpret_cast<TcState*>(saved + kEpi * geo.chunks * kSaved * 32);
     if ((tc::smem_u32(dyn) & 1023u) != 0u) {                   // uniform over the CTA
         if (threadIdx.x == 0) report_error(p.status, CTCSD_ERR_INTERNAL, 45);
         return;
@@ -58,8 +71,8 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
     volatile int* abort_flag = &sh->abort_flag;
     if (tid == 0) {
         for (int s = 0; s < p.nring; ++s) { tc::mbar_init(&sh->raw_full[s], 1); tc::mbar_init(&sh->raw_empty[s], kMakers); }
-        for (int s = 0; s < kStages; ++s) { tc::mbar_init(&sh->a_full[s], 1); tc::mbar_init(&sh->b_full[s], kMakers); tc::mbar_init(&sh->empty[s], 1); }
-        for (int a = 0; a < 2; ++a) { tc::mbar_init(&sh->acc_full[a], 1); tc::mbar_init(&sh->acc_empty[a], kEpi); }
+        for (int s = 0; s < kStages; ++s) { tc::mbar_init(&sh->x_full[s], 1); tc::mbar_init(&sh->v_full[s], 4); tc::mbar_init(&sh->empty[s], 1); }
+        for (int a = 0; a < geo.accs; ++a) { tc::mbar_init(&sh->acc_full[a], geo.issuers); tc::mbar_init(&sh->acc_empty[a], kEpi); }
         sh->abort_flag = 0;
         sh->never_set = 0;
         tc::fence_barrier_init();
@@ -71,7 +84,8 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
     tc::tc_fence_before_sync();
     __syncthreads();
     tc::tc_fence_after_sync();
-    const uint32_t tmem = sh->tmem_base;
+    // columns: values of the stages, the sums, the total
+    const uint32_t tmem = sh->tmem_base, tmem_d = tmem + 64u * kStages, acc_cols = 32u * geo.chunks, tmem_t = tmem_d + geo.accs * geo.issuers * acc_cols;
     // this CTA's tiles: u0 .. u1-1 of the line of all slots' tiles
     const long long total = (long long)geo.tiles * p.slots;
     const int u0 = (int)(total * blockIdx.x / gridDim.x), u1 = (int)(total * (blockIdx.x + 1) / gridDim.x);
@@ -79,178 +93,253 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
     const int segs = u1 > (slot0 + 1) * geo.tiles ? 2 : 1;
     // Every CTA begins at a place of its own along the hidden axis (and wraps), so that at any moment the CTAs ask L2 for different parts of the
     // activations that they all share.
-    const int pieces = (p.blocks + p.piece - 1) / p.piece, start = (int)((long long)blockIdx.x * pieces / gridDim.x);
+    const int pairs = (p.blocks + 1) / 2, start = (int)((long long)blockIdx.x * pairs / gridDim.x);       // pairs of blocks; the last may be one block
+    const int stretch = kStretch * geo.issuers;
+    const int copy_rows = geo.n == 16 ? 16 : geo.chunks * 32;                 // rows from a row's state to its next one
     bool failed = false;
 
     if (warp < kEpi) {
         // ---------------- logits ----------------
         pdl_wait();
         pdl_trigger();
-        // A warp reads a quarter of the tensor memory's lanes.  Up to 32 rows stand there twice, and two warps take turns with chunks of 32
-        // columns (four copies take room from the ring: 444 us against 400 for 32 rows of the 70B shape).
-        const int copy = warp * 32 / geo.rows, row = warp * 32 + lane, m = row - copy * geo.rows;
-        const uint32_t lane_addr = tmem + ((uint32_t)(warp * 32) << 16);
-        const bool live = row < geo.a_rows && m < p.mcount, warp_live = warp * 32 < geo.a_rows && m - lane < p.mcount;
-        float bias = 0.f;
-        if (live && p.blank_bias != nullptr) bias = p.blank_bias[p.row_seq ? p.row_seq[p.m0 + m] : p.m0 + m];
+        const uint32_t lane_off = (uint32_t)(warp * 32) << 16;                // the quarter of the tensor memory's lanes that the warp reads
+        float* const my_turn = turn + warp * kTurn;
+        uint32_t* const my_saved = saved + warp * geo.chunks * kSaved * 32 + lane;
         RunState st;
-        st.init();
-        float floor = -INFINITY;                               // a logit has to be above it to be among the k best,
-        int have = 0;                                          // unless the list holds fewer
-        int n = 0, seg = 0;
-        for (int u = u0; u < u1; ++u, ++n) {
-            const int slot = u / geo.tiles, v0 = (u - slot * geo.tiles) * kTileN;
-            if (slot - slot0 != seg) {
-                if (live) st.store(p.part + ((size_t)row * gridDim.x + blockIdx.x) * 2);
-                st.init();
-                floor = -INFINITY;
-                have = 0;
-                seg = 1;
+        float floor;                                           // a logit has to be above it to be among the k best,
+        bool listed;                                           // unless the list holds fewer
+        auto look = [&]() {
+#pragma unroll
+            for (int s = 0; s < kTopSlots; ++s) {
+                float f = st.val[s];
+                int i = st.id[s];
+                asm("" : "+f"(f), "+r"(i));                    // (else the compiler makes it a look-up by k, and the list leaves the registers)
+                if (s == p.k - 1) { floor = f; listed = i != INT_MAX; }
             }
-            if (!tc::mbar_wait_suspended(&sh->acc_full[n & 1], (uint32_t)(n >> 1) & 1u, abort_flag)) failed = true;
-            failed = __any_sync(0xffffffffu, failed);
-            if (failed) break;
-            tc::tc_fence_after_sync();
-            if (warp_live) {
-#pragma unroll 1
-                for (int c0 = copy * 32; c0 < kTileN && v0 + c0 < p.classes; c0 += 32 * geo.copies) {
-                    uint32_t r[32];
-                    const uint32_t addr = lane_addr + (uint32_t)((n & 1) * kAccCols + c0);
-                    tc::tmem_read32(addr, r);
-                    const int left = p.classes - v0 - c0;      // classes of the chunk
-                    const bool blank = left <= 32;             // its last one is the blank
-                    float top = -INFINITY;
+        };
+        auto save = [&](int c) {
+            uint32_t* to = my_saved + c * kSaved * 32;
+            to[0] = __float_as_uint(st.mx); to[32] = __float_as_uint(st.sum);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        float z = __uint_as_float(r[j]);
-                        if (blank && j == left - 1) z += bias;
-                        if (j < left) {
-                            if (p.logits_dbg != nullptr && live)
-                                p.logits_dbg[((size_t)(p.m0 + m) * p.slots + slot) * p.classes + v0 + c0 + j] = z;
+            for (int s = 0; s < kTopSlots; ++s) { to[(2 + 2 * s) * 32] = __float_as_uint(st.val[s]); to[(3 + 2 * s) * 32] = (uint32_t)st.id[s]; }
+        };
+        auto load = [&](int c) {
+            const uint32_t* from = my_saved + c * kSaved * 32;
+            st.mx = __uint_as_float(from[0]); st.sum = __uint_as_float(from[32]);
+#pragma unroll
+            for (int s = 0; s < kTopSlots; ++s) { st.val[s] = __uint_as_float(from[(2 + 2 * s) * 32]); st.id[s] = (int)from[(3 + 2 * s) * 32]; }
+        };
+        // the states of a draft slot: a row has one of every warp (two where a lane has half of the classes), copy_rows rows apart
+        auto publish = [&](int seg) {
+            for (int c = 0; c < geo.chunks; ++c) {
+                load(c);
+                const int i = (warp * geo.chunks + c) * 32 + lane;
+                if (i % copy_rows < p.mcount) st.store(p.part + ((size_t)i * gridDim.x + blockIdx.x) * 2 + seg);
+            }
+        };
+        auto begin = [&]() {
+            st.init();
+            for (int c = 0; c < geo.chunks; ++c) save(c);
+        };
+        // A chunk of a tile's logits: R rows of 32 classes, turned so that a lane has a row (R = 16: and half of the classes).
+        auto look_through = [&](auto rows, int c, int slot, int v0, int left) __attribute__((always_inline)) {
+            constexpr int R = decltype(rows)::value, J = R;     // J classes a lane
+            uint32_t r[32];
+            if constexpr (R == 32) tc::tmem_read32(tmem_t + c * 32 + lane_off, r);
+            else tc::tmem_read16(tmem_t + lane_off, reinterpret_cast<uint32_t(&)[16]>(r));
+#pragma unroll
+            for (int j = 0; j < R; ++j) my_turn[j * 33 + lane] = __uint_as_float(r[j]);
+            __syncwarp();
+            float z[J];
+            const int row = lane % R, j0 = lane / R * J;
+#pragma unroll
+            for (int j = 0; j < J; ++j) z[j] = my_turn[row * 33 + j0 + j];      // class v0 + j0 + j, row c * 32 + row
+            __syncwarp();
+            const int m = c * 32 + row;
+            const bool live = m < p.mcount;
+            load(c);
+            look();
+            v0 += j0;
+            left -= j0;                                        // classes that the lane has
+            if (left <= J) {                                   // (the last one is the blank)
+                float bias = 0.f;
+                if (live && left > 0 && p.blank_bias != nullptr) bias = p.blank_bias[p.row_seq ? p.row_seq[p.m0 + m] : p.m0 + m];
+#pragma unroll
+                for (int j = 0; j < J; ++j) z[j] = j < left ? z[j] + (j == left - 1 ? bias : 0.f) : -INFINITY;
+            }
+            if (p.logits_dbg != nullptr && live) {
+                float* out = p.logits_dbg + ((size_t)(p.m0 + m) * p.slots + slot) * p.classes + v0;
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+                    if (j < left) out[j] = z[j];
+            }
+            float top = z[0];
+#pragma unroll
+            for (int j = 1; j < J; ++j) top = fmaxf(top, z[j]);
+            if (top > st.mx) {
+                st.sum *= __expf(st.mx - top);                 // exp(-inf) = 0 covers the first chunk
+                st.mx = top;
+            }
+            float add = 0.f;
+#pragma unroll
+            for (int j = 0; j < J; ++j) add += __expf(z[j] - st.mx);
+            if (left > 0) st.sum += add;                       // (none: -inf - -inf)
+            if (__any_sync(0xffffffffu, live && left > 0 && (top > floor || !listed))) {
+                uint32_t above = 0u;                           // logits that may be among the best
+#pragma unroll
+                for (int j = 0; j < J; ++j) above |= z[j] > floor || !listed ? 1u << j : 0u;
+                if (left < J) above &= left > 0 ? (1u << left) - 1u : 0u;
+                if (!live) above = 0u;
+                // every lane takes its own, the largest first, so that few come to be tried (at most one more than stay)
+                while (__any_sync(0xffffffffu, above != 0u)) {
+                    float best = -INFINITY;
+                    int at = -1;
+#pragma unroll
+                    for (int j = 0; j < J; ++j) {
+                        const bool better = ((above >> j) & 1u) && (at < 0 || z[j] > best);
+                        best = better ? z[j] : best;
+                        at = better ? j : at;
+                    }
+                    if (at >= 0) {
+                        above &= ~(1u << at);
+                        if (best > floor || !listed) {
+                            topk_insert(st.val, st.id, best, v0 + at);
+                            look();
                         } else {
-                            z = -INFINITY;
-                        }
-                        r[j] = __float_as_uint(z);
-                        top = fmaxf(top, z);
-                    }
-                    if (top > st.mx) {
-                        st.sum *= __expf(st.mx - top);         // exp(-inf) = 0 covers the first chunk
-                        st.mx = top;
-                    }
-                    uint32_t above = 0u;                       // logits that may be among the best
-                    float add = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const float z = __uint_as_float(r[j]);
-                        add += j < left ? __expf(z - st.mx) : 0.f;
-                        above |= z > floor ? 1u << j : 0u;
-                    }
-                    st.sum += add;
-                    if (have < p.k) above = left >= 32 ? 0xffffffffu : (1u << left) - 1u;
-                    // every lane takes its own, the largest first, so that few come to be tried (at most one more than stay)
-                    while (__any_sync(0xffffffffu, above != 0u)) {
-                        float z = -INFINITY;
-                        int at = -1;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const bool better = ((above >> j) & 1u) && (at < 0 || __uint_as_float(r[j]) > z);
-                            z = better ? __uint_as_float(r[j]) : z;
-                            at = better ? j : at;
-                        }
-                        if (at >= 0) {
-                            above &= ~(1u << at);
-                            if (z > floor || have < p.k) {
-                                topk_insert(st.val, st.id, z, v0 + c0 + at);
-                                have += z == z ? 1 : 0;
-#pragma unroll
-                                for (int s = 0; s < kTopSlots; ++s) {
-                                    float f = st.val[s];
-                                    asm("" : "+f"(f));         // (else the compiler makes it a look-up by k, and the list leaves the registers)
-                                    if (s == p.k - 1) floor = f;
-                                }
-                            } else {
-                                above = 0u;
-                            }
+                            above = 0u;
                         }
                     }
                 }
             }
-            tc::tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&sh->acc_empty[n & 1]);
+            save(c);
+        };
+        begin();
+        int a = 0, seg = 0;
+        uint32_t phase = 0u;
+        for (int u = u0; u < u1 && !failed; ++u) {
+            const int slot = u / geo.tiles, v0 = (u - slot * geo.tiles) * kTile + warp * 32;
+            const int left = p.classes - v0;                   // classes that the warp has
+            if (slot - slot0 != seg) {
+                publish(0);
+                begin();
+                seg = 1;
+            }
+            for (int kb0 = 0; kb0 < p.blocks; kb0 += stretch) {
+                if (!tc::mbar_wait_ready(&sh->acc_full[a], phase, abort_flag)) failed = true;
+                failed = __any_sync(0xffffffffu, failed);
+                if (failed) break;
+                tc::tc_fence_after_sync();
+                if (left > 0) {
+                    const uint32_t from = tmem_d + a * geo.issuers * acc_cols + lane_off;
+                    // (one block: one of two issuers has had it)
+                    const int i0 = p.blocks - kb0 == 1 && geo.issuers == 2 ? ((u - u0) * p.blocks + kb0) & 1 : 0, i1 = p.blocks - kb0 == 1 ? i0 + 1 : geo.issuers;
+                    for (int c = 0; c < 2 * geo.chunks && c * 16 < geo.n; ++c) {                     // 16 rows at a time
+                        uint32_t r[16];
+                        tc::tmem_read16(from + i0 * acc_cols + c * 16, r);
+                        if (i1 - i0 == 2) {
+                            uint32_t s[16];
+                            tc::tmem_read16(from + acc_cols + c * 16, s);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(s[j]));
+                        }
+                        if (kb0 > 0) {
+                            uint32_t s[16];
+                            tc::tmem_read16(tmem_t + c * 16 + lane_off, s);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(s[j]));
+                        }
+                        tc::tmem_st16(tmem_t + c * 16 + lane_off, r);
+                    }
+                    tc::tmem_st_wait();
+                }
+                tc::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sh->acc_empty[a]);
+                if (++a == geo.accs) { a = 0; phase ^= 1u; }
+            }
+            if (failed) break;
+            if (left <= 0) continue;
+            if (geo.n == 16) look_through(std::integral_constant<int, 16>(), 0, slot, v0, left);
+            else
+                for (int c = 0; c < geo.chunks; ++c) look_through(std::integral_constant<int, 32>(), c, slot, v0, left);
         }
         if (failed && lane == 0) give_up(sh, p.status, 46);
-        if (!failed && live) st.store(p.part + ((size_t)row * gridDim.x + blockIdx.x) * 2 + seg);
+        if (!failed) publish(seg);
     } else if (warp < kEpi + kMakers) {
         // ---------------- values ----------------
         pdl_wait();
         pdl_trigger();
-        const int mk = warp - kEpi;
-        const int g = lane >> 2, t = lane & 3;
+        const int q = warp & 3, stage = (warp - kEpi) >> 2;    // (a warp writes the quarter of the tensor memory's lanes that its number names)
+        const int panel = 2 * q + (lane >> 4), cls = lane & 15;
         const int gpb = kQ4Block / p.group;
-        const unsigned so_a = 1024u + (g * gpb + t * 32 / p.group) * 4, so_b = so_a + 8 * gpb * 4;
-        // word i of row g: place in the stage (row g + 8 stands 1024 bytes behind)
-        unsigned put[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            put[i] = a_bytes + (t >> 1) * (kTileN * 128) + (mk * kQ4Panel + g) * 128 + ((((t & 1) * 4 + (i ^ ((t >> 1) << 1))) ^ g) << 4);
-        int it = 0, s = 0;
+        int it = 0, s = 0;                                     // blocks so far, ring slot
         uint32_t phase = 0u;
         for (int u = u0; u < u1 && !failed; ++u) {
-            const bool there = (u % geo.tiles) * kMakers + mk < p.panels;     // (behind a slot's last panel: nothing to make)
-            for (int pc = 0, at = start; pc < pieces && !failed; ++pc, at = at + 1 == pieces ? 0 : at + 1) {
-                const int nb = min(p.piece, p.blocks - at * p.piece);
-                if (!tc::mbar_wait_suspended(&sh->raw_full[s], phase, abort_flag)) failed = true;
-                for (int kb = 0; kb < nb; ++kb, ++it) {
-                    const int st = it % kStages;
-                    if (!failed && !tc::mbar_wait_suspended(&sh->empty[st], ((uint32_t)(it / kStages) & 1u) ^ 1u, abort_flag)) failed = true;
+            const bool there = (u % geo.tiles) * kTile + q * 32 < p.classes;  // (behind a slot's last class: nothing to make)
+            for (int pc = 0, at = start; pc < pairs; ++pc, at = at + 1 == pairs ? 0 : at + 1) {
+                const int nb = 2 * at + 1 < p.blocks ? 2 : 1;
+                if (!tc::mbar_wait_ready(&sh->raw_full[s], phase, abort_flag)) failed = true;
+                failed = __any_sync(0xffffffffu, failed);
+                if (failed) break;
+                const int kb = (stage - it) & (kStages - 1);   // the group's block, if it is one of the slot's
+                if (kb < nb) {
+                    if (!tc::mbar_wait_ready(&sh->empty[stage], ((uint32_t)((it + kb) / kStages) & 1u) ^ 1u, abort_flag)) failed = true;
                     failed = __any_sync(0xffffffffu, failed);
                     if (failed) break;
+                    tc::tc_fence_after_sync();
                     if (there) {
-                        const unsigned char* blk = ring + s * slot_bytes + (mk * p.piece + kb) * bb;
-                        unsigned char* dst = dyn + st * stage_bytes;
-                        const uint4 wa = *reinterpret_cast<const uint4*>(blk + lane * 16);
-                        const uint4 wb = *reinterpret_cast<const uint4*>(blk + 512 + lane * 16);
-                        const uint32_t sa = *reinterpret_cast<const uint32_t*>(blk + so_a);
-                        const uint32_t sb = *reinterpret_cast<const uint32_t*>(blk + so_b);
-                        const uint32_t a4[4] = {wa.x, wa.y, wa.z, wa.w}, b4[4] = {wb.x, wb.y, wb.z, wb.w};
+                        const unsigned char* blk = ring + s * slot_bytes + (panel * 2 + kb) * bb;
+                        const uint32_t* so = reinterpret_cast<const uint32_t*>(blk + 1024) + cls * gpb;
+                        const uint32_t to = tmem + 64u * stage + ((uint32_t)(q * 32) << 16);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            *reinterpret_cast<uint4*>(dst + put[i]) = q4_values_bf16(a4[i], sa);
-                            *reinterpret_cast<uint4*>(dst + put[i] + 1024) = q4_values_bf16(b4[i], sb);
+                        for (int half = 0; half < 2; ++half) {
+                            uint32_t v[32];
+#pragma unroll
+                            for (int t = 0; t < 2; ++t) {
+                                const uint4 w = *reinterpret_cast<const uint4*>(blk + ((2 * half + t) * kQ4Panel + cls) * 16);
+                                const uint32_t pr = so[((2 * half + t) * gpb) >> 2];
+                                const uint32_t w4[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const uint4 x = q4_values_bf16(w4[i], pr);
+                                    v[(t * 4 + i) * 4] = x.x; v[(t * 4 + i) * 4 + 1] = x.y; v[(t * 4 + i) * 4 + 2] = x.z; v[(t * 4 + i) * 4 + 3] = x.w;
+                                }
+                            }
+                            tc::tmem_st32(to + 32u * half, v);
                         }
-                        tc::fence_proxy_async();
+                        tc::tmem_st_wait();
                     }
+                    tc::tc_fence_before_sync();
                     __syncwarp();
-                    if (lane == 0) {
-                        tc::mbar_arrive(&sh->b_full[st]);
-                        if (kb == nb - 1) tc::mbar_arrive(&sh->raw_empty[s]);
-                    }
+                    if (lane == 0) tc::mbar_arrive(&sh->v_full[stage]);
                 }
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&sh->raw_empty[s]);
+                it += nb;
                 if (++s == p.nring) { s = 0; phase ^= 1u; }
             }
         }
         if (failed && lane == 0) give_up(sh, p.status, 47);
-    } else if (warp == kEpi + kMakers + 2) {
+    } else if (warp == kEpi + kMakers + 1) {
         // ---------------- levels ----------------
         if (lane == 0) {
             // (weights are not written while they are in use: the ring fills while the predecessor in the stream drains, and nothing else is
             // read before this kernel's other warps have waited for it)
             const uint64_t pol = tc::policy_evict_first();
-            const uint32_t bytes = (uint32_t)(kMakers * p.piece * bb);
+            const uint32_t bytes = (uint32_t)slot_bytes;
             int s = 0, fill = 0;
             uint32_t phase = 1u;
             for (int u = u0; u < u1 && !failed; ++u) {
-                const int slot = u / geo.tiles, pan = slot * p.panels + (u - slot * geo.tiles) * kMakers;
-                for (int pc = 0, at = start; pc < pieces; ++pc, at = at + 1 == pieces ? 0 : at + 1, ++fill) {
+                const int slot = u / geo.tiles, pan = slot * p.panels + (u - slot * geo.tiles) * kTilePanels;
+                for (int pc = 0, at = start; pc < pairs; ++pc, at = at + 1 == pairs ? 0 : at + 1, ++fill) {
                     if (fill == p.nring) {
                         pdl_wait();
                         pdl_trigger();
                     }
-                    if (!tc::mbar_wait_suspended(&sh->raw_empty[s], phase, abort_flag)) { failed = true; break; }
+                    if (!tc::mbar_wait_ready(&sh->raw_empty[s], phase, abort_flag)) { failed = true; break; }
                     tc::mbar_arrive_expect_tx(&sh->raw_full[s], bytes);
-                    // (64 bytes x the blocks' lines x twelve panels; what lies behind a panel's end or the last panel arrives as zeros)
-                    tc::tma_load_3d(ring + s * slot_bytes, &tmW, &sh->raw_full[s], 0, at * p.piece * (bb / 64), pan, pol);
+                    // (64 bytes x the blocks' lines x eight panels; what lies behind a panel's end or the last panel arrives as zeros)
+                    tc::tma_load_3d(ring + s * slot_bytes, &tmW, &sh->raw_full[s], 0, at * 2 * (bb / 64), pan, pol);
                     if (++s == p.nring) { s = 0; phase ^= 1u; }
                 }
             }
@@ -271,24 +360,22 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
         if (lane == 0) {
             const uint64_t pol = tc::policy_evict_last();
             const int steps = (u1 - u0) * p.blocks;
-            int it = 0, kb = start * p.piece;
+            int it = 0, kb = 2 * start;
             for (; it < steps; ++it) {
                 const int st = it % kStages;
-                if (!tc::mbar_wait_suspended(&sh->empty[st], ((uint32_t)(it / kStages) & 1u) ^ 1u, abort_flag)) { failed = true; break; }
-                unsigned char* dst = dyn + st * stage_bytes;
-                tc::mbar_arrive_expect_tx(&sh->a_full[st], (uint32_t)a_bytes);
+                if (!tc::mbar_wait_ready(&sh->empty[st], ((uint32_t)(it / kStages) & 1u) ^ 1u, abort_flag)) { failed = true; break; }
+                unsigned char* dst = dyn + st * x_bytes;
+                tc::mbar_arrive_expect_tx(&sh->x_full[st], (uint32_t)x_bytes);
                 // (elements behind H and rows behind the last are outside the tensor and arrive as zeros)
-                for (int c = 0; c < geo.copies; ++c) {
-                    tc::tma_load_2d(dst + c * geo.rows * 128, &tmX, &sh->a_full[st], kb * kQ4Block, 0, pol);
-                    tc::tma_load_2d(dst + a_plane + c * geo.rows * 128, &tmX, &sh->a_full[st], kb * kQ4Block + 64, 0, pol);
-                }
+                tc::tma_load_2d(dst, &tmX, &sh->x_full[st], kb * kQ4Block, 0, pol);
+                tc::tma_load_2d(dst + x_plane, &tmX, &sh->x_full[st], kb * kQ4Block + 64, 0, pol);
                 if (++kb == p.blocks) kb = 0;
             }
             if (failed) {
                 give_up(sh, p.status, 48);
                 for (int back = 1; back <= kStages && back <= it; ++back) {              // copies in flight land before the exit
                     const int j = it - back;
-                    tc::mbar_wait_suspended(&sh->a_full[j % kStages], (uint32_t)(j / kStages) & 1u, &sh->never_set, 1ll << 24);
+                    tc::mbar_wait_suspended(&sh->x_full[j % kStages], (uint32_t)(j / kStages) & 1u, &sh->never_set, 1ll << 24);
                 }
             }
         }
@@ -296,32 +383,54 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
         // ---------------- products ----------------
         pdl_wait();
         pdl_trigger();
-        if (lane == 0) {
-            const uint32_t idesc = tc::idesc_bf16_f32(128, kTileN);
-            int it = 0, n = 0;
-            for (int u = u0; u < u1 && !failed; ++u, ++n) {
-                const uint32_t d = tmem + (uint32_t)((n & 1) * kAccCols);
-                if (!tc::mbar_wait_suspended(&sh->acc_empty[n & 1], ((uint32_t)(n >> 1) & 1u) ^ 1u, abort_flag)) { failed = true; break; }
-                tc::tc_fence_after_sync();
-                for (int kb = 0; kb < p.blocks; ++kb, ++it) {
-                    const int st = it % kStages;
-                    const uint32_t ph = (uint32_t)(it / kStages) & 1u;
-                    if (!tc::mbar_wait_suspended(&sh->a_full[st], ph, abort_flag) || !tc::mbar_wait_suspended(&sh->b_full[st], ph, abort_flag)) { failed = true; break; }
+        // (the whole warp goes through the loop and one lane issues: descriptors stay in uniform registers.  Turns are counted, not divided for: a
+        // division takes some 200 cycles.)
+        const uint32_t idesc = tc::idesc_bf16_f32(kTile, geo.n);
+        const uint64_t x_desc0 = tc::smem_desc_k_sw128(tc::smem_u32(dyn));
+        const int mine = warp - (kEpi + kMakers + 2);
+        int it = 0, a = 0, done = -1;                          // blocks so far, the last one that was issued here
+        uint32_t a_phase = 1u;
+        for (int u = u0; u < u1 && !failed && mine < geo.issuers; ++u) {
+            for (int kb0 = 0; kb0 < p.blocks && !failed; kb0 += stretch) {
+                const int nb = min(stretch, p.blocks - kb0);
+                const uint32_t d = tmem_d + (a * geo.issuers + mine) * acc_cols;
+                bool first = true;
+                for (int k0 = (geo.issuers == 2 ? (it & 1) ^ mine : 0); k0 < nb; k0 += geo.issuers) {
+                    const int st = (it + k0) % kStages;
+                    // (three lanes wait for a barrier each: a wait takes some 150 cycles also when the barrier is complete)
+                    const uint32_t ph = (uint32_t)((it + k0) / kStages) & 1u;
+                    uint64_t* bar = lane == 0 ? &sh->x_full[st] : (lane == 1 ? &sh->v_full[st] : &sh->acc_empty[a]);
+                    const bool ok = !(lane < 2 || (lane == 2 && first)) || tc::mbar_wait_ready(bar, lane < 2 ? ph : a_phase, abort_flag);
+                    if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
                     tc::tc_fence_after_sync();
-                    const uint32_t base = tc::smem_u32(dyn + st * stage_bytes);
+                    if (tc::elect_one()) {
+                        const uint64_t xd = x_desc0 + (uint64_t)((uint32_t)(st * x_bytes) >> 4);
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const uint64_t adesc = tc::smem_desc_k_sw128(base + (uint32_t)(half * a_plane));
-                        const uint64_t bdesc = tc::smem_desc_k_sw128(base + (uint32_t)(a_bytes + half * (kTileN * 128)));
+                        for (int half = 0; half < 2; ++half)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)            // 16 elements along K = 32 bytes
-                            tc::mma_bf16_ss(d, adesc + 2 * k, bdesc + 2 * k, idesc, (kb | half | k) != 0 ? 1u : 0u);
+                            for (int k = 0; k < 4; ++k)        // 16 elements along K: 8 columns of A, 32 bytes of B
+                                tc::mma_bf16_ts(d, tmem + 64u * st + 32u * half + 8u * k, xd + (uint64_t)((uint32_t)(half * x_plane) >> 4) + 2 * k, idesc,
+                                                first && (half | k) == 0 ? 0u : 1u);
+                        tc::mma_commit(&sh->empty[st]);
                     }
-                    tc::mma_commit(&sh->empty[st]);
+                    __syncwarp();
+                    first = false;
+                    done = it + k0;
                 }
-                if (!failed) tc::mma_commit(&sh->acc_full[n & 1]);
+                if (failed) break;
+                // (an issuer without a block waits for its turn all the same)
+                if (first && !tc::mbar_wait_ready(&sh->acc_empty[a], a_phase, abort_flag)) failed = true;
+                failed = __any_sync(0xffffffffu, failed);
+                if (failed) break;
+                if (tc::elect_one()) tc::mma_commit(&sh->acc_full[a]);
+                __syncwarp();
+                if (++a == geo.accs) { a = 0; a_phase ^= 1u; }
+                it += nb;
             }
-            if (failed) give_up(sh, p.status, 49);
+        }
+        if (failed && lane == 0) {
+            give_up(sh, p.status, 49);
+            if (done >= 0) tc::mbar_wait_suspended(&sh->empty[done % kStages], (uint32_t)(done / kStages) & 1u, &sh->never_set, 1ll << 24);
         }
     }
     tc::tc_fence_before_sync();
@@ -331,7 +440,18 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
         tc::tmem_dealloc(tmem, 512);
     }
     if (*abort_flag != 0) return;                              // (uniform: set before the barrier or not at all)
-    draft_q4_finish(p, geo.tiles, geo.rows, geo.copies, slot0, segs, sh->merge);
+    // a row's states in this CTA become one, in the place of the first
+    const int copies = kEpi * geo.chunks * 32 / copy_rows;
+    for (int i = warp; i < segs * p.mcount; i += kThreads / 32) {
+        const int seg = i / p.mcount, m = i - seg * p.mcount;
+        DraftPartial* at = p.part + ((size_t)m * gridDim.x + blockIdx.x) * 2 + seg;
+        RunState ms;
+        ms.init();
+        if (lane < copies) ms.absorb(load_partial_cg(at + (size_t)lane * copy_rows * gridDim.x * 2));
+        combine_best<31>(ms, p.k);
+        if (lane == 0) ms.store(at);
+    }
+    draft_q4_finish(p, geo.tiles, slot0, segs, sh->merge);
 }
 
 // Activation rows picked by a row map, one behind the other; a map that leaves x gives a zero row.
@@ -369,13 +489,13 @@ bool make_x_map(CUtensorMap* map, const void* x, int rows, int H, int box_rows) 
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Packed weights as [panels][lines][64 bytes], box = [twelve panels][`lines` lines][64 bytes].
+// Packed weights as [panels][lines][64 bytes], box = [eight panels][`lines` lines][64 bytes].
 bool make_w_map(CUtensorMap* map, const void* w, long long panels, int panel_bytes, int lines) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dims[3] = {16, (cuuint64_t)(panel_bytes / 64), (cuuint64_t)panels};
     cuuint64_t strides[2] = {64, (cuuint64_t)panel_bytes};
-    cuuint32_t box[3] = {16, (cuuint32_t)lines, (cuuint32_t)kMakers};
+    cuuint32_t box[3] = {16, (cuuint32_t)lines, (cuuint32_t)kTilePanels};
     cuuint32_t estr[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void*>(w), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -395,21 +515,23 @@ int launch_draft_q4_tc(Handle* h, cudaStream_t s, DraftQ4Params p) {
     }
     p.part = reinterpret_cast<DraftPartial*>(h->ws + h->lay.q4_part_off);
     TcGeo geo;
-    geo.tiles = (p.panels + kMakers - 1) / kMakers;
-    geo.rows = p.mcount <= 32 ? 32 : (p.mcount <= 64 ? 64 : 128);
-    geo.a_rows = geo.rows <= 64 ? 64 : 128;
-    geo.copies = geo.a_rows / geo.rows;
-    const size_t bb = q4_block_bytes(p.group), fixed = (size_t)kStages * (geo.a_rows * 256 + kBBytes) + sizeof(TcState);
-    // ring slots of two blocks a panel where three of them fit, else of one
-    const size_t room = kMaxDynamicSmem - 1024 - fixed;
-    p.piece = p.blocks > 1 && room >= 3 * (kMakers * 2 * bb + 128) ? 2 : 1;
-    const size_t slot = (kMakers * p.piece * bb + 127) / 128 * 128;
-    p.nring = (int)(room / slot < kMaxRing ? room / slot : kMaxRing);
+    geo.tiles = (p.panels + kTilePanels - 1) / kTilePanels;
+    geo.n = (p.mcount + 15) / 16 * 16;
+    geo.chunks = (p.mcount + 31) / 32;
+    // Two issuers where the columns hold their sums (more than 64 rows: one; the activations then take as long as its issues).  As many sums
+    // as there is room for: products go on while a tile's logits are looked through.
+    geo.issuers = geo.chunks <= 2 ? 2 : 1;
+    const int accs = ((512 - 64 * kStages) / (32 * geo.chunks) - 1) / geo.issuers;
+    geo.accs = accs < kMaxAccs ? accs : kMaxAccs;
+    const size_t bb = q4_block_bytes(p.group);
+    const size_t fixed = (size_t)kStages * geo.n * 256 + sizeof(float) * kEpi * kTurn + sizeof(uint32_t) * kEpi * geo.chunks * kSaved * 32 + sizeof(TcState);
+    const size_t room = kMaxDynamicSmem - 1024 - fixed, slot = kTilePanels * 2 * bb;
+    p.nring = (int)(room / slot < kMaxRing ? room / slot : kMaxRing);         // (two at least: 128 rows and groups of 32 take 2 x 20 KB of 44 KB)
     if (p.nring < 2) return CTCSD_ERR_UNSUPPORTED;
     CUtensorMap tmX;
     CUtensorMap tmW;
-    if (!make_x_map(&tmX, x, p.mcount, p.H, geo.rows) ||
-        !make_w_map(&tmW, p.W, (long long)p.panels * p.slots, (int)(p.blocks * bb), (int)(p.piece * bb / 64))) return CTCSD_ERR_CUDA;
+    if (!make_x_map(&tmX, x, p.mcount, p.H, geo.n) ||
+        !make_w_map(&tmW, p.W, (long long)p.panels * p.slots, (int)(p.blocks * bb), (int)(2 * bb / 64))) return CTCSD_ERR_CUDA;
     CTCSD_CUDA_CHECK(h, prepare_kernel(h, kPrepDraftQ4Tc, draft_q4_tc_kernel));
     const long long total = (long long)geo.tiles * p.slots;
     const unsigned grid = (unsigned)(total < h->num_sms ? total : h->num_sms);         // (total >= slots: a range touches two slots at most)

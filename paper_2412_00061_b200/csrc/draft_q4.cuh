@@ -24,7 +24,7 @@ struct DraftQ4Params {
     int m0, mcount;                      // rows of this pass
     int H, classes, panels, blocks, group;   // panels per draft slot, blocks per panel
     int slots;                           // draft slots (T)
-    int piece, nring;                    // blocks of a ring slot, ring slots of a warp
+    int piece, nring;                    // blocks of a ring slot, ring slots
     DraftPartial* part;                  // [rows of a pass][grid][2]
     unsigned* counter;                   // [draft slots], zero between calls
     int k;
@@ -43,7 +43,7 @@ __device__ __forceinline__ uint32_t rank_of(float v, int id) {
     const uint32_t u = __float_as_uint(v);
     return (u >> 31) ? ~u : u | 0x80000000u;
 }
-// Combines the states of the lanes that differ in the bits of `over` (31: all of the warp; 28: the eight with the same lane % 4): maximum, sum, and
+// Combines the states of the lanes that differ in the bits of `over` (31: all of the warp; 7: the eight with the same lane / 8): maximum, sum, and
 // the k best (ties to the lower id) in each of them.
 template <int over> __device__ __forceinline__ void combine_best(RunState& st, int k) {
     float gmx = st.mx;
@@ -95,8 +95,8 @@ template <int over> __device__ __forceinline__ void combine_best(RunState& st, i
 // The end of a pass.  The line of units (panels or tiles, `per_slot` of them in each draft slot) is divided evenly among the CTAs in order, so the CTAs whose
 // units touch a draft slot are neighbours; a CTA touches two slots at most and leaves a state for each (p.part).  Called by the whole
 // block when its states are written: for each of its slots, the CTA that ends last merges the states and writes the outputs.
-// A row has `copies` states a CTA, `stride` rows apart.  `merge`: two ints in shared memory.
-__device__ inline void draft_q4_finish(const DraftQ4Params& p, int per_slot, int stride, int copies, int slot0, int segs, int* merge) {
+// `merge`: two ints in shared memory.
+__device__ inline void draft_q4_finish(const DraftQ4Params& p, int per_slot, int slot0, int segs, int* merge) {
     const long long n = gridDim.x, total = (long long)per_slot * p.slots;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     __threadfence();
@@ -130,10 +130,9 @@ __device__ inline void draft_q4_finish(const DraftQ4Params& p, int per_slot, int
         for (int m = warp; m < p.mcount; m += warps) {
             RunState fs;
             fs.init();
-            for (int i = lane; i < (c1 - c0 + 1) * copies; i += 32) {
-                const int c = c0 + i / copies, copy = i % copies;
+            for (int c = c0 + lane; c <= c1; c += 32) {
                 const int which = slot - (int)(total * c / n / per_slot);                  // the slot is the CTA's first or second
-                fs.absorb(load_partial_cg(p.part + ((size_t)(m + copy * stride) * n + c) * 2 + which));
+                fs.absorb(load_partial_cg(p.part + ((size_t)m * n + c) * 2 + which));
             }
             combine_best<31>(fs, p.k);
             if (lane == 0) {
