@@ -10,8 +10,9 @@
 // The tensor core cuts a sum's last bits off at every addition, always towards zero, and long chains drift (log-probabilities off by
 // 6e-6 at H = 8192).  So sums begin again every kStretch blocks, and the four warps that read D back add them up in rounded arithmetic, in tensor memory.
 // They then turn 32 classes x 32 rows through shared memory, so that a lane has a row, and keep each row's maximum, sum of exponentials and best k.
-// Roles: warps 0-3 read sums back (32 classes each), 4-19 make values, 20 loads activations, 21 loads levels, 22 and 23 issue the
-// products of every other block each, into sums of their own (an issue takes some 500 cycles of waiting, describing and committing, more than its products).
+// Roles: warps 0-3 read sums back (32 classes each), 4-19 make values, 20 loads activations, 21 loads levels, 22 and 23 issue
+// products, of every other block each, into sums of their own (an issue takes some 700 cycles of waiting, describing and committing, more than its
+// products: 32 rows of the 70B shape 346 us with one issuer, 255 with two, 311 with four).
 #include "draft_q4.cuh"
 #include "tc_primitives.cuh"
 
@@ -24,17 +25,20 @@ constexpr int kEpi = 4;
 constexpr int kGroups = 4;               // groups of four warps that make values
 constexpr int kMakers = 4 * kGroups;
 constexpr int kStages = kGroups;         // a stage holds a block; each group has its own, so that it sees every fill of it and no turn of its barriers goes by unseen
+constexpr int kMaxXStages = 8;           // of activations
 constexpr int kMaxRing = 8;
 constexpr int kMaxAccs = 4;              // sums in tensor memory that take turns
-constexpr int kThreads = (kEpi + kMakers + 4) * 32;
+constexpr int kIssuers = 2;              // warps that issue products
+constexpr int kThreads = (kEpi + kMakers + 2 + kIssuers) * 32;
 constexpr int kTile = 128, kTilePanels = kTile / kQ4Panel;
-constexpr int kStretch = 4;              // blocks whose products the tensor core adds up, per issuing warp
+constexpr int kStretch = 8;              // blocks whose products the tensor core adds up, per issuing warp
 constexpr int kTurn = 32 * 33;           // floats of a warp's 32 x 32 turning buffer
 constexpr int kSaved = 2 * kTopSlots + 2;    // words of a row's running state
 
 struct __align__(8) TcState {
     uint64_t raw_full[kMaxRing], raw_empty[kMaxRing];    // levels of the tile's panels, two blocks of each
-    uint64_t x_full[kStages], v_full[kStages], empty[kStages];               // activations; values; both have been multiplied
+    uint64_t v_full[kStages], v_empty[kStages];          // values
+    uint64_t x_full[kMaxXStages], x_empty[kMaxXStages];  // activations
     uint64_t acc_full[kMaxAccs], acc_empty[kMaxAccs];
     uint32_t tmem_base;
     int abort_flag, never_set, merge[2];
@@ -44,8 +48,10 @@ struct TcGeo {
     int tiles;                           // tiles of a draft slot
     int n;                               // rows of the product: those there are, rounded up to 16 (those behind the last are zeros)
     int chunks;                          // 32-row chunks
-    int issuers;                         // warps that issue products, of every issuers-th block each, into sums of their own
-    int accs;                            // sums that take turns, of each (512 columns: 64 a stage, 32 a chunk of each of the sums and of the total)
+    int xstages;                         // stages of activations (a multiple of the issuers: each sees every fill of its own)
+    int issuers;                         // issuing warps at work (a power of two), with every issuers-th block each, into sums of their own
+    int accs;                            // sums that take turns, of each
+    int cols;                            // columns of a sum: the rows, rounded up to 32 where they are more than 16 (512: 64 a stage, the sums, the total)
 };
 
 __device__ __forceinline__ void give_up(TcState* sh, int* status, int site) {
@@ -58,7 +64,7 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
                                                                   TcGeo geo) {
     extern __shared__ __align__(1024) unsigned char dyn[];
     const int x_plane = geo.n * 128, x_bytes = 2 * x_plane;                   // activations of a stage (a plane: 64 elements)
-    unsigned char* ring = dyn + kStages * x_bytes;
+    unsigned char* ring = dyn + geo.xstages * x_bytes;
     const int bb = q4_block_bytes(p.group), slot_bytes = kTilePanels * 2 * bb;
     float* turn = reinterpret_cast<float*>(ring + (size_t)p.nring * slot_bytes);            // [kEpi][kTurn]
     uint32_t* saved = reinterpret_cast<uint32_t*>(turn + kEpi * kTurn);                     // [kEpi][chunks][kSaved][32]
@@ -71,7 +77,8 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
     volatile int* abort_flag = &sh->abort_flag;
     if (tid == 0) {
         for (int s = 0; s < p.nring; ++s) { tc::mbar_init(&sh->raw_full[s], 1); tc::mbar_init(&sh->raw_empty[s], kMakers); }
-        for (int s = 0; s < kStages; ++s) { tc::mbar_init(&sh->x_full[s], 1); tc::mbar_init(&sh->v_full[s], 4); tc::mbar_init(&sh->empty[s], 1); }
+        for (int s = 0; s < kStages; ++s) { tc::mbar_init(&sh->v_full[s], 4); tc::mbar_init(&sh->v_empty[s], 1); }
+        for (int s = 0; s < geo.xstages; ++s) { tc::mbar_init(&sh->x_full[s], 1); tc::mbar_init(&sh->x_empty[s], 1); }
         for (int a = 0; a < geo.accs; ++a) { tc::mbar_init(&sh->acc_full[a], geo.issuers); tc::mbar_init(&sh->acc_empty[a], kEpi); }
         sh->abort_flag = 0;
         sh->never_set = 0;
@@ -85,7 +92,7 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
     __syncthreads();
     tc::tc_fence_after_sync();
     // columns: values of the stages, the sums, the total
-    const uint32_t tmem = sh->tmem_base, tmem_d = tmem + 64u * kStages, acc_cols = 32u * geo.chunks, tmem_t = tmem_d + geo.accs * geo.issuers * acc_cols;
+    const uint32_t tmem = sh->tmem_base, tmem_d = tmem + 64u * kStages, acc_cols = geo.cols, tmem_t = tmem_d + geo.accs * geo.issuers * acc_cols;
     // this CTA's tiles: u0 .. u1-1 of the line of all slots' tiles
     const long long total = (long long)geo.tiles * p.slots;
     const int u0 = (int)(total * blockIdx.x / gridDim.x), u1 = (int)(total * (blockIdx.x + 1) / gridDim.x);
@@ -230,15 +237,15 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
                 if (failed) break;
                 tc::tc_fence_after_sync();
                 if (left > 0) {
+                    // (where the blocks are fewer than the issuers, those that have had one)
                     const uint32_t from = tmem_d + a * geo.issuers * acc_cols + lane_off;
-                    // (one block: one of two issuers has had it)
-                    const int i0 = p.blocks - kb0 == 1 && geo.issuers == 2 ? ((u - u0) * p.blocks + kb0) & 1 : 0, i1 = p.blocks - kb0 == 1 ? i0 + 1 : geo.issuers;
-                    for (int c = 0; c < 2 * geo.chunks && c * 16 < geo.n; ++c) {                     // 16 rows at a time
+                    const int i0 = (u - u0) * p.blocks + kb0, parts = min(geo.issuers, p.blocks - kb0);
+                    for (int c = 0; c * 16 < geo.n; ++c) {                                           // 16 rows at a time
                         uint32_t r[16];
-                        tc::tmem_read16(from + i0 * acc_cols + c * 16, r);
-                        if (i1 - i0 == 2) {
+                        tc::tmem_read16(from + (i0 & (geo.issuers - 1)) * acc_cols + c * 16, r);
+                        for (int i = 1; i < parts; ++i) {
                             uint32_t s[16];
-                            tc::tmem_read16(from + acc_cols + c * 16, s);
+                            tc::tmem_read16(from + ((i0 + i) & (geo.issuers - 1)) * acc_cols + c * 16, s);
 #pragma unroll
                             for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(s[j]));
                         }
@@ -283,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
                 if (failed) break;
                 const int kb = (stage - it) & (kStages - 1);   // the group's block, if it is one of the slot's
                 if (kb < nb) {
-                    if (!tc::mbar_wait_ready(&sh->empty[stage], ((uint32_t)((it + kb) / kStages) & 1u) ^ 1u, abort_flag)) failed = true;
+                    if (!tc::mbar_wait_ready(&sh->v_empty[stage], ((uint32_t)((it + kb) / kStages) & 1u) ^ 1u, abort_flag)) failed = true;
                     failed = __any_sync(0xffffffffu, failed);
                     if (failed) break;
                     tc::tc_fence_after_sync();
@@ -360,22 +367,23 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
         if (lane == 0) {
             const uint64_t pol = tc::policy_evict_last();
             const int steps = (u1 - u0) * p.blocks;
-            int it = 0, kb = 2 * start;
+            int it = 0, kb = 2 * start, st = 0;
+            uint32_t phase = 1u;
             for (; it < steps; ++it) {
-                const int st = it % kStages;
-                if (!tc::mbar_wait_ready(&sh->empty[st], ((uint32_t)(it / kStages) & 1u) ^ 1u, abort_flag)) { failed = true; break; }
+                if (!tc::mbar_wait_ready(&sh->x_empty[st], phase, abort_flag)) { failed = true; break; }
                 unsigned char* dst = dyn + st * x_bytes;
                 tc::mbar_arrive_expect_tx(&sh->x_full[st], (uint32_t)x_bytes);
                 // (elements behind H and rows behind the last are outside the tensor and arrive as zeros)
                 tc::tma_load_2d(dst, &tmX, &sh->x_full[st], kb * kQ4Block, 0, pol);
                 tc::tma_load_2d(dst + x_plane, &tmX, &sh->x_full[st], kb * kQ4Block + 64, 0, pol);
                 if (++kb == p.blocks) kb = 0;
+                if (++st == geo.xstages) { st = 0; phase ^= 1u; }
             }
             if (failed) {
                 give_up(sh, p.status, 48);
-                for (int back = 1; back <= kStages && back <= it; ++back) {              // copies in flight land before the exit
+                for (int back = 1; back <= geo.xstages && back <= it; ++back) {          // copies in flight land before the exit
                     const int j = it - back;
-                    tc::mbar_wait_suspended(&sh->x_full[j % kStages], (uint32_t)(j / kStages) & 1u, &sh->never_set, 1ll << 24);
+                    tc::mbar_wait_suspended(&sh->x_full[j % geo.xstages], (uint32_t)(j / geo.xstages) & 1u, &sh->never_set, 1ll << 24);
                 }
             }
         }
@@ -389,33 +397,36 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
         const uint64_t x_desc0 = tc::smem_desc_k_sw128(tc::smem_u32(dyn));
         const int mine = warp - (kEpi + kMakers + 2);
         int it = 0, a = 0, done = -1;                          // blocks so far, the last one that was issued here
-        uint32_t a_phase = 1u;
+        int xs = mine;
+        uint32_t a_phase = 1u, x_phase = 0u;
         for (int u = u0; u < u1 && !failed && mine < geo.issuers; ++u) {
             for (int kb0 = 0; kb0 < p.blocks && !failed; kb0 += stretch) {
                 const int nb = min(stretch, p.blocks - kb0);
                 const uint32_t d = tmem_d + (a * geo.issuers + mine) * acc_cols;
                 bool first = true;
-                for (int k0 = (geo.issuers == 2 ? (it & 1) ^ mine : 0); k0 < nb; k0 += geo.issuers) {
+                for (int k0 = (mine - it) & (geo.issuers - 1); k0 < nb; k0 += geo.issuers) {
                     const int st = (it + k0) % kStages;
                     // (three lanes wait for a barrier each: a wait takes some 150 cycles also when the barrier is complete)
                     const uint32_t ph = (uint32_t)((it + k0) / kStages) & 1u;
-                    uint64_t* bar = lane == 0 ? &sh->x_full[st] : (lane == 1 ? &sh->v_full[st] : &sh->acc_empty[a]);
-                    const bool ok = !(lane < 2 || (lane == 2 && first)) || tc::mbar_wait_ready(bar, lane < 2 ? ph : a_phase, abort_flag);
+                    uint64_t* bar = lane == 0 ? &sh->x_full[xs] : (lane == 1 ? &sh->v_full[st] : &sh->acc_empty[a]);
+                    const bool ok = !(lane < 2 || (lane == 2 && first)) || tc::mbar_wait_ready(bar, lane == 0 ? x_phase : (lane == 1 ? ph : a_phase), abort_flag);
                     if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
                     tc::tc_fence_after_sync();
                     if (tc::elect_one()) {
-                        const uint64_t xd = x_desc0 + (uint64_t)((uint32_t)(st * x_bytes) >> 4);
+                        const uint64_t xd = x_desc0 + (uint64_t)((uint32_t)(xs * x_bytes) >> 4);
 #pragma unroll
                         for (int half = 0; half < 2; ++half)
 #pragma unroll
                             for (int k = 0; k < 4; ++k)        // 16 elements along K: 8 columns of A, 32 bytes of B
                                 tc::mma_bf16_ts(d, tmem + 64u * st + 32u * half + 8u * k, xd + (uint64_t)((uint32_t)(half * x_plane) >> 4) + 2 * k, idesc,
                                                 first && (half | k) == 0 ? 0u : 1u);
-                        tc::mma_commit(&sh->empty[st]);
+                        tc::mma_commit(&sh->v_empty[st]);
+                        tc::mma_commit(&sh->x_empty[xs]);
                     }
                     __syncwarp();
                     first = false;
                     done = it + k0;
+                    if ((xs += geo.issuers) >= geo.xstages) { xs -= geo.xstages; x_phase ^= 1u; }
                 }
                 if (failed) break;
                 // (an issuer without a block waits for its turn all the same)
@@ -430,7 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
         }
         if (failed && lane == 0) {
             give_up(sh, p.status, 49);
-            if (done >= 0) tc::mbar_wait_suspended(&sh->empty[done % kStages], (uint32_t)(done / kStages) & 1u, &sh->never_set, 1ll << 24);
+            if (done >= 0) tc::mbar_wait_suspended(&sh->v_empty[done % kStages], (uint32_t)(done / kStages) & 1u, &sh->never_set, 1ll << 24);
         }
     }
     tc::tc_fence_before_sync();
@@ -518,13 +529,16 @@ int launch_draft_q4_tc(Handle* h, cudaStream_t s, DraftQ4Params p) {
     geo.tiles = (p.panels + kTilePanels - 1) / kTilePanels;
     geo.n = (p.mcount + 15) / 16 * 16;
     geo.chunks = (p.mcount + 31) / 32;
-    // Two issuers where the columns hold their sums (more than 64 rows: one; the activations then take as long as its issues).  As many sums
+    // As many issuers as the columns hold sums for (more than 64 rows: one; the activations then take as long as its issues).  As many sums
     // as there is room for: products go on while a tile's logits are looked through.
-    geo.issuers = geo.chunks <= 2 ? 2 : 1;
-    const int accs = ((512 - 64 * kStages) / (32 * geo.chunks) - 1) / geo.issuers;
-    geo.accs = accs < kMaxAccs ? accs : kMaxAccs;
+    geo.cols = geo.n == 16 ? 16 : geo.chunks * 32;
+    const int sums = (512 - 64 * kStages) / geo.cols - 1;
+    geo.issuers = sums >= kIssuers ? kIssuers : 1;
+    geo.accs = sums / geo.issuers < kMaxAccs ? sums / geo.issuers : kMaxAccs;
+    // (activations come from L2, some 1000 cycles a request: eight blocks ahead, six or three where the rows take the room)
+    geo.xstages = geo.chunks == 1 ? 8 : (geo.chunks == 2 ? 6 : 3);
     const size_t bb = q4_block_bytes(p.group);
-    const size_t fixed = (size_t)kStages * geo.n * 256 + sizeof(float) * kEpi * kTurn + sizeof(uint32_t) * kEpi * geo.chunks * kSaved * 32 + sizeof(TcState);
+    const size_t fixed = (size_t)geo.xstages * geo.n * 256 + sizeof(float) * kEpi * kTurn + sizeof(uint32_t) * kEpi * geo.chunks * kSaved * 32 + sizeof(TcState);
     const size_t room = kMaxDynamicSmem - 1024 - fixed, slot = kTilePanels * 2 * bb;
     p.nring = (int)(room / slot < kMaxRing ? room / slot : kMaxRing);         // (two at least: 128 rows and groups of 32 take 2 x 20 KB of 44 KB)
     if (p.nring < 2) return CTCSD_ERR_UNSUPPORTED;

@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
                     const int kv = pl.kv[at.b];
                     for (int row = at.blk0 * kKeys; row < at.blk1 * kKeys && row < kv; row += kPart, ++fill) {
                         const int n = kv - row < kPart ? kv - row : kPart;
-                        if (!tc::mbar_wait_suspended(empty + s, phase, abort_flag)) { failed = true; break; }
+                        if (!tc::mbar_wait_ready(empty + s, phase, abort_flag)) { failed = true; break; }
                         RawQ4<D>::request_levels(ring + s * kSlot, side ? p.Vq : p.Kq, base + row, n, full + s, pol);
                         RawQ4<D>::request_pairs(ring + s * kSlot, side ? p.Vs : p.Ks, kPart, base + row, n, rows, full + s, pol);
                         if (++s == nraw) { s = 0; phase ^= 1u; }
@@ -174,41 +174,44 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
             }
         } else if (warp < 3) {
             // ---------------- products of one half ----------------
-            // Both issuers visit every tile in order; for a block that is not its half's, an issuer only hands the tiles back.
-            if (lane == 0) {
-                const int half = warp - 1;
-                const uint32_t idesc_s = tc::idesc_bf16_f32(kHalf, kStep);
-                const uint32_t idesc_o = tc::idesc_bf16_f32_b_mn(kHalf, D);
-                const uint32_t tmem_s = tmem + (uint32_t)(half * 128), tmem_o = tmem + 256u + (uint32_t)(half * D);
-                const uint64_t kdesc0 = tc::smem_desc_k_sw128(tc::smem_u32(Ks));
-                const uint64_t vdesc0 = tc::smem_desc_mn_sw128(tc::smem_u32(Vs), kKeys * 128);
-                int fill = 0, piece = 0;
-                uint32_t count = 0u;                           // blocks whose P this issuer has waited for
-                bool ok = true;
-                for (; more && ok; more = at.next(pl, p.B, kKeys), ++piece) {
-                    const bool split = TR == kHalf || pl.n[at.b] * p.grp - at.t * TR <= kHalf;
-                    const uint64_t qdesc0 = tc::smem_desc_k_sw128(tc::smem_u32(Qs + (split ? 0 : half * kQHalf)));
-                    int pend = -1;                             // block (fill number) whose P V is still to be issued
-                    bool first = true;
-                    auto issue_pv = [&](int e) -> bool {
-                        const int st = pend % kStages;
-                        if (e == 0 && !tc::mbar_wait_suspended(&sh->v_full[st], (uint32_t)(pend / kStages) & 1u, abort_flag)) return false;
-                        if (!tc::mbar_wait_suspended(&sh->p_full[half][e], count & 1u, abort_flag)) return false;
-                        tc::tc_fence_after_sync();
+            // Both issuers visit every tile in order; for a block that is not its half's, an issuer only hands the tiles back.  The whole warp goes
+            // through the loops and one lane issues, so that descriptors stay in uniform registers.
+            const int half = warp - 1;
+            const uint32_t idesc_s = tc::idesc_bf16_f32(kHalf, kStep);
+            const uint32_t idesc_o = tc::idesc_bf16_f32_b_mn(kHalf, D);
+            const uint32_t tmem_s = tmem + (uint32_t)(half * 128), tmem_o = tmem + 256u + (uint32_t)(half * D);
+            const uint64_t kdesc0 = tc::smem_desc_k_sw128(tc::smem_u32(Ks));
+            const uint64_t vdesc0 = tc::smem_desc_mn_sw128(tc::smem_u32(Vs), kKeys * 128);
+            int fill = 0, piece = 0;
+            uint32_t count = 0u;                               // blocks whose P this issuer has waited for
+            bool ok = true;
+            auto wait = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, tc::mbar_wait_ready(bar, parity, abort_flag)) != 0; };
+            for (; more && ok; more = at.next(pl, p.B, kKeys), ++piece) {
+                const bool split = TR == kHalf || pl.n[at.b] * p.grp - at.t * TR <= kHalf;
+                const uint64_t qdesc0 = tc::smem_desc_k_sw128(tc::smem_u32(Qs + (split ? 0 : half * kQHalf)));
+                int pend = -1;                                 // block (fill number) whose P V is still to be issued
+                bool first = true;
+                auto issue_pv = [&](int e) -> bool {
+                    const int st = pend % kStages;
+                    if (e == 0 && !wait(&sh->v_full[st], (uint32_t)(pend / kStages) & 1u)) return false;
+                    if (!wait(&sh->p_full[half][e], count & 1u)) return false;
+                    tc::tc_fence_after_sync();
+                    if (tc::elect_one()) {
                         const uint64_t vdesc = vdesc0 + (uint64_t)((st * kTile + e * kStep * 128) >> 4);
 #pragma unroll
                         for (int kk = 0; kk < kStep / 16; ++kk)               // 16 keys: 8 columns of P, 16 rows of V
                             tc::mma_bf16_ts(tmem_o, tmem_s + (uint32_t)(e * kStep + kk * 8), vdesc + (uint64_t)((kk * 16 * 128) >> 4), idesc_o,
                                             !first || kk != 0 ? 1u : 0u);
                         tc::mma_commit(&sh->pv_done[half]);
-                        first = false;
-                        if (e == 1) {
-                            tc::mma_commit(&sh->v_empty[st]);
-                            ++count;
-                        }
-                        return true;
-                    };
-                    auto issue_s = [&](int e, int st) {
+                        if (e == 1) tc::mma_commit(&sh->v_empty[st]);
+                    }
+                    __syncwarp();
+                    first = false;
+                    if (e == 1) ++count;
+                    return true;
+                };
+                auto issue_s = [&](int e, int st) {
+                    if (tc::elect_one()) {
                         const uint64_t kdesc = kdesc0 + (uint64_t)((st * kTile + e * kStep * 128) >> 4);
 #pragma unroll
                         for (int kk = 0; kk < D / 16; ++kk) {
@@ -216,42 +219,44 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
                             tc::mma_bf16_ss(tmem_s + (uint32_t)(e * kStep), qdesc0 + along, kdesc + along, idesc_s, kk != 0 ? 1u : 0u);
                         }
                         tc::mma_commit(&sh->s_full[half][e]);
-                    };
-                    ok = tc::mbar_wait_suspended(&sh->q_full, (uint32_t)piece & 1u, abort_flag);
-                    // (one more round than blocks: the last block's P V)
-                    for (int blk = at.blk0; blk <= at.blk1 && ok; ++blk) {
-                        const int st = fill % kStages;
-                        const uint32_t ph = (uint32_t)(fill / kStages) & 1u;
-                        const bool more_blocks = blk < at.blk1;
-                        const bool mine = more_blocks && (!split || ((blk - at.blk0) & 1) == half);
-                        // a step's P is read by P V before the next S overwrites it: the tensor core works in issue order
-#pragma unroll 1
-                        for (int e = 0; e < 2 && ok; ++e) {
-                            if (pend >= 0) ok = issue_pv(e);
-                            if (ok && mine) {
-                                if (e == 0) {
-                                    ok = tc::mbar_wait_suspended(&sh->k_full[st], ph, abort_flag);
-                                    tc::tc_fence_after_sync();
-                                }
-                                if (ok) issue_s(e, st);
-                            }
-                        }
-                        if (!ok || !more_blocks) break;
-                        pend = mine ? fill : -1;
-                        if (mine) {
-                            tc::mma_commit(&sh->k_empty[st]);
-                        } else {
-                            ok = tc::mbar_wait_suspended(&sh->k_full[st], ph, abort_flag);
-                            if (ok) tc::mbar_arrive(&sh->k_empty[st]);
-                            ok = ok && tc::mbar_wait_suspended(&sh->v_full[st], ph, abort_flag);
-                            if (ok) tc::mbar_arrive(&sh->v_empty[st]);
-                        }
-                        ++fill;
+                        if (e == 1) tc::mma_commit(&sh->k_empty[st]);
                     }
-                    if (ok) tc::mma_commit(&sh->o_full[half]);
+                    __syncwarp();
+                };
+                ok = wait(&sh->q_full, (uint32_t)piece & 1u);
+                // (one more round than blocks: the last block's P V)
+                for (int blk = at.blk0; blk <= at.blk1 && ok; ++blk) {
+                    const int st = fill % kStages;
+                    const uint32_t ph = (uint32_t)(fill / kStages) & 1u;
+                    const bool more_blocks = blk < at.blk1;
+                    const bool mine = more_blocks && (!split || ((blk - at.blk0) & 1) == half);
+                    // a step's P is read by P V before the next S overwrites it: the tensor core works in issue order
+#pragma unroll 1
+                    for (int e = 0; e < 2 && ok; ++e) {
+                        if (pend >= 0) ok = issue_pv(e);
+                        if (ok && mine) {
+                            if (e == 0) {
+                                ok = wait(&sh->k_full[st], ph);
+                                tc::tc_fence_after_sync();
+                            }
+                            if (ok) issue_s(e, st);
+                        }
+                    }
+                    if (!ok || !more_blocks) break;
+                    pend = mine ? fill : -1;
+                    if (!mine) {
+                        ok = wait(&sh->k_full[st], ph);
+                        if (ok && lane == 0) tc::mbar_arrive(&sh->k_empty[st]);
+                        ok = ok && wait(&sh->v_full[st], ph);
+                        if (ok && lane == 0) tc::mbar_arrive(&sh->v_empty[st]);
+                        __syncwarp();
+                    }
+                    ++fill;
                 }
-                if (!ok) give_up(sh, p.status, 63);
+                if (ok && tc::elect_one()) tc::mma_commit(&sh->o_full[half]);
+                __syncwarp();
             }
+            if (!ok && lane == 0) give_up(sh, p.status, 63);
         }
     } else if (warp >= 12) {
         // ---------------- tiles of values ----------------
@@ -275,12 +280,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
                 const int st = fill % kStages;
                 const uint32_t ph = ((uint32_t)(fill / kStages) & 1u) ^ 1u;
                 unsigned char* tile = (side ? Vs : Ks) + st * kTile;
-                if (!tc::mbar_wait_suspended(side ? &sh->v_empty[st] : &sh->k_empty[st], ph, abort_flag)) failed = true;
+                if (!tc::mbar_wait_ready(side ? &sh->v_empty[st] : &sh->k_empty[st], ph, abort_flag)) failed = true;
                 if (blk < at.cached) {
 #pragma unroll 1
                     for (int part = 0; part < kParts; ++part) {
                         const int row = blk * kKeys + part * kPart, left = kv - row;       // rows there are
-                        if (!failed && left > 0 && !tc::mbar_wait_suspended(full + s, phase, abort_flag)) failed = true;
+                        if (!failed && left > 0 && !tc::mbar_wait_ready(full + s, phase, abort_flag)) failed = true;
                         failed = __any_sync(0xffffffffu, failed);
                         if (failed) break;
                         const unsigned char* from = ring + s * kSlot;
@@ -364,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
         // After a wait that ran out, nothing is waited for any more: the loops run to their ends on meaningless scores,
         // and no output is written.
         auto wait = [&](uint64_t* bar, uint32_t parity, int site) {
-            if (!failed && !tc::mbar_wait_suspended(bar, parity, abort_flag)) {
+            if (!failed && !tc::mbar_wait_ready(bar, parity, abort_flag)) {
                 failed = true;
                 give_up(sh, p.status, site);
             }
