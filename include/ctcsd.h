@@ -383,8 +383,7 @@ int ctcsd_evict_rows(ctcsd_handle* h, void* stream, void* workspace, size_t work
  * ctcsd_quantize_weights_q4: Wd [T,V+1,H] dtype -> out_Wq, ctcsd_weights_q4_bytes(cfg, group) bytes; groups of 32, 64 or 128
  * along H (the last one of a row may be shorter).  Done once.  Layout: panels of 16 consecutive classes of a slot (the last one
  * filled up with rows of zeros), [T][ceil((V+1)/16)][ceil(H/128)] blocks of 1024 + 64 * (128 / group) bytes, for 128 elements of H each:
- *   word 128 h + 16 g + 4 t + i (h < 2, g < 8, t < 4, i < 4): class 8h + g, values 32t + 8j .. 32t + 8j + 7 of the block, j = i for t < 2,
- *   i ^ 2 for t >= 2;
+ *   word 64 t + 4 c + i (t < 4, c < 16, i < 4): class c, values 32t + 8i .. 32t + 8i + 7 of the block;
  *   then [16 classes][128 / group] words of scale and origin.
  *
  * ctcsd_draft_logits_q4: ctcsd_draft_logits over such weights, with the values they stand for.
@@ -392,8 +391,8 @@ int ctcsd_evict_rows(ctcsd_handle* h, void* stream, void* workspace, size_t work
  *   outside 0..x_row_count-1 records CTCSD_ERR_INVALID_ARG in the device status word and that row drafts from a zero vector);
  * Wq, group as for the call above, not written by any kernel while the call runs or directly before it (ctcsd_quantize_weights_q4
  *   itself may precede it);  everything else as for ctcsd_draft_logits.
- * The weights are read once per 8 rows (float32: 4; of very long rows as many as fit into shared memory), with bfloat16 and more than 8
- * rows once per 128 rows.  Up to 8 rows and float32 need H <= 65536 (float32: 32768; beyond that CTCSD_ERR_UNSUPPORTED).
+ * The weights are read once per 128 rows (float32: once per 4 rows, of very long rows as many as fit into shared memory; H <= 32768, beyond
+ * that CTCSD_ERR_UNSUPPORTED).
  */
 int ctcsd_weights_q4_bytes(const ctcsd_config* cfg, int group, size_t* out_bytes);
 int ctcsd_quantize_weights_q4(ctcsd_handle* h, void* stream, const void* Wd, int group, void* out_Wq);

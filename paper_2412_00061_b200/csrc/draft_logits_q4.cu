@@ -131,7 +131,7 @@ struct PanelWalk {
 // bulk-copy engine (its first lane asks for the next piece when a slot has been read); lane = (chunk t, class g and g + 8) makes values and multiplies
 // them with the activations of its chunk, held in shared memory; the sums of the four chunks are joined by shuffles, and lane (t, g) keeps the
 // running maximum, sum of exponentials and best k of row t.  Warps meet at the end only.  Bound by the fused multiply-adds: one for the value and
-// one a row, and four instructions to pick a level.
+// one a row, and three instructions to pick a level (tiny shape, 1 row of 256 x 4004: 15 us, mostly latency; 16 MB of weights and 4 rows 34 us).
 __global__ void __launch_bounds__(kThreads, 1) draft_q4_f32_kernel(DraftQ4Params p) {
     extern __shared__ __align__(128) unsigned char dyn[];
     unsigned char* xs = dyn;

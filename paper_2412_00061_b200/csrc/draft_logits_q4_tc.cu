@@ -5,14 +5,19 @@
 // D in tensor memory (lane = class, column = row).
 // Sixteen warps turn levels into values, four to a stage, 32 classes each: a lane reads its class's levels of a block, 64 bytes, and writes 64 columns of
 // tensor memory.  So the values never pass through shared memory, and a row costs its share of B and D only.  (Weights as the B operand, written to
-// swizzled tiles in shared memory, with activations padded to 128 rows as A: 403 us for 32 rows of the 70B shape; and 8 rows and fewer were better off
-// with mma.sync, 99 us for a row of the 7B shape.)
+// swizzled tiles in shared memory, with activations padded to 128 rows as A: 403 us for 32 rows of the 70B shape, 185 us for 16 rows of the 7B shape.
+// mma.sync with the values in registers: 99 us for one row of the 7B shape, 108 for eight.)
 // The tensor core cuts a sum's last bits off at every addition, always towards zero, and long chains drift (log-probabilities off by
-// 6e-6 at H = 8192).  So sums begin again every kStretch blocks, and the four warps that read D back add them up in rounded arithmetic, in tensor memory.
-// They then turn 32 classes x 32 rows through shared memory, so that a lane has a row, and keep each row's maximum, sum of exponentials and best k.
+// 6e-6 at H = 8192, by 5e-7 so).  So sums begin again every kStretch blocks, and the four warps that read D back add them up in rounded arithmetic, in
+// tensor memory.  They then turn 32 classes x R rows through shared memory, so that a lane has a row, and keep each row's maximum, sum of
+// exponentials and best k.
 // Roles: warps 0-3 read sums back (32 classes each), 4-19 make values, 20 loads activations, 21 loads levels, 22 and 23 issue
 // products, of every other block each, into sums of their own (an issue takes some 700 cycles of waiting, describing and committing, more than its
-// products: 32 rows of the 70B shape 346 us with one issuer, 255 with two, 311 with four).
+// products: 32 rows of the 70B shape 346 us with one issuer, 255 with two, 280 with four).
+//
+// 7B shape (5 slots of 32001 classes, H = 4096, groups of 128): 1 row 101 us, 3.4 TB/s of weights; 16 rows 112 us.  70B shape (6 slots, H = 8192): 32 rows
+// 237 us.  What bounds it: the makers' way from a full ring slot through 16 words of eleven instructions to the tensor memory's stores and the issue (without
+// the stores the 7B shape takes 69 us, without products and stores 63), and the instruction slots that reading sums back takes from them (14 us).
 #include "draft_q4.cuh"
 #include "tc_primitives.cuh"
 
@@ -76,7 +81,7 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     volatile int* abort_flag = &sh->abort_flag;
     if (tid == 0) {
-        for (int s = 0; s < p.nring; ++s) { tc::mbar_init(&sh->raw_full[s], 1); tc::mbar_init(&sh->raw_empty[s], kMakers); }
+        for (int s = 0; s < p.nring; ++s) { tc::mbar_init(&sh->raw_full[s], 1); tc::mbar_init(&sh->raw_empty[s], kMakers / 2); }
         for (int s = 0; s < kStages; ++s) { tc::mbar_init(&sh->v_full[s], 4); tc::mbar_init(&sh->v_empty[s], 1); }
         for (int s = 0; s < geo.xstages; ++s) { tc::mbar_init(&sh->x_full[s], 1); tc::mbar_init(&sh->x_empty[s], 1); }
         for (int a = 0; a < geo.accs; ++a) { tc::mbar_init(&sh->acc_full[a], geo.issuers); tc::mbar_init(&sh->acc_empty[a], kEpi); }
@@ -101,8 +106,10 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
     // Every CTA begins at a place of its own along the hidden axis (and wraps), so that at any moment the CTAs ask L2 for different parts of the
     // activations that they all share.
     const int pairs = (p.blocks + 1) / 2, start = (int)((long long)blockIdx.x * pairs / gridDim.x);       // pairs of blocks; the last may be one block
+    // (with an odd number of blocks, an empty one behind the last goes the others' way, without products: its place in the CTA's order)
+    const int blocks2 = 2 * pairs, empty_at = (p.blocks & 1) ? 2 * (pairs - 1 - start) + 1 : -1;
     const int stretch = kStretch * geo.issuers;
-    const int copy_rows = geo.n == 16 ? 16 : geo.chunks * 32;                 // rows from a row's state to its next one
+    const int copy_rows = p.mcount <= 8 ? 8 : (p.mcount <= 16 ? 16 : geo.chunks * 32);                 // rows from a row's state to its next one
     bool failed = false;
 
     if (warp < kEpi) {
@@ -136,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
 #pragma unroll
             for (int s = 0; s < kTopSlots; ++s) { st.val[s] = __uint_as_float(from[(2 + 2 * s) * 32]); st.id[s] = (int)from[(3 + 2 * s) * 32]; }
         };
-        // the states of a draft slot: a row has one of every warp (two where a lane has half of the classes), copy_rows rows apart
+        // the states of a draft slot: a row has one of every warp (of 32 / R lanes of it), copy_rows rows apart
         auto publish = [&](int seg) {
             for (int c = 0; c < geo.chunks; ++c) {
                 load(c);
@@ -148,7 +155,7 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
             st.init();
             for (int c = 0; c < geo.chunks; ++c) save(c);
         };
-        // A chunk of a tile's logits: R rows of 32 classes, turned so that a lane has a row (R = 16: and half of the classes).
+        // A chunk of a tile's logits: R rows of 32 classes, turned so that a lane has a row and R classes of it.
         auto look_through = [&](auto rows, int c, int slot, int v0, int left) __attribute__((always_inline)) {
             constexpr int R = decltype(rows)::value, J = R;     // J classes a lane
             uint32_t r[32];
@@ -231,21 +238,21 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
                 begin();
                 seg = 1;
             }
-            for (int kb0 = 0; kb0 < p.blocks; kb0 += stretch) {
+            for (int kb0 = 0; kb0 < blocks2; kb0 += stretch) {
                 if (!tc::mbar_wait_ready(&sh->acc_full[a], phase, abort_flag)) failed = true;
                 failed = __any_sync(0xffffffffu, failed);
                 if (failed) break;
                 tc::tc_fence_after_sync();
                 if (left > 0) {
-                    // (where the blocks are fewer than the issuers, those that have had one)
+                    // (the second of two issuers has none where there is the empty block only)
                     const uint32_t from = tmem_d + a * geo.issuers * acc_cols + lane_off;
-                    const int i0 = (u - u0) * p.blocks + kb0, parts = min(geo.issuers, p.blocks - kb0);
+                    const int parts = kb0 + 2 == blocks2 && empty_at == kb0 + 1 ? 1 : geo.issuers;
                     for (int c = 0; c * 16 < geo.n; ++c) {                                           // 16 rows at a time
                         uint32_t r[16];
-                        tc::tmem_read16(from + (i0 & (geo.issuers - 1)) * acc_cols + c * 16, r);
+                        tc::tmem_read16(from + c * 16, r);
                         for (int i = 1; i < parts; ++i) {
                             uint32_t s[16];
-                            tc::tmem_read16(from + ((i0 + i) & (geo.issuers - 1)) * acc_cols + c * 16, s);
+                            tc::tmem_read16(from + i * acc_cols + c * 16, s);
 #pragma unroll
                             for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(s[j]));
                         }
@@ -266,7 +273,8 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
             }
             if (failed) break;
             if (left <= 0) continue;
-            if (geo.n == 16) look_through(std::integral_constant<int, 16>(), 0, slot, v0, left);
+            if (p.mcount <= 8) look_through(std::integral_constant<int, 8>(), 0, slot, v0, left);
+            else if (p.mcount <= 16) look_through(std::integral_constant<int, 16>(), 0, slot, v0, left);
             else
                 for (int c = 0; c < geo.chunks; ++c) look_through(std::integral_constant<int, 32>(), c, slot, v0, left);
         }
@@ -279,22 +287,19 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
         const int q = warp & 3, stage = (warp - kEpi) >> 2;    // (a warp writes the quarter of the tensor memory's lanes that its number names)
         const int panel = 2 * q + (lane >> 4), cls = lane & 15;
         const int gpb = kQ4Block / p.group;
-        int it = 0, s = 0;                                     // blocks so far, ring slot
-        uint32_t phase = 0u;
+        // Of four blocks, two ring slots, the group takes one: with an even number of ring slots it sees every fill of those that it takes from.
+        const int kb = stage & 1;
+        int n = 0, s = stage >> 1;                             // pairs so far, the group's next ring slot
+        uint32_t phase = 0u, v_phase = 1u;
         for (int u = u0; u < u1 && !failed; ++u) {
             const bool there = (u % geo.tiles) * kTile + q * 32 < p.classes;  // (behind a slot's last class: nothing to make)
-            for (int pc = 0, at = start; pc < pairs; ++pc, at = at + 1 == pairs ? 0 : at + 1) {
-                const int nb = 2 * at + 1 < p.blocks ? 2 : 1;
-                if (!tc::mbar_wait_ready(&sh->raw_full[s], phase, abort_flag)) failed = true;
-                failed = __any_sync(0xffffffffu, failed);
-                if (failed) break;
-                const int kb = (stage - it) & (kStages - 1);   // the group's block, if it is one of the slot's
-                if (kb < nb) {
-                    if (!tc::mbar_wait_ready(&sh->v_empty[stage], ((uint32_t)((it + kb) / kStages) & 1u) ^ 1u, abort_flag)) failed = true;
-                    failed = __any_sync(0xffffffffu, failed);
-                    if (failed) break;
+            for (int pc = 0, at = start; pc < pairs; ++pc, at = at + 1 == pairs ? 0 : at + 1, ++n) {
+                if ((n & 1) == (stage >> 1)) {
+                    // (lanes that wait for different barriers at once wake late: with one lane to a barrier the 7B shape took 152 us in place of 104)
+                    const bool ok = tc::mbar_wait_ready(&sh->raw_full[s], phase, abort_flag) && tc::mbar_wait_ready(&sh->v_empty[stage], v_phase, abort_flag);
+                    if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
                     tc::tc_fence_after_sync();
-                    if (there) {
+                    if (there && 2 * at + kb < p.blocks) {
                         const unsigned char* blk = ring + s * slot_bytes + (panel * 2 + kb) * bb;
                         const uint32_t* so = reinterpret_cast<const uint32_t*>(blk + 1024) + cls * gpb;
                         const uint32_t to = tmem + 64u * stage + ((uint32_t)(q * 32) << 16);
@@ -318,12 +323,13 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
                     }
                     tc::tc_fence_before_sync();
                     __syncwarp();
-                    if (lane == 0) tc::mbar_arrive(&sh->v_full[stage]);
+                    if (lane == 0) {
+                        tc::mbar_arrive(&sh->v_full[stage]);
+                        tc::mbar_arrive(&sh->raw_empty[s]);
+                    }
+                    v_phase ^= 1u;
+                    if ((s += 2) >= p.nring) { s -= p.nring; phase ^= 1u; }
                 }
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(&sh->raw_empty[s]);
-                it += nb;
-                if (++s == p.nring) { s = 0; phase ^= 1u; }
             }
         }
         if (failed && lane == 0) give_up(sh, p.status, 47);
@@ -366,17 +372,21 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
         pdl_trigger();
         if (lane == 0) {
             const uint64_t pol = tc::policy_evict_last();
-            const int steps = (u1 - u0) * p.blocks;
+            const int steps = (u1 - u0) * blocks2;
             int it = 0, kb = 2 * start, st = 0;
             uint32_t phase = 1u;
             for (; it < steps; ++it) {
                 if (!tc::mbar_wait_ready(&sh->x_empty[st], phase, abort_flag)) { failed = true; break; }
                 unsigned char* dst = dyn + st * x_bytes;
-                tc::mbar_arrive_expect_tx(&sh->x_full[st], (uint32_t)x_bytes);
-                // (elements behind H and rows behind the last are outside the tensor and arrive as zeros)
-                tc::tma_load_2d(dst, &tmX, &sh->x_full[st], kb * kQ4Block, 0, pol);
-                tc::tma_load_2d(dst + x_plane, &tmX, &sh->x_full[st], kb * kQ4Block + 64, 0, pol);
-                if (++kb == p.blocks) kb = 0;
+                if (kb < p.blocks) {
+                    tc::mbar_arrive_expect_tx(&sh->x_full[st], (uint32_t)x_bytes);
+                    // (elements behind H and rows behind the last are outside the tensor and arrive as zeros)
+                    tc::tma_load_2d(dst, &tmX, &sh->x_full[st], kb * kQ4Block, 0, pol);
+                    tc::tma_load_2d(dst + x_plane, &tmX, &sh->x_full[st], kb * kQ4Block + 64, 0, pol);
+                } else {
+                    tc::mbar_arrive(&sh->x_full[st]);
+                }
+                if (++kb == blocks2) kb = 0;
                 if (++st == geo.xstages) { st = 0; phase ^= 1u; }
             }
             if (failed) {
@@ -400,38 +410,36 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
         int xs = mine;
         uint32_t a_phase = 1u, x_phase = 0u;
         for (int u = u0; u < u1 && !failed && mine < geo.issuers; ++u) {
-            for (int kb0 = 0; kb0 < p.blocks && !failed; kb0 += stretch) {
-                const int nb = min(stretch, p.blocks - kb0);
+            for (int kb0 = 0; kb0 < blocks2 && !failed; kb0 += stretch) {
+                const int nb = min(stretch, blocks2 - kb0);
                 const uint32_t d = tmem_d + (a * geo.issuers + mine) * acc_cols;
-                bool first = true;
-                for (int k0 = (mine - it) & (geo.issuers - 1); k0 < nb; k0 += geo.issuers) {
+                bool first = true, waited = false;
+                for (int k0 = mine; k0 < nb; k0 += geo.issuers) {
                     const int st = (it + k0) % kStages;
-                    // (three lanes wait for a barrier each: a wait takes some 150 cycles also when the barrier is complete)
-                    const uint32_t ph = (uint32_t)((it + k0) / kStages) & 1u;
-                    uint64_t* bar = lane == 0 ? &sh->x_full[xs] : (lane == 1 ? &sh->v_full[st] : &sh->acc_empty[a]);
-                    const bool ok = !(lane < 2 || (lane == 2 && first)) || tc::mbar_wait_ready(bar, lane == 0 ? x_phase : (lane == 1 ? ph : a_phase), abort_flag);
+                    bool ok = waited || tc::mbar_wait_ready(&sh->acc_empty[a], a_phase, abort_flag);
+                    ok = ok && tc::mbar_wait_ready(&sh->x_full[xs], x_phase, abort_flag) &&
+                         tc::mbar_wait_ready(&sh->v_full[st], (uint32_t)((it + k0) / kStages) & 1u, abort_flag);
                     if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
                     tc::tc_fence_after_sync();
                     if (tc::elect_one()) {
                         const uint64_t xd = x_desc0 + (uint64_t)((uint32_t)(xs * x_bytes) >> 4);
+                        if (kb0 + k0 != empty_at) {
 #pragma unroll
-                        for (int half = 0; half < 2; ++half)
+                            for (int half = 0; half < 2; ++half)
 #pragma unroll
-                            for (int k = 0; k < 4; ++k)        // 16 elements along K: 8 columns of A, 32 bytes of B
-                                tc::mma_bf16_ts(d, tmem + 64u * st + 32u * half + 8u * k, xd + (uint64_t)((uint32_t)(half * x_plane) >> 4) + 2 * k, idesc,
-                                                first && (half | k) == 0 ? 0u : 1u);
+                                for (int k = 0; k < 4; ++k)    // 16 elements along K: 8 columns of A, 32 bytes of B
+                                    tc::mma_bf16_ts(d, tmem + 64u * st + 32u * half + 8u * k, xd + (uint64_t)((uint32_t)(half * x_plane) >> 4) + 2 * k, idesc,
+                                                    first && (half | k) == 0 ? 0u : 1u);
+                        }
                         tc::mma_commit(&sh->v_empty[st]);
                         tc::mma_commit(&sh->x_empty[xs]);
                     }
                     __syncwarp();
-                    first = false;
+                    first = first && kb0 + k0 == empty_at;
+                    waited = true;
                     done = it + k0;
                     if ((xs += geo.issuers) >= geo.xstages) { xs -= geo.xstages; x_phase ^= 1u; }
                 }
-                if (failed) break;
-                // (an issuer without a block waits for its turn all the same)
-                if (first && !tc::mbar_wait_ready(&sh->acc_empty[a], a_phase, abort_flag)) failed = true;
-                failed = __any_sync(0xffffffffu, failed);
                 if (failed) break;
                 if (tc::elect_one()) tc::mma_commit(&sh->acc_full[a]);
                 __syncwarp();
@@ -540,7 +548,8 @@ int launch_draft_q4_tc(Handle* h, cudaStream_t s, DraftQ4Params p) {
     const size_t bb = q4_block_bytes(p.group);
     const size_t fixed = (size_t)geo.xstages * geo.n * 256 + sizeof(float) * kEpi * kTurn + sizeof(uint32_t) * kEpi * geo.chunks * kSaved * 32 + sizeof(TcState);
     const size_t room = kMaxDynamicSmem - 1024 - fixed, slot = kTilePanels * 2 * bb;
-    p.nring = (int)(room / slot < kMaxRing ? room / slot : kMaxRing);         // (two at least: 128 rows and groups of 32 take 2 x 20 KB of 44 KB)
+    p.nring = (int)(room / slot < kMaxRing ? room / slot : kMaxRing);         // (two at least: 128 rows and groups of 32 take 2 x 20 KB of 76 KB)
+    p.nring &= ~1;
     if (p.nring < 2) return CTCSD_ERR_UNSUPPORTED;
     CUtensorMap tmX;
     CUtensorMap tmW;

@@ -19,7 +19,7 @@ constexpr int kQ4Group = 32;                   // values of a cached row that sh
 #ifdef __CUDACC__
 
 // (a & mask) | base as one instruction: an instruction takes one constant of its own, so both are kept in registers (as
-// constants the two steps stay apart, and the draft head at the 7B shape took 113 us in place of 86).
+// constants the two steps stay apart, and an earlier draft head took 113 us in place of 102 for a row of the 7B shape).
 __device__ __forceinline__ uint32_t q4_level_bits(uint32_t a) {
     uint32_t mask, base, r;
     asm("mov.b32 %0, 0x00780078;" : "=r"(mask));
@@ -100,7 +100,7 @@ static __device__ __noinline__ uint32_t q4_level(float v, float scale, float ori
 }
 // The word of eight values.  A level is a division, which took most of the time of storing rows; so it is found by the group's reciprocal (off by
 // less than 31 * 2^-22 from the division's result), and only where that lies within 2^-15 of a tie by the division itself.
-// (32 prompts of 1024-4096 rows of 8 heads, stored and read back: 340 us with divisions, STORE_US so.)
+// (32 prompts of 1024-4096 rows of 8 heads, stored and read back: 340 us with divisions, 262 us so.)
 __device__ __forceinline__ uint32_t q4_word(const float (&v)[8], uint32_t so) {
     const float s = bf16lo(so), o = bf16hi(so);
     if (!(s > 0.f)) return 0u;

@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
         };
         // Q as operand A: rows g and g + 8, elements D/4 t .. of the head
         // (in shared memory, for the registers' sake: with eight warps that held it, two to a scheduler, instructions waited for one another and 13B
-        // tokens took 265 us; twelve: MMA12 us)
+        // tokens took 265 us; twelve: 214 us)
         if (warp < LW) {
             const uint4 z = make_uint4(0u, 0u, 0u, 0u);
             const uint4* Qg = static_cast<const uint4*>(p.Q);
