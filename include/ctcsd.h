@@ -391,7 +391,7 @@ int ctcsd_evict_rows(ctcsd_handle* h, void* stream, void* workspace, size_t work
  *   outside 0..x_row_count-1 records CTCSD_ERR_INVALID_ARG in the device status word and that row drafts from a zero vector);
  * Wq, group as for the call above, not written by any kernel while the call runs or directly before it (ctcsd_quantize_weights_q4
  *   itself may precede it);  everything else as for ctcsd_draft_logits.
- * The weights are read once per 128 rows (float32: once per 4 rows, of very long rows as many as fit into shared memory; H <= 32768, beyond
+ * The weights are read once per 128 rows (float32: once per 4 rows, of very long rows as many as fit into shared memory; H <= 44800, beyond
  * that CTCSD_ERR_UNSUPPORTED).
  */
 int ctcsd_weights_q4_bytes(const ctcsd_config* cfg, int group, size_t* out_bytes);
