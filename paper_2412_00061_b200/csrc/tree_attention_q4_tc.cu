@@ -13,13 +13,14 @@
 // references, sums (of the unrounded weights), O and the parts are float32.
 //
 // Warps 0 and 3 bring levels in by bulk copies, warps 1 and 2 issue the products of one half each, warps 4-7 and 8-11 are the softmax warps of the
-// halves, 12-15 make the tiles.  All have 128 registers (168 for the softmax warps, taken from the others with setmaxnreg: 64 us in place of 62 for
-// case B below).
+// halves, 12-15 make the tiles.  All have 128 registers (168 for the softmax warps, taken from the others with setmaxnreg, made case B below
+// 2 us slower).
 //
-// What bounds it: the round of a block from the makers through S, the softmax, P V and back, about 3100 cycles where the products alone
-// take 2100 (D = 128, TR = 256); then a piece's beginning and end (6500 cycles), which short sequences pay often.
-//   A: 16 sequences of 4096 cached rows, 64 nodes, 64 query heads on 8 kv heads    235 us, 574 TFLOP/s (bfloat16 rows: 247 us)
-//   B: 4 sequences of 2048 rows, 64 nodes, 32 heads of their own                    62 us with the merge (bfloat16 rows: 42 us)
+// What bounds it: the softmax warps, about 1300 cycles a step of 64 keys (the exponentials alone take their units 512 for each of the two warps of a
+// scheduler), so 3100 cycles a block of 128 keys and 256 rows where the products take 2100 with their hand-overs; and a piece's beginning, last products and
+// output, some 12,000 cycles, which short sequences pay often.
+//   A: 32 sequences of 1024-4096 cached rows, 64 nodes, 64 query heads on 8 kv heads    228 us with the merge, 590 TFLOP/s (bfloat16 rows: 247 us)
+//   B: 8 sequences of 512-2048 rows, 64 nodes, 32 heads of their own                     59 us with the merge (bfloat16 rows: 42 us)
 //
 // A weight of zero does not cancel a NaN.  Cached rows are seen by every row of the tile, and those behind the last are made zeros; a
 // tree row whose value holds a NaN or an infinity is made zeros too and noted, and a row that does see it becomes NaN at the end.
@@ -393,18 +394,15 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
                 const int cc = lane % LR;
                 const unsigned there = __ballot_sync(0xffffffffu, live);
                 const uint4* Qg = static_cast<const uint4*>(p.Q) + cc;
-#pragma unroll 1
-                for (int i0 = 0; i0 < LR; i0 += 8) {
-                    uint4 w[8];
+                uint4 w[LR];                                   // (all loads at once: a piece waits for them once)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)                // (a row that is not there reads row 0)
-                        w[i] = __ldg(Qg + (size_t)__shfl_sync(0xffffffffu, orow, (i0 + i) * RI + lane / LR) * LR);
+                for (int i = 0; i < LR; ++i)                   // (a row that is not there reads row 0)
+                    w[i] = __ldg(Qg + (size_t)__shfl_sync(0xffffffffu, orow, i * RI + lane / LR) * LR);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int rr = (i0 + i) * RI + lane / LR;
-                        if (!((there >> rr) & 1u)) w[i] = make_uint4(0u, 0u, 0u, 0u);
-                        *reinterpret_cast<uint4*>(dst + rr * 128 + (cc / 8) * (kHalf * 128) + (((cc % 8) ^ (rr & 7)) << 4)) = w[i];
-                    }
+                for (int i = 0; i < LR; ++i) {
+                    const int rr = i * RI + lane / LR;
+                    if (!((there >> rr) & 1u)) w[i] = make_uint4(0u, 0u, 0u, 0u);
+                    *reinterpret_cast<uint4*>(dst + rr * 128 + (cc / 8) * (kHalf * 128) + (((cc % 8) ^ (rr & 7)) << 4)) = w[i];
                 }
                 tc::fence_proxy_async();
             }
@@ -532,9 +530,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
             if (live && at.blk1 > at.cached) {
                 const int t0 = (at.blk0 > at.cached ? at.blk0 - at.cached : 0) * 4, t1 = min((at.blk1 - at.cached) * 4, (n + 31) / 32);
 #pragma unroll 1
-                for (int i = t0; i < t1; ++i)
+                for (int i = t0; i < t1; ++i) {
                     // (of the blocks that this half took: the others' notes may not be there yet, and their half looks at them)
-                    if ((!split || ((at.cached + (i >> 2) - at.blk0) & 1) == half) && (*(volatile unsigned*)&sh->bad[piece & 3][i] & tree_bits32(mrow, MW, i * 32, n))) poisoned = true;
+                    if (split && ((at.cached + (i >> 2) - at.blk0) & 1) != half) continue;
+                    const unsigned cleared = *(volatile unsigned*)&sh->bad[piece & 3][i];
+                    if (cleared != 0u && (cleared & tree_bits32(mrow, MW, i * 32, n)) != 0u) poisoned = true;
+                }
             }
             if (poisoned) sum = __uint_as_float(0x7fc00000u);
             float mine = 1.f, other = 0.f;                      // weights of this half's output and of the other's
@@ -561,36 +562,51 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_tc_kernel(AttnQ4Para
                 const size_t part = (size_t)blockIdx.x * 2 + at.slot();
                 const int c_lo = split ? half * (D / 2) : 0, c_hi = split ? c_lo + D / 2 : D;
                 const uint32_t tmem_other = tmem + 256u + (uint32_t)((half ^ 1) * D) + lane_off;
+                // Whole rows go through Q's memory, which no product reads any more, so that neighbouring lanes write neighbouring 16 bytes (a row a lane took
+                // 32 lines an instruction).
+                unsigned char* stage = Qs + (split ? 0 : half * kQHalf) + (q * 32) * 128;
+                // (16 columns at a time: code that runs once a piece is mostly fetched, so it is kept short)
+                if (first) mine = 0.f;
+                if (!other_there) other = 0.f;
+                mine *= inv;
+                other *= inv;
 #pragma unroll 1
-                for (int c0 = c_lo; c0 < c_hi; c0 += 32) {
-                    float o[32];
+                for (int c0 = c_lo; c0 < c_hi; c0 += 16) {
+                    float o[16];
+                    uint32_t u[16];
+                    tc::tmem_read16(tmem_o + (uint32_t)c0, u);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) o[j] = 0.f;
-                    if (!first) {
-                        uint32_t u[32];
-                        tc::tmem_read32(tmem_o + (uint32_t)c0, u);
+                    for (int j = 0; j < 16; ++j) o[j] = mine != 0.f ? __uint_as_float(u[j]) * mine : 0.f;
+                    if (split) {
+                        tc::tmem_read16(tmem_other + (uint32_t)c0, u);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) o[j] = mine != 0.f ? __uint_as_float(u[j]) * mine : 0.f;
+                        for (int j = 0; j < 16; ++j) o[j] = other != 0.f ? fmaf(__uint_as_float(u[j]), other, o[j]) : o[j];
                     }
-                    if (other_there) {
-                        uint32_t u[32];
-                        tc::tmem_read32(tmem_other + (uint32_t)c0, u);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) o[j] = other != 0.f ? fmaf(__uint_as_float(u[j]), other, o[j]) : o[j];
-                    }
-                    if (!live) continue;
                     if (whole) {
-                        if (!CTCSD_IN_BOUNDS(p.status, 151, orow, out_rows(p))) continue;
-                        uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.O) + (size_t)orow * D + c0);
+                        unsigned char* to = stage + (c0 / 64) * (kHalf * 128) + lane * 128;
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            *reinterpret_cast<uint4*>(to + (((c0 % 64 / 8 + j) ^ (lane & 7)) << 4)) =
+                                make_uint4(pack_bf16(o[8 * j], o[8 * j + 1]), pack_bf16(o[8 * j + 2], o[8 * j + 3]), pack_bf16(o[8 * j + 4], o[8 * j + 5]),
+                                           pack_bf16(o[8 * j + 6], o[8 * j + 7]));
+                    } else if (live && CTCSD_IN_BOUNDS(p.status, 152, part * TR + rt, 2ll * gridDim.x * TR)) {
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
-                            out[j] = make_uint4(pack_bf16(o[8 * j] * inv, o[8 * j + 1] * inv), pack_bf16(o[8 * j + 2] * inv, o[8 * j + 3] * inv),
-                                                pack_bf16(o[8 * j + 4] * inv, o[8 * j + 5] * inv), pack_bf16(o[8 * j + 6] * inv, o[8 * j + 7] * inv));
-                    } else if (CTCSD_IN_BOUNDS(p.status, 152, part * TR + rt, 2ll * gridDim.x * TR)) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
                             p.part_o[(part * (D / 4) + c0 / 4 + j) * TR + rt] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
                     }
+                }
+                if (whole) {
+                    const unsigned there = __ballot_sync(0xffffffffu, live);
+                    const int per = (c_hi - c_lo) / 8, c = c_lo / 8 + lane % per;          // 16-byte places of a row; this lane's
+                    __syncwarp();
+#pragma unroll 4
+                    for (int r0 = 0; r0 < 32; r0 += 32 / per) {
+                        const int rr = r0 + lane / per;
+                        const unsigned row = __shfl_sync(0xffffffffu, orow, rr);
+                        const uint4 w = *reinterpret_cast<const uint4*>(stage + (c / 8) * (kHalf * 128) + rr * 128 + (((c % 8) ^ (rr & 7)) << 4));
+                        if (((there >> rr) & 1u) && CTCSD_IN_BOUNDS(p.status, 151, row, out_rows(p))) static_cast<uint4*>(p.O)[(size_t)row * (D / 8) + c] = w;
+                    }
+                    __syncwarp();
                 }
                 if (live && (!split || half == 0)) {
                     if (!whole) {
@@ -620,12 +636,6 @@ int launch_tc(Handle* h, cudaStream_t s, const AttnQ4Params& p) {
     if (n > kMaxRaw / 2) n = kMaxRaw / 2;
     if (n < 1) return CTCSD_ERR_UNSUPPORTED;
     auto kern = attention_q4_tc_kernel<D, TR>;
-    if (!(h->prepared & kPrepAttnQ4Tc)) {
-        // the register split waits for ever if the launch holds fewer registers than it hands out
-        cudaFuncAttributes fa;
-        CTCSD_CUDA_CHECK(h, cudaFuncGetAttributes(&fa, kern));
-        if (fa.numRegs < 128) return CTCSD_ERR_INTERNAL;
-    }
     CTCSD_CUDA_CHECK(h, prepare_kernel(h, kPrepAttnQ4Tc, kern));
     CTCSD_CUDA_CHECK(h, launch_pdl(kern, dim3(h->num_sms), dim3(kThreads), fixed + n * slots, s, 1, p, (int)n));
     h->launches++;
