@@ -141,24 +141,19 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream], device_index: Optional[int]
 
 
 class Q4Cache(dict):
-    """A 4-bit cache: levels Kq, Vq [B,Hkv,Lcap,D/2] uint8, (scale, origin) Ks, Vs [B,Hkv,Lcap,D/32,2] bfloat16.  Its tensors are checked
-    when they are put in, not again by every call."""
+    """A 4-bit cache: levels Kq, Vq [B,Hkv,Lcap,D/2] uint8, (scale, origin) Ks, Vs [B,Hkv,Lcap,D/32,2] bfloat16.  Types, sizes and layout of
+    the four tensors are checked by the first call that gets them, and again when one of them is another tensor or has moved."""
 
     def __init__(self, handle, **tensors):
         super().__init__(**tensors)
-        self.handle = handle
-        self._check()
+        self.handle, self.tensors, self.ptrs, self.Lcap = handle, (), None, 0
 
-    def _check(self):
-        self.ptrs, self.Lcap = self.handle._q4_check(self)
-
-    def __setitem__(self, name, tensor):
-        super().__setitem__(name, tensor)
-        self._check()
-
-    def update(self, *args, **kw):
-        super().update(*args, **kw)
-        self._check()
+    def checked(self):
+        tensors = self["Kq"], self["Ks"], self["Vq"], self["Vs"]
+        if len(self.tensors) != 4 or any(a is not b for a, b in zip(tensors, self.tensors)) or [t.data_ptr() for t in tensors] != self.ptrs:
+            self.ptrs, self.Lcap = self.handle._q4_check(self)
+            self.tensors = tensors
+        return self.ptrs, self.Lcap
 
 
 class Handle:
@@ -544,7 +539,7 @@ class Handle:
 
     def _q4_cache(self, cache):
         if type(cache) is Q4Cache and cache.handle is self:
-            return cache.ptrs, cache.Lcap
+            return cache.checked()
         return self._q4_check(cache)
 
     def _q4_check(self, cache):

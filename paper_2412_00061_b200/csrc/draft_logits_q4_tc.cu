@@ -194,10 +194,11 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
                 st.sum *= __expf(st.mx - top);                 // exp(-inf) = 0 covers the first chunk
                 st.mx = top;
             }
+            const float base = st.mx == -INFINITY ? 0.f : st.mx;                   // (nothing but -inf so far: they add nothing)
             float add = 0.f;
 #pragma unroll
-            for (int j = 0; j < J; ++j) add += __expf(z[j] - st.mx);
-            if (left > 0) st.sum += add;                       // (none: -inf - -inf)
+            for (int j = 0; j < J; ++j) add += __expf(z[j] - base);
+            st.sum += add;
             if (__any_sync(0xffffffffu, live && left > 0 && (top > floor || !listed))) {
                 uint32_t above = 0u;                           // logits that may be among the best
 #pragma unroll

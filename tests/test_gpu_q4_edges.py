@@ -132,3 +132,46 @@ def test_rows_stored_on_another_stream_are_read_behind_it():
     c.run(stream=s)
     s.synchronize()
     assert c.h.poll_status() == 0 and torch.equal(c.O, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("M,V", [(1, 8), (3, 300), (20, 32), (40, 129)])
+def test_a_blank_that_is_ruled_out(dtype, M, V):
+    """blank_bias = -inf: the blank has no part in the sum and ranks last."""
+    c = draft._Case(dtype, M, 256, V, 2, 3, 32)
+    c.bias.fill_(-np.inf)
+    c.run()
+    assert c.h.poll_status() == 0
+    z, tol = c.reference()
+    assert torch.all(z[..., V] == -np.inf) and torch.all(c.z[..., V] == -np.inf)
+    ids = c.z.sort(dim=-1, descending=True, stable=True)[1]
+    assert torch.equal(c.out[0].long(), ids[..., :3])
+    assert torch.all((c.out[2].double() - torch.logsumexp(z, -1)).abs() <= tol[..., :V].amax(-1) + 3e-5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("Hq,nodes", [(2, 3), (2, 40), (2, 200)])
+def test_a_batch_without_nodes_and_one_without_rows(dtype, Hq, nodes):
+    for n, kv in (([0, 0, 0], [50, 0, 7]), ([0, nodes, 1], [0, 0, 0])):
+        c = attention._Case(dtype, 3, Hq, 1, 64, nodes, n, kv)
+        c.run()
+        c.check()
+
+
+def test_a_cache_whose_tensors_are_exchanged_is_checked_again():
+    c = attention._Case("bf16", 1, 2, 1, 64, 3, [3], [70])
+    c.run()
+    want = c.O.clone()
+    good = dict(c.cache)
+    c.cache |= {name: t.clone() for name, t in good.items()}
+    for t in good.values():
+        t.zero_()
+    c.run()
+    assert torch.equal(c.O, want)
+    c.cache["Vs"] = c.cache["Vs"][:, :, :5].contiguous()
+    with pytest.raises(u.binding.CtcsdError):
+        c.run()
+    short = c.h.make_q4_cache(20)
+    short["Kq"].resize_(1, 1, 10, 32)
+    with pytest.raises(u.binding.CtcsdError):
+        c.h.store_rows_q4(short, c.K, c.V, u.i32([10]))
