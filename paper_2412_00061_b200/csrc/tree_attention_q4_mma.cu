@@ -88,19 +88,20 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
         if (lane == 0) {
             const uint64_t pol = tc::policy_evict_first();
             const long long rows = (long long)p.B * p.Hkv * p.Lcap;
-            int fill = 0;
+            int fill = 0, s = 0;
+            uint32_t phase = 1u;
             bool failed = false;
             for (; more && !failed; more = at.next(pl, p.B, kKeys)) {
                 const long long base = ((long long)at.b * p.Hkv + at.g) * p.Lcap;
                 const int kv = pl.kv[at.b];
                 for (int blk = at.blk0; blk < at.blk1 && blk < at.cached; ++blk, ++fill) {
-                    const int s = fill % nstages;
-                    if (!tc::mbar_wait_suspended(&sh->empty[s], ((uint32_t)(fill / nstages) & 1u) ^ 1u, abort_flag)) { failed = true; break; }
+                    if (!tc::mbar_wait_ready(&sh->empty[s], phase, abort_flag)) { failed = true; break; }
                     const long long row0 = base + (long long)blk * kKeys;
                     const int n = kv - blk * kKeys < kKeys ? kv - blk * kKeys : kKeys;
                     unsigned char* dst = ring + (size_t)s * 2 * kSide;
                     if (what & 1) RawQ4<D>::request_pairs(dst + (what >> 1) * kSide, what >> 1 ? p.Vs : p.Ks, kKeys, row0, n, rows, &sh->full[s], pol);
                     else RawQ4<D>::request_levels(dst + (what >> 1) * kSide, what >> 1 ? p.Vq : p.Kq, row0, n, &sh->full[s], pol);
+                    if (++s == nstages) { s = 0; phase ^= 1u; }
                 }
             }
             if (failed) {
@@ -119,7 +120,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
     const int g = lane >> 2, t = lane & 3;
     const int MW = (p.max_nodes + 63) / 64;
     const float sl2 = p.scale * kLog2e;
-    int fill = 0;
+    int st = 0;                                              // stage of the ring, and its turn
+    uint32_t phase = 0u;
     bool failed = false;
     for (; more; more = at.next(pl, p.B, kKeys)) {
         const int b = at.b, kv = pl.kv[b], n = pl.n[b], row0 = at.t * kRows;
@@ -131,7 +133,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
         };
         // Q as operand A: rows g and g + 8, elements D/4 t .. of the head
         // (in shared memory, for the registers' sake: with eight warps that held it, two to a scheduler, instructions waited for one another and 13B
-        // tokens took 265 us; twelve: 214 us)
+        // tokens took 265 us; twelve: 202 us)
         if (warp < LW) {
             const uint4 z = make_uint4(0u, 0u, 0u, 0u);
             const uint4* Qg = static_cast<const uint4*>(p.Q);
@@ -248,10 +250,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
                 }
                 continue;
             }
-            const int st = fill % nstages;
-            if (!failed && !tc::mbar_wait_suspended(&sh->full[st], (uint32_t)(fill / nstages) & 1u, abort_flag)) failed = true;
+            if (!failed && !tc::mbar_wait_ready(&sh->full[st], phase, abort_flag)) failed = true;
             failed = __any_sync(0xffffffffu, failed);
-            ++fill;
             const int left = kv - blk * kKeys - warp * 16;                    // keys of this warp that there are
             if (!failed && left > 0) {
                 const unsigned char* Kside = ring + (size_t)st * 2 * kSide;
@@ -333,6 +333,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_q4_mma_kernel(AttnQ4Par
             }
             __syncwarp();
             if (lane == 0 && !failed) tc::mbar_arrive(&sh->empty[st]);
+            if (++st == nstages) { st = 0; phase ^= 1u; }              // (counted: a division by a number not known to the compiler costs as much as a word's values)
         }
         if (failed && lane == 0) {
             if (*abort_flag == 0) report_error(p.status, CTCSD_ERR_TIMEOUT, 52);
