@@ -149,10 +149,12 @@ class Q4Cache(dict):
         self.handle, self.tensors, self.ptrs, self.Lcap = handle, (), None, 0
 
     def checked(self):
-        tensors = self["Kq"], self["Ks"], self["Vq"], self["Vs"]
-        if len(self.tensors) != 4 or any(a is not b for a, b in zip(tensors, self.tensors)) or [t.data_ptr() for t in tensors] != self.ptrs:
+        a, b, c, d = self["Kq"], self["Ks"], self["Vq"], self["Vs"]
+        seen, p = self.tensors, self.ptrs
+        if not (seen and a is seen[0] and b is seen[1] and c is seen[2] and d is seen[3] and
+                a.data_ptr() == p[0] and b.data_ptr() == p[1] and c.data_ptr() == p[2] and d.data_ptr() == p[3]):
             self.ptrs, self.Lcap = self.handle._q4_check(self)
-            self.tensors = tensors
+            self.tensors = a, b, c, d
         return self.ptrs, self.Lcap
 
 
