@@ -771,10 +771,10 @@ def evict_rows(K: np.ndarray, Vc: np.ndarray, mass: np.ndarray, row_pos: np.ndar
 # Weights and cached rows in 4 bits (no counterpart in the paper)
 # --------------------------------------------------------------------------------------
 def round_to_bf16(a: np.ndarray) -> np.ndarray:
-    """Nearest bfloat16 (ties to even) of float64 values, as float64: 8 significant bits."""
+    """Nearest bfloat16 (ties to even) of float64 values, as float64: 8 significant bits, and no finer than 2^-133 (subnormal numbers)."""
     a = np.asarray(a, dtype=np.float64)
-    m, e = np.frexp(a)
-    return np.ldexp(np.rint(m * 256.0), e - 8)
+    e = np.maximum(np.frexp(a)[1], -125)
+    return np.ldexp(np.rint(np.ldexp(a, 8 - e)), e - 8)
 
 
 def q4_quantize(v: np.ndarray, group: int) -> Tuple[np.ndarray, np.ndarray, np.ndarray]:

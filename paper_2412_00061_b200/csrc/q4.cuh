@@ -106,8 +106,9 @@ __device__ __forceinline__ uint32_t q4_word(const float (&v)[8], uint32_t so) {
     if (!(s > 0.f)) return 0u;
     const float r = __frcp_rn(s), magic = 12582912.f;                        // 1.5 * 2^23: adding it rounds to a whole number
     float q[8];
-    if (fabsf(o) <= 100.f * s && r < INFINITY) {
-        // no limits needed: the scale's rounding (2^-8 of 15 levels) and the origin's (2^-8 of 100 at most) move a level by 0.45 at most
+    if (fabsf(o) <= 100.f * s && s >= 1.17549435e-38f) {
+        // no limits needed: the scale's rounding (2^-8 of 15 levels) and the origin's (2^-8 of 100 at most) move a level by 0.45 at most.
+        // (a subnormal scale has fewer than 8 bits: there it can be 0.9, and a level 16)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float d = __fsub_rn(v[i], o), x = __fmaf_rn(d, r, -16.f);
