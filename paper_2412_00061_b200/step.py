@@ -101,9 +101,12 @@ class DraftVerifyStep:
 
     def _use_shared_attention(self):
         self.shared = self.h.make_shared_attention()
-        z = lambda *s, dtype: torch.zeros(*s, dtype=dtype, device=self.device)
-        self.out["attn_lse"] = z(self.cfg.B, self.cfg.max_nodes, self.cfg.Hq, dtype=torch.float32)
-        self.pos_base = z(self.cfg.B, dtype=torch.int32)
+        self._want_lse()
+        self.pos_base = torch.zeros(self.cfg.B, dtype=torch.int32, device=self.device)
+
+    def _want_lse(self):
+        if "attn_lse" not in self.out:
+            self.out["attn_lse"] = torch.zeros(self.cfg.B, self.cfg.max_nodes, self.cfg.Hq, dtype=torch.float32, device=self.device)
 
     def _has_prefix(self):
         return self.inp.get("Kp") is not None and self.inp["Kp"].shape[1] > 0
@@ -178,23 +181,33 @@ class DraftVerifyStep:
     # weights and cache in 4 bits --------------------------------------------------------
     def quantize_draft_weights(self, group: int = 128, stream=None):
         """Packs the draft head's weights in 4 bits (`group` neighbours along the hidden axis share a scale), once; the draft head reads
-        them from then on, and inp["Wd"] may be let go with set_inputs(Wd=None)."""
+        them from then on, and inp["Wd"] may be let go with set_inputs(Wd=None).  Called again while packed weights of that group are
+        in use, it packs in their place (captured graphs go on using them).  Otherwise it returns new ones, and whoever
+        replays a graph captured before holds on to those that it was captured with."""
         if self.inp.get("Wd") is None:
             raise ValueError("quantize_draft_weights() needs the weights (set_inputs(Wd=...))")
-        self.inp["Wd_q4"] = self.h.quantize_weights_q4(self.inp["Wd"], group, stream=stream)
+        there = self.inp.get("Wd_q4")
+        place = dict(out=there) if there is not None and there["group"] == group else {}
+        self.inp["Wd_q4"] = self.h.quantize_weights_q4(self.inp["Wd"], group, stream=stream, **place)
         return self.inp["Wd_q4"]
 
     def use_q4_cache(self, Lcap: Optional[int] = None):
         """Keeps the sequences' caches in 4 bits: an empty cache of Lcap rows (default: the configuration's), which store_prompt() fills,
         the attention reads and the history update extends; the inputs K and V are not looked at any more.  A step's tree
-        keys and values come as inputs Kt and Vt.  Called again, it starts with an empty cache."""
+        keys and values come as inputs Kt and Vt.  Called again, it starts with an empty cache: one of as many rows is cleared in
+        place (captured graphs go on using it), one of another number of rows takes new tensors, and graphs captured before are not to be replayed."""
         if self.cache is not None or self.inp.get("Kp") is not None:
             raise ValueError("a 4-bit cache has no shared prefix and no budget beside it")
         Lcap = self.cfg.Lcap if Lcap is None else Lcap
         if Lcap < 1:
             raise ValueError("a cache holds a row at least")
-        self.q4 = dict(cache=self.h.make_q4_cache(Lcap), ws=self.h.make_q4_attention())
-        self.out["attn_lse"] = torch.zeros(self.cfg.B, self.cfg.max_nodes, self.cfg.Hq, dtype=torch.float32, device=self.device)
+        if self.q4 is not None and self.q4["Lcap"] == Lcap:
+            for t in self.q4["cache"].values():
+                t.zero_()
+            return self.q4["cache"]
+        ws = self.h.make_q4_attention() if self.q4 is None else self.q4["ws"]
+        self.q4 = dict(cache=self.h.make_q4_cache(Lcap), ws=ws, Lcap=Lcap)
+        self._want_lse()
         return self.q4["cache"]
 
     def store_prompt(self, K, V, n_rows, at=None, stream=None):
