@@ -498,18 +498,24 @@ class Handle:
     def quantize_weights_q4(self, Wd, group=128, stream=None, out=None):
         """Packs the draft head's weights [T,V+1,H] in 4 bits, `group` (32, 64 or 128) neighbours along H to a scale.
         Returns what draft_logits_q4 takes; Wd is not needed any more.  out: what an earlier call with that group returned, to be
-        packed anew in its place."""
+        packed anew in its place.  stream: waits for what the current one has been given so far (the new tensor's memory may still be in
+        use there); whoever reads the weights on another stream waits for it."""
         c = self.cfg
         if out is not None and out["group"] != int(group):
             raise CtcsdError("out was packed in groups of %r, not of %r" % (out["group"], group))
         n = ctypes.c_size_t(0)
         self._check(self.lib.ctcsd_weights_q4_bytes(ctypes.byref(self.cfg), int(group), ctypes.byref(n)), "weights_q4_bytes")
         w = torch.empty(n.value, dtype=torch.uint8, device=self.device) if out is None else out["w"]
+        if stream is not None:
+            here = torch.cuda.current_stream(self.device)
+            if stream.cuda_stream != here.cuda_stream:
+                stream.wait_stream(here)
         rc = self.lib.ctcsd_quantize_weights_q4(
             self._h, _stream_ptr(stream, self._dev), _ptr(Wd, self.act_dtype, c.T * (c.V + 1) * c.H, "Wd"), int(group),
             _ptr(w, torch.uint8, n.value, "Wq"))
         self._check(rc, "quantize_weights_q4")
-        if stream is not None:         # (allocated on the current stream, written on another)
+        if stream is not None:         # (allocated on other streams, and let go by the caller while this one may still be at it)
+            Wd.record_stream(stream)
             w.record_stream(stream)
         return dict(w=w, group=int(group)) if out is None else out
 

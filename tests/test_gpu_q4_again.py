@@ -51,3 +51,30 @@ def test_a_graph_follows_another_batch_in_the_same_cache(name):
         assert all(torch.equal(c["rec"][k], t) for k, t in zip(keep, want))
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(cache.values(), rows))
     assert all(torch.all(t == 1) for t in junk)
+
+
+def test_weights_packed_on_a_side_stream_and_let_go_at_once():
+    """The side stream is behind, the weights are dropped, and their memory and more like it is written over on the current stream."""
+    import test_gpu_q4_draft as draft
+    c = draft._Case("bf16", 2, 1024, 4000, 2, 3, 64)
+    c.run()
+    want = [t.clone() for t in c.out]
+    plain, packed = c.W, c.Wq["w"].clone()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        W = plain.clone()
+        busy = torch.full_like(packed, 3)                    # in use on the current stream when it is let go
+        torch.cuda._sleep(20_000_000)
+        busy.add_(1)
+        del busy
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(40_000_000)
+        got = c.h.quantize_weights_q4(W, 64, stream=side)
+        del W
+        over = [torch.full_like(plain, float("nan")) for _ in range(2)]
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(got["w"], packed)
+        c.Wq = got
+        c.run()
+        assert all(torch.equal(a, b) for a, b in zip(c.out, want))
+        del over, got
