@@ -140,24 +140,6 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream], device_index: Optional[int]
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device_index is None else device_index)
 
 
-class Q4Cache(dict):
-    """A 4-bit cache: levels Kq, Vq [B,Hkv,Lcap,D/2] uint8, (scale, origin) Ks, Vs [B,Hkv,Lcap,D/32,2] bfloat16.  Types, sizes and layout of
-    the four tensors are checked by the first call that gets them, and again when one of them is another tensor or has moved."""
-
-    def __init__(self, handle, **tensors):
-        super().__init__(**tensors)
-        self.handle, self.tensors, self.ptrs, self.Lcap = handle, (), None, 0
-
-    def checked(self):
-        a, b, c, d = self["Kq"], self["Ks"], self["Vq"], self["Vs"]
-        seen, p = self.tensors, self.ptrs
-        if not (seen and a is seen[0] and b is seen[1] and c is seen[2] and d is seen[3] and
-                a.data_ptr() == p[0] and b.data_ptr() == p[1] and c.data_ptr() == p[2] and d.data_ptr() == p[3]):
-            self.ptrs, self.Lcap = self.handle._q4_check(self)
-            self.tensors = a, b, c, d
-        return self.ptrs, self.Lcap
-
-
 class Handle:
     """Owns a ctcsd handle and its device workspace (a torch uint8 tensor)."""
 
@@ -542,25 +524,23 @@ class Handle:
         return _ptr(Wq["w"], torch.uint8, c.T * ((c.V + 16) // 16) * ((c.H + 127) // 128) * (1024 + 64 * (128 // group)), "Wq")
 
     def make_q4_cache(self, Lcap):
-        """An empty 4-bit cache (Q4Cache) of Lcap rows a sequence."""
+        """An empty 4-bit cache of Lcap rows a sequence: levels Kq, Vq [B,Hkv,Lcap,D/2] uint8, (scale, origin) Ks, Vs [B,Hkv,Lcap,D/32,2]
+        bfloat16.  Every call checks the four tensors it is given."""
         c = self.cfg
         levels = lambda: torch.zeros(c.B, c.Hkv, Lcap, c.D // 2, dtype=torch.uint8, device=self.device)
         pairs = lambda: torch.zeros(c.B, c.Hkv, Lcap, c.D // self.Q4_GROUP, 2, dtype=torch.bfloat16, device=self.device)
-        return Q4Cache(self, Kq=levels(), Ks=pairs(), Vq=levels(), Vs=pairs())
+        return dict(Kq=levels(), Ks=pairs(), Vq=levels(), Vs=pairs())
 
     def _q4_cache(self, cache):
-        if type(cache) is Q4Cache and cache.handle is self:
-            return cache.checked()
-        return self._q4_check(cache)
-
-    def _q4_check(self, cache):
+        """Addresses of the cache's tensors, and its rows a sequence."""
         c = self.cfg
-        Lcap = cache["Kq"].shape[2]
+        Kq = cache["Kq"]
+        Lcap, D = Kq.shape[2], c.D
         rows = c.B * c.Hkv * Lcap
-        return [_ptr(cache["Kq"], torch.uint8, rows * (c.D // 2), "Kq"),
-                _ptr(cache["Ks"], torch.bfloat16, rows * (c.D // self.Q4_GROUP) * 2, "Ks"),
-                _ptr(cache["Vq"], torch.uint8, rows * (c.D // 2), "Vq"),
-                _ptr(cache["Vs"], torch.bfloat16, rows * (c.D // self.Q4_GROUP) * 2, "Vs")], Lcap
+        levels, pairs = rows * (D // 2), rows * (D // self.Q4_GROUP) * 2
+        u8, bf16 = torch.uint8, torch.bfloat16
+        return (_ptr(Kq, u8, levels, "Kq"), _ptr(cache["Ks"], bf16, pairs, "Ks"),
+                _ptr(cache["Vq"], u8, levels, "Vq"), _ptr(cache["Vs"], bf16, pairs, "Vs")), Lcap
 
     def store_rows_q4(self, cache, K, V, n_rows, at=None, stream=None):
         """The first n_rows[b] rows of K, V [B,Hkv,Lsrc,D] to rows at[b].. of the cache (at None: from 0)."""
