@@ -83,7 +83,7 @@ class DraftVerifyStep:
         With a cache budget, K and V of a new batch need reset_cache() as well.  Kt, Vt [B,Hkv,max_nodes,D]: the tree's keys and
         values of a step over a 4-bit cache (use_q4_cache).  Wd_q4: packed weights that the draft head reads in place
         of Wd (quantize_draft_weights()); weights given as Wd afterwards put them aside."""
-        if self.q4 is not None and tensors.get("Kp") is not None:
+        if self.q4 is not None and self._is_prefix(tensors.get("Kp")):
             raise ValueError("a 4-bit cache has no shared prefix beside it")
         if tensors.get("Wd") is not None and "Wd_q4" not in tensors:
             tensors["Wd_q4"] = None
@@ -108,8 +108,12 @@ class DraftVerifyStep:
         if "attn_lse" not in self.out:
             self.out["attn_lse"] = torch.zeros(self.cfg.B, self.cfg.max_nodes, self.cfg.Hq, dtype=torch.float32, device=self.device)
 
+    @staticmethod
+    def _is_prefix(Kp):
+        return Kp is not None and Kp.shape[1] > 0
+
     def _has_prefix(self):
-        return self.inp.get("Kp") is not None and self.inp["Kp"].shape[1] > 0
+        return self._is_prefix(self.inp.get("Kp"))
 
     def _shared_in_use(self):
         """Whether the attention takes the shared form: for a prefix, or for the log-sum-exp (out["attn_lse"]) that a
@@ -196,7 +200,7 @@ class DraftVerifyStep:
         the attention reads and the history update extends; the inputs K and V are not looked at any more.  A step's tree
         keys and values come as inputs Kt and Vt.  Called again, it starts with an empty cache: one of as many rows is cleared in
         place (captured graphs go on using it), one of another number of rows takes new tensors, and graphs captured before are not to be replayed."""
-        if self.cache is not None or self.inp.get("Kp") is not None:
+        if self.cache is not None or self._has_prefix():
             raise ValueError("a 4-bit cache has no shared prefix and no budget beside it")
         Lcap = self.cfg.Lcap if Lcap is None else Lcap
         if Lcap < 1:
