@@ -214,6 +214,13 @@ class DraftVerifyStep:
         self._want_lse()
         return self.q4["cache"]
 
+    def leave_q4_cache(self):
+        """Back to 16-bit rows: the attention and the history update take the inputs K and V again (load_rows_q4 gives the cached
+        rows as values), a shared prefix and a cache budget are open.  The cache is let go; graphs captured with it are not to be replayed."""
+        if self.q4 is None:
+            raise ValueError("leave_q4_cache() needs a 4-bit cache (use_q4_cache)")
+        self.q4 = None
+
     def store_prompt(self, K, V, n_rows, at=None, stream=None):
         """The first n_rows[b] rows of K, V [B,Hkv,L,D] to the 4-bit cache, from row at[b] (None: 0) on; kv_len is the caller's to set."""
         if self.q4 is None:
