@@ -39,8 +39,8 @@ struct Layout {
     size_t tc_part_bytes;
     size_t lm_rows_off;       // act[lm_key_count][H]: the LM head's live activation rows packed densely (bf16, more than 128 tree rows)
     size_t lm_rowmap_off;     // int[lm_key_count + 1]: packed row -> tree row; the last entry is the number of live rows
-    size_t q4_rows_off;       // act[max_draft_rows][H]: activation rows picked by a row map, for the draft head over 4-bit weights (bf16)
-    size_t q4_part_off;       // DraftPartial[4 * rows of a pass, a multiple of 32][SMs][2]: its states (bf16)
+    size_t q4_rows_off;       // act[rows of a pass][H]: activation rows picked by a row map, for the draft head over 4-bit weights (bf16)
+    size_t q4_part_off;       // DraftPartial[4][rows of a pass][SMs][2]: its states (bf16).  Both lie over the scratch from draft_part on
     size_t total;
     int gemv_grid_max;        // largest grid the GEMV may use
     int lm_key_count;

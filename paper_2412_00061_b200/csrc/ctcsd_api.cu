@@ -1,5 +1,6 @@
 // Handle management, configuration checks and workspace layout for the ctcsd C ABI.
 #include "common.cuh"
+#include "draft_q4.cuh"
 #include "lm_head_tc.cuh"
 
 #include <stdlib.h>
@@ -60,14 +61,14 @@ Layout make_layout(const ctcsd_config& c, int num_sms) {
         l.lm_rows_off = off;    off = align_up(off + (size_t)l.lm_key_count * c.H * 2, 256);
         l.lm_rowmap_off = off;  off = align_up(off + sizeof(int) * ((size_t)l.lm_key_count + 1), 256);
     }
-    l.q4_rows_off = l.q4_part_off = off;
-    {
-        const int rows = c.max_draft_rows > 0 ? c.max_draft_rows : c.B;
-        if (c.dtype == CTCSD_DTYPE_BF16) {
-            const int states = 4 * (rows < 128 ? (rows + 31) / 32 * 32 : 128);
-            l.q4_rows_off = off;  off = align_up(off + (size_t)rows * c.H * 2, 256);
-            l.q4_part_off = off;  off = align_up(off + sizeof(DraftPartial) * (size_t)states * (size_t)num_sms * 2, 256);
-        }
+    l.q4_rows_off = l.q4_part_off = l.draft_part_off;
+    if (c.dtype == CTCSD_DTYPE_BF16) {
+        // over the scratch of the other draft heads and of the LM head, from draft_part on: nothing in there outlives a call, and calls of a
+        // handle do not overlap.  (It reaches beyond it for more than 15 rows of a vocabulary of a few thousand only.)
+        const int most = c.max_draft_rows > 0 ? c.max_draft_rows : c.B, rows = most < kDraftQ4TcRows ? most : kDraftQ4TcRows;
+        l.q4_part_off = align_up(l.q4_rows_off + (size_t)rows * c.H * 2, 256);
+        const size_t end = align_up(l.q4_part_off + sizeof(DraftPartial) * kDraftQ4TcStates * (size_t)rows * (size_t)num_sms * 2, 256);
+        if (end > off) off = end;
     }
     l.total = off;
     return l;

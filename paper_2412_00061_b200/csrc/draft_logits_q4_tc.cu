@@ -26,7 +26,7 @@
 namespace ctcsd {
 namespace {
 
-constexpr int kEpi = 4;
+constexpr int kEpi = kDraftQ4TcStates;
 constexpr int kGroups = 4;               // groups of four warps that make values
 constexpr int kMakers = 4 * kGroups;
 constexpr int kStages = kGroups;         // a stage holds a block; each group has its own, so that it sees every fill of it and no turn of its barriers goes by unseen
@@ -109,7 +109,6 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
     // (with an odd number of blocks, an empty one behind the last goes the others' way, without products: its place in the CTA's order)
     const int blocks2 = 2 * pairs, empty_at = (p.blocks & 1) ? 2 * (pairs - 1 - start) + 1 : -1;
     const int stretch = kStretch * geo.issuers;
-    const int copy_rows = p.mcount <= 8 ? 8 : (p.mcount <= 16 ? 16 : geo.chunks * 32);                 // rows from a row's state to its next one
     bool failed = false;
 
     if (warp < kEpi) {
@@ -143,12 +142,14 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
 #pragma unroll
             for (int s = 0; s < kTopSlots; ++s) { st.val[s] = __uint_as_float(from[(2 + 2 * s) * 32]); st.id[s] = (int)from[(3 + 2 * s) * 32]; }
         };
-        // the states of a draft slot: a row has one of every warp (of 32 / R lanes of it), copy_rows rows apart
+        // the warp's states of a draft slot, one for every row (few rows stand in a warp two or four times, with other classes)
         auto publish = [&](int seg) {
             for (int c = 0; c < geo.chunks; ++c) {
                 load(c);
-                const int i = (warp * geo.chunks + c) * 32 + lane;
-                if (i % copy_rows < p.mcount) st.store(p.part + ((size_t)i * gridDim.x + blockIdx.x) * 2 + seg);
+                if (p.mcount <= 8) combine_best<24>(st, p.k);
+                else if (p.mcount <= 16) combine_best<16>(st, p.k);
+                const int m = c * 32 + lane;
+                if (m < p.mcount) st.store(p.part + ((size_t)(warp * p.mcount + m) * gridDim.x + blockIdx.x) * 2 + seg);
             }
         };
         auto begin = [&]() {
@@ -461,13 +462,12 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
     }
     if (*abort_flag != 0) return;                              // (uniform: set before the barrier or not at all)
     // a row's states in this CTA become one, in the place of the first
-    const int copies = kEpi * geo.chunks * 32 / copy_rows;
     for (int i = warp; i < segs * p.mcount; i += kThreads / 32) {
         const int seg = i / p.mcount, m = i - seg * p.mcount;
         DraftPartial* at = p.part + ((size_t)m * gridDim.x + blockIdx.x) * 2 + seg;
         RunState ms;
         ms.init();
-        if (lane < copies) ms.absorb(load_partial_cg(at + (size_t)lane * copy_rows * gridDim.x * 2));
+        if (lane < kEpi) ms.absorb(load_partial_cg(at + (size_t)lane * p.mcount * gridDim.x * 2));
         combine_best<31>(ms, p.k);
         if (lane == 0) ms.store(at);
     }

@@ -155,6 +155,7 @@ __device__ inline void draft_q4_finish(const DraftQ4Params& p, int per_slot, int
 
 // bf16, up to kDraftQ4TcRows activation rows in a pass, on tcgen05 / tensor memory.
 constexpr int kDraftQ4TcRows = 128;
+constexpr int kDraftQ4TcStates = 4;      // states of a row that a CTA keeps for a while (one of each warp that reads sums)
 int launch_draft_q4_tc(Handle* h, cudaStream_t s, DraftQ4Params p);
 
 }  // namespace ctcsd
