@@ -22,6 +22,7 @@ struct PackParams {
     const void* W;                       // [T,V+1,H]
     unsigned char* out;
     int H, classes, panels, blocks, group;
+    int* status;
 };
 
 // One warp per two classes of a block: lane = (class parity, eight elements).
@@ -31,7 +32,8 @@ __global__ void __launch_bounds__(256) quantize_weights_q4_kernel(PackParams p) 
     const int kb = blockIdx.x, t = blockIdx.z;
     const int bytes = q4_block_bytes(p.group), per = p.group / 8;                // lanes of a group
     for (int panel = blockIdx.y; panel < p.panels; panel += gridDim.y) {
-        unsigned char* blk = p.out + (((size_t)t * p.panels + panel) * p.blocks + kb) * bytes;
+        const size_t base = (((size_t)t * p.panels + panel) * p.blocks + kb) * (bytes / 4);
+        uint32_t* blk = reinterpret_cast<uint32_t*>(p.out) + base;
         const int r = warp * 2 + (lane >> 4), e = (lane & 15) * 8;            // class of the panel, first element of the block
         const int cls = panel * kQ4Panel + r, k = kb * kQ4Block + e;
         const bool in = cls < p.classes && k < p.H;                           // (H is a multiple of 8)
@@ -51,8 +53,10 @@ __global__ void __launch_bounds__(256) quantize_weights_q4_kernel(PackParams p) 
         const bool some = cls < p.classes && kb * kQ4Block + e / p.group * p.group < p.H;
         const uint32_t so = some ? q4_scale_origin(lo, hi) : 0u;
         const uint32_t w = in ? q4_word(v, so) : 0u;
-        reinterpret_cast<uint32_t*>(blk)[((e >> 5) * kQ4Panel + r) * 4 + ((e >> 3) & 3)] = w;
-        if ((lane & 15) % per == 0) reinterpret_cast<uint32_t*>(blk + 1024)[r * (kQ4Block / p.group) + e / p.group] = so;
+        const int at = ((e >> 5) * kQ4Panel + r) * 4 + ((e >> 3) & 3), at_so = 256 + r * (kQ4Block / p.group) + e / p.group;
+        const long long room = (long long)gridDim.z * p.panels * p.blocks * (bytes / 4);
+        if (CTCSD_IN_BOUNDS(p.status, 163, base + at, room)) blk[at] = w;
+        if ((lane & 15) % per == 0 && CTCSD_IN_BOUNDS(p.status, 164, base + at_so, room)) blk[at_so] = so;
     }
 }
 
@@ -204,7 +208,8 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_f32_kernel(DraftQ4Params
     // the warp's states of a draft slot, one for every row, to shared memory
     auto put_states = [&](int seg) __attribute__((always_inline)) {
         combine_best<7>(best.st, p.k);
-        if (g == 0) best.st.store(&s_state[(seg * kWarps + warp) * kRows + t]);
+        if (g == 0 && CTCSD_IN_BOUNDS(p.status, 166, (seg * kWarps + warp) * kRows + t, 2 * kWarps * kRows))
+            best.st.store(&s_state[(seg * kWarps + warp) * kRows + t]);
         best.init();
     };
     int cur_seg = 0;
@@ -218,7 +223,8 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_f32_kernel(DraftQ4Params
             const int v = v0 + 8 * u;
             if (t < p.mcount && v < p.classes) {
                 const float zz = z[u] + (v == p.classes - 1 ? bias : 0.f);
-                if (p.logits_dbg) p.logits_dbg[((size_t)(p.m0 + t) * p.slots + slot) * p.classes + v] = zz;
+                const size_t o = ((size_t)(p.m0 + t) * p.slots + slot) * p.classes + v;
+                if (p.logits_dbg && CTCSD_IN_BOUNDS(p.status, 165, o, (long long)p.rows * p.slots * p.classes)) p.logits_dbg[o] = zz;
                 best.push(zz, v, p.k);
             }
         }
@@ -324,7 +330,8 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_f32_kernel(DraftQ4Params
         ms.init();
         if (lane < kWarps) ms.absorb(s_state[(seg * kWarps + lane) * kRows + m]);
         combine_best<31>(ms, p.k);
-        if (lane == 0) ms.store(p.part + ((size_t)m * gridDim.x + blockIdx.x) * 2 + seg);
+        const size_t o = ((size_t)m * gridDim.x + blockIdx.x) * 2 + seg;
+        if (lane == 0 && CTCSD_IN_BOUNDS(p.status, 167, o, p.part_room)) ms.store(p.part + o);
     }
     draft_q4_finish(p, p.panels, slot0, segs, sh->merge);
 }
@@ -383,6 +390,7 @@ extern "C" int ctcsd_quantize_weights_q4(ctcsd_handle* hh, void* stream, const v
     PackParams p;
     p.W = Wd; p.out = static_cast<unsigned char*>(out_Wq);
     p.H = c.H; p.classes = c.V + 1; p.panels = panels_of(c); p.blocks = blocks_of(c); p.group = group;
+    p.status = status_ptr(h);
     const DeviceGuard on(h->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const dim3 grid(p.blocks, p.panels < 65535 ? p.panels : 65535, c.T);
@@ -408,7 +416,9 @@ extern "C" int ctcsd_draft_logits_q4(ctcsd_handle* hh, void* stream, int M, cons
     p.W = static_cast<const unsigned char*>(Wq);
     p.row_seq = row_seq; p.blank_bias = blank_bias;
     p.H = c.H; p.classes = c.V + 1; p.panels = panels_of(c); p.blocks = blocks_of(c); p.group = group; p.slots = c.T;
+    p.rows = M;
     p.part = reinterpret_cast<DraftPartial*>(h->ws + h->lay.draft_part_off);
+    p.part_room = (long long)((h->lay.part_slot_off - h->lay.draft_part_off) / sizeof(DraftPartial));
     p.counter = counter_ptr(h);
     p.k = c.k; p.out_topk_id = out_topk_id; p.out_topk_lp = out_topk_lp; p.out_lse = out_lse; p.logits_dbg = out_logits_dbg;
     p.status = status_ptr(h);

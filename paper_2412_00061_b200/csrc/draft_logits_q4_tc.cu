@@ -149,7 +149,8 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
                 if (p.mcount <= 8) combine_best<24>(st, p.k);
                 else if (p.mcount <= 16) combine_best<16>(st, p.k);
                 const int m = c * 32 + lane;
-                if (m < p.mcount) st.store(p.part + ((size_t)(warp * p.mcount + m) * gridDim.x + blockIdx.x) * 2 + seg);
+                const size_t o = ((size_t)(warp * p.mcount + m) * gridDim.x + blockIdx.x) * 2 + seg;
+                if (m < p.mcount && CTCSD_IN_BOUNDS(p.status, 171, o, p.part_room)) st.store(p.part + o);
             }
         };
         auto begin = [&]() {
@@ -183,10 +184,10 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
                 for (int j = 0; j < J; ++j) z[j] = j < left ? z[j] + (j == left - 1 ? bias : 0.f) : -INFINITY;
             }
             if (p.logits_dbg != nullptr && live) {
-                float* out = p.logits_dbg + ((size_t)(p.m0 + m) * p.slots + slot) * p.classes + v0;
+                const size_t o = ((size_t)(p.m0 + m) * p.slots + slot) * p.classes + v0;
 #pragma unroll
                 for (int j = 0; j < J; ++j)
-                    if (j < left) out[j] = z[j];
+                    if (j < left && CTCSD_IN_BOUNDS(p.status, 172, o + j, (long long)p.rows * p.slots * p.classes)) p.logits_dbg[o + j] = z[j];
             }
             float top = z[0];
 #pragma unroll
@@ -464,24 +465,26 @@ __global__ void __launch_bounds__(kThreads, 1) draft_q4_tc_kernel(const __grid_c
     // a row's states in this CTA become one, in the place of the first
     for (int i = warp; i < segs * p.mcount; i += kThreads / 32) {
         const int seg = i / p.mcount, m = i - seg * p.mcount;
-        DraftPartial* at = p.part + ((size_t)m * gridDim.x + blockIdx.x) * 2 + seg;
+        const size_t o = ((size_t)m * gridDim.x + blockIdx.x) * 2 + seg;
+        DraftPartial* at = p.part + o;
         RunState ms;
         ms.init();
         if (lane < kEpi) ms.absorb(load_partial_cg(at + (size_t)lane * p.mcount * gridDim.x * 2));
         combine_best<31>(ms, p.k);
-        if (lane == 0) ms.store(at);
+        if (lane == 0 && CTCSD_IN_BOUNDS(p.status, 173, o, p.part_room)) ms.store(at);
     }
     draft_q4_finish(p, geo.tiles, slot0, segs, sh->merge);
 }
 
 // Activation rows picked by a row map, one behind the other; a map that leaves x gives a zero row.
-__global__ void __launch_bounds__(256) draft_q4_gather_kernel(const uint4* x, int x_row_count, const int* x_rows, int m0, int chunks, uint4* out, int* status) {
+__global__ void __launch_bounds__(256) draft_q4_gather_kernel(const uint4* x, int x_row_count, const int* x_rows, int m0, int chunks, uint4* out, long long room, int* status) {
     pdl_wait();
     pdl_trigger();
     const int m = blockIdx.x, r = x_rows[m0 + m];
     const bool there = r >= 0 && r < x_row_count;
     if (!there && threadIdx.x == 0) report_error(status, CTCSD_ERR_INVALID_ARG, m0 + m);
-    for (int c = threadIdx.x; c < chunks; c += 256) out[(size_t)m * chunks + c] = there ? x[(size_t)r * chunks + c] : make_uint4(0u, 0u, 0u, 0u);
+    for (int c = threadIdx.x; c < chunks; c += 256)
+        if (CTCSD_IN_BOUNDS(status, 174, (size_t)m * chunks + c, room)) out[(size_t)m * chunks + c] = there ? x[(size_t)r * chunks + c] : make_uint4(0u, 0u, 0u, 0u);
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -529,11 +532,12 @@ int launch_draft_q4_tc(Handle* h, cudaStream_t s, DraftQ4Params p) {
     if (p.x_rows) {
         uint4* rows = reinterpret_cast<uint4*>(h->ws + h->lay.q4_rows_off);
         CTCSD_CUDA_CHECK(h, launch_pdl(draft_q4_gather_kernel, dim3(p.mcount), dim3(256), 0, s, 1, static_cast<const uint4*>(p.x), p.x_row_count, p.x_rows, p.m0,
-                                       p.H / 8, rows, p.status));
+                                       p.H / 8, rows, (long long)((h->lay.q4_part_off - h->lay.q4_rows_off) / sizeof(uint4)), p.status));
         h->launches++;
         x = reinterpret_cast<const __nv_bfloat16*>(rows);
     }
     p.part = reinterpret_cast<DraftPartial*>(h->ws + h->lay.q4_part_off);
+    p.part_room = (long long)((h->lay.total - h->lay.q4_part_off) / sizeof(DraftPartial));
     TcGeo geo;
     geo.tiles = (p.panels + kTilePanels - 1) / kTilePanels;
     geo.n = (p.mcount + 15) / 16 * 16;

@@ -21,11 +21,12 @@ struct DraftQ4Params {
     const unsigned char* W;              // packed
     const int* row_seq;
     const float* blank_bias;
-    int m0, mcount;                      // rows of this pass
+    int m0, mcount, rows;                // rows of this pass, rows of the call
     int H, classes, panels, blocks, group;   // panels per draft slot, blocks per panel
     int slots;                           // draft slots (T)
     int piece, nring;                    // blocks of a ring slot, ring slots
     DraftPartial* part;                  // [rows of a pass][grid][2]
+    long long part_room;                 // states that the workspace has room for
     unsigned* counter;                   // [draft slots], zero between calls
     int k;
     int* out_topk_id;
@@ -138,11 +139,12 @@ __device__ inline void draft_q4_finish(const DraftQ4Params& p, int per_slot, int
             if (lane == 0) {
                 const int row = p.m0 + m;
                 const float lse = fs.mx + logf(fs.sum);
-                p.out_lse[(size_t)row * p.slots + slot] = lse;
+                if (CTCSD_IN_BOUNDS(p.status, 161, (long long)row * p.slots + slot, (long long)p.rows * p.slots)) p.out_lse[(size_t)row * p.slots + slot] = lse;
 #pragma unroll
                 for (int j = 0; j < kTopSlots; ++j)
                     if (j < p.k) {
                         const size_t o = ((size_t)row * p.slots + slot) * p.k + j;
+                        if (!CTCSD_IN_BOUNDS(p.status, 162, o, (long long)p.rows * p.slots * p.k)) continue;
                         p.out_topk_id[o] = fs.id[j];
                         p.out_topk_lp[o] = fs.val[j] - lse;
                     }

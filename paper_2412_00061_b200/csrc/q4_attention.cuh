@@ -24,6 +24,7 @@ struct AttnQ4Params {
     int B, Hq, Hkv, D, max_nodes, Lcap, grp;      // grp = Hq / Hkv
     float scale;
     int* status;
+    int spans;                           // that the workspace has room for
     int4* cuts;                          // workspace: [span] (written by its CTA, read by the merge): kv head, sequence, tile and last span of the tile
                                          // that the span continues from the one before it, -1 if there is none or a span further back began it
     float2* part_ml;                     // workspace: [span][2][TR] (reference in log2 units, sum)
@@ -173,7 +174,8 @@ __device__ inline void attn_q4_sides(const AttnQ4Params& a, const PlanQ4& p, con
             if (CTCSD_IN_BOUNDS(a.status, 131, (long long)i * words + w, (long long)a.B * a.max_nodes * words)) out[w] = make_uint4(0u, 0u, 0u, 0u);
         if (a.lse)
 #pragma unroll 1
-            for (int h = threadIdx.x; h < a.Hq; h += blockDim.x) a.lse[(size_t)i * a.Hq + h] = -INFINITY;
+            for (int h = threadIdx.x; h < a.Hq; h += blockDim.x)
+                if (CTCSD_IN_BOUNDS(a.status, 135, (long long)i * a.Hq + h, (long long)a.B * a.max_nodes * a.Hq)) a.lse[(size_t)i * a.Hq + h] = -INFINITY;
     }
     if (threadIdx.x == 0) {
         int4 cut = make_int4(-1, 0, 0, 0);
@@ -181,7 +183,7 @@ __device__ inline void attn_q4_sides(const AttnQ4Params& a, const PlanQ4& p, con
             const long long x0 = (long long)at.g * m.per_head + p.blk_off[at.b] + at.t * at.nblk;
             if (m.span_of(x0) == (int)blockIdx.x - 1) cut = make_int4(at.g, at.b, at.t, m.span_of(x0 + at.nblk - 1));
         }
-        a.cuts[blockIdx.x] = cut;
+        if (CTCSD_IN_BOUNDS(a.status, 136, blockIdx.x, a.spans)) a.cuts[blockIdx.x] = cut;
     }
 }
 

@@ -370,6 +370,7 @@ extern "C" int ctcsd_tree_attention_q4(ctcsd_handle* hh, void* stream, void* wor
     p.scale = scale;
     p.status = status_ptr(h);
     char* ws = static_cast<char*>(workspace);
+    p.spans = f.spans;
     p.cuts = reinterpret_cast<int4*>(ws + l.cuts);
     p.part_ml = reinterpret_cast<float2*>(ws + l.ml);
     p.part_o = reinterpret_cast<float4*>(ws + l.o);

@@ -47,3 +47,17 @@ def test_both_heads_in_turn(M, H, V):
     clear()
     g.replay()
     check()
+
+
+@pytest.mark.parametrize("dtype,M,H,V,T,k,group", [("bf16", 8, 2048, 500, 2, 8, 64), ("bf16", 17, 4096, 130, 2, 4, 128), ("bf16", 130, 72, 400, 2, 4, 32),
+                                                   ("fp32", 1, 8, 3, 1, 1, 32), ("fp32", 9, 520, 47, 8, 8, 128), ("fp32", 4, 1000, 9000, 3, 2, 32)])
+def test_the_4_bit_head_under_the_debug_bounds_build(dtype, M, H, V, T, k, group):
+    """Every index of a store that is formed from data lies in its array (the status word stays clean)."""
+    from paper_2412_00061_b200 import binding, build
+    assert binding.use_library(build.build(debug_bounds=True)).ctcsd_debug_bounds_enabled() == 1
+    try:
+        c = draft._Case(dtype, M, H, V, T, k, group, mapped=True)
+        c.run()
+        c.check()
+    finally:
+        binding.use_library(None)
