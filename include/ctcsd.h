@@ -379,6 +379,9 @@ int ctcsd_evict_rows(ctcsd_handle* h, void* stream, void* workspace, size_t work
  *   scale = bfloat16((hi - lo) * (1/15));  origin = bfloat16(lo - 16 scale);
  *   q = (v - origin) / scale - 16, rounded half to even and clamped to 0..15;  0 where scale = 0.
  * A group that holds a NaN or an infinity, or whose scale or origin would not be finite, stands for NaN (scale 0, origin NaN).
+ * A value comes back within half a level, and what rounding scale (1/8 of a level at most) and origin to 8 bits moves it by: the origin, 16 scales
+ * below the least value, by n/17 of a level where that lies n ranges of its group from zero.  So float32 values lose levels behind an
+ * offset of many times their range (all of them behind 1000 times it); bfloat16 values there lie 2n/17 levels apart anyway.
  *
  * ctcsd_quantize_weights_q4: Wd [T,V+1,H] dtype -> out_Wq, ctcsd_weights_q4_bytes(cfg, group) bytes; groups of 32, 64 or 128
  * along H (the last one of a row may be shorter).  Done once.  Layout: panels of 16 consecutive classes of a slot (the last one

@@ -503,7 +503,9 @@ class Handle:
 
     def draft_logits_q4(self, x, x_rows, Wq, row_seq, blank_bias, out_topk_id, out_topk_lp, out_lse,
                         out_logits_dbg=None, stream=None):
-        """draft_logits over 4-bit weights (quantize_weights_q4); x_rows None or an int32 row map as for draft_logits_rows."""
+        """draft_logits over 4-bit weights (quantize_weights_q4); x_rows None or an int32 row map as for draft_logits_rows.  The weights are
+        read before the kernel that precedes the call has ended: packing may directly precede it, another kernel that writes them (a copy
+        from the device's memory) may not, unless the stream is waited for in between."""
         c = self.cfg
         R = x.shape[0]
         M = R if x_rows is None else x_rows.shape[0]

@@ -134,8 +134,9 @@ struct PanelWalk {
 // float32.  One CTA per SM with a contiguous range of panels.  Every warp streams panels of its own through a small ring in shared memory with the
 // bulk-copy engine (its first lane asks for the next piece when a slot has been read); lane = (chunk t, class g and g + 8) makes values and multiplies
 // them with the activations of its chunk, held in shared memory; the sums of the four chunks are joined by shuffles, and lane (t, g) keeps the
-// running maximum, sum of exponentials and best k of row t.  Warps meet at the end only.  Bound by the fused multiply-adds: one for the value and
-// one a row, and three instructions to pick a level (tiny shape, 1 row of 256 x 4004: 15 us, mostly latency; 16 MB of weights and 4 rows 34 us).
+// running maximum, sum of exponentials and best k of row t.  Warps meet at the end only.  A weight takes four instructions (three to pick its level, a
+// multiply-add for its value) and one a row, which is half of the time where there are many weights: 5 slots of 32001 classes, H = 4096: 170 us for 1 row, 259 for
+// 4 (its bytes 53; the instructions alone 88 and 141).  Small shapes are latency: 1 row of 256 x 4004 15 us, 4 rows and 26 million weights 28.
 __global__ void __launch_bounds__(kThreads, 1) draft_q4_f32_kernel(DraftQ4Params p) {
     extern __shared__ __align__(128) unsigned char dyn[];
     unsigned char* xs = dyn;

@@ -6,7 +6,8 @@
 // Sixteen warps turn levels into values, four to a stage, 32 classes each: a lane reads its class's levels of a block, 64 bytes, and writes 64 columns of
 // tensor memory.  So the values never pass through shared memory, and a row costs its share of B and D only.  (Weights as the B operand, written to
 // swizzled tiles in shared memory, with activations padded to 128 rows as A: 403 us for 32 rows of the 70B shape, 185 us for 16 rows of the 7B shape.
-// mma.sync with the values in registers: 99 us for one row of the 7B shape, 108 for eight.)
+// mma.sync with the values in registers, for up to eight rows: 95-99 us for one row of the 7B shape, 108 for eight, 179 for four mapped rows of the
+// 13B shape, which it read without the kernel that gathers them here: one form serves all numbers of rows.)
 // The tensor core cuts a sum's last bits off at every addition, always towards zero, and long chains drift (log-probabilities off by
 // 6e-6 at H = 8192, by 5e-7 so).  So sums begin again every kStretch blocks, and the four warps that read D back add them up in rounded arithmetic, in
 // tensor memory.  They then turn 32 classes x R rows through shared memory, so that a lane has a row, and keep each row's maximum, sum of
@@ -15,9 +16,11 @@
 // products, of every other block each, into sums of their own (an issue takes some 700 cycles of waiting, describing and committing, more than its
 // products: 32 rows of the 70B shape 346 us with one issuer, 255 with two, 280 with four).
 //
-// 7B shape (5 slots of 32001 classes, H = 4096, groups of 128): 1 row 101 us, 3.4 TB/s of weights; 16 rows 112 us.  70B shape (6 slots, H = 8192): 32 rows
-// 237 us.  What bounds it: the makers' way from a full ring slot through 16 words of eleven instructions to the tensor memory's stores and the issue (without
-// the stores the 7B shape takes 69 us, without products and stores 63), and the instruction slots that reading sums back takes from them (14 us).
+// 7B shape (5 slots of 32001 classes, H = 4096, groups of 128): 1 row 101 us, 3.4 TB/s of weights; 16 rows 112 us.  13B shape (8 slots, H = 5120, groups of 64):
+// 4 mapped rows 182 us.  70B shape (6 slots, H = 8192): 32 rows 258 us.  No unit is at its limit (7B shape, 1 row: DRAM 36 %, ALU pipe 58 %, 0.59
+// instructions a cycle and scheduler).  24 instructions are issued for each word of eight weights where the makers' loop has eleven: the rest are waits,
+// hand-overs, sums that are read back and looked through, and what is how much of that was not taken apart.  Left out one at a time, the stores to tensor memory
+// are worth 32 us of the 7B shape, products and stores 38, reading sums back 14.
 #include "draft_q4.cuh"
 #include "tc_primitives.cuh"
 

@@ -5,7 +5,8 @@
 // Levels count from 16 because 16..31 are the bfloat16 numbers 0x4180 | q << 3: a level becomes a number by one shift and
 // one and-or, two levels at a time, and one packed multiply-add makes it the value.  (Levels from 0 took a
 // subtraction more; the origin is then farther from the values, by 16 scales, and rounding it to 8 bits moves all levels of a group
-// together by 1/16 of a level at most where the group spans zero.)
+// together: by 1/16 of a level at most where the group spans zero, by n/17 of one behind an offset of n times the group's range.  bfloat16
+// values there lie 2n/17 levels apart themselves; float32 values behind an offset of 1000 times their range all end on one level.)
 // Eight consecutive values share a 32-bit word, at the nibbles that begin at bits 3, 19, 7, 23, 11, 27, 31 (and 0..2), 15: a pair's two
 // lie 16 bits apart and three shifts bring all pairs to bits 3..6 and 19..22, where a bfloat16 number takes them.
 #pragma once

@@ -16,9 +16,10 @@
 // halves, 12-15 make the tiles.  All have 128 registers (168 for the softmax warps, taken from the others with setmaxnreg, made case B below
 // 2 us slower).
 //
-// What bounds it: the softmax warps, about 1300 cycles a step of 64 keys (the exponentials alone take their units 512 for each of the two warps of a
-// scheduler), so 3100 cycles a block of 128 keys and 256 rows where the products take 2100 with their hand-overs; and a piece's beginning, last products and
-// output, some 12,000 cycles, which short sequences pay often.
+// What bounds it: no unit, but what stands in line.  A step of 64 keys takes the softmax warps about 1300 cycles (the exponentials alone take their units 512
+// for each of the two warps of a scheduler), and they wait another 450-1600 for its scores; where those go was not taken apart.  (With no waiting it would be
+// 3100 cycles a block of 128 keys and 256 rows, 1570 TFLOP/s.)  A piece's beginning, last products and output take some 12,000 cycles, in which the next piece's Q
+// cannot come, since its memory is also where outputs are turned; short sequences pay that often.
 //   A: 32 sequences of 1024-4096 cached rows, 64 nodes, 64 query heads on 8 kv heads    228 us with the merge, 590 TFLOP/s (bfloat16 rows: 247 us)
 //   B: 8 sequences of 512-2048 rows, 64 nodes, 32 heads of their own                     59 us with the merge (bfloat16 rows: 42 us)
 //

@@ -196,10 +196,12 @@ class DraftVerifyStep:
         return self.inp["Wd_q4"]
 
     def use_q4_cache(self, Lcap: Optional[int] = None):
-        """Keeps the sequences' caches in 4 bits: an empty cache of Lcap rows (default: the configuration's), which store_prompt() fills,
+        """Keeps the sequences' caches in 4 bits (a third of the bytes): an empty cache of Lcap rows (default: the configuration's), which store_prompt() fills,
         the attention reads and the history update extends; the inputs K and V are not looked at any more.  A step's tree
         keys and values come as inputs Kt and Vt.  Called again, it starts with an empty cache: one of as many rows is cleared in
-        place (captured graphs go on using it), one of another number of rows takes new tensors, and graphs captured before are not to be replayed."""
+        place (captured graphs go on using it), one of another number of rows takes new tensors, and graphs captured before are not to be replayed.
+        The attention is faster over 4 bits for long caches only: single tokens from some thousand rows on (32768 rows of 32 heads 63 us for 91; 1024
+        rows 16 for 13), 64-node trees from 8192 (8 sequences 187 us for 192; 1280 rows 54 for 44, one sequence of 1024 rows 21 for 13)."""
         if self.cache is not None or self._has_prefix():
             raise ValueError("a 4-bit cache has no shared prefix and no budget beside it")
         Lcap = self.cfg.Lcap if Lcap is None else Lcap
