@@ -64,7 +64,8 @@ Layout make_layout(const ctcsd_config& c, int num_sms) {
     l.q4_rows_off = l.q4_part_off = l.draft_part_off;
     if (c.dtype == CTCSD_DTYPE_BF16) {
         // over the scratch of the other draft heads and of the LM head, from draft_part on: nothing in there outlives a call, and calls of a
-        // handle do not overlap.  (It reaches beyond it for more than 15 rows of a vocabulary of a few thousand only.)
+        // handle do not overlap.  (It reaches beyond it for more than 15 rows of few classes only: for 32 rows of fewer than some 10,000 over all slots, for
+        // 128 of fewer than some 70,000.)
         const int most = c.max_draft_rows > 0 ? c.max_draft_rows : c.B, rows = most < kDraftQ4TcRows ? most : kDraftQ4TcRows;
         l.q4_part_off = align_up(l.q4_rows_off + (size_t)rows * c.H * 2, 256);
         const size_t end = align_up(l.q4_part_off + sizeof(DraftPartial) * kDraftQ4TcStates * (size_t)rows * (size_t)num_sms * 2, 256);
